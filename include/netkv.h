@@ -470,6 +470,142 @@ netkv_status netkv_flow_sim(netkv_handle h, uint32_t n_inst, uint32_t n_links, c
                             const uint32_t *path, uint64_t n_path, const double *bytes, const double *start,
                             double *finish, uint64_t *stats, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The block cache of a decode instance: the keys and values of the blocks
+ * whose hashes are its resident set K_d (Sec. III-B), in 8 bits (Sec. VII:
+ * block-quantised KV halves s_r), the attention that reads them, and the
+ * choice of the blocks that stay when memory is short (m_d, Eq. (5)).  One
+ * netkv_kv_t is one layer's cache.
+ *
+ * A page holds one block of block_tokens tokens for every KV head.  Elements
+ * are e4m3 (OCP FP8: 1 sign, 4 exponent, 3 mantissa bits, largest 448, no
+ * infinity, NaN 0x7F); an element stands for its value times the scale of its
+ * (page, head).  All arrays DEVICE; a caller may copy whole pages.
+ *   k        [n_pages][n_kv_heads][block_tokens][head_dim], 16-byte aligned
+ *   v        [n_pages][n_kv_heads][block_tokens / T][head_dim][T] with
+ *            T = min(block_tokens, 64), 16-byte aligned
+ *   k_scale, v_scale  [n_pages][n_kv_heads], finite and > 0 for every page
+ *            that holds a token (netkv_kv_store writes powers of two)
+ */
+typedef struct {
+    uint32_t n_pages;               /* 1 .. 2^31 - 1 */
+    uint32_t block_tokens;          /* B_tok: a power of two, 16 .. 1024 */
+    uint32_t n_kv_heads;            /* 1 .. 1024 */
+    uint32_t head_dim;              /* 64, 128 or 256 */
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+} netkv_kv_t;
+
+/* A batch of sequences over the cache (DEVICE arrays).  Sequence s holds
+ * ctx_len[s] tokens, token i in slot i % block_tokens of page
+ * pages[s * max_pages + i / block_tokens]; a page may be in several
+ * sequences (shared prefixes).  Rows tok_off[s] .. tok_off[s+1] of a call's
+ * token arrays are its last tokens, in order.  n_tok bounds tok_off, max_tok
+ * one sequence's rows; both are host values, as large as needed or larger.
+ * A sequence with offsets that decrease or pass n_tok, more than max_tok
+ * rows, more tokens than max_pages pages hold, or a page >= n_pages among
+ * those that a call reads is invalid and reported by netkv_sync_errors;
+ * nothing outside the arrays is read or written for it. */
+typedef struct {
+    uint32_t n_seq;                 /* <= 65535 */
+    uint32_t max_pages;             /* >= 1, max_pages * block_tokens <= 2^31 */
+    uint64_t n_tok, max_tok;        /* n_tok <= 2^31 */
+    const uint64_t *tok_off;        /* [n_seq + 1] */
+    const uint32_t *ctx_len;        /* [n_seq] */
+    const uint32_t *pages;          /* [n_seq * max_pages] */
+} netkv_kv_seqs_t;
+
+enum { NETKV_BF16 = 1, NETKV_FP16 = 2 };
+
+/* Write the rows k and v ([n_tok][n_kv_heads][head_dim] of dtype, k_stride
+ * and v_stride elements from token to token, multiples of 8, rows 16-byte
+ * aligned) into the sequences' pages.  The scale of a (page, head) becomes
+ * the smallest power of two s (>= 2^-126) with |x| <= 448 s for every finite
+ * new x, or stays what it is if the page already held tokens of the sequence
+ * and that is larger; if it grows, those tokens are brought under the new
+ * scale.  Rounding is to nearest even: at most half a step, 2^-4 of a value
+ * down to 2^-6 s and 2^-10 s below.  What is not finite is stored as NaN.  A
+ * page that the call writes must be in no other sequence of the call that
+ * writes it.  An invalid sequence, or one with more rows than tokens, is left
+ * out.  Asynchronous; allocates nothing. */
+netkv_status netkv_kv_store(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *k,
+                            uint64_t k_stride, const void *v, uint64_t v_stride, int dtype, void *stream);
+
+/* The reverse: the sequences' last rows as held (value times scale, rounded
+ * to dtype: exact in bf16 wherever it is normal) into k and v, laid out as
+ * for netkv_kv_store.  Rows of invalid sequences and rows past the last
+ * sequence are left as they were; a row on an invalid page is NaN. */
+netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, void *k,
+                           uint64_t k_stride, void *v, uint64_t v_stride, int dtype, void *stream);
+
+/* Attention of the sequences' last rows over their cached tokens, the rows'
+ * own tokens among them (store first): row t of the n rows of a sequence
+ * with c tokens sees tokens 0 .. c - n + t (causal), and
+ *     out = sum_i p_i v_i,  p = softmax_i(scale * q . k_i)
+ * per query head; n_heads is a multiple of n_kv_heads (at most 64 times), and
+ * query head j reads KV head j / (n_heads / n_kv_heads).  q and out
+ * [n_tok][n_heads][head_dim] of dtype with strides as for netkv_kv_store.  A
+ * row that sees no token (c < n) is 0.  What a row does not see never reaches
+ * it, be it NaN.  Products are exact and summed in fp32, the softmax is fp32,
+ * and its weights are rounded to 11 bits before the product with the values.
+ * Rows of invalid sequences become NaN; rows past the last sequence are left
+ * as they were.
+ * block_weight (NULL: none; DEVICE f32[n_seq * max_pages], overwritten): the
+ * sum over the sequence's rows and query heads of p over each block's
+ * tokens, 0 past the last block; NaN for an invalid sequence.
+ * work: DEVICE, 256-byte aligned, of netkv_kv_attend_workspace's bytes for
+ * the same arguments; its contents need not be kept between calls, and calls
+ * that may overlap need their own.  Results do not depend on other sequences
+ * of the batch except through how a long one is split (fp32 sums in another
+ * order); the same call gives the same bytes.  Asynchronous; allocates
+ * nothing.  ECAPACITY: more than 2^24 workgroups (tens of millions of
+ * query rows). */
+netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *q,
+                             int dtype, uint32_t n_heads, uint64_t q_stride, float scale, void *out,
+                             uint64_t out_stride, float *block_weight, void *work, uint64_t work_bytes,
+                             void *stream);
+
+/* Bytes of work for a netkv_kv_attend of these shapes (weights: whether it
+ * gives block weights).  Depends on the host values only: n_seq, max_pages,
+ * n_tok, max_tok, the cache's shape and n_heads. */
+netkv_status netkv_kv_attend_workspace(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
+                                       uint32_t n_heads, int weights, uint64_t *bytes);
+
+/* Add block weights (as netkv_kv_attend gives them) to the weights of their
+ * pages, page_weight u64[n_pages] (DEVICE), in units of 2^-24 and rounded to
+ * the nearest one: integer sums, so pages shared between sequences come out
+ * the same in any order.  A page takes 2^40 rows' whole attention before it
+ * wraps; halve the weights before (which also lets old attention fade).  Only
+ * ctx_len, pages, n_seq and max_pages of seqs are read.  A weight that is
+ * NaN, negative or >= 2^32, and a page >= n_pages, add nothing and are
+ * reported by netkv_sync_errors.  Asynchronous; allocates nothing. */
+netkv_status netkv_kv_weigh(netkv_handle h, const netkv_kv_seqs_t *seqs, uint32_t block_tokens,
+                            const float *block_weight, uint32_t n_pages, uint64_t *page_weight, void *stream);
+
+/* Eviction from resident sets by accumulated attention weight: segment i
+ * (a decode's resident hashes, in netkv_cache_load's CSR form: entries
+ * hash_off[i] .. hash_off[i+1], oldest first) keeps the min(keep[i], its
+ * size) entries of largest weight, ties to the lowest index, in their order.
+ * The last min(newest, kept) entries of a segment stay whatever their
+ * weight (and count as kept).  Writes out_off [n_seg + 1], and at
+ * out_off[i] .. out_off[i+1] the kept entries' hashes (out_hashes, may be
+ * NULL) and places in their segment (out_pos, may be NULL): out_off and
+ * out_hashes are what netkv_cache_load takes for the sets that remain.
+ * All arrays DEVICE; weight u64 (2^64 - 1 counts as 2^64 - 2), keep u32[n_seg];
+ * n_out is what out_pos and out_hashes hold: entries past it are not written
+ * and reported by netkv_sync_errors, as are offsets that decrease or pass
+ * n_entries (every segment then counts as empty).  Inputs and outputs must
+ * not overlap.  work: as for netkv_kv_attend, of
+ * netkv_cache_evict_workspace's bytes.  Needs no loads.  Asynchronous;
+ * allocates nothing.  ECAPACITY: 2^31 or more entries, more than 2^23 - 1
+ * segments. */
+netkv_status netkv_cache_evict(netkv_handle h, uint32_t n_seg, const uint64_t *hash_off, uint64_t n_entries,
+                               const uint64_t *weight, const uint64_t *hashes, const uint32_t *keep,
+                               uint32_t newest, uint64_t n_out, uint64_t *out_off, uint32_t *out_pos,
+                               uint64_t *out_hashes, void *work, uint64_t work_bytes, void *stream);
+
+netkv_status netkv_cache_evict_workspace(netkv_handle h, uint64_t n_entries, uint64_t *bytes);
+
 #ifdef __cplusplus
 }
 #endif

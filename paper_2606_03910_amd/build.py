@@ -6,8 +6,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "netkv.hip")
-# the selection path and the handle; the flow-level transfer simulation
-SOURCES = [SRC, os.path.join(HERE, "csrc", "flowsim.hip")]
+# the selection path and the handle; the flow-level transfer simulation; the
+# decode instance's block cache and the eviction from it
+SOURCES = [SRC] + [os.path.join(HERE, "csrc", f) for f in ("flowsim.hip", "blockcache.hip", "evict.hip")]
 LIB = os.path.join(HERE, "libnetkv.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

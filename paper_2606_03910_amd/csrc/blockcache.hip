@@ -1,0 +1,1454 @@
+// The decode instance's block cache for MI355X (gfx950): keys and values of
+// resident blocks in 8 bits, and the operators on them.
+//
+//   store_kernel    -- new keys and values quantised into their blocks.
+//   read_kernel     -- tokens given back in 16 bits.
+//   plan_kernel     -- a call's work list: (sequence, row tile, token range).
+//   attend_kernel   -- attention of a row tile over a token range.
+//   join_kernel     -- joins the ranges of the rows that were split.
+//   unit_kernel, column_kernel, block_kernel -- block weights.
+//   weigh_kernel    -- block weights summed over pages in fixed point.
+//
+// A block ("page") holds block_tokens tokens of every head.  An element is
+// e4m3 (1 sign, 4 exponent, 3 mantissa bits; largest 448; no infinity); a
+// (page, head) has one scale for its keys and one for its values.  Keys lie
+// token by token, values dimension by dimension within tiles of
+// min(block_tokens, 64) tokens: the product with the keys contracts over
+// dimensions and the one with the values over tokens, and each operand's
+// lane then reads 16 bytes in a row.
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "netkv.h"
+#include "netkv_internal.h"
+
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr uint32_t kStep = 64;        // tokens a wavefront takes at a time
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kMaxGrow = 8.0f;      // how far (in powers of two) a row's maximum may be passed before it is raised
+constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
+
+struct Kv {
+    uint8_t *k, *v;
+    float *ks, *vs;
+    uint32_t n_pages, hk, btl;        // 2^btl tokens a block
+    uint32_t n_seq, max_pages, max_tok;
+    const uint64_t *off;
+    const uint32_t *ctx, *pages;
+    uint64_t n_tok;
+    uint32_t *err;
+};
+
+struct Head {
+    uint64_t row0;       // first row of the token arrays
+    uint32_t n, ctx;     // rows, tokens held (rows included)
+    bool rows_ok, ok;
+};
+
+__device__ inline Head seq_head(const Kv &a, uint32_t s) {
+    const uint64_t b = a.off[s], e = a.off[s + 1];
+    Head h;
+    h.row0 = b;
+    h.ctx = a.ctx[s];
+    h.rows_ok = b <= e && e <= a.n_tok;
+    h.ok = h.rows_ok && e - b <= a.max_tok && (uint64_t)h.ctx <= ((uint64_t)a.max_pages << a.btl);
+    h.n = h.ok ? (uint32_t)(e - b) : 0u;
+    if (!h.ok) h.ctx = 0;
+    return h;
+}
+
+__device__ inline void report(const Kv &a) { atomicOr(a.err, kErrBlockBit); }
+
+// bytes of one head of one page
+__device__ inline uint64_t head_bytes(const Kv &a, int D) { return (uint64_t)D << a.btl; }
+
+template <bool HALF>
+struct Elem;
+template <>
+struct Elem<true> {
+    typedef _Float16 T;
+    typedef f16x2 T2;
+    typedef f16x8 T8;
+};
+template <>
+struct Elem<false> {
+    typedef __bf16 T;
+    typedef bf16x2 T2;
+    typedef bf16x8 T8;
+};
+
+// 8 e4m3 bytes to 16 bits, exactly (4 significant bits, exponents -9 to 8)
+__device__ inline f16x8 widen_f16(uint32_t a, uint32_t b) {
+    const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
+    const f16x2 q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
+    const f16x2 r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false);
+    const f16x2 s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
+    return f16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+
+__device__ inline bf16x8 widen_bf16(uint32_t a, uint32_t b) {
+    const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false);
+    const bf16x2 q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+    const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false);
+    const bf16x2 s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+    return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+
+template <bool HALF>
+__device__ inline typename Elem<HALF>::T8 widen(uint32_t a, uint32_t b) {
+    if constexpr (HALF)
+        return widen_f16(a, b);
+    else
+        return widen_bf16(a, b);
+}
+
+__device__ inline f32x4 product(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 product(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// over the four lanes of a row (lanes l, l ^ 16, l ^ 32, l ^ 48)
+__device__ inline float row_max(float x) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float pair16_sum(float x) {   // lanes l, l ^ 16
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ inline float row_sum(float x) {
+    x = pair16_sum(x);
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+
+// ------------------------------------------------------------------ work list
+
+struct Item {
+    uint32_t seq, tile, k0, k1;   // row tile, steps [k0, k1)
+    uint32_t slot, pad[3];        // partial result, or kNoSlot
+};
+struct Join {
+    uint32_t seq, tile, slot, n;  // ranges slot .. slot + n - 1
+};
+struct PlanHead {
+    uint32_t n_items, n_joins, n_slots, pad;
+};
+
+struct PlanArgs {
+    Kv kv;
+    uint32_t G, tile_rows, target, least, round;   // ranges of at least `least` steps, multiples of `round`
+    uint32_t item_cap, slot_cap, join_cap;
+    PlanHead *head;
+    Item *items;
+    Join *joins;
+    // rows of sequences that cannot be answered
+    uint16_t *out;
+    uint64_t out_stride;
+    uint32_t row_elems, nan16;
+};
+
+constexpr int kPlanThreads = 1024;
+
+// Exclusive scan of three counts over the workgroup; totals in tot.
+__device__ inline void scan3(uint32_t (&x)[3], uint32_t (&tot)[3], uint32_t (*wsum)[3]) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint32_t in[3];
+    for (int i = 0; i < 3; ++i) {
+        uint32_t y = x[i];
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t z = __shfl_up(y, d, 64);
+            if (lane >= d) y += z;
+        }
+        in[i] = y;
+        if (lane == 63) wsum[w][i] = y;
+    }
+    __syncthreads();
+    for (int i = 0; i < 3; ++i) {
+        uint32_t before = 0, all = 0;
+        for (int v = 0; v < kPlanThreads / 64; ++v) {
+            const uint32_t z = wsum[v][i];
+            if (v < w) before += z;
+            all += z;
+        }
+        x[i] = before + in[i] - x[i];
+        tot[i] = all;
+    }
+    __syncthreads();
+}
+
+// The last step (exclusive) that a row tile of a sequence sees.
+__device__ inline uint32_t tile_end(const Head &h, uint32_t G, uint32_t tile, uint32_t rows) {
+    const uint64_t last = min((uint64_t)(tile + 1) * rows, (uint64_t)h.n * G) - 1;
+    const int64_t seen = (int64_t)h.ctx - h.n + (int64_t)(last / G) + 1;
+    return seen <= 0 ? 0u : (uint32_t)((seen + kStep - 1) / kStep);
+}
+
+// One workgroup.  Ranges are as long as spreads the call's steps over
+// `target` of them, so a batch of unequal sequences fills the card evenly; a
+// sequence no longer than one range is not split and writes its rows itself.
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
+    __shared__ uint32_t wsum[kPlanThreads / 64][3];
+    __shared__ uint32_t base[kPlanThreads + 1][3], geo[kPlanThreads][2];
+    __shared__ unsigned long long work;
+    if (threadIdx.x == 0) work = 0;
+    __syncthreads();
+    unsigned long long mine = 0;
+    for (uint32_t s = threadIdx.x; s < a.kv.n_seq; s += kPlanThreads) {
+        const Head h = seq_head(a.kv, s);
+        const uint64_t rt = ((uint64_t)h.n * a.G + a.tile_rows - 1) / a.tile_rows;
+        mine += rt * ((h.ctx + kStep - 1) / kStep);
+        if (!h.ok) report(a.kv);
+    }
+    atomicAdd(&work, mine);
+    __syncthreads();
+    unsigned long long len = (work + a.target - 1) / a.target;
+    if (len < a.least) len = a.least;
+    len = (len + a.round - 1) / a.round * a.round;
+    const uint32_t C = len > 0x7FFFFFFFull ? 0x7FFFFFFFu : (uint32_t)len;
+    uint32_t at[3] = {0, 0, 0};   // items, slots, joins so far
+    for (uint32_t s0 = 0; s0 < a.kv.n_seq; s0 += kPlanThreads) {
+        const uint32_t s = s0 + threadIdx.x;
+        uint32_t x[3] = {0, 0, 0}, rt = 0, sp = 1;
+        if (s < a.kv.n_seq) {
+            const Head h = seq_head(a.kv, s);
+            rt = (uint32_t)(((uint64_t)h.n * a.G + a.tile_rows - 1) / a.tile_rows);
+            const uint32_t kt = (h.ctx + kStep - 1) / kStep;
+            sp = kt > C ? (kt + C - 1) / C : 1u;
+            x[0] = rt * sp;
+            x[1] = sp > 1 ? x[0] : 0u;
+            x[2] = sp > 1 ? rt : 0u;
+        }
+        geo[threadIdx.x][0] = rt;
+        geo[threadIdx.x][1] = sp;
+        uint32_t tot[3];
+        scan3(x, tot, wsum);
+        for (int i = 0; i < 3; ++i) base[threadIdx.x][i] = x[i];
+        if (threadIdx.x == 0) base[kPlanThreads][0] = tot[0];
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < tot[0]; i += kPlanThreads) {
+            uint32_t lo = 0, hi = kPlanThreads;   // the last sequence that starts at or before i and has items
+            while (hi - lo > 1) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (base[mid][0] <= i) lo = mid; else hi = mid;
+            }
+            const uint32_t j = i - base[lo][0], n = geo[lo][0], p = geo[lo][1];
+            const uint32_t tile = n - 1 - j / p, part = j % p;   // the tiles that see most first
+            const Head h = seq_head(a.kv, s0 + lo);
+            const uint32_t end = tile_end(h, a.G, tile, a.tile_rows);
+            Item it;
+            it.seq = s0 + lo;
+            it.tile = tile;
+            it.k0 = part * C;
+            it.k1 = min(end, p > 1 ? (part + 1) * C : end);
+            const uint32_t slot = at[1] + base[lo][1] + tile * p + part;
+            it.slot = p > 1 ? slot : kNoSlot;
+            const uint32_t idx = at[0] + i;
+            if (idx < a.item_cap && (p == 1 || slot < a.slot_cap)) a.items[idx] = it;
+            if (p > 1 && part == 0) {
+                const uint32_t q = at[2] + base[lo][2] + tile;
+                if (q < a.join_cap) a.joins[q] = Join{s0 + lo, tile, slot, p};
+            }
+        }
+        for (int i = 0; i < 3; ++i) at[i] += tot[i];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *a.head = PlanHead{min(at[0], a.item_cap), min(at[2], a.join_cap), at[1], 0};
+    // rows of the sequences that cannot be answered
+    for (uint32_t s = 0; s < a.kv.n_seq; ++s) {
+        const Head h = seq_head(a.kv, s);
+        if (h.ok || !h.rows_ok) continue;
+        const uint64_t rows = a.kv.off[s + 1] - h.row0;
+        for (uint64_t i = threadIdx.x; i < rows * a.row_elems; i += kPlanThreads)
+            a.out[(h.row0 + i / a.row_elems) * a.out_stride + i % a.row_elems] = (uint16_t)a.nan16;
+    }
+}
+
+// ------------------------------------------------------------------ attention
+
+struct AttendArgs {
+    Kv kv;
+    uint32_t G, Hq, tile_rows;
+    uint64_t q_stride, out_stride;   // elements between tokens
+    const void *q;
+    void *out;
+    float c0;                        // scale * log2(e)
+    const PlanHead *head;
+    const Item *items;
+    float *part;                     // [slot][head][tile_rows][D]
+    f32x4 *part_ml;                  // [slot][head][tile_rows] m, l, y
+    float *lse;                      // [row][query head] log2 of the row's sum, or null
+    float *units;                    // [seq][head][unit][tile_rows] log2 of the unit's sum, or null
+    uint32_t n_units;
+};
+
+// What a part with maximum m counts for beside the maximum of all; a part
+// that saw nothing finite holds zeros, or NaN.
+__device__ inline float joined(float m, float all) { return m == -INFINITY ? 1.0f : exp2_of(m - all); }
+
+// One step's operands: keys of 64 tokens (lane: key row token, 16 dimensions)
+// and values (lane: dimension, 16 tokens).
+template <int D>
+struct KeyRegs {
+    u32x4 f[4][D / 64];
+};
+template <int D>
+struct ValRegs {
+    u32x4 f[D / 16];
+};
+
+// Attention of one row tile over steps [k0, k1), the maximum and sum of its
+// softmax kept as they run: with x = q.k scale log2(e), m the maximum of x so
+// far and l = sum 2^(x - m); with s a block's value scale and v its e4m3
+// values, y the maximum of x + log2(s) so far and O = sum 2^(x - y) s v.  The
+// row is O 2^(y - m) / l.
+//
+// A wavefront multiplies 16-row tiles of S^T = K Q^T and O^T = V^T P^T, so
+// that a lane of S^T (a query row, 16 tokens in a row) holds the very P^T
+// operand of the second product: the token that key row r of product t means
+// is 16 (r / 4) + 4 t + r % 4, and nothing moves between lanes.  P = 2^(x - y) s
+// is rounded to fp16 for both types of query, since e4m3 is exact in it: 11
+// bits for what is within 2^-14 of the largest (y is the maximum with s in it,
+// so that a block of small values that a row attends to keeps them).  l takes
+// the weights before that rounding.  A maximum is raised, and O rescaled, only
+// when it is passed by more than 2^8: P stays below 2^8.
+//
+// ROWS: the four wavefronts take row tiles of their own and the same tokens
+// (prompts); else the same rows and every fourth step, joined through LDS.
+template <int D, int NT, bool ROWS, bool HALF, bool UNITS>
+__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
+    typedef typename Elem<HALF>::T T;
+    typedef typename Elem<HALF>::T8 T8;
+    constexpr int kDT = D / 16;
+    constexpr int kPitch = D + 4;
+    __shared__ float lds[ROWS ? 4 : kWaves * 16 * kPitch];
+    __shared__ float lds_ml[ROWS ? 1 : kWaves][16 * NT][3];
+
+    const uint32_t hk = a.kv.hk;
+    const uint32_t h = blockIdx.x % hk, item = blockIdx.x / hk;
+    if (item >= a.head->n_items) return;
+    const Item it = a.items[item];
+    const Head hd = seq_head(a.kv, it.seq);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint32_t c = lane & 15, g = lane >> 4;
+    const uint32_t n_rows = hd.n * a.G;
+    const uint32_t row0 = it.tile * a.tile_rows + (ROWS ? w * 16 * NT : 0);
+    if (ROWS && row0 >= n_rows) return;
+    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep);
+    const uint64_t hb = head_bytes(a.kv, D);
+    const uint32_t *pages = a.kv.pages + (uint64_t)it.seq * a.kv.max_pages;
+    const uint32_t last_block = hd.ctx ? (hd.ctx - 1) >> a.kv.btl : 0u;
+
+    // queries: 16 dimensions a lane, as the keys
+    T8 qf[NT][D / 32];
+    uint32_t lim[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t r = row0 + n * 16 + c;
+        const bool valid = r < n_rows;
+        const uint32_t t = valid ? r / a.G : 0u, qh = h * a.G + (valid ? r % a.G : 0u);
+        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
+        lim[n] = !valid ? hd.ctx : seen > 0 ? (uint32_t)seen : 0u;
+        const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)qh * D + 16 * g;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            u32x4 x = {0, 0, 0, 0};
+            if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
+            qf[n][i] = __builtin_bit_cast(T8, x);
+        }
+    }
+    // tokens that every row of this wavefront sees, and that any does
+    const uint32_t row_last = min(row0 + (ROWS ? 16 * NT : a.tile_rows), n_rows) - 1;
+    const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
+    const int64_t see_any = (int64_t)hd.ctx - hd.n + row_last / a.G + 1;
+    const uint32_t all_lim = see_all > 0 ? (uint32_t)see_all : 0u;
+    const uint32_t end = min(it.k1, see_any > 0 ? (uint32_t)((see_any + kStep - 1) / kStep) : 0u);
+
+    f32x4 acc[NT][kDT];
+    float m[NT], l[NT], y[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = y[n] = -INFINITY;
+        l[n] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) acc[n][d] = f32x4{0, 0, 0, 0};
+    }
+
+    auto page_at = [&](uint32_t kt, uint32_t group) {
+        const uint32_t b = min((kt * kStep + 16 * group) >> a.kv.btl, last_block);
+        return pages[b];
+    };
+    auto load_keys = [&](KeyRegs<D> &x, uint32_t kt, uint32_t page) {
+        page = page < a.kv.n_pages ? page : 0u;
+        const uint32_t tok = ((kt * kStep + 16 * (c >> 2)) & (bt - 1)) + (c & 3);
+        const uint8_t *p = a.kv.k + ((uint64_t)page * hk + h) * hb + (uint64_t)tok * D + 16 * g;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) x.f[t][i] = *(const u32x4 *)(p + 4 * t * D + 64 * i);
+    };
+    auto load_vals = [&](ValRegs<D> &x, uint32_t kt, uint32_t page) {
+        page = page < a.kv.n_pages ? page : 0u;
+        const uint32_t tok = (kt * kStep + 16 * g) & (bt - 1);
+        const uint8_t *p = a.kv.v + ((uint64_t)page * hk + h) * hb + (uint64_t)(tok & ~(tile - 1)) * D + c * tile + (tok & (tile - 1));
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) x.f[d] = *(const u32x4 *)(p + d * 16 * tile);
+    };
+
+    constexpr uint32_t kBy = ROWS ? 1 : kWaves;
+    KeyRegs<D> kf;
+    ValRegs<D> vf;
+    for (uint32_t kt = it.k0 + (ROWS ? 0 : w); kt < end; kt += kBy) {
+        const uint32_t pk = page_at(kt, c >> 2), pv = page_at(kt, g);
+        load_keys(kf, kt, pk);
+        load_vals(vf, kt, pv);
+        const bool bad = pv >= a.kv.n_pages;
+        if (bad) report(a.kv);
+        const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk + h;
+        const float sc = bad ? NAN : a.kv.ks[si] * a.c0;
+        const float vsl = bad ? NAN : a.kv.vs[si], vlog = log2_of(vsl);
+
+        f32x4 st[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) st[n][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                const T8 lo = widen<HALF>(kf.f[t][i][0], kf.f[t][i][1]);
+                const T8 hi = widen<HALF>(kf.f[t][i][2], kf.f[t][i][3]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    st[n][t] = product(lo, qf[n][2 * i], st[n][t]);
+                    st[n][t] = product(hi, qf[n][2 * i + 1], st[n][t]);
+                }
+            }
+        const uint32_t tok0 = kt * kStep + 16 * g;
+        const bool masked = kt * kStep + kStep > all_lim;
+        bool grow = false;
+        float mx[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            mx[n] = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = st[n][t][i] * sc;
+                    if (masked && tok0 + 4 * t + i >= lim[n]) x = -INFINITY;
+                    st[n][t][i] = x;
+                    mx[n] = fmaxf(mx[n], x);
+                }
+            grow |= mx[n] > m[n] + kMaxGrow || mx[n] + vlog > y[n] + kMaxGrow;
+        }
+        if (__any(grow)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float mn = fmaxf(m[n], row_max(mx[n])), yn = fmaxf(y[n], row_max(mx[n] + vlog));
+                l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
+                const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
+                m[n] = mn;
+                y[n] = yn;
+#pragma unroll
+                for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
+            }
+        }
+        f16x8 pf[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float sum = 0.0f;
+            const float mm = m[n] == -INFINITY ? 0.0f : m[n];
+            const float f = y[n] == -INFINITY ? 0.0f : fminf(vsl * exp2_of(mm - y[n]), 3.0e38f);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                float p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[i] = exp2_of(st[n][t][i] - mm);
+                    sum += p[i];
+                }
+                const f16x2 x = __builtin_convertvector((f32x2{p[0] * f, p[1] * f}), f16x2);
+                const f16x2 y = __builtin_convertvector((f32x2{p[2] * f, p[3] * f}), f16x2);
+                const int j = 4 * (t & 1);
+                pf[n][t >> 1][j] = x[0];
+                pf[n][t >> 1][j + 1] = x[1];
+                pf[n][t >> 1][j + 2] = y[0];
+                pf[n][t >> 1][j + 3] = y[1];
+            }
+            l[n] += sum;
+            if constexpr (UNITS) {
+                // the unit's sum: 64 tokens are the row's four lanes, 32 two of them, 16 one
+                if (tile >= 32) sum = pair16_sum(sum);
+                if (tile >= 64) {
+                    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+                    sum = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+                }
+                const uint32_t per = kStep / tile;
+                const uint32_t u = kt * per + 16 * g / tile;
+                if (((16 * g) & (tile - 1)) == 0 && u < a.n_units)
+                    a.units[(((uint64_t)it.seq * hk + h) * a.n_units + u) * a.tile_rows + n * 16 + c] =
+                        mm + log2_of(sum);
+            }
+        }
+        if (masked) {
+            // tokens that no row holds: their bytes may be anything
+            const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
+            u32x4 keep;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int b = have - 4 * i;
+                keep[i] = b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << (8 * b)) - 1u;
+            }
+            bool nan = false;
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) {
+                vf.f[d] &= keep;
+                const u32x4 y = ((vf.f[d] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+                nan |= (y[0] | y[1] | y[2] | y[3]) != 0;
+            }
+            if (__any(nan)) {
+                // A NaN among values that some rows see and others do not: a
+                // product with P = 0 would carry it to all.  The rows that see
+                // one are found by a product of the masks, and it is left out
+                // of the values.
+                f16x8 see[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) see[n][j >> 3][j & 7] = tok0 + j < lim[n] ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+                for (int d = 0; d < kDT; ++d) {
+                    const u32x4 y = (((vf.f[d] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;   // 1 per NaN byte
+                    const u32x4 one = y * 0x38u;                                                     // 1.0 per NaN byte
+                    vf.f[d] &= ~(y * 0xFFu);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        f32x4 hit = {0, 0, 0, 0};
+                        hit = product(widen_f16(one[0], one[1]), see[n][0], hit);
+                        hit = product(widen_f16(one[2], one[3]), see[n][1], hit);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[n][d][i] = hit[i] > 0.0f ? NAN : acc[n][d][i];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) {
+            const f16x8 lo = widen_f16(vf.f[d][0], vf.f[d][1]);
+            const f16x8 hi = widen_f16(vf.f[d][2], vf.f[d][3]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                acc[n][d] = product(lo, pf[n][0], acc[n][d]);
+                acc[n][d] = product(hi, pf[n][1], acc[n][d]);
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) l[n] = row_sum(l[n]);
+
+    if constexpr (ROWS) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t tr = w * 16 * NT + n * 16 + c, r = row0 + n * 16 + c;
+            if (r >= n_rows) continue;
+            if (it.slot != kNoSlot) {
+                const uint64_t at = ((uint64_t)it.slot * hk + h) * a.tile_rows + tr;
+                if (g == 0) a.part_ml[at] = f32x4{m[n], l[n], y[n], 0.0f};
+#pragma unroll
+                for (int d = 0; d < kDT; ++d) *(f32x4 *)(a.part + at * D + d * 16 + 4 * g) = acc[n][d];
+            } else {
+                const uint64_t t = hd.row0 + r / a.G;
+                const uint32_t qh = h * a.G + r % a.G;
+                const float inv = l[n] == 0.0f ? 0.0f : exp2_of(y[n] - m[n]) / l[n];
+                T *out = (T *)a.out + t * a.out_stride + (uint64_t)qh * D + 4 * g;
+#pragma unroll
+                for (int d = 0; d < kDT; ++d) {
+                    T o[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = (T)(acc[n][d][i] * inv);
+                    *(u32x2 *)(out + d * 16) = *(u32x2 *)o;
+                }
+                if (a.lse && g == 0) a.lse[t * a.Hq + qh] = l[n] == 0.0f ? INFINITY : m[n] + log2_of(l[n]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (g == 0) {
+                lds_ml[w][n * 16 + c][0] = m[n];
+                lds_ml[w][n * 16 + c][1] = l[n];
+                lds_ml[w][n * 16 + c][2] = y[n];
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            __syncthreads();
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) *(f32x4 *)&lds[(w * 16 + c) * kPitch + d * 16 + 4 * g] = acc[n][d];
+            __syncthreads();
+            for (uint32_t e = threadIdx.x; e < 16 * D / 4; e += kThreads) {
+                const uint32_t row = e / (D / 4), d4 = e % (D / 4) * 4;
+                const uint32_t r = row0 + n * 16 + row;
+                if (r >= n_rows) continue;
+                float M = -INFINITY, Y = -INFINITY;
+                for (int v = 0; v < kWaves; ++v) {
+                    M = fmaxf(M, lds_ml[v][n * 16 + row][0]);
+                    Y = fmaxf(Y, lds_ml[v][n * 16 + row][2]);
+                }
+                float L = 0.0f;
+                f32x4 o = {0, 0, 0, 0};
+                for (int v = 0; v < kWaves; ++v) {
+                    const float *ml = lds_ml[v][n * 16 + row];
+                    L += joined(ml[0], M) * ml[1];
+                    const float f = joined(ml[2], Y);
+                    const f32x4 x = *(const f32x4 *)&lds[(v * 16 + row) * kPitch + d4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] += x[i] * f;
+                }
+                if (it.slot != kNoSlot) {
+                    const uint64_t at = ((uint64_t)it.slot * hk + h) * a.tile_rows + n * 16 + row;
+                    if (d4 == 0) a.part_ml[at] = f32x4{M, L, Y, 0.0f};
+                    *(f32x4 *)(a.part + at * D + d4) = o;
+                } else {
+                    const uint64_t t = hd.row0 + r / a.G;
+                    const uint32_t qh = h * a.G + r % a.G;
+                    const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
+                    T z[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) z[i] = (T)(o[i] * inv);
+                    *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + d4) = *(u32x2 *)z;
+                    if (a.lse && d4 == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
+                }
+            }
+        }
+    }
+}
+
+// Joins the ranges of one row: with M and Y the largest of their maxima,
+// O = sum 2^(y - Y) O_i, l = sum 2^(m - M) l_i.  A workgroup a row, its
+// threads the row's columns by four times a share of the ranges.
+template <int D, bool HALF>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, const Join *joins) {
+    typedef typename Elem<HALF>::T T;
+    constexpr int kCols = D / 4, kGroups = kThreads / kCols;
+    __shared__ f32x4 lo[kGroups][kCols];
+    __shared__ float ll[kGroups];
+    const uint32_t hk = a.kv.hk, rows = a.tile_rows;
+    const uint32_t col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
+    const uint64_t all = (uint64_t)a.head->n_joins * hk * rows;
+    for (uint64_t task = blockIdx.x; task < all; task += gridDim.x) {
+        const uint32_t tr = (uint32_t)(task % rows), h = (uint32_t)(task / rows % hk);
+        const Join j = joins[task / rows / hk];
+        const Head hd = seq_head(a.kv, j.seq);
+        const uint32_t r = j.tile * rows + tr;
+        if (r >= hd.n * a.G) continue;
+        auto at = [&](uint32_t i) { return ((uint64_t)(j.slot + i) * hk + h) * rows + tr; };
+        float M = -INFINITY, Y = -INFINITY;
+        for (uint32_t i = 0; i < j.n; ++i) {
+            const f32x4 ml = a.part_ml[at(i)];
+            M = fmaxf(M, ml[0]);
+            Y = fmaxf(Y, ml[2]);
+        }
+        float L = 0.0f;
+        f32x4 o = {0, 0, 0, 0};
+        for (uint32_t i = grp; i < j.n; i += kGroups) {
+            const f32x4 ml = a.part_ml[at(i)];
+            const f32x4 x = *(const f32x4 *)(a.part + at(i) * D + col * 4);
+            const float f = joined(ml[2], Y);
+            L += joined(ml[0], M) * ml[1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += f * x[e];
+        }
+        lo[grp][col] = o;
+        if (col == 0) ll[grp] = L;
+        __syncthreads();
+        if (grp == 0) {
+            L = 0.0f;
+            o = f32x4{0, 0, 0, 0};
+            for (int i = 0; i < kGroups; ++i) {
+                L += ll[i];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += lo[i][col][e];
+            }
+            const uint64_t t = hd.row0 + r / a.G;
+            const uint32_t qh = h * a.G + r % a.G;
+            const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
+            T z[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = (T)(o[e] * inv);
+            *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + col * 4) = *(u32x2 *)z;
+            if (a.lse && col == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ block weights
+
+struct WeightArgs {
+    float *w;            // [seq][max_pages]
+    float *cols;         // [seq][head][unit], or null
+};
+
+// Block weights of a call of few rows: a wavefront a block, lanes over (head,
+// row); every unit's sum was kept as its log2, so
+// w = sum over rows and units of 2^(unit - lse).
+__global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs wa) {
+    const uint32_t s = blockIdx.y, b = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (b >= a.kv.max_pages) return;
+    const Head hd = seq_head(a.kv, s);
+    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep), per = bt / tile;
+    const uint32_t have = (hd.ctx + tile - 1) / tile;   // units that hold tokens
+    const uint32_t u0 = b * per, u1 = min(u0 + per, have);
+    float sum = 0.0f;
+    if (u0 < u1)
+        for (uint32_t i = lane; i < hd.n * a.Hq; i += 64) {
+            const uint32_t h = i / (hd.n * a.G), row = i % (hd.n * a.G);
+            const float lse = a.lse[(hd.row0 + row / a.G) * a.Hq + h * a.G + row % a.G];
+            const float *p = a.units + (((uint64_t)s * a.kv.hk + h) * a.n_units + u0) * a.tile_rows + row;
+            for (uint32_t u = u0; u < u1; ++u, p += a.tile_rows) sum += exp2_of(*p - lse);
+        }
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    if (lane == 0) wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? sum : NAN;
+}
+
+// Block weights of a call of many rows: with every row's lse known, the
+// scores are formed once more, 64 tokens a workgroup against all rows, and
+// 2^(x - lse) is summed over them (a prompt's partial sums of every row would
+// be larger than its cache).
+template <int D, bool HALF>
+__global__ __launch_bounds__(kThreads) void column_kernel(AttendArgs a, WeightArgs wa) {
+    typedef typename Elem<HALF>::T T;
+    typedef typename Elem<HALF>::T8 T8;
+    __shared__ float lds[kWaves][4];
+    const uint32_t hk = a.kv.hk;
+    const uint32_t h = blockIdx.x % hk, kt = blockIdx.x / hk, s = blockIdx.y;
+    const Head hd = seq_head(a.kv, s);
+    if ((uint64_t)kt * kStep >= hd.ctx) return;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const uint32_t c = lane & 15, g = lane >> 4;
+    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep);
+    const uint32_t *pages = a.kv.pages + (uint64_t)s * a.kv.max_pages;
+    const uint32_t last_block = (hd.ctx - 1) >> a.kv.btl;
+    const uint32_t pk = pages[min((kt * kStep + 16 * (c >> 2)) >> a.kv.btl, last_block)];
+    const uint32_t pv = pages[min((kt * kStep + 16 * g) >> a.kv.btl, last_block)];
+    const bool bad = pv >= a.kv.n_pages;
+    const float sc = bad ? NAN : a.kv.ks[(uint64_t)pv * hk + h] * a.c0;
+    const uint32_t tok = ((kt * kStep + 16 * (c >> 2)) & (bt - 1)) + (c & 3);
+    const uint8_t *p = a.kv.k + ((uint64_t)(pk < a.kv.n_pages ? pk : 0u) * hk + h) * head_bytes(a.kv, D) + (uint64_t)tok * D + 16 * g;
+    T8 kf[4][D / 32];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            const u32x4 x = *(const u32x4 *)(p + 4 * t * D + 64 * i);
+            kf[t][2 * i] = widen<HALF>(x[0], x[1]);
+            kf[t][2 * i + 1] = widen<HALF>(x[2], x[3]);
+        }
+    const uint32_t tok0 = kt * kStep + 16 * g;
+    const uint32_t n_rows = hd.n * a.G;
+    // the first row that sees a token of this step
+    const int64_t t0 = (int64_t)kt * kStep - ((int64_t)hd.ctx - hd.n);
+    const uint32_t first = t0 > 0 ? (uint32_t)t0 * a.G : 0u;
+    float sum = 0.0f;
+    for (uint32_t r0 = first / 16 * 16 + 16 * w; r0 < n_rows; r0 += 16 * kWaves) {
+        const uint32_t r = r0 + c;
+        const bool valid = r < n_rows;
+        const uint32_t t = valid ? r / a.G : 0u, qh = h * a.G + (valid ? r % a.G : 0u);
+        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
+        const uint32_t lim = valid && seen > 0 ? (uint32_t)seen : 0u;
+        const float lse = valid ? a.lse[(hd.row0 + t) * a.Hq + qh] : 0.0f;
+        const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)qh * D + 16 * g;
+        f32x4 st[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            u32x4 x = {0, 0, 0, 0};
+            if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
+            const T8 qf = __builtin_bit_cast(T8, x);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) st[u] = product(kf[u][i], qf, st[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = exp2_of(st[u][i] * sc - lse);
+                sum += tok0 + 4 * u + i < lim ? e : 0.0f;
+            }
+    }
+    // over the rows (16 lanes), then the group's 16 tokens join their unit
+    for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor(sum, d, 64);
+    if (c == 0) lds[w][g] = sum;
+    __syncthreads();
+    const uint32_t per = kStep / tile, gr = tile / 16;
+    if (threadIdx.x < per) {
+        float x = 0.0f;
+        for (uint32_t i = 0; i < gr; ++i)
+            for (int v = 0; v < kWaves; ++v) x += lds[v][threadIdx.x * gr + i];
+        const uint32_t u = kt * per + threadIdx.x;
+        if (u < a.n_units) wa.cols[((uint64_t)s * hk + h) * a.n_units + u] = x;
+    }
+}
+
+// The units of a block and the heads, in order.
+__global__ __launch_bounds__(kThreads) void block_kernel(AttendArgs a, WeightArgs wa) {
+    const uint32_t s = blockIdx.y, b = blockIdx.x * kThreads + threadIdx.x;
+    if (b >= a.kv.max_pages) return;
+    const Head hd = seq_head(a.kv, s);
+    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep), per = bt / tile;
+    const uint32_t have = (hd.ctx + tile - 1) / tile;
+    const uint32_t u0 = b * per, u1 = min(u0 + per, have);
+    float sum = 0.0f;
+    if (hd.n)
+        for (uint32_t h = 0; h < a.kv.hk; ++h)
+            for (uint32_t u = u0; u < u1; ++u) sum += wa.cols[((uint64_t)s * a.kv.hk + h) * a.n_units + u];
+    wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? sum : NAN;
+}
+
+// A page's weight is the sum over the sequences that hold it, in fixed point
+// (2^-24 of one row's whole attention) so that their order does not matter.
+__global__ __launch_bounds__(kThreads) void weigh_kernel(Kv a, const float *w, unsigned long long *page_weight) {
+    const uint32_t s = blockIdx.y, b = blockIdx.x * kThreads + threadIdx.x;
+    const uint32_t held = a.ctx[s];
+    if ((uint64_t)held > ((uint64_t)a.max_pages << a.btl)) {
+        if (b == 0) report(a);
+        return;
+    }
+    if (b >= (held + (1u << a.btl) - 1) >> a.btl) return;
+    const uint32_t page = a.pages[(uint64_t)s * a.max_pages + b];
+    const float x = w[(uint64_t)s * a.max_pages + b];
+    if (page >= a.n_pages || !(x >= 0.0f && x < 4294967296.0f)) {
+        report(a);
+        return;
+    }
+    const unsigned long long q = (unsigned long long)rint((double)x * 16777216.0);
+    if (q) atomicAdd(page_weight + page, q);
+}
+
+// ------------------------------------------------------------------ store and read
+
+// The `task`-th of the sequences' consecutive shares, where count(s) is
+// sequence s's: found by the whole workgroup, 256 sequences at a time.
+// Returns the sequence (n_seq if there is none) and the share in `rest`.
+template <typename F>
+__device__ inline uint32_t locate(uint32_t n_seq, uint64_t task, F count, uint64_t *rest) {
+    __shared__ unsigned long long sums[kWaves];
+    __shared__ uint32_t found;
+    __shared__ unsigned long long left;
+    const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) & (kWaves - 1);
+    const bool in = threadIdx.x < kThreads;
+    if (threadIdx.x == 0) found = n_seq;
+    unsigned long long before = 0;
+    for (uint32_t s0 = 0; s0 < n_seq; s0 += kThreads) {
+        const uint32_t s = s0 + threadIdx.x;
+        const unsigned long long x = in && s < n_seq ? count(s) : 0ull;
+        unsigned long long y = x;
+        for (int d = 1; d < 64; d <<= 1) {
+            const unsigned long long z = __shfl_up(y, d, 64);
+            if (lane >= d) y += z;
+        }
+        if (in && lane == 63) sums[w] = y;
+        __syncthreads();
+        unsigned long long base = before, all = 0;
+        for (int v = 0; v < kWaves; ++v) {
+            if (v < w) base += sums[v];
+            all += sums[v];
+        }
+        y += base;   // inclusive
+        if (in && x && task >= y - x && task < y) {
+            found = s;
+            left = task - (y - x);
+        }
+        __syncthreads();
+        before += all;
+        if (found < n_seq || task < before) break;
+    }
+    __syncthreads();
+    *rest = left;
+    return found;
+}
+
+struct MoveArgs {
+    Kv kv;
+    const void *k, *v;            // store: the new rows; read: the outputs
+    uint64_t k_stride, v_stride;
+};
+
+// The smallest power of two s >= 2^-126 with amax <= 448 s: 448 = 1.75 * 2^8.
+__device__ inline float scale_for(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    int e = (int)(b >> 23) - 127;
+    if (e < -126) return 1.17549435e-38f;
+    e += (b & 0x7FFFFFu) <= 0x600000u ? -8 : -7;
+    e = e < -126 ? -126 : e;
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+__device__ inline float to_f32(uint32_t bits16, bool half) {
+    return half ? (float)__builtin_bit_cast(_Float16, (uint16_t)bits16) : __uint_as_float(bits16 << 16);
+}
+
+// Four values to e4m3, nearest even; what is not finite becomes NaN.
+__device__ inline uint32_t narrow4(const float *x, float inv) {
+    int r = 0;
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, r, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, r, true);
+    uint32_t y = (uint32_t)r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (!(fabsf(x[i]) < INFINITY)) y = (y & ~(0xFFu << (8 * i))) | (0x7Fu << (8 * i));
+    return y;
+}
+
+// Four e4m3 bytes under another scale (ratio <= 1, a power of two).
+__device__ inline uint32_t rescale4(uint32_t x, float ratio) {
+    const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false);
+    const f16x2 q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true);
+    const float y[4] = {(float)p[0], (float)p[1], (float)q[0], (float)q[1]};
+    return narrow4(y, ratio);
+}
+
+// One workgroup quantises the keys (blockIdx.z = 0) or values of one head
+// that a call brings to one block.  The block's scale is the smallest power of
+// two that holds them, or the present one if the block was begun with a larger
+// one; where it grows, what the block holds is brought under the new scale
+// (exact but for values that become subnormal).
+template <int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
+    constexpr int kEach = 8;                                  // 16-byte pieces a thread keeps
+    __shared__ float red[THREADS / 64];
+    const Kv &kv = a.kv;
+    const uint32_t bt = 1u << kv.btl;
+    uint64_t rest;
+    const uint32_t s = locate(kv.n_seq, blockIdx.x, [&](uint32_t q) -> unsigned long long {
+        const Head h = seq_head(kv, q);
+        if (!h.n || h.n > h.ctx) return 0;
+        return ((h.ctx - 1) >> kv.btl) - ((h.ctx - h.n) >> kv.btl) + 1;
+    }, &rest);
+    if (s >= kv.n_seq) return;
+    const Head hd = seq_head(kv, s);
+    const uint32_t start = hd.ctx - hd.n;                     // the first new token
+    const uint32_t blk = (start >> kv.btl) + (uint32_t)rest;
+    const uint32_t page = kv.pages[(uint64_t)s * kv.max_pages + blk];
+    if (page >= kv.n_pages) {
+        if (threadIdx.x == 0) report(kv);
+        return;
+    }
+    const bool vals = blockIdx.z;
+    const uint32_t h = blockIdx.y;
+    const uint32_t p0 = max(start, blk << kv.btl) - (blk << kv.btl);     // slots [p0, p1) are new
+    const uint32_t p1 = min(hd.ctx - (blk << kv.btl), bt);
+    const uint64_t row0 = hd.row0 + ((blk << kv.btl) + p0 - start);
+    const uint16_t *src = (const uint16_t *)(vals ? a.v : a.k);
+    const uint64_t stride = vals ? a.v_stride : a.k_stride;
+    const uint64_t at = (uint64_t)page * kv.hk + h;
+    uint8_t *dst = (vals ? kv.v : kv.k) + at * head_bytes(kv, D);
+    float *scale = (vals ? kv.vs : kv.ks) + at;
+    const uint32_t pieces = (p1 - p0) * (D / 8);
+
+    u32x4 x[kEach];
+    auto load = [&](uint32_t base) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t e = base + i * THREADS + threadIdx.x;
+            if (e < pieces) x[i] = *(const u32x4 *)(src + (row0 + e / (D / 8)) * stride + (uint64_t)h * D + e % (D / 8) * 8);
+        }
+    };
+    float amax = 0.0f;
+    for (uint32_t base = 0; base < pieces; base += THREADS * kEach) {
+        load(base);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (base + i * THREADS + threadIdx.x < pieces)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const float y = fabsf(to_f32(q ? x[i][j] >> 16 : x[i][j] & 0xFFFFu, half));
+                        amax = y < INFINITY ? fmaxf(amax, y) : amax;
+                    }
+    }
+    for (int d = 32; d; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = amax;
+    __syncthreads();
+    for (int i = 0; i < THREADS / 64; ++i) amax = fmaxf(amax, red[i]);
+    float sc = scale_for(amax);
+    if (p0) {
+        const float was = *scale;
+        sc = was > sc ? was : sc;
+        if (was != sc) {
+            const float ratio = was / sc;
+            if (!vals) {
+                for (uint32_t i = threadIdx.x; i < p0 * (D / 4); i += THREADS) ((uint32_t *)dst)[i] = rescale4(((uint32_t *)dst)[i], ratio);
+            } else {
+                // by 4 tokens of a dimension; a group that the new tokens share with old ones by bytes
+                const uint32_t tile = min(bt, kStep), quads = (p0 + 3) / 4;
+                for (uint32_t i = threadIdx.x; i < quads * D; i += THREADS) {
+                    const uint32_t d = i % D, tok = i / D * 4;
+                    uint8_t *p = dst + (uint64_t)(tok & ~(tile - 1)) * D + d * tile + (tok & (tile - 1));
+                    const uint32_t y = rescale4(*(uint32_t *)p, ratio);
+                    if (tok + 4 <= p0)
+                        *(uint32_t *)p = y;
+                    else
+                        for (uint32_t j = 0; tok + j < p0; ++j) p[j] = (uint8_t)(y >> (8 * j));
+                }
+            }
+        }
+    }
+    __syncthreads();   // every thread has read the old scale
+    if (threadIdx.x == 0) *scale = sc;
+    const float inv = 1.0f / sc;
+    const uint32_t tile = min(bt, kStep);
+    for (uint32_t base = 0; base < pieces; base += THREADS * kEach) {
+        if (pieces > THREADS * kEach) load(base);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t e = base + i * THREADS + threadIdx.x;
+            u32x2 y = {0, 0};
+            if (e < pieces) {
+                float z[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    z[2 * j] = to_f32(x[i][j] & 0xFFFFu, half);
+                    z[2 * j + 1] = to_f32(x[i][j] >> 16, half);
+                }
+                y = u32x2{narrow4(z, inv), narrow4(z + 4, inv)};
+            }
+            const uint32_t tok = p0 + e / (D / 8), d = e % (D / 8) * 8;
+            if (!vals) {
+                if (e < pieces) *(u32x2 *)(dst + (uint64_t)tok * D + d) = y;
+            } else if (e < pieces) {
+                uint8_t *p = dst + (uint64_t)(tok & ~(tile - 1)) * D + (uint64_t)d * tile + (tok & (tile - 1));
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j * tile] = (uint8_t)(y[j >> 2] >> (8 * (j & 3)));
+            }
+        }
+    }
+}
+
+// Reports the sequences that a store or a read leaves out.
+__global__ __launch_bounds__(kThreads) void check_kernel(Kv kv) {
+    const uint32_t s = blockIdx.x * kThreads + threadIdx.x;
+    if (s >= kv.n_seq) return;
+    const Head h = seq_head(kv, s);
+    if (!h.ok || h.n > h.ctx) report(kv);
+}
+
+// One workgroup gives back up to 64 tokens (one tile of positions) of one
+// head: keys in rows as they lie, values turned through LDS.
+template <int D>
+__global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
+    __shared__ uint32_t turn[D * (kStep + 4) / 4];
+    const Kv &kv = a.kv;
+    uint64_t rest;
+    const uint32_t s = locate(kv.n_seq, blockIdx.x, [&](uint32_t q) -> unsigned long long {
+        const Head h = seq_head(kv, q);
+        if (!h.n || h.n > h.ctx) return 0;
+        return (h.ctx - 1) / kStep - (h.ctx - h.n) / kStep + 1;
+    }, &rest);
+    if (s >= kv.n_seq) return;
+    const Head hd = seq_head(kv, s);
+    const uint32_t start = hd.ctx - hd.n, h = blockIdx.y, bt = 1u << kv.btl, tile = min(bt, kStep);
+    const uint32_t q0 = (start / kStep + (uint32_t)rest) * kStep;
+    const uint32_t t0 = max(start, q0), t1 = min(hd.ctx, q0 + kStep);
+    const uint32_t *pages = kv.pages + (uint64_t)s * kv.max_pages;
+    auto put8 = [&](void *base, uint64_t stride, uint32_t tok, uint32_t d, u32x2 y, float sc) {
+        const f16x8 z = widen_f16(y[0], y[1]);
+        u32x4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f32x2 p = {(float)z[2 * j] * sc, (float)z[2 * j + 1] * sc};
+            o[j] = half ? __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2))
+                        : __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+        }
+        *(u32x4 *)((uint16_t *)base + (hd.row0 + (tok - start)) * stride + (uint64_t)h * D + d) = o;
+    };
+    for (uint32_t e = threadIdx.x; e < (t1 - t0) * (D / 8); e += kThreads) {
+        const uint32_t tok = t0 + e / (D / 8), d = e % (D / 8) * 8;
+        const uint32_t page = pages[tok >> kv.btl];
+        const bool bad = page >= kv.n_pages;
+        if (bad) report(kv);
+        const uint64_t at = (uint64_t)(bad ? 0u : page) * kv.hk + h;
+        const u32x2 y = *(const u32x2 *)(kv.k + at * head_bytes(kv, D) + (uint64_t)(tok & (bt - 1)) * D + d);
+        put8((void *)a.k, a.k_stride, tok, d, y, bad ? NAN : kv.ks[at]);
+    }
+    // four tokens of a dimension a thread
+    uint8_t *tb = (uint8_t *)turn;
+    for (uint32_t e = threadIdx.x; e < D * (kStep / 4); e += kThreads) {
+        const uint32_t q = e % (tile / 4), d = e / (tile / 4) % D, tok = q0 + e / (tile / 4) / D * tile + q * 4;
+        if (tok >= t1 || tok + 4 <= t0) continue;
+        const uint32_t page = pages[tok >> kv.btl];
+        const uint64_t at = (uint64_t)(page < kv.n_pages ? page : 0u) * kv.hk + h;
+        const uint32_t slot = tok & (bt - 1);
+        const uint32_t y = *(const uint32_t *)(kv.v + at * head_bytes(kv, D) + (uint64_t)(slot & ~(tile - 1)) * D + d * tile + (slot & (tile - 1)));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tb[(tok - q0 + j) * (D + 4) + d] = (uint8_t)(y >> (8 * j));
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < (t1 - t0) * (D / 8); e += kThreads) {
+        const uint32_t tok = t0 + e / (D / 8), d = e % (D / 8) * 8;
+        const uint32_t page = pages[tok >> kv.btl];
+        const bool bad = page >= kv.n_pages;
+        const uint32_t *p = (const uint32_t *)(tb + (tok - q0) * (D + 4) + d);
+        put8((void *)a.v, a.v_stride, tok, d, u32x2{p[0], p[1]}, bad ? NAN : kv.vs[(uint64_t)page * kv.hk + h]);
+    }
+}
+
+// ------------------------------------------------------------------ host
+
+struct DeviceScope {
+    int prev = -1;
+    explicit DeviceScope(int dev) {
+        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+        if (prev == dev) prev = -1;
+        else (void)hipSetDevice(dev);
+    }
+    ~DeviceScope() {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
+netkv_status invalid(netkv_handle h, const char *msg) { return netkv_internal_fail(h, NETKV_EINVAL, msg); }
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// Checks what the host can and fills the kernels' view of it.
+netkv_status make_kv(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *q, Kv &a) {
+    if (!kv || !q) return invalid(h, "kv and seqs must not be NULL");
+    uint32_t btl = 0;
+    while (btl < 31 && (1u << btl) < kv->block_tokens) ++btl;
+    if (kv->block_tokens < 16 || kv->block_tokens > 1024 || (1u << btl) != kv->block_tokens)
+        return invalid(h, "block_tokens must be a power of two from 16 to 1024");
+    if (kv->head_dim != 64 && kv->head_dim != 128 && kv->head_dim != 256) return invalid(h, "head_dim must be 64, 128 or 256");
+    if (kv->n_kv_heads < 1 || kv->n_kv_heads > 1024) return invalid(h, "n_kv_heads must be in [1, 1024]");
+    if (kv->n_pages < 1 || kv->n_pages > 0x7FFFFFFFu) return invalid(h, "n_pages must be in [1, 2^31)");
+    if (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale) return invalid(h, "a cache array is NULL");
+    if (!aligned16(kv->k) || !aligned16(kv->v)) return invalid(h, "k and v must be 16-byte aligned");
+    if (q->n_seq && (!q->tok_off || !q->ctx_len || !q->pages)) return invalid(h, "a sequence array is NULL");
+    if (q->n_seq > 65535) return invalid(h, "n_seq must be <= 65535");
+    if (q->n_seq && q->max_pages < 1) return invalid(h, "max_pages must be >= 1");
+    if (((uint64_t)q->max_pages << btl) > (1ull << 31)) return invalid(h, "max_pages * block_tokens must be <= 2^31");
+    if (q->n_tok > (1ull << 31)) return invalid(h, "n_tok must be <= 2^31");
+    a.k = (uint8_t *)kv->k;
+    a.v = (uint8_t *)kv->v;
+    a.ks = kv->k_scale;
+    a.vs = kv->v_scale;
+    a.n_pages = kv->n_pages;
+    a.hk = kv->n_kv_heads;
+    a.btl = btl;
+    a.n_seq = q->n_seq;
+    a.max_pages = q->max_pages;
+    a.max_tok = (uint32_t)(q->max_tok < q->n_tok ? q->max_tok : q->n_tok);
+    a.off = q->tok_off;
+    a.ctx = q->ctx_len;
+    a.pages = q->pages;
+    a.n_tok = q->n_tok;
+    a.err = netkv_internal_errword(h);
+    return NETKV_OK;
+}
+
+constexpr uint64_t align256(uint64_t x) { return (x + 255) & ~255ull; }
+
+// How a call is split, and its workspace.
+struct Layout {
+    int NT;
+    bool rows;             // the wavefronts take rows of their own
+    uint32_t G, tile_rows, target, item_cap, slot_cap, join_cap, n_units;
+    uint64_t head, items, joins, ml, part, lse, units, cols, total;
+};
+
+netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads, bool weights, Layout &y) {
+    if (heads < 1 || heads % a.hk) return invalid(h, "n_heads must be a multiple of n_kv_heads");
+    y.G = heads / a.hk;
+    if (y.G > 64) return invalid(h, "n_heads / n_kv_heads must be <= 64");
+    const uint64_t most = (uint64_t)a.max_tok * y.G;   // rows of the longest sequence's head
+    if (most > 0xFFFFFFFFull - 1024) return invalid(h, "max_tok * n_heads / n_kv_heads must be < 2^32 - 1024");
+    y.rows = most > (D == 256 ? 32u : 64u);
+    y.NT = y.rows ? (D == 256 ? 2 : 4) : most <= 16 ? 1 : most <= 32 ? 2 : 4;
+    y.tile_rows = 16u * y.NT * (y.rows ? kWaves : 1);
+    y.target = ((y.rows ? 512u : 1024u) + a.hk - 1) / a.hk;
+    const uint64_t tiles = a.n_tok * y.G / y.tile_rows + a.n_seq;
+    const uint64_t items = 2ull * y.target + tiles;
+    if (items * a.hk > (1ull << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
+    y.item_cap = (uint32_t)items;
+    y.slot_cap = 2 * y.target;
+    y.join_cap = y.target;
+    const uint32_t bt = 1u << a.btl;
+    y.n_units = (uint32_t)(((uint64_t)a.max_pages << a.btl) / (bt < kStep ? bt : kStep)) + (uint32_t)(kStep / 16);
+    if (weights && (((uint64_t)a.max_pages << a.btl) / kStep + 1) * a.hk > (1ull << 24))
+        return netkv_internal_fail(h, NETKV_ECAPACITY, "too many cache blocks for one call with weights");
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        const uint64_t p = at;
+        at += align256(bytes);
+        return p;
+    };
+    y.head = take(sizeof(PlanHead));
+    y.items = take(sizeof(Item) * items);
+    y.joins = take(sizeof(Join) * y.join_cap);
+    y.ml = take(16ull * y.slot_cap * a.hk * y.tile_rows);
+    y.part = take(4ull * y.slot_cap * a.hk * y.tile_rows * D);
+    y.lse = y.units = y.cols = 0;
+    if (weights) {
+        y.lse = take(4ull * a.n_tok * heads);
+        const uint64_t u = (uint64_t)a.n_seq * a.hk * y.n_units;
+        if (y.rows)
+            y.cols = take(4 * u);
+        else
+            y.units = take(4 * u * y.tile_rows);
+    }
+    y.total = at;
+    return NETKV_OK;
+}
+
+template <int D, bool HALF>
+void launch_attend(const Layout &y, const AttendArgs &a, const Join *joins, const WeightArgs &wa, hipStream_t s) {
+    const dim3 grid(y.item_cap * a.kv.hk);
+#define NETKV_ATTEND(NT, ROWS, UNITS) attend_kernel<D, NT, ROWS, HALF, UNITS><<<grid, kThreads, 0, s>>>(a)
+    if (y.rows) {
+        if constexpr (D == 256)
+            NETKV_ATTEND(2, true, false);
+        else
+            NETKV_ATTEND(4, true, false);
+    } else if (y.NT == 1) {
+        if (wa.w) NETKV_ATTEND(1, false, true);
+        else NETKV_ATTEND(1, false, false);
+    } else if (y.NT == 2) {
+        if (wa.w) NETKV_ATTEND(2, false, true);
+        else NETKV_ATTEND(2, false, false);
+    } else if constexpr (D != 256) {
+        if (wa.w) NETKV_ATTEND(4, false, true);
+        else NETKV_ATTEND(4, false, false);
+    }
+#undef NETKV_ATTEND
+    const uint64_t joins_most = (uint64_t)y.join_cap * a.kv.hk * y.tile_rows;
+    join_kernel<D, HALF><<<(uint32_t)(joins_most < 2048 ? joins_most : 2048), kThreads, 0, s>>>(a, joins);
+    if (!wa.w) return;
+    if (y.rows) {
+        const uint32_t steps = (uint32_t)((((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep);
+        column_kernel<D, HALF><<<dim3(steps * a.kv.hk, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
+        block_kernel<<<dim3((a.kv.max_pages + kThreads - 1) / kThreads, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
+    } else {
+        unit_kernel<<<dim3((a.kv.max_pages + kWaves - 1) / kWaves, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
+    }
+}
+
+netkv_status launched(netkv_handle h, const char *what) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? NETKV_OK : netkv_internal_fail(h, NETKV_EDEVICE, what);
+}
+
+netkv_status check_rows(netkv_handle h, const void *p, uint64_t stride, uint64_t width, uint64_t n_tok, const char *msg) {
+    if (n_tok && (!p || !aligned16(p) || stride % 8 || stride < width)) return invalid(h, msg);
+    return NETKV_OK;
+}
+
+}  // namespace
+
+extern "C" netkv_status netkv_kv_attend_workspace(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
+                                                  uint32_t n_heads, int weights, uint64_t *bytes) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    if (!bytes) return invalid(h, "bytes must not be NULL");
+    Kv a{};
+    netkv_status st = make_kv(h, kv, seqs, a);
+    if (st != NETKV_OK) return st;
+    Layout y{};
+    st = make_layout(h, a, kv->head_dim, n_heads, weights != 0, y);
+    if (st != NETKV_OK) return st;
+    *bytes = y.total;
+    return NETKV_OK;
+}
+
+extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *q,
+                                        int dtype, uint32_t n_heads, uint64_t q_stride, float scale, void *out,
+                                        uint64_t out_stride, float *block_weight, void *work, uint64_t work_bytes,
+                                        void *stream) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    Kv a{};
+    netkv_status st = make_kv(h, kv, seqs, a);
+    if (st != NETKV_OK) return st;
+    if (dtype != NETKV_BF16 && dtype != NETKV_FP16) return invalid(h, "dtype must be NETKV_BF16 or NETKV_FP16");
+    Layout y{};
+    st = make_layout(h, a, kv->head_dim, n_heads, block_weight != nullptr, y);
+    if (st != NETKV_OK) return st;
+    if (!std::isfinite(scale)) return invalid(h, "scale must be finite");
+    const uint64_t width = (uint64_t)n_heads * kv->head_dim;
+    if ((st = check_rows(h, q, q_stride, width, a.n_tok, "q must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    if ((st = check_rows(h, out, out_stride, width, a.n_tok, "out must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    if (a.n_seq == 0) return NETKV_OK;
+    if (!work || ((uintptr_t)work & 255) || work_bytes < y.total) return invalid(h, "work must be 256-byte aligned and of at least netkv_kv_attend_workspace's bytes");
+    DeviceScope scope(netkv_internal_device(h));
+    hipStream_t s = (hipStream_t)stream;
+    uint8_t *ws = (uint8_t *)work;
+    const bool half = dtype == NETKV_FP16;
+    PlanArgs p{};
+    p.kv = a;
+    p.G = y.G;
+    p.tile_rows = y.tile_rows;
+    p.target = y.target;
+    p.least = y.rows ? 8 : kWaves;
+    p.round = y.rows ? 1 : kWaves;
+    p.item_cap = y.item_cap;
+    p.slot_cap = y.slot_cap;
+    p.join_cap = y.join_cap;
+    p.head = (PlanHead *)(ws + y.head);
+    p.items = (Item *)(ws + y.items);
+    p.joins = (Join *)(ws + y.joins);
+    p.out = (uint16_t *)out;
+    p.out_stride = out_stride;
+    p.row_elems = (uint32_t)width;
+    p.nan16 = half ? 0x7E00u : 0x7FC0u;
+    plan_kernel<<<1, kPlanThreads, 0, s>>>(p);
+    AttendArgs t{};
+    t.kv = a;
+    t.G = y.G;
+    t.Hq = n_heads;
+    t.tile_rows = y.tile_rows;
+    t.q_stride = q_stride;
+    t.out_stride = out_stride;
+    t.q = q;
+    t.out = out;
+    t.c0 = scale * kLog2e;
+    t.head = p.head;
+    t.items = p.items;
+    t.part = (float *)(ws + y.part);
+    t.part_ml = (f32x4 *)(ws + y.ml);
+    t.lse = block_weight ? (float *)(ws + y.lse) : nullptr;
+    t.units = block_weight && !y.rows ? (float *)(ws + y.units) : nullptr;
+    t.n_units = y.n_units;
+    WeightArgs wa{};
+    wa.w = block_weight;
+    wa.cols = y.rows ? (float *)(ws + y.cols) : nullptr;
+    switch (kv->head_dim) {
+        case 64: half ? launch_attend<64, true>(y, t, p.joins, wa, s) : launch_attend<64, false>(y, t, p.joins, wa, s); break;
+        case 128: half ? launch_attend<128, true>(y, t, p.joins, wa, s) : launch_attend<128, false>(y, t, p.joins, wa, s); break;
+        default: half ? launch_attend<256, true>(y, t, p.joins, wa, s) : launch_attend<256, false>(y, t, p.joins, wa, s); break;
+    }
+    return launched(h, "attention launch failed");
+}
+
+extern "C" netkv_status netkv_kv_weigh(netkv_handle h, const netkv_kv_seqs_t *q, uint32_t block_tokens, const float *block_weight,
+                                       uint32_t n_pages, uint64_t *page_weight, void *stream) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    // the cache itself is not touched: any address stands for it in the checks
+    netkv_kv_t kv{};
+    kv.n_pages = n_pages;
+    kv.block_tokens = block_tokens;
+    kv.n_kv_heads = 1;
+    kv.head_dim = 64;
+    kv.k = kv.v = (uint8_t *)16;
+    kv.k_scale = kv.v_scale = (float *)16;
+    Kv a{};
+    netkv_status st = make_kv(h, &kv, q, a);
+    if (st != NETKV_OK) return st;
+    if (a.n_seq == 0) return NETKV_OK;
+    if (!block_weight || !page_weight) return invalid(h, "block_weight and page_weight must not be NULL");
+    DeviceScope scope(netkv_internal_device(h));
+    weigh_kernel<<<dim3((a.max_pages + kThreads - 1) / kThreads, a.n_seq), kThreads, 0, (hipStream_t)stream>>>(
+        a, block_weight, (unsigned long long *)page_weight);
+    return launched(h, "weight launch failed");
+}
+
+namespace {
+
+template <int D>
+void launch_store(const MoveArgs &a, bool half, uint32_t tasks, uint32_t rows, hipStream_t s) {
+    const dim3 grid(tasks, a.kv.hk, 2);
+    // one pass over the data where the workgroup's registers hold a block's rows
+    if (rows * (uint32_t)D <= 256 * 64)
+        store_kernel<D, 256><<<grid, 256, 0, s>>>(a, half);
+    else
+        store_kernel<D, 1024><<<grid, 1024, 0, s>>>(a, half);
+}
+
+}  // namespace
+
+extern "C" netkv_status netkv_kv_store(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *k,
+                                       uint64_t k_stride, const void *v, uint64_t v_stride, int dtype, void *stream) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    MoveArgs a{};
+    netkv_status st = make_kv(h, kv, seqs, a.kv);
+    if (st != NETKV_OK) return st;
+    if (dtype != NETKV_BF16 && dtype != NETKV_FP16) return invalid(h, "dtype must be NETKV_BF16 or NETKV_FP16");
+    const uint64_t width = (uint64_t)kv->n_kv_heads * kv->head_dim;
+    if ((st = check_rows(h, k, k_stride, width, a.kv.n_tok, "k must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    if ((st = check_rows(h, v, v_stride, width, a.kv.n_tok, "v must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    if (a.kv.n_seq == 0 || a.kv.n_tok == 0) return NETKV_OK;
+    a.k = k;
+    a.v = v;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    // blocks that the rows can touch: n rows of a sequence at most n / bt + 2, and at most n
+    uint64_t tasks = (a.kv.n_tok >> a.kv.btl) + 2ull * a.kv.n_seq;
+    if (tasks > a.kv.n_tok) tasks = a.kv.n_tok;
+    if (tasks > (1u << 22)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many blocks for one call");
+    DeviceScope scope(netkv_internal_device(h));
+    hipStream_t s = (hipStream_t)stream;
+    const bool half = dtype == NETKV_FP16;
+    const uint32_t rows = a.kv.max_tok < kv->block_tokens ? a.kv.max_tok : kv->block_tokens;
+    check_kernel<<<(a.kv.n_seq + kThreads - 1) / kThreads, kThreads, 0, s>>>(a.kv);
+    switch (kv->head_dim) {
+        case 64: launch_store<64>(a, half, (uint32_t)tasks, rows, s); break;
+        case 128: launch_store<128>(a, half, (uint32_t)tasks, rows, s); break;
+        default: launch_store<256>(a, half, (uint32_t)tasks, rows, s); break;
+    }
+    return launched(h, "store launch failed");
+}
+
+extern "C" netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, void *k,
+                                      uint64_t k_stride, void *v, uint64_t v_stride, int dtype, void *stream) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    MoveArgs a{};
+    netkv_status st = make_kv(h, kv, seqs, a.kv);
+    if (st != NETKV_OK) return st;
+    if (dtype != NETKV_BF16 && dtype != NETKV_FP16) return invalid(h, "dtype must be NETKV_BF16 or NETKV_FP16");
+    const uint64_t width = (uint64_t)kv->n_kv_heads * kv->head_dim;
+    if ((st = check_rows(h, k, k_stride, width, a.kv.n_tok, "k must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    if ((st = check_rows(h, v, v_stride, width, a.kv.n_tok, "v must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    if (a.kv.n_seq == 0 || a.kv.n_tok == 0) return NETKV_OK;
+    a.k = k;
+    a.v = v;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    uint64_t tasks = a.kv.n_tok / kStep + 2ull * a.kv.n_seq;
+    if (tasks > a.kv.n_tok) tasks = a.kv.n_tok;
+    if (tasks > (1u << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many tokens for one call");
+    DeviceScope scope(netkv_internal_device(h));
+    hipStream_t s = (hipStream_t)stream;
+    const bool half = dtype == NETKV_FP16;
+    const dim3 grid((uint32_t)tasks, kv->n_kv_heads);
+    check_kernel<<<(a.kv.n_seq + kThreads - 1) / kThreads, kThreads, 0, s>>>(a.kv);
+    switch (kv->head_dim) {
+        case 64: read_kernel<64><<<grid, kThreads, 0, s>>>(a, half); break;
+        case 128: read_kernel<128><<<grid, kThreads, 0, s>>>(a, half); break;
+        default: read_kernel<256><<<grid, kThreads, 0, s>>>(a, half); break;
+    }
+    return launched(h, "read launch failed");
+}

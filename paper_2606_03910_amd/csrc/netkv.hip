@@ -66,7 +66,8 @@
 //   pair / parts / dedupe / build kernels -- build the holder index; whole_*
 //                         kernels where its blocks cannot hold the hashes.
 //   commit kernels     -- between-batch counter / queue / memory update.
-// The flow-level transfer simulation is in flowsim.hip.
+// The flow-level transfer simulation is in flowsim.hip; the block cache of a
+// decode instance and the eviction from it are in blockcache.hip and evict.hip.
 #include <hip/hip_runtime.h>
 #include <rocprim/device/device_radix_sort.hpp>
 
@@ -103,6 +104,8 @@ enum : uint32_t {
     kErrTableFull = 8u,  // insertion found no free slot
     kErrFlow = kErrFlowBit,           // flow simulation: invalid flow set
     kErrFlowStall = kErrFlowStallBit,   // flow simulation: an iteration bound was reached
+    kErrBlock = kErrBlockBit,         // block cache: sequence, page or weight out of range
+    kErrEntry = kErrEntryBit,         // eviction: offsets or outputs out of range
 };
 
 // ------------------------------------------------------------------ device data
@@ -6339,12 +6342,14 @@ netkv_status netkv_sync_errors(netkv_handle h, void *stream) {
     HIPCHK(h, hipMemcpy(&e, h->errword, 4, hipMemcpyDeviceToHost));
     HIPCHK(h, hipMemset(h->errword, 0, 4));
     if (e)
-        return fail(h, NETKV_EINVAL, "input errors:%s%s%s%s%s%s",
+        return fail(h, NETKV_EINVAL, "input errors:%s%s%s%s%s%s%s%s",
                     (e & kErrRequest) ? " inconsistent request header" : "",
                     (e & kErrObservation) ? " congestion observation outside [0,1)" : "",
                     (e & kErrSelection) ? " selection index >= D" : "", (e & kErrTableFull) ? " table full" : "",
                     (e & kErrFlow) ? " invalid flow set" : "",
-                    (e & kErrFlowStall) ? " flow simulation reached its iteration bound" : "");
+                    (e & kErrFlowStall) ? " flow simulation reached its iteration bound" : "",
+                    (e & kErrBlock) ? " block cache sequence, page or weight out of range" : "",
+                    (e & kErrEntry) ? " eviction offsets or outputs out of range" : "");
     return NETKV_OK;
 }
 

@@ -1,6 +1,6 @@
 // Declarations shared by the library's translation units (netkv.hip, the
 // selection path and the handle; flowsim.hip, the flow-level transfer
-// simulation).  Not part of the public interface (include/netkv.h).
+// simulation; blockcache.hip and evict.hip, the block cache's operators).  Not part of the public interface (include/netkv.h).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -12,6 +12,9 @@
 // bits of the handle's device error word that the flow simulation sets
 constexpr uint32_t kErrFlowBit = 16u;        // invalid flow set
 constexpr uint32_t kErrFlowStallBit = 32u;   // an iteration bound was reached
+// ... and those of the block cache's operators
+constexpr uint32_t kErrBlockBit = 64u;       // a sequence, page or weight out of range
+constexpr uint32_t kErrEntryBit = 128u;      // offsets of an eviction that decrease or end past the entries
 
 // Record `msg` as the handle's last error and return `st`.
 netkv_status netkv_internal_fail(netkv_handle h, netkv_status st, const char *msg);

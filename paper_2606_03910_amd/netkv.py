@@ -51,6 +51,17 @@ class netkv_requests_t(C.Structure):
                 ("hash_off", C.c_void_p), ("hashes", C.c_void_p), ("n_hashes", C.c_uint64)]
 
 
+class netkv_kv_t(C.Structure):
+    _fields_ = [("n_pages", C.c_uint32), ("block_tokens", C.c_uint32), ("n_kv_heads", C.c_uint32),
+                ("head_dim", C.c_uint32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p)]
+
+
+class netkv_kv_seqs_t(C.Structure):
+    _fields_ = [("n_seq", C.c_uint32), ("max_pages", C.c_uint32), ("n_tok", C.c_uint64), ("max_tok", C.c_uint64),
+                ("tok_off", C.c_void_p), ("ctx_len", C.c_void_p), ("pages", C.c_void_p)]
+
+
 class netkv_pairs_t(C.Structure):
     _fields_ = [("prefix_blocks", C.c_void_p), ("feasible", C.c_void_p), ("score", C.c_void_p)]
 
@@ -99,6 +110,21 @@ _SIGS = {
     "netkv_flow_sim": (C.c_int32, [C.c_void_p, C.c_uint32, C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint64,
                                    C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p,
                                    C.c_void_p, C.c_void_p]),
+    "netkv_kv_store": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_t), C.POINTER(netkv_kv_seqs_t), C.c_void_p,
+                                   C.c_uint64, C.c_void_p, C.c_uint64, C.c_int, C.c_void_p]),
+    "netkv_kv_read": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_t), C.POINTER(netkv_kv_seqs_t), C.c_void_p,
+                                  C.c_uint64, C.c_void_p, C.c_uint64, C.c_int, C.c_void_p]),
+    "netkv_kv_attend": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_t), C.POINTER(netkv_kv_seqs_t), C.c_void_p, C.c_int,
+                                    C.c_uint32, C.c_uint64, C.c_float, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p,
+                                    C.c_uint64, C.c_void_p]),
+    "netkv_kv_attend_workspace": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_t), C.POINTER(netkv_kv_seqs_t),
+                                              C.c_uint32, C.c_int, C.POINTER(C.c_uint64)]),
+    "netkv_kv_weigh": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_seqs_t), C.c_uint32, C.c_void_p, C.c_uint32,
+                                   C.c_void_p, C.c_void_p]),
+    "netkv_cache_evict": (C.c_int32, [C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_uint32, C.c_uint64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_uint64, C.c_void_p]),
+    "netkv_cache_evict_workspace": (C.c_int32, [C.c_void_p, C.c_uint64, C.POINTER(C.c_uint64)]),
 }
 
 NETKV_OPT_RUN_LEN = 1
@@ -107,6 +133,10 @@ NETKV_OPT_COLS = 3
 NETKV_OPT_POLICY = 4
 NETKV_OPT_LEAD_CAP = 5
 NETKV_OPT_FORM = 6
+
+NETKV_BF16 = 1
+NETKV_FP16 = 2
+_DTYPE = {torch.bfloat16: NETKV_BF16, torch.float16: NETKV_FP16}
 
 
 def load_library(path: str = LIB_PATH):
@@ -388,6 +418,129 @@ def netkv_cache_info(h: int) -> Dict[str, int]:
                 shared_hashes=int(v[2].value), index_bytes=int(v[3].value))
 
 
+def _on(t: torch.Tensor, device, name: str) -> None:
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the handle on {device}")
+
+
+def _rows(t: torch.Tensor, n_tok: int, heads: int, dim: int, device, name: str):
+    """Address and token stride of rows [n_tok][heads][dim] of 16-bit values,
+    dense within a token."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPE or not t.is_cuda:
+        raise TypeError(f"{name} must be a bfloat16 or float16 CUDA tensor")
+    _on(t, device, name)
+    if t.dim() != 3 or t.shape[0] < n_tok or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"{name} must be [{n_tok}][{heads}][{dim}], not {list(t.shape)}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{name} must be dense within a token")
+    stride = t.stride(0) if t.shape[0] > 1 else heads * dim
+    if t.data_ptr() % 16 or stride % 8 or stride < heads * dim:
+        raise ValueError(f"{name} must be 16-byte aligned with a token stride of a multiple of 8 elements")
+    return t.data_ptr(), stride
+
+
+def _on_all(device, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None:
+            _on(t, device, name)
+
+
+class Sequences:
+    """A batch of sequences over a block cache (netkv_kv_seqs_t): tok_off
+    u64[S + 1], ctx_len u32[S], pages u32[S][max_pages], all on the device;
+    n_tok rows in all and at most max_tok of one sequence.  A program keeps it
+    for all layers of a step."""
+
+    def __init__(self, tok_off: torch.Tensor, ctx_len: torch.Tensor, pages: torch.Tensor, n_tok: int, max_tok: int):
+        S = int(ctx_len.numel())
+        if pages.dim() != 2 or pages.shape[0] != S:
+            raise ValueError(f"pages must be [{S}][max_pages], not {list(pages.shape)}")
+        if n_tok < 0 or max_tok < 0:
+            raise ValueError("n_tok and max_tok must be >= 0")
+        c = netkv_kv_seqs_t()
+        c.n_seq, c.max_pages, c.n_tok, c.max_tok = S, int(pages.shape[1]), int(n_tok), int(max_tok)
+        c.tok_off = _dptr(tok_off, torch.uint64, S + 1, "tok_off")
+        c.ctx_len = _dptr(ctx_len, torch.uint32, S, "ctx_len")
+        c.pages = _dptr(pages, torch.uint32, None, "pages")
+        self.device = ctx_len.device
+        _on_all(self.device, tok_off=tok_off, pages=pages)
+        self.c, self.n_seq, self.n_tok, self.max_pages = c, S, int(n_tok), int(pages.shape[1])
+        self._held = (tok_off, ctx_len, pages)
+
+
+def netkv_kv_store(h: int, kv: netkv_kv_t, seqs: Sequences, k: torch.Tensor, v: torch.Tensor, device) -> None:
+    _on(seqs, device, "the sequences")
+    kp, ks = _rows(k, seqs.n_tok, kv.n_kv_heads, kv.head_dim, device, "k")
+    vp, vs = _rows(v, seqs.n_tok, kv.n_kv_heads, kv.head_dim, device, "v")
+    if k.dtype != v.dtype:
+        raise TypeError("k and v must have one dtype")
+    _check(h, load_library().netkv_kv_store(h, C.byref(kv), C.byref(seqs.c), kp, ks, vp, vs, _DTYPE[k.dtype],
+                                            _stream(device)))
+
+
+def netkv_kv_read(h: int, kv: netkv_kv_t, seqs: Sequences, k: torch.Tensor, v: torch.Tensor, device) -> None:
+    _on(seqs, device, "the sequences")
+    kp, ks = _rows(k, seqs.n_tok, kv.n_kv_heads, kv.head_dim, device, "k")
+    vp, vs = _rows(v, seqs.n_tok, kv.n_kv_heads, kv.head_dim, device, "v")
+    if k.dtype != v.dtype:
+        raise TypeError("k and v must have one dtype")
+    _check(h, load_library().netkv_kv_read(h, C.byref(kv), C.byref(seqs.c), kp, ks, vp, vs, _DTYPE[k.dtype],
+                                           _stream(device)))
+
+
+def netkv_kv_attend_workspace(h: int, kv: netkv_kv_t, seqs: Sequences, n_heads: int, weights: bool) -> int:
+    n = C.c_uint64()
+    _check(h, load_library().netkv_kv_attend_workspace(h, C.byref(kv), C.byref(seqs.c), int(n_heads), int(bool(weights)),
+                                                       C.byref(n)))
+    return int(n.value)
+
+
+def netkv_kv_attend(h: int, kv: netkv_kv_t, seqs: Sequences, q: torch.Tensor, scale: float, out: torch.Tensor,
+                    block_weight: Optional[torch.Tensor], work: torch.Tensor, device) -> None:
+    _on(seqs, device, "the sequences")
+    heads = int(q.shape[1]) if q.dim() == 3 else 0
+    qp, qs = _rows(q, seqs.n_tok, heads, kv.head_dim, device, "q")
+    op, os_ = _rows(out, seqs.n_tok, heads, kv.head_dim, device, "out")
+    if q.dtype != out.dtype:
+        raise TypeError("q and out must have one dtype")
+    _on_all(device, block_weight=block_weight, work=work)
+    _check(h, load_library().netkv_kv_attend(
+        h, C.byref(kv), C.byref(seqs.c), qp, _DTYPE[q.dtype], heads, qs, float(scale), op, os_,
+        _dptr(block_weight, torch.float32, seqs.n_seq * seqs.max_pages, "block_weight"),
+        _dptr(work, torch.uint8, name="work"), int(work.numel()), _stream(device)))
+
+
+def netkv_kv_weigh(h: int, seqs: Sequences, block_tokens: int, block_weight: torch.Tensor, page_weight: torch.Tensor,
+                   device) -> None:
+    _on(seqs, device, "the sequences")
+    _on_all(device, block_weight=block_weight, page_weight=page_weight)
+    _check(h, load_library().netkv_kv_weigh(
+        h, C.byref(seqs.c), int(block_tokens),
+        _dptr(block_weight, torch.float32, seqs.n_seq * seqs.max_pages, "block_weight"), int(page_weight.numel()),
+        _dptr(page_weight, torch.uint64, name="page_weight"), _stream(device)))
+
+
+def netkv_cache_evict_workspace(h: int, n_entries: int) -> int:
+    n = C.c_uint64()
+    _check(h, load_library().netkv_cache_evict_workspace(h, int(n_entries), C.byref(n)))
+    return int(n.value)
+
+
+def netkv_cache_evict(h: int, hash_off: torch.Tensor, weight: torch.Tensor, hashes: Optional[torch.Tensor],
+                      keep: torch.Tensor, newest: int, out_off: torch.Tensor, out_pos: Optional[torch.Tensor],
+                      out_hashes: Optional[torch.Tensor], work: torch.Tensor, device) -> None:
+    _on_all(device, hash_off=hash_off, weight=weight, hashes=hashes, keep=keep, out_off=out_off, out_pos=out_pos,
+            out_hashes=out_hashes, work=work)
+    n_seg, n = int(hash_off.numel()) - 1, int(weight.numel())
+    outs = [int(t.numel()) for t in (out_pos, out_hashes) if t is not None]
+    _check(h, load_library().netkv_cache_evict(
+        h, n_seg, _dptr(hash_off, torch.uint64, 1, "hash_off"), n, _dptr(weight, torch.uint64, n, "weight"),
+        _dptr(hashes, torch.uint64, n, "hashes"), _dptr(keep, torch.uint32, n_seg, "keep"), int(newest),
+        min(outs) if outs else 0, _dptr(out_off, torch.uint64, n_seg + 1, "out_off"),
+        _dptr(out_pos, torch.uint32, name="out_pos"), _dptr(out_hashes, torch.uint64, name="out_hashes"),
+        _dptr(work, torch.uint8, name="work"), int(work.numel()), _stream(device)))
+
+
 # ---------------------------------------------------------------- convenience
 
 _SIGNED_TWIN = {np.dtype(np.uint16): (np.int16, torch.uint16),
@@ -473,6 +626,29 @@ class Selector:
         hs = to_device(np.asarray(cache["hashes"], np.uint64), dev)
         netkv_cache_load(self.h, len(off) - 1, off, hs, max_load_factor, dev)
         del off, hs
+
+    def evict(self, cache: Dict[str, torch.Tensor], weight: torch.Tensor, keep: torch.Tensor, newest: int = 0,
+              n_keep: Optional[int] = None) -> Dict[str, torch.Tensor]:
+        """The resident sets that stay when decode i keeps its keep[i]
+        heaviest blocks (device tensors: hash_off u64[n + 1], hashes u64 or
+        None, weight u64, keep u32[n]): hash_off, hashes and each kept
+        block's place in its old set (pos), for load_evicted.  n_keep: how
+        many stay in all, if the caller knows; else it is read back."""
+        dev, off, hs = self.device, cache["hash_off"], cache.get("hashes")
+        if n_keep is None:
+            size = off.view(torch.int64)[1:] - off.view(torch.int64)[:-1]
+            most = keep.view(torch.int32).to(torch.int64) & 0xFFFFFFFF
+            n_keep = int(torch.minimum(most, size).sum()) if len(size) else 0
+        out = dict(hash_off=torch.empty_like(off), pos=torch.empty(n_keep, dtype=torch.uint32, device=dev),
+                   hashes=None if hs is None else torch.empty(n_keep, dtype=torch.uint64, device=dev))
+        work = torch.empty(netkv_cache_evict_workspace(self.h, int(weight.numel())), dtype=torch.uint8, device=dev)
+        netkv_cache_evict(self.h, off, weight, hs, keep, newest, out["hash_off"], out["pos"], out["hashes"], work, dev)
+        return out
+
+    def load_evicted(self, cache: Dict[str, torch.Tensor], max_load_factor: float = 0.5) -> None:
+        """Load resident sets that are on the device already (evict's)."""
+        netkv_cache_load(self.h, int(cache["hash_off"].numel()) - 1, cache["hash_off"], cache["hashes"],
+                         max_load_factor, self.device)
 
     def select(self, req_dev: Dict[str, torch.Tensor], k: int = 1, pairs: bool = False,
                out=None):
@@ -568,3 +744,62 @@ class Selector:
         netkv_sync_errors(self.h, self.device)
 
 
+class BlockCache:
+    """One layer's keys and values of a decode instance's resident blocks in
+    8 bits (netkv_kv_t), on the device of `sel`'s handle.  k and v u8[n_pages *
+    n_kv_heads * block_tokens * head_dim], k_scale and v_scale f32[n_pages *
+    n_kv_heads]; see `empty`."""
+
+    def __init__(self, sel: Selector, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
+                 n_kv_heads: int, head_dim: int, block_tokens: int):
+        c = netkv_kv_t()
+        c.n_kv_heads, c.head_dim, c.block_tokens = int(n_kv_heads), int(head_dim), int(block_tokens)
+        c.n_pages = int(k_scale.numel()) // max(1, c.n_kv_heads)
+        n = c.n_pages * c.n_kv_heads
+        c.k = _dptr(k, torch.uint8, n * c.block_tokens * c.head_dim, "k")
+        c.v = _dptr(v, torch.uint8, n * c.block_tokens * c.head_dim, "v")
+        c.k_scale = _dptr(k_scale, torch.float32, n, "k_scale")
+        c.v_scale = _dptr(v_scale, torch.float32, n, "v_scale")
+        _on_all(sel.device, k=k, v=v, k_scale=k_scale, v_scale=v_scale)
+        self.sel, self.c, self.device = sel, c, sel.device
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+
+    @classmethod
+    def empty(cls, sel: Selector, n_pages: int, n_kv_heads: int, head_dim: int, block_tokens: int) -> "BlockCache":
+        n = n_pages * n_kv_heads
+        k, v = (torch.empty(n * block_tokens * head_dim, dtype=torch.uint8, device=sel.device) for _ in range(2))
+        ks, vs = (torch.ones(n, dtype=torch.float32, device=sel.device) for _ in range(2))
+        return cls(sel, k, v, ks, vs, n_kv_heads, head_dim, block_tokens)
+
+    def store(self, seqs: Sequences, k: torch.Tensor, v: torch.Tensor) -> None:
+        """Quantise the sequences' new tokens [n_tok][n_kv_heads][head_dim]
+        into their blocks."""
+        netkv_kv_store(self.sel.h, self.c, seqs, k, v, self.device)
+
+    def read(self, seqs: Sequences, dtype: torch.dtype = torch.bfloat16):
+        """(k, v) [n_tok][n_kv_heads][head_dim] of the sequences' last tokens."""
+        k, v = (torch.empty((seqs.n_tok, self.c.n_kv_heads, self.c.head_dim), dtype=dtype, device=self.device)
+                for _ in range(2))
+        netkv_kv_read(self.sel.h, self.c, seqs, k, v, self.device)
+        return k, v
+
+    def attend(self, seqs: Sequences, q: torch.Tensor, scale: Optional[float] = None,
+               out: Optional[torch.Tensor] = None, weights: bool = False):
+        """Causal attention of the sequences' last tokens q
+        [n_tok][n_heads][head_dim] over their blocks (scale: 1 /
+        sqrt(head_dim)); with weights=True (out, block weights
+        [n_seq][max_pages])."""
+        if scale is None:
+            scale = self.c.head_dim ** -0.5
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        heads = int(q.shape[1]) if q.dim() == 3 else 0
+        work = torch.empty(netkv_kv_attend_workspace(self.sel.h, self.c, seqs, heads, weights), dtype=torch.uint8,
+                           device=self.device)
+        w = torch.empty((seqs.n_seq, seqs.max_pages), dtype=torch.float32, device=self.device) if weights else None
+        netkv_kv_attend(self.sel.h, self.c, seqs, q, scale, out, w, work, self.device)
+        return (out, w) if weights else out
+
+    def weigh(self, seqs: Sequences, block_weight: torch.Tensor, page_weight: torch.Tensor) -> None:
+        """Add attend's block weights to page_weight u64[n_pages]."""
+        netkv_kv_weigh(self.sel.h, seqs, self.c.block_tokens, block_weight, page_weight, self.device)
