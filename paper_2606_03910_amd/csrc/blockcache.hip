@@ -4,7 +4,8 @@
 //   store_kernel    -- new keys and values quantised into their blocks.
 //   read_kernel     -- tokens given back in 16 bits.
 //   plan_kernel     -- a call's work list: (sequence, row tile, token range).
-//   attend_kernel   -- attention of a row tile over a token range.
+//   attend_kernel   -- attention of up to 64 rows over a token range.
+//   prompt_kernel   -- the same of up to 256 rows.
 //   join_kernel     -- joins the ranges of the rows that were split.
 //   unit_kernel, column_kernel, block_kernel -- block weights.
 //   weigh_kernel    -- block weights summed over pages in fixed point.
@@ -38,6 +39,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
+constexpr int kPromptThreads = 512;
 constexpr uint32_t kStep = 64;        // tokens a wavefront takes at a time
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMaxGrow = 8.0f;      // how far (in powers of two) a row's maximum may be passed before it is raised
@@ -290,7 +292,8 @@ struct AttendArgs {
     uint64_t q_stride, out_stride;   // elements between tokens
     const void *q;
     void *out;
-    float c0;                        // scale * log2(e)
+    float c0;                        // |scale| * log2(e)
+    uint32_t q_sign;                 // flips the queries' signs where scale < 0
     const PlanHead *head;
     const Item *items;
     float *part;                     // [slot][head][tile_rows][D]
@@ -331,16 +334,16 @@ struct ValRegs {
 // the weights before that rounding.  A maximum is raised, and O rescaled, only
 // when it is passed by more than 2^8: P stays below 2^8.
 //
-// ROWS: the four wavefronts take row tiles of their own and the same tokens
-// (prompts); else the same rows and every fourth step, joined through LDS.
-template <int D, int NT, bool ROWS, bool HALF, bool UNITS>
+// The four wavefronts take the same rows and every fourth step each, joined
+// through LDS.
+template <int D, int NT, bool HALF, bool UNITS>
 __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
     constexpr int kDT = D / 16;
     constexpr int kPitch = D + 4;
-    __shared__ float lds[ROWS ? 4 : kWaves * 16 * kPitch];
-    __shared__ float lds_ml[ROWS ? 1 : kWaves][16 * NT][3];
+    __shared__ float lds[kWaves * 16 * kPitch];
+    __shared__ float lds_ml[kWaves][16 * NT][3];
 
     const uint32_t hk = a.kv.hk;
     const uint32_t h = blockIdx.x % hk, item = blockIdx.x / hk;
@@ -350,8 +353,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const uint32_t c = lane & 15, g = lane >> 4;
     const uint32_t n_rows = hd.n * a.G;
-    const uint32_t row0 = it.tile * a.tile_rows + (ROWS ? w * 16 * NT : 0);
-    if (ROWS && row0 >= n_rows) return;
+    const uint32_t row0 = it.tile * a.tile_rows;
     const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep);
     const uint64_t hb = head_bytes(a.kv, D);
     const uint32_t *pages = a.kv.pages + (uint64_t)it.seq * a.kv.max_pages;
@@ -372,11 +374,11 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
         for (int i = 0; i < D / 32; ++i) {
             u32x4 x = {0, 0, 0, 0};
             if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
-            qf[n][i] = __builtin_bit_cast(T8, x);
+            qf[n][i] = __builtin_bit_cast(T8, x ^ a.q_sign);
         }
     }
-    // tokens that every row of this wavefront sees, and that any does
-    const uint32_t row_last = min(row0 + (ROWS ? 16 * NT : a.tile_rows), n_rows) - 1;
+    // tokens that every row sees, and steps that any row sees
+    const uint32_t row_last = min(row0 + a.tile_rows, n_rows) - 1;
     const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
     const int64_t see_any = (int64_t)hd.ctx - hd.n + row_last / a.G + 1;
     const uint32_t all_lim = see_all > 0 ? (uint32_t)see_all : 0u;
@@ -413,10 +415,9 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
         for (int d = 0; d < kDT; ++d) x.f[d] = *(const u32x4 *)(p + d * 16 * tile);
     };
 
-    constexpr uint32_t kBy = ROWS ? 1 : kWaves;
     KeyRegs<D> kf;
     ValRegs<D> vf;
-    for (uint32_t kt = it.k0 + (ROWS ? 0 : w); kt < end; kt += kBy) {
+    for (uint32_t kt = it.k0 + w; kt < end; kt += kWaves) {
         const uint32_t pk = page_at(kt, c >> 2), pv = page_at(kt, g);
         load_keys(kf, kt, pk);
         load_vals(vf, kt, pv);
@@ -568,80 +569,399 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) l[n] = row_sum(l[n]);
 
-    if constexpr (ROWS) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const uint32_t tr = w * 16 * NT + n * 16 + c, r = row0 + n * 16 + c;
+    for (int n = 0; n < NT; ++n) {
+        if (g == 0) {
+            lds_ml[w][n * 16 + c][0] = m[n];
+            lds_ml[w][n * 16 + c][1] = l[n];
+            lds_ml[w][n * 16 + c][2] = y[n];
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) *(f32x4 *)&lds[(w * 16 + c) * kPitch + d * 16 + 4 * g] = acc[n][d];
+        __syncthreads();
+        for (uint32_t e = threadIdx.x; e < 16 * D / 4; e += kThreads) {
+            const uint32_t row = e / (D / 4), d4 = e % (D / 4) * 4;
+            const uint32_t r = row0 + n * 16 + row;
             if (r >= n_rows) continue;
-            if (it.slot != kNoSlot) {
-                const uint64_t at = ((uint64_t)it.slot * hk + h) * a.tile_rows + tr;
-                if (g == 0) a.part_ml[at] = f32x4{m[n], l[n], y[n], 0.0f};
+            float M = -INFINITY, Y = -INFINITY;
+            for (int v = 0; v < kWaves; ++v) {
+                M = fmaxf(M, lds_ml[v][n * 16 + row][0]);
+                Y = fmaxf(Y, lds_ml[v][n * 16 + row][2]);
+            }
+            float L = 0.0f;
+            f32x4 o = {0, 0, 0, 0};
+            for (int v = 0; v < kWaves; ++v) {
+                const float *ml = lds_ml[v][n * 16 + row];
+                L += joined(ml[0], M) * ml[1];
+                const float f = joined(ml[2], Y);
+                const f32x4 x = *(const f32x4 *)&lds[(v * 16 + row) * kPitch + d4];
 #pragma unroll
-                for (int d = 0; d < kDT; ++d) *(f32x4 *)(a.part + at * D + d * 16 + 4 * g) = acc[n][d];
+                for (int i = 0; i < 4; ++i) o[i] += x[i] * f;
+            }
+            if (it.slot != kNoSlot) {
+                const uint64_t at = ((uint64_t)it.slot * hk + h) * a.tile_rows + n * 16 + row;
+                if (d4 == 0) a.part_ml[at] = f32x4{M, L, Y, 0.0f};
+                *(f32x4 *)(a.part + at * D + d4) = o;
             } else {
                 const uint64_t t = hd.row0 + r / a.G;
                 const uint32_t qh = h * a.G + r % a.G;
-                const float inv = l[n] == 0.0f ? 0.0f : exp2_of(y[n] - m[n]) / l[n];
-                T *out = (T *)a.out + t * a.out_stride + (uint64_t)qh * D + 4 * g;
+                const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
+                T z[4];
 #pragma unroll
-                for (int d = 0; d < kDT; ++d) {
-                    T o[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] = (T)(acc[n][d][i] * inv);
-                    *(u32x2 *)(out + d * 16) = *(u32x2 *)o;
-                }
-                if (a.lse && g == 0) a.lse[t * a.Hq + qh] = l[n] == 0.0f ? INFINITY : m[n] + log2_of(l[n]);
+                for (int i = 0; i < 4; ++i) z[i] = (T)(o[i] * inv);
+                *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + d4) = *(u32x2 *)z;
+                if (a.lse && d4 == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
             }
         }
-    } else {
+    }
+}
+
+// The same for prompts: eight wavefronts with 16 NT rows each go through the
+// tokens together, two on a SIMD.  Every step's keys and values are widened to
+// 16 bits once, into LDS in the operands' own order (a fragment is 64 lanes
+// times 16 bytes in a row).  The wavefronts are two groups half a step apart,
+// with a barrier between the halves: while one multiplies (O of the step
+// before, S of this one) the other one does its softmax, so a SIMD's matrix
+// and vector units work at once.  Slot 2 k is the first group's products of
+// step k and the second one's softmax of step k - 1, slot 2 k + 1 the reverse.
+// The first group widens keys k + 1 with its softmax k (slot 2 k + 1: keys
+// k - 1, in the same buffer, were last read in slot 2 k - 1), the second one
+// values k + 1 with its own (slot 2 k + 2: values k - 1 were last read in slot
+// 2 k + 1, values k + 1 are first read in slot 2 k + 4).
+template <int D, int NT, bool HALF>
+__global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a) {
+    typedef typename Elem<HALF>::T T;
+    typedef typename Elem<HALF>::T8 T8;
+    constexpr int kDT = D / 16;
+    constexpr int kShare = D / 64;                    // 16-byte pieces of keys or values a lane stages
+    __shared__ u32x4 lds_k[2][4 * (D / 32)][64];
+    __shared__ u32x4 lds_v[2][2 * kDT][64];
+    __shared__ uint32_t lds_nan[2];
+
+    const uint32_t hk = a.kv.hk;
+    const uint32_t h = blockIdx.x % hk, item = blockIdx.x / hk;
+    if (item >= a.head->n_items) return;
+    const Item it = a.items[item];
+    const Head hd = seq_head(a.kv, it.seq);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const bool second = w >= 4;
+    const uint32_t c = lane & 15, g = lane >> 4;
+    const uint32_t n_rows = hd.n * a.G;
+    const uint32_t row0 = it.tile * a.tile_rows + w * 16 * NT;
+    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep);
+    const uint64_t hb = head_bytes(a.kv, D);
+    const uint32_t *pages = a.kv.pages + (uint64_t)it.seq * a.kv.max_pages;
+    const uint32_t last_block = hd.ctx ? (hd.ctx - 1) >> a.kv.btl : 0u;
+
+    T8 qf[NT][D / 32];
+    uint32_t lim[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (g == 0) {
-                lds_ml[w][n * 16 + c][0] = m[n];
-                lds_ml[w][n * 16 + c][1] = l[n];
-                lds_ml[w][n * 16 + c][2] = y[n];
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t r = row0 + n * 16 + c;
+        const bool valid = r < n_rows;
+        const uint32_t t = valid ? r / a.G : 0u, qh = h * a.G + (valid ? r % a.G : 0u);
+        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
+        lim[n] = !valid ? hd.ctx : seen > 0 ? (uint32_t)seen : 0u;
+        const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)qh * D + 16 * g;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            u32x4 x = {0, 0, 0, 0};
+            if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
+            qf[n][i] = __builtin_bit_cast(T8, x ^ a.q_sign);
+        }
+    }
+    // tokens that every row of this wavefront sees, and steps that any row sees
+    const bool idle = row0 >= n_rows;
+    const uint32_t row_last = min(row0 + 16 * NT, n_rows) - 1;
+    const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
+    const int64_t see_any = (int64_t)hd.ctx - hd.n + row_last / a.G + 1;
+    const uint32_t all_lim = see_all > 0 ? (uint32_t)see_all : 0u;
+    const uint32_t end = idle || see_any <= 0 ? 0u : (uint32_t)((see_any + kStep - 1) / kStep);
+
+    f32x4 acc[NT][kDT], st[NT][4];
+    f16x8 pf[NT][2];
+    float m[NT], l[NT], y[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = y[n] = -INFINITY;
+        l[n] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) acc[n][d] = f32x4{0, 0, 0, 0};
+    }
+
+    // this lane's pieces: 64 dimensions of key row c of a product, or 16
+    // tokens of dimension 16 d + c
+    u32x4 px[kShare];
+    float sc_at[3], vs_at[3];                          // scales of this step, the next, the one after
+    auto block_at = [&](uint32_t kt, uint32_t group) { return min((kt * kStep + 16 * group) >> a.kv.btl, last_block); };
+    const uint32_t own_group = second ? g : c >> 2;    // whose 16 tokens this lane's pieces are of
+    auto fetch = [&](uint32_t kt, uint32_t po, uint32_t pv, float &sc, float &vs) {
+        const bool bad = pv >= a.kv.n_pages;
+        if (bad) report(a.kv);
+        const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk + h;
+        sc = bad ? NAN : a.kv.ks[si];
+        vs = bad ? NAN : a.kv.vs[si];
+        const uint64_t at = ((uint64_t)(po < a.kv.n_pages ? po : 0u) * hk + h) * hb;
+        const uint32_t tok = (kt * kStep + 16 * own_group) & (bt - 1);
+        if (second) {
+            const uint8_t *v = a.kv.v + at + (uint64_t)(tok & ~(tile - 1)) * D + c * tile + (tok & (tile - 1));
+#pragma unroll
+            for (int i = 0; i < kShare; ++i) px[i] = *(const u32x4 *)(v + ((w - 4) * kShare + i) * 16 * tile);
+        } else {
+            const uint8_t *k = a.kv.k + at + (uint64_t)(tok + (c & 3) + 4 * w) * D + 16 * g;
+#pragma unroll
+            for (int i = 0; i < kShare; ++i) px[i] = *(const u32x4 *)(k + 64 * i);
+        }
+    };
+    auto stage = [&](uint32_t kt) {
+        const int b = kt & 1;
+        if (!second) {
+#pragma unroll
+            for (int i = 0; i < kShare; ++i) {
+                const uint32_t j = w * kShare + i;
+                lds_k[b][2 * j][lane] = __builtin_bit_cast(u32x4, widen<HALF>(px[i][0], px[i][1]));
+                lds_k[b][2 * j + 1][lane] = __builtin_bit_cast(u32x4, widen<HALF>(px[i][2], px[i][3]));
             }
+            return;
+        }
+        if ((uint64_t)kt * kStep + kStep + hd.n > hd.ctx) {
+            // tokens that not every row sees: bytes of slots that hold no token
+            // are cleared, a NaN is told to the products
+            const uint32_t tok0 = kt * kStep + 16 * g;
+            const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
+            bool nan = false;
+#pragma unroll
+            for (int i = 0; i < kShare; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int n = have - 4 * j;
+                    px[i][j] &= n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+                    nan |= (((px[i][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+                }
+            if (__any(nan) && lane == 0) lds_nan[b] = kt + 1;
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            __syncthreads();
+        for (int i = 0; i < kShare; ++i) {
+            const uint32_t j = (w - 4) * kShare + i;
+            lds_v[b][2 * j][lane] = __builtin_bit_cast(u32x4, widen_f16(px[i][0], px[i][1]));
+            lds_v[b][2 * j + 1][lane] = __builtin_bit_cast(u32x4, widen_f16(px[i][2], px[i][3]));
+        }
+    };
+    // LDS alone is handed over: loads from memory stay in flight
+    auto meet = [&]() {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    };
+    auto scores = [&](uint32_t kt) {
+        const int b = kt & 1;
 #pragma unroll
-            for (int d = 0; d < kDT; ++d) *(f32x4 *)&lds[(w * 16 + c) * kPitch + d * 16 + 4 * g] = acc[n][d];
-            __syncthreads();
-            for (uint32_t e = threadIdx.x; e < 16 * D / 4; e += kThreads) {
-                const uint32_t row = e / (D / 4), d4 = e % (D / 4) * 4;
-                const uint32_t r = row0 + n * 16 + row;
-                if (r >= n_rows) continue;
-                float M = -INFINITY, Y = -INFINITY;
-                for (int v = 0; v < kWaves; ++v) {
-                    M = fmaxf(M, lds_ml[v][n * 16 + row][0]);
-                    Y = fmaxf(Y, lds_ml[v][n * 16 + row][2]);
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) st[n][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const T8 kf = __builtin_bit_cast(T8, lds_k[b][t * (D / 32) + i][lane]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) st[n][t] = product(kf, qf[n][i], st[n][t]);
+            }
+    };
+    auto values = [&](uint32_t kt) {
+        const int b = kt & 1;
+        if (kt * kStep + kStep > all_lim && lds_nan[b] == kt + 1) {
+            // as in attend_kernel: rows that see a NaN value are found by a
+            // product of the masks, and it is left out of the values
+            const uint32_t tok0 = kt * kStep + 16 * g;
+            f16x8 see[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) see[n][j >> 3][j & 7] = tok0 + j < lim[n] ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) {
+                f16x8 v[2], one[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    v[u] = __builtin_bit_cast(f16x8, lds_v[b][2 * d + u][lane]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const bool nan = v[u][j] != v[u][j];
+                        one[u][j] = nan ? (_Float16)1.0f : (_Float16)0.0f;
+                        v[u][j] = nan ? (_Float16)0.0f : v[u][j];
+                    }
                 }
-                float L = 0.0f;
-                f32x4 o = {0, 0, 0, 0};
-                for (int v = 0; v < kWaves; ++v) {
-                    const float *ml = lds_ml[v][n * 16 + row];
-                    L += joined(ml[0], M) * ml[1];
-                    const float f = joined(ml[2], Y);
-                    const f32x4 x = *(const f32x4 *)&lds[(v * 16 + row) * kPitch + d4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] += x[i] * f;
-                }
-                if (it.slot != kNoSlot) {
-                    const uint64_t at = ((uint64_t)it.slot * hk + h) * a.tile_rows + n * 16 + row;
-                    if (d4 == 0) a.part_ml[at] = f32x4{M, L, Y, 0.0f};
-                    *(f32x4 *)(a.part + at * D + d4) = o;
-                } else {
-                    const uint64_t t = hd.row0 + r / a.G;
-                    const uint32_t qh = h * a.G + r % a.G;
-                    const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
-                    T z[4];
+                for (int n = 0; n < NT; ++n) {
+                    f32x4 hit = {0, 0, 0, 0};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = (T)(o[i] * inv);
-                    *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + d4) = *(u32x2 *)z;
-                    if (a.lse && d4 == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
+                    for (int u = 0; u < 2; ++u) {
+                        hit = product(one[u], see[n][u], hit);
+                        acc[n][d] = product(v[u], pf[n][u], acc[n][d]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][d][i] = hit[i] > 0.0f ? NAN : acc[n][d][i];
                 }
             }
+        } else {
+#pragma unroll
+            for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const f16x8 vf = __builtin_bit_cast(f16x8, lds_v[b][2 * d + u][lane]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[n][d] = product(vf, pf[n][u], acc[n][d]);
+                }
+        }
+    };
+    auto softmax = [&](uint32_t kt) {
+        // not 0, which would turn a masked score's -inf into NaN
+        const float sc0 = sc_at[0] * a.c0, sc = sc0 == 0.0f ? 1.0e-30f : sc0;
+        const float vsl = vs_at[0], vlog = log2_of(vsl);
+        const uint32_t tok0 = kt * kStep + 16 * g;
+        if (kt * kStep + kStep > all_lim) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (tok0 + 4 * t + i >= lim[n]) st[n][t][i] = -INFINITY;
+        }
+        bool grow = false;
+        float mx[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            mx[n] = st[n][0][0];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx[n] = fmaxf(mx[n], st[n][t][i]);
+            mx[n] = mx[n] == -INFINITY ? -INFINITY : mx[n] * sc;
+            grow |= mx[n] > m[n] + kMaxGrow || mx[n] + vlog > y[n] + kMaxGrow;
+        }
+        if (__any(grow)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float mn = fmaxf(m[n], row_max(mx[n])), yn = fmaxf(y[n], row_max(mx[n] + vlog));
+                l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
+                const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
+                m[n] = mn;
+                y[n] = yn;
+#pragma unroll
+                for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
+            }
+        }
+        // P in units of 2^y; its sum is turned into l's units of 2^m at once,
+        // unless one of them would leave fp32's range
+        float up[NT];                                  // log2 of a weight over its P
+        bool far = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            up[n] = y[n] - vlog - m[n];
+            far |= !(fabsf(up[n]) < 64.0f);
+        }
+        if (__any(far)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float sum = 0.0f;
+                const float mm = m[n] == -INFINITY ? 0.0f : m[n];
+                const float f = y[n] == -INFINITY ? 0.0f : fminf(vsl * exp2_of(mm - y[n]), 3.0e38f);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float p = exp2_of(fmaf(st[n][j >> 2][j & 3], sc, -mm));
+                    sum += p;
+                    pf[n][j >> 3][j & 7] = (_Float16)(p * f);
+                }
+                l[n] += sum;
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float sum = 0.0f;
+                const float by = vlog - y[n];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    float p[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[i] = exp2_of(fmaf(st[n][t][i], sc, by));
+                        sum += p[i];
+                    }
+                    const f16x2 u = __builtin_convertvector((f32x2{p[0], p[1]}), f16x2);
+                    const f16x2 v = __builtin_convertvector((f32x2{p[2], p[3]}), f16x2);
+                    const int j = 4 * (t & 1);
+                    pf[n][t >> 1][j] = u[0];
+                    pf[n][t >> 1][j + 1] = u[1];
+                    pf[n][t >> 1][j + 2] = v[0];
+                    pf[n][t >> 1][j + 3] = v[1];
+                }
+                l[n] += sum * exp2_of(up[n]);
+            }
+        }
+    };
+
+    uint32_t po = 0, pv = 0;
+    if (threadIdx.x < 2) lds_nan[threadIdx.x] = 0;
+    meet();
+    sc_at[0] = vs_at[0] = sc_at[1] = vs_at[1] = 0.0f;
+    if (it.k0 < it.k1) {
+        fetch(it.k0, pages[block_at(it.k0, own_group)], pages[block_at(it.k0, g)], sc_at[0], vs_at[0]);
+        stage(it.k0);
+        if (it.k0 + 1 < it.k1)
+            fetch(it.k0 + 1, pages[block_at(it.k0 + 1, own_group)], pages[block_at(it.k0 + 1, g)], sc_at[1], vs_at[1]);
+        po = pages[block_at(it.k0 + 2, own_group)];
+        pv = pages[block_at(it.k0 + 2, g)];
+    }
+    meet();
+    if (second) meet();
+    for (uint32_t kt = it.k0; kt < it.k1; ++kt) {
+        if (kt > it.k0 && kt - 1 < end) values(kt - 1);
+        if (kt < end) scores(kt);
+        meet();
+        if (kt < end) softmax(kt);
+        if (kt + 1 < it.k1) stage(kt + 1);
+        sc_at[0] = sc_at[1];
+        vs_at[0] = vs_at[1];
+        if (kt + 2 < it.k1) {
+            fetch(kt + 2, po, pv, sc_at[1], vs_at[1]);
+            po = pages[block_at(kt + 3, own_group)];
+            pv = pages[block_at(kt + 3, g)];
+        }
+        meet();
+    }
+    if (!second) meet();
+    if (it.k0 < it.k1 && it.k1 - 1 < end) values(it.k1 - 1);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        l[n] = row_sum(l[n]);
+        const uint32_t tr = w * 16 * NT + n * 16 + c, r = row0 + n * 16 + c;
+        if (r >= n_rows) continue;
+        if (it.slot != kNoSlot) {
+            const uint64_t at = ((uint64_t)it.slot * hk + h) * a.tile_rows + tr;
+            if (g == 0) a.part_ml[at] = f32x4{m[n], l[n], y[n], 0.0f};
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) *(f32x4 *)(a.part + at * D + d * 16 + 4 * g) = acc[n][d];
+        } else {
+            const uint64_t t = hd.row0 + r / a.G;
+            const uint32_t qh = h * a.G + r % a.G;
+            const float inv = l[n] == 0.0f ? 0.0f : exp2_of(y[n] - m[n]) / l[n];
+            T *out = (T *)a.out + t * a.out_stride + (uint64_t)qh * D + 4 * g;
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) {
+                T o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = (T)(acc[n][d][i] * inv);
+                *(u32x2 *)(out + d * 16) = *(u32x2 *)o;
+            }
+            if (a.lse && g == 0) a.lse[t * a.Hq + qh] = l[n] == 0.0f ? INFINITY : m[n] + log2_of(l[n]);
         }
     }
 }
@@ -786,7 +1106,7 @@ __global__ __launch_bounds__(kThreads) void column_kernel(AttendArgs a, WeightAr
         for (int i = 0; i < D / 32; ++i) {
             u32x4 x = {0, 0, 0, 0};
             if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
-            const T8 qf = __builtin_bit_cast(T8, x);
+            const T8 qf = __builtin_bit_cast(T8, x ^ a.q_sign);
 #pragma unroll
             for (int u = 0; u < 4; ++u) st[u] = product(kf[u][i], qf, st[u]);
         }
@@ -1174,7 +1494,7 @@ constexpr uint64_t align256(uint64_t x) { return (x + 255) & ~255ull; }
 // How a call is split, and its workspace.
 struct Layout {
     int NT;
-    bool rows;             // the wavefronts take rows of their own
+    bool rows;             // prompt_kernel
     uint32_t G, tile_rows, target, item_cap, slot_cap, join_cap, n_units;
     uint64_t head, items, joins, ml, part, lse, units, cols, total;
 };
@@ -1186,8 +1506,8 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     const uint64_t most = (uint64_t)a.max_tok * y.G;   // rows of the longest sequence's head
     if (most > 0xFFFFFFFFull - 1024) return invalid(h, "max_tok * n_heads / n_kv_heads must be < 2^32 - 1024");
     y.rows = most > (D == 256 ? 32u : 64u);
-    y.NT = y.rows ? (D == 256 ? 2 : 4) : most <= 16 ? 1 : most <= 32 ? 2 : 4;
-    y.tile_rows = 16u * y.NT * (y.rows ? kWaves : 1);
+    y.NT = most <= 16 ? 1 : most <= 32 ? 2 : 4;
+    y.tile_rows = y.rows ? (D == 256 ? 128u : 256u) : 16u * y.NT;
     y.target = ((y.rows ? 512u : 1024u) + a.hk - 1) / a.hk;
     const uint64_t tiles = a.n_tok * y.G / y.tile_rows + a.n_seq;
     const uint64_t items = 2ull * y.target + tiles;
@@ -1226,21 +1546,18 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
 template <int D, bool HALF>
 void launch_attend(const Layout &y, const AttendArgs &a, const Join *joins, const WeightArgs &wa, hipStream_t s) {
     const dim3 grid(y.item_cap * a.kv.hk);
-#define NETKV_ATTEND(NT, ROWS, UNITS) attend_kernel<D, NT, ROWS, HALF, UNITS><<<grid, kThreads, 0, s>>>(a)
+#define NETKV_ATTEND(NT, UNITS) attend_kernel<D, NT, HALF, UNITS><<<grid, kThreads, 0, s>>>(a)
     if (y.rows) {
-        if constexpr (D == 256)
-            NETKV_ATTEND(2, true, false);
-        else
-            NETKV_ATTEND(4, true, false);
+        prompt_kernel<D, D == 256 ? 1 : 2, HALF><<<grid, kPromptThreads, 0, s>>>(a);
     } else if (y.NT == 1) {
-        if (wa.w) NETKV_ATTEND(1, false, true);
-        else NETKV_ATTEND(1, false, false);
+        if (wa.w) NETKV_ATTEND(1, true);
+        else NETKV_ATTEND(1, false);
     } else if (y.NT == 2) {
-        if (wa.w) NETKV_ATTEND(2, false, true);
-        else NETKV_ATTEND(2, false, false);
+        if (wa.w) NETKV_ATTEND(2, true);
+        else NETKV_ATTEND(2, false);
     } else if constexpr (D != 256) {
-        if (wa.w) NETKV_ATTEND(4, false, true);
-        else NETKV_ATTEND(4, false, false);
+        if (wa.w) NETKV_ATTEND(4, true);
+        else NETKV_ATTEND(4, false);
     }
 #undef NETKV_ATTEND
     const uint64_t joins_most = (uint64_t)y.join_cap * a.kv.hk * y.tile_rows;
@@ -1332,7 +1649,8 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     t.out_stride = out_stride;
     t.q = q;
     t.out = out;
-    t.c0 = scale * kLog2e;
+    t.c0 = std::fabs(scale) * kLog2e;
+    t.q_sign = scale < 0.0f ? 0x80008000u : 0u;
     t.head = p.head;
     t.items = p.items;
     t.part = (float *)(ws + y.part);
