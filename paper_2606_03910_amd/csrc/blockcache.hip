@@ -22,6 +22,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "netkv.h"
 #include "netkv_internal.h"
@@ -121,6 +122,9 @@ __device__ inline typename Elem<HALF>::T8 widen(uint32_t a, uint32_t b) {
 
 __device__ inline f32x4 product(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ inline f32x4 product(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// 1 in the lowest bit of each byte that is a NaN
+__device__ inline uint32_t nan_bytes(uint32_t x) { return (((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7; }
 
 // over the four lanes of a row (lanes l, l ^ 16, l ^ 32, l ^ 48)
 __device__ inline float row_max(float x) {
@@ -350,7 +354,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     if (item >= a.head->n_items) return;
     const Item it = a.items[item];
     const Head hd = seq_head(a.kv, it.seq);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
     const uint32_t c = lane & 15, g = lane >> 4;
     const uint32_t n_rows = hd.n * a.G;
     const uint32_t row0 = it.tile * a.tile_rows;
@@ -526,8 +530,8 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
 #pragma unroll
             for (int d = 0; d < kDT; ++d) {
                 vf.f[d] &= keep;
-                const u32x4 y = ((vf.f[d] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-                nan |= (y[0] | y[1] | y[2] | y[3]) != 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) nan |= nan_bytes(vf.f[d][i]) != 0;
             }
             if (__any(nan)) {
                 // A NaN among values that some rows see and others do not: a
@@ -541,8 +545,10 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
                     for (int j = 0; j < 16; ++j) see[n][j >> 3][j & 7] = tok0 + j < lim[n] ? (_Float16)1.0f : (_Float16)0.0f;
 #pragma unroll
                 for (int d = 0; d < kDT; ++d) {
-                    const u32x4 y = (((vf.f[d] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;   // 1 per NaN byte
-                    const u32x4 one = y * 0x38u;                                                     // 1.0 per NaN byte
+                    u32x4 y;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = nan_bytes(vf.f[d][i]);
+                    const u32x4 one = y * 0x38u;          // 1.0 per NaN
                     vf.f[d] &= ~(y * 0xFFu);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -640,6 +646,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
     constexpr int kShare = D / 64;                    // 16-byte pieces of keys or values a lane stages
     __shared__ u32x4 lds_k[2][4 * (D / 32)][64];
     __shared__ u32x4 lds_v[2][2 * kDT][64];
+    __shared__ uint8_t lds_bits[2][2 * kDT][64];      // which of a fragment lane's 8 values were NaN
     __shared__ uint32_t lds_nan[2];
 
     const uint32_t hk = a.kv.hk;
@@ -647,7 +654,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
     if (item >= a.head->n_items) return;
     const Item it = a.items[item];
     const Head hd = seq_head(a.kv, it.seq);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
     const bool second = w >= 4;
     const uint32_t c = lane & 15, g = lane >> 4;
     const uint32_t n_rows = hd.n * a.G;
@@ -674,21 +681,22 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
             qf[n][i] = __builtin_bit_cast(T8, x ^ a.q_sign);
         }
     }
-    // tokens that every row of this wavefront sees, and steps that any row sees
-    const bool idle = row0 >= n_rows;
-    const uint32_t row_last = min(row0 + 16 * NT, n_rows) - 1;
+    // tokens that every row of this wavefront sees.  A wavefront whose rows see
+    // no more goes on with the others: they wait for one another anyway, and
+    // without a branch around the products their sums stay where they are.
     const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
-    const int64_t see_any = (int64_t)hd.ctx - hd.n + row_last / a.G + 1;
-    const uint32_t all_lim = see_all > 0 ? (uint32_t)see_all : 0u;
-    const uint32_t end = idle || see_any <= 0 ? 0u : (uint32_t)((see_any + kStep - 1) / kStep);
+    const uint32_t all_lim = see_all > 0 ? (uint32_t)min(see_all, (int64_t)hd.ctx) : 0u;
 
     f32x4 acc[NT][kDT], st[NT][4];
     f16x8 pf[NT][2];
     float m[NT], l[NT], y[NT];
+    uint64_t nan_sums = 0;                            // sums of this lane that a NaN value belongs to
+    static_assert(4 * NT * kDT <= 64, "a bit a sum");
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         m[n] = y[n] = -INFINITY;
         l[n] = 0.0f;
+        pf[n][0] = pf[n][1] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
         for (int d = 0; d < kDT; ++d) acc[n][d] = f32x4{0, 0, 0, 0};
     }
@@ -696,7 +704,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
     // this lane's pieces: 64 dimensions of key row c of a product, or 16
     // tokens of dimension 16 d + c
     u32x4 px[kShare];
-    float sc_at[3], vs_at[3];                          // scales of this step, the next, the one after
+    float sc_at[2], vs_at[2];                          // scales of this step and the next
     auto block_at = [&](uint32_t kt, uint32_t group) { return min((kt * kStep + 16 * group) >> a.kv.btl, last_block); };
     const uint32_t own_group = second ? g : c >> 2;    // whose 16 tokens this lane's pieces are of
     auto fetch = [&](uint32_t kt, uint32_t po, uint32_t pv, float &sc, float &vs) {
@@ -729,8 +737,8 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
             return;
         }
         if ((uint64_t)kt * kStep + kStep + hd.n > hd.ctx) {
-            // tokens that not every row sees: bytes of slots that hold no token
-            // are cleared, a NaN is told to the products
+            // tokens that not every row of the sequence sees: bytes of slots
+            // that hold no token are cleared, a NaN is taken out and noted
             const uint32_t tok0 = kt * kStep + 16 * g;
             const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
             bool nan = false;
@@ -740,9 +748,26 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
                 for (int j = 0; j < 4; ++j) {
                     const int n = have - 4 * j;
                     px[i][j] &= n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
-                    nan |= (((px[i][j] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+                    nan |= nan_bytes(px[i][j]) != 0;
                 }
-            if (__any(nan) && lane == 0) lds_nan[b] = kt + 1;
+            if (__any(nan)) {
+#pragma unroll
+                for (int i = 0; i < kShare; ++i) {
+                    const uint32_t j = (w - 4) * kShare + i;
+                    uint32_t bits = 0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t y = nan_bytes(px[i][q]);
+                        px[i][q] &= ~(y * 0xFFu);
+                        bits |= ((y | y >> 7 | y >> 14 | y >> 21) & 15u) << (4 * q);
+                    }
+                    lds_bits[b][2 * j][lane] = (uint8_t)bits;
+                    lds_bits[b][2 * j + 1][lane] = (uint8_t)(bits >> 8);
+                }
+                if (lane == 0) atomicOr(&lds_nan[b], 1u << (w - 4));
+            } else if (lane == 0) {
+                atomicAnd(&lds_nan[b], ~(1u << (w - 4)));
+            }
         }
 #pragma unroll
         for (int i = 0; i < kShare; ++i) {
@@ -757,6 +782,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     };
+    // a product's sums are four fragments apart: each waits for none
     auto scores = [&](uint32_t kt) {
         const int b = kt & 1;
 #pragma unroll
@@ -764,60 +790,39 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 #pragma unroll
             for (int t = 0; t < 4; ++t) st[n][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; t += 2)
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                const T8 kf = __builtin_bit_cast(T8, lds_k[b][t * (D / 32) + i][lane]);
+            for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) st[n][t] = product(kf, qf[n][i], st[n][t]);
-            }
+                for (int q = 0; q < 2; ++q) {
+                    const T8 kf = __builtin_bit_cast(T8, lds_k[b][(t + q) * (D / 32) + i][lane]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) st[n][t + q] = product(kf, qf[n][i], st[n][t + q]);
+                }
     };
     auto values = [&](uint32_t kt) {
         const int b = kt & 1;
-        if (kt * kStep + kStep > all_lim && lds_nan[b] == kt + 1) {
-            // as in attend_kernel: rows that see a NaN value are found by a
-            // product of the masks, and it is left out of the values
-            const uint32_t tok0 = kt * kStep + 16 * g;
-            f16x8 see[NT][2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int d = 0; d < kDT; d += 2)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) see[n][j >> 3][j & 7] = tok0 + j < lim[n] ? (_Float16)1.0f : (_Float16)0.0f;
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int d = 0; d < kDT; ++d) {
-                f16x8 v[2], one[2];
+                for (int q = 0; q < 2; ++q) {
+                    const f16x8 vf = __builtin_bit_cast(f16x8, lds_v[b][2 * (d + q) + u][lane]);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    v[u] = __builtin_bit_cast(f16x8, lds_v[b][2 * d + u][lane]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool nan = v[u][j] != v[u][j];
-                        one[u][j] = nan ? (_Float16)1.0f : (_Float16)0.0f;
-                        v[u][j] = nan ? (_Float16)0.0f : v[u][j];
-                    }
+                    for (int n = 0; n < NT; ++n) acc[n][d + q] = product(vf, pf[n][u], acc[n][d + q]);
                 }
+    };
+    // `reads` fragments in all, each for NT products: six on their way
+    auto interleave = [&](auto reads) {
+        constexpr int kReads = decltype(reads)::value;
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    f32x4 hit = {0, 0, 0, 0};
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        hit = product(one[u], see[n][u], hit);
-                        acc[n][d] = product(v[u], pf[n][u], acc[n][d]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[n][d][i] = hit[i] > 0.0f ? NAN : acc[n][d][i];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int d = 0; d < kDT; ++d)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const f16x8 vf = __builtin_bit_cast(f16x8, lds_v[b][2 * d + u][lane]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[n][d] = product(vf, pf[n][u], acc[n][d]);
-                }
+        for (int i = 0; i < kReads - 6; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, NT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, 6 * NT, 0);
     };
     auto softmax = [&](uint32_t kt) {
         // not 0, which would turn a masked score's -inf into NaN
@@ -832,6 +837,36 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (tok0 + 4 * t + i >= lim[n]) st[n][t][i] = -INFINITY;
+        }
+        if ((uint64_t)kt * kStep + kStep + hd.n > hd.ctx) {
+            const uint32_t noted = lds_nan[kt & 1];
+            if (noted) {
+                // as in attend_kernel: the rows that see a NaN value are found
+                // by a product of the masks
+                for (int d = 0; d < kDT; ++d) {
+                    if (!(noted >> (d / kShare) & 1)) continue;
+                    f32x4 hit[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) hit[n] = f32x4{0, 0, 0, 0};
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t bits = lds_bits[kt & 1][2 * d + u][lane];
+                        f16x8 one;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) one[j] = bits >> j & 1 ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            f16x8 see;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) see[j] = tok0 + 8 * u + j < lim[n] ? (_Float16)1.0f : (_Float16)0.0f;
+                            hit[n] = product(one, see, hit[n]);
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) nan_sums |= (uint64_t)(hit[n][i] > 0.0f) << (4 * (n * kDT + d) + i);
+                }
+            }
         }
         bool grow = false;
         float mx[NT];
@@ -910,6 +945,8 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 
     uint32_t po = 0, pv = 0;
     if (threadIdx.x < 2) lds_nan[threadIdx.x] = 0;
+    // the first step's products with "the step before" are of zeros
+    for (uint32_t i = threadIdx.x; i < 2 * kDT * 64; i += kPromptThreads) (&lds_v[~it.k0 & 1][0][0])[i] = u32x4{0, 0, 0, 0};
     meet();
     sc_at[0] = vs_at[0] = sc_at[1] = vs_at[1] = 0.0f;
     if (it.k0 < it.k1) {
@@ -923,10 +960,11 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
     meet();
     if (second) meet();
     for (uint32_t kt = it.k0; kt < it.k1; ++kt) {
-        if (kt > it.k0 && kt - 1 < end) values(kt - 1);
-        if (kt < end) scores(kt);
+        values(kt - 1);
+        scores(kt);
+        interleave(std::integral_constant<int, D / 4>());
         meet();
-        if (kt < end) softmax(kt);
+        softmax(kt);
         if (kt + 1 < it.k1) stage(kt + 1);
         sc_at[0] = sc_at[1];
         vs_at[0] = vs_at[1];
@@ -938,10 +976,16 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
         meet();
     }
     if (!second) meet();
-    if (it.k0 < it.k1 && it.k1 - 1 < end) values(it.k1 - 1);
+    if (it.k0 < it.k1) values(it.k1 - 1);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         l[n] = row_sum(l[n]);
+        if (nan_sums)
+#pragma unroll
+            for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (nan_sums >> (4 * (n * kDT + d) + i) & 1) acc[n][d][i] = NAN;
         const uint32_t tr = w * 16 * NT + n * 16 + c, r = row0 + n * 16 + c;
         if (r >= n_rows) continue;
         if (it.slot != kNoSlot) {
