@@ -44,6 +44,7 @@ constexpr int kPromptThreads = 512;
 constexpr uint32_t kStep = 64;        // tokens a wavefront takes at a time
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMaxGrow = 8.0f;      // how far (in powers of two) a row's maximum may be passed before it is raised
+constexpr float kMaxSum = 1024.0f;    // ... and how large 16 weights' sum may become instead
 constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
 
 struct Kv {
@@ -141,6 +142,13 @@ __device__ inline float row_sum(float x) {
     x = pair16_sum(x);
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// Memory that no kernel writes while this one runs, at an address that is the
+// same for the whole wavefront: loads go through the scalar cache.
+template <typename T>
+__device__ inline const __attribute__((address_space(4))) T *scalar(const T *p) {
+    return (const __attribute__((address_space(4))) T *)p;
 }
 
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -626,6 +634,31 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
     }
 }
 
+// 2^(x + by) of 16 scores, as the operand of the product with the values, and
+// their sum.  (The empty statement: the weights are rounded here, not where
+// they are used, which would keep them in twice the registers.)
+__device__ __forceinline__ float weights_of(const f32x4 (&st)[4], float sc, float by, f16x8 (&pf)[2]) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = exp2_of(fmaf(st[t][i], sc, by));
+            sum += p[i];
+        }
+        const f16x2 u = __builtin_convertvector((f32x2{p[0], p[1]}), f16x2);
+        const f16x2 v = __builtin_convertvector((f32x2{p[2], p[3]}), f16x2);
+        const int j = 4 * (t & 1);
+        pf[t >> 1][j] = u[0];
+        pf[t >> 1][j + 1] = u[1];
+        pf[t >> 1][j + 2] = v[0];
+        pf[t >> 1][j + 3] = v[1];
+    }
+    asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(sum));
+    return sum;
+}
+
 // The same for prompts: eight wavefronts with 16 NT rows each go through the
 // tokens together, two on a SIMD.  Every step's keys and values are widened to
 // 16 bits once, into LDS in the operands' own order (a fragment is 64 lanes
@@ -638,11 +671,15 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
 // k - 1, in the same buffer, were last read in slot 2 k - 1), the second one
 // values k + 1 with its own (slot 2 k + 2: values k - 1 were last read in slot
 // 2 k + 1, values k + 1 are first read in slot 2 k + 4).
-template <int D, int NT, bool HALF>
+//
+// SMALL: blocks of less than 64 tokens, so a step's four groups of 16 tokens
+// may be in different pages; else pages, scales and addresses are scalar.
+template <int D, int NT, bool HALF, bool SMALL>
 __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
     constexpr int kDT = D / 16;
+    constexpr int kAhead = 6;                         // fragments read ahead of their products
     constexpr int kShare = D / 64;                    // 16-byte pieces of keys or values a lane stages
     __shared__ u32x4 lds_k[2][4 * (D / 32)][64];
     __shared__ u32x4 lds_v[2][2 * kDT][64];
@@ -686,6 +723,8 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
     // without a branch around the products their sums stay where they are.
     const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
     const uint32_t all_lim = see_all > 0 ? (uint32_t)min(see_all, (int64_t)hd.ctx) : 0u;
+    // tokens that every row of the sequence sees
+    const uint32_t own_from = hd.ctx > hd.n ? hd.ctx - hd.n : 0u;
 
     f32x4 acc[NT][kDT], st[NT][4];
     f16x8 pf[NT][2];
@@ -705,25 +744,29 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
     // tokens of dimension 16 d + c
     u32x4 px[kShare];
     float sc_at[2], vs_at[2];                          // scales of this step and the next
-    auto block_at = [&](uint32_t kt, uint32_t group) { return min((kt * kStep + 16 * group) >> a.kv.btl, last_block); };
-    const uint32_t own_group = second ? g : c >> 2;    // whose 16 tokens this lane's pieces are of
-    auto fetch = [&](uint32_t kt, uint32_t po, uint32_t pv, float &sc, float &vs) {
+    const uint32_t own_group = SMALL ? second ? g : c >> 2 : 0u;   // whose page this lane's pieces are in
+    auto page_at = [&](uint32_t kt, uint32_t group) {
+        const uint32_t block = min((kt * kStep + (SMALL ? 16 * group : 0u)) >> a.kv.btl, last_block);
+        return SMALL ? pages[block] : scalar(pages)[block];
+    };
+    const uint8_t *own = (second ? a.kv.v : a.kv.k) + h * hb;
+    const uint64_t page_bytes = hk * hb;
+    const uint32_t in_page = second ? c * tile + ((16 * g) & (tile - 1)) + (w - 4) * kShare * 16 * tile
+                                    : ((16 * (c >> 2)) & (tile - 1)) * D + ((c & 3) + 4 * w) * D + 16 * g;
+    const uint32_t piece = second ? 16 * tile : 64;
+    const float *ks = a.kv.ks + h, *vs = a.kv.vs + h;
+    auto scales_of = [&](uint32_t pv, float &sc, float &vsc) {
         const bool bad = pv >= a.kv.n_pages;
         if (bad) report(a.kv);
-        const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk + h;
-        sc = bad ? NAN : a.kv.ks[si];
-        vs = bad ? NAN : a.kv.vs[si];
-        const uint64_t at = ((uint64_t)(po < a.kv.n_pages ? po : 0u) * hk + h) * hb;
-        const uint32_t tok = (kt * kStep + 16 * own_group) & (bt - 1);
-        if (second) {
-            const uint8_t *v = a.kv.v + at + (uint64_t)(tok & ~(tile - 1)) * D + c * tile + (tok & (tile - 1));
+        const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk;
+        sc = SMALL ? ks[si] : scalar(ks)[si];
+        vsc = SMALL ? vs[si] : scalar(vs)[si];
+        if (bad) sc = vsc = NAN;
+    };
+    auto fetch = [&](uint32_t kt, uint32_t po) {
+        const uint8_t *p = own + (po < a.kv.n_pages ? po : 0u) * page_bytes + (uint64_t)((kt * kStep) & (bt - 1)) * D;
 #pragma unroll
-            for (int i = 0; i < kShare; ++i) px[i] = *(const u32x4 *)(v + ((w - 4) * kShare + i) * 16 * tile);
-        } else {
-            const uint8_t *k = a.kv.k + at + (uint64_t)(tok + (c & 3) + 4 * w) * D + 16 * g;
-#pragma unroll
-            for (int i = 0; i < kShare; ++i) px[i] = *(const u32x4 *)(k + 64 * i);
-        }
+        for (int i = 0; i < kShare; ++i) px[i] = *(const u32x4 *)(p + in_page + i * piece);
     };
     auto stage = [&](uint32_t kt) {
         const int b = kt & 1;
@@ -736,9 +779,9 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
             }
             return;
         }
-        if ((uint64_t)kt * kStep + kStep + hd.n > hd.ctx) {
-            // tokens that not every row of the sequence sees: bytes of slots
-            // that hold no token are cleared, a NaN is taken out and noted
+        if (kt * kStep + kStep > own_from) {
+            // bytes of slots that hold no token are cleared, a NaN is taken out
+            // and noted
             const uint32_t tok0 = kt * kStep + 16 * g;
             const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
             bool nan = false;
@@ -813,41 +856,59 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
                     for (int n = 0; n < NT; ++n) acc[n][d + q] = product(vf, pf[n][u], acc[n][d + q]);
                 }
     };
-    // `reads` fragments in all, each for NT products: six on their way
+    // `reads` fragments in all, each for NT products: kAhead on their way
     auto interleave = [&](auto reads) {
         constexpr int kReads = decltype(reads)::value;
-        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
-        for (int i = 0; i < kReads - 6; ++i) {
+        for (int i = 0; i < kReads - kAhead; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, NT, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, 6 * NT, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead * NT, 0);
     };
-    auto softmax = [&](uint32_t kt) {
-        // not 0, which would turn a masked score's -inf into NaN
-        const float sc0 = sc_at[0] * a.c0, sc = sc0 == 0.0f ? 1.0e-30f : sc0;
-        const float vsl = vs_at[0], vlog = log2_of(vsl);
-        const uint32_t tok0 = kt * kStep + 16 * g;
-        if (kt * kStep + kStep > all_lim) {
+    // not 0, which would turn a masked score's -inf into NaN
+    auto scale_of = [&]() {
+        const float x = sc_at[0] * a.c0;
+        return x == 0.0f ? 1.0e-30f : x;
+    };
+    // P in units of 2^y with y as it is, its sum in l's units of 2^m at once;
+    // false (and l as it was) where that will not do: a weight passes 2^y by
+    // too much (the first step, a larger score), scales are further apart than
+    // fp32 takes in one, NaN
+    auto softmax = [&]() {
+        const float sc = scale_of(), vlog = log2_of(vs_at[0]);
+        float up[NT], sum[NT];                         // up: log2 of a weight over its P
+        bool fits = true;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (tok0 + 4 * t + i >= lim[n]) st[n][t][i] = -INFINITY;
+        for (int n = 0; n < NT; ++n) {
+            const float by = vlog - y[n];
+            up[n] = -by - m[n];
+            sum[n] = weights_of(st[n], sc, by, pf[n]);
+            fits &= sum[n] <= kMaxSum && fabsf(up[n]) < 64.0f;
         }
-        if ((uint64_t)kt * kStep + kStep + hd.n > hd.ctx) {
+        if (!__all(fits)) return false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) l[n] += sum[n] * exp2_of(up[n]);
+        return true;
+    };
+    // any step: masks, NaN values among those that not every row sees, maxima
+    // raised
+    auto softmax_any = [&](uint32_t kt) {
+        const float sc = scale_of(), vlog = log2_of(vs_at[0]);
+        const uint32_t tok0 = kt * kStep + 16 * g;
+        if (kt * kStep + kStep > own_from) {
             const uint32_t noted = lds_nan[kt & 1];
-            if (noted) {
-                // as in attend_kernel: the rows that see a NaN value are found
-                // by a product of the masks
+            // as in attend_kernel: the rows that see a NaN value are found by
+            // a product of the masks
+            if (noted)
+#pragma unroll 1
                 for (int d = 0; d < kDT; ++d) {
                     if (!(noted >> (d / kShare) & 1)) continue;
                     f32x4 hit[NT];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) hit[n] = f32x4{0, 0, 0, 0};
+#pragma unroll 1
                     for (int u = 0; u < 2; ++u) {
                         const uint32_t bits = lds_bits[kt & 1][2 * d + u][lane];
                         f16x8 one;
@@ -855,9 +916,10 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
                         for (int j = 0; j < 8; ++j) one[j] = bits >> j & 1 ? (_Float16)1.0f : (_Float16)0.0f;
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
+                            const int left = (int)lim[n] - (int)tok0 - 8 * u;
                             f16x8 see;
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) see[j] = tok0 + 8 * u + j < lim[n] ? (_Float16)1.0f : (_Float16)0.0f;
+                            for (int j = 0; j < 8; ++j) see[j] = left > j ? (_Float16)1.0f : (_Float16)0.0f;
                             hit[n] = product(one, see, hit[n]);
                         }
                     }
@@ -866,114 +928,93 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) nan_sums |= (uint64_t)(hit[n][i] > 0.0f) << (4 * (n * kDT + d) + i);
                 }
-            }
         }
-        bool grow = false;
-        float mx[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            mx[n] = st[n][0][0];
+            const int left = (int)lim[n] - (int)tok0;
+            float mx = -INFINITY;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mx[n] = fmaxf(mx[n], st[n][t][i]);
-            mx[n] = mx[n] == -INFINITY ? -INFINITY : mx[n] * sc;
-            grow |= mx[n] > m[n] + kMaxGrow || mx[n] + vlog > y[n] + kMaxGrow;
-        }
-        if (__any(grow)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float mn = fmaxf(m[n], row_max(mx[n])), yn = fmaxf(y[n], row_max(mx[n] + vlog));
-                l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
-                const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
-                m[n] = mn;
-                y[n] = yn;
-#pragma unroll
-                for (int d = 0; d < kDT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
-            }
-        }
-        // P in units of 2^y; its sum is turned into l's units of 2^m at once,
-        // unless one of them would leave fp32's range
-        float up[NT];                                  // log2 of a weight over its P
-        bool far = false;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            up[n] = y[n] - vlog - m[n];
-            far |= !(fabsf(up[n]) < 64.0f);
-        }
-        if (__any(far)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float sum = 0.0f;
-                const float mm = m[n] == -INFINITY ? 0.0f : m[n];
-                const float f = y[n] == -INFINITY ? 0.0f : fminf(vsl * exp2_of(mm - y[n]), 3.0e38f);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float p = exp2_of(fmaf(st[n][j >> 2][j & 3], sc, -mm));
-                    sum += p;
-                    pf[n][j >> 3][j & 7] = (_Float16)(p * f);
+                for (int i = 0; i < 4; ++i) {
+                    st[n][t][i] = left > 4 * t + i ? st[n][t][i] : -INFINITY;
+                    mx = fmaxf(mx, st[n][t][i]);
                 }
-                l[n] += sum;
-            }
-        } else {
+            mx = mx == -INFINITY ? -INFINITY : mx * sc;
+            const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog));
+            l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
+            const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
+            m[n] = mn;
+            y[n] = yn;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float sum = 0.0f;
-                const float by = vlog - y[n];
+            for (int d = 0; d < kDT; ++d)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    float p[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        p[i] = exp2_of(fmaf(st[n][t][i], sc, by));
-                        sum += p[i];
-                    }
-                    const f16x2 u = __builtin_convertvector((f32x2{p[0], p[1]}), f16x2);
-                    const f16x2 v = __builtin_convertvector((f32x2{p[2], p[3]}), f16x2);
-                    const int j = 4 * (t & 1);
-                    pf[n][t >> 1][j] = u[0];
-                    pf[n][t >> 1][j + 1] = u[1];
-                    pf[n][t >> 1][j + 2] = v[0];
-                    pf[n][t >> 1][j + 3] = v[1];
-                }
-                l[n] += sum * exp2_of(up[n]);
-            }
+                for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
+            l[n] += weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
+            weights_of(st[n], sc, yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
         }
     };
 
-    uint32_t po = 0, pv = 0;
+    // pages of the step after next and the one after it
+    uint32_t po = 0, pv = 0, po_on = 0, pv_on = 0;
+    float sc_on = 0.0f, vs_on = 0.0f;                 // scales of the step after next
     if (threadIdx.x < 2) lds_nan[threadIdx.x] = 0;
     // the first step's products with "the step before" are of zeros
     for (uint32_t i = threadIdx.x; i < 2 * kDT * 64; i += kPromptThreads) (&lds_v[~it.k0 & 1][0][0])[i] = u32x4{0, 0, 0, 0};
     meet();
     sc_at[0] = vs_at[0] = sc_at[1] = vs_at[1] = 0.0f;
     if (it.k0 < it.k1) {
-        fetch(it.k0, pages[block_at(it.k0, own_group)], pages[block_at(it.k0, g)], sc_at[0], vs_at[0]);
+        fetch(it.k0, page_at(it.k0, own_group));
+        scales_of(page_at(it.k0, g), sc_at[0], vs_at[0]);
         stage(it.k0);
-        if (it.k0 + 1 < it.k1)
-            fetch(it.k0 + 1, pages[block_at(it.k0 + 1, own_group)], pages[block_at(it.k0 + 1, g)], sc_at[1], vs_at[1]);
-        po = pages[block_at(it.k0 + 2, own_group)];
-        pv = pages[block_at(it.k0 + 2, g)];
+        fetch(it.k0 + 1, page_at(it.k0 + 1, own_group));
+        scales_of(page_at(it.k0 + 1, g), sc_at[1], vs_at[1]);
+        po = page_at(it.k0 + 2, own_group);
+        pv = SMALL ? page_at(it.k0 + 2, g) : po;
     }
     meet();
     if (second) meet();
-    for (uint32_t kt = it.k0; kt < it.k1; ++kt) {
-        values(kt - 1);
-        scores(kt);
-        interleave(std::integral_constant<int, D / 4>());
-        meet();
-        softmax(kt);
-        if (kt + 1 < it.k1) stage(kt + 1);
+    // Small loads for later steps go out before the softmax, which hides them
+    // (page_at stays within the sequence's blocks past its end).
+    auto look_ahead = [&](uint32_t kt) {
+        scales_of(pv, sc_on, vs_on);
+        po_on = page_at(kt + 3, own_group);
+        pv_on = SMALL ? page_at(kt + 3, g) : po_on;
+    };
+    auto pass_on = [&](uint32_t kt) {
+        if (kt + 1 < it.k1) {
+            stage(kt + 1);
+            fetch(kt + 2, po);
+        }
         sc_at[0] = sc_at[1];
         vs_at[0] = vs_at[1];
-        if (kt + 2 < it.k1) {
-            fetch(kt + 2, po, pv, sc_at[1], vs_at[1]);
-            po = pages[block_at(kt + 3, own_group)];
-            pv = pages[block_at(kt + 3, g)];
-        }
+        sc_at[1] = sc_on;
+        vs_at[1] = vs_on;
+        po = po_on;
+        pv = pv_on;
         meet();
+    };
+    // The ordinary steps have a loop of their own: with the other ones as a
+    // branch in it the compiler keeps the sums in two places and moves them
+    // back and forth in every step.
+    for (uint32_t kt = it.k0; kt < it.k1; ++kt) {
+        bool done;
+        do {
+            values(kt - 1);
+            scores(kt);
+            interleave(std::integral_constant<int, D / 4>());
+            meet();
+            done = kt * kStep + kStep <= all_lim;
+            if (kt * kStep + kStep > own_from) done = done && __builtin_amdgcn_readfirstlane(lds_nan[kt & 1]) == 0;
+            look_ahead(kt);
+            if (done) done = softmax();
+            if (!done) break;
+            pass_on(kt);
+            ++kt;
+        } while (kt < it.k1);
+        if (done) break;
+        softmax_any(kt);
+        pass_on(kt);
     }
     if (!second) meet();
     if (it.k0 < it.k1) values(it.k1 - 1);
@@ -1592,7 +1633,10 @@ void launch_attend(const Layout &y, const AttendArgs &a, const Join *joins, cons
     const dim3 grid(y.item_cap * a.kv.hk);
 #define NETKV_ATTEND(NT, UNITS) attend_kernel<D, NT, HALF, UNITS><<<grid, kThreads, 0, s>>>(a)
     if (y.rows) {
-        prompt_kernel<D, D == 256 ? 1 : 2, HALF><<<grid, kPromptThreads, 0, s>>>(a);
+        if (a.kv.btl < 6)
+            prompt_kernel<D, D == 256 ? 1 : 2, HALF, true><<<grid, kPromptThreads, 0, s>>>(a);
+        else
+            prompt_kernel<D, D == 256 ? 1 : 2, HALF, false><<<grid, kPromptThreads, 0, s>>>(a);
     } else if (y.NT == 1) {
         if (wa.w) NETKV_ATTEND(1, true);
         else NETKV_ATTEND(1, false);
