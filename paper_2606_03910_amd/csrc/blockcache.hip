@@ -1140,27 +1140,32 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
 }
 
 // Block weights of a call of many rows: with every row's lse known, the
-// scores are formed once more, 64 tokens a workgroup against all rows, and
-// 2^(x - lse) is summed over them (a prompt's partial sums of every row would
-// be larger than its cache).
+// scores are formed once more, 256 tokens a workgroup (64 a wavefront, their
+// keys in registers) against all rows, and 2^(x - lse) is summed over them (a
+// prompt's partial sums of every row would be larger than its cache).  Rows
+// come 64 at a time, 16 by each wavefront, through LDS: read by each wavefront
+// for itself, every CU of a head's XCD asked its cache for the same lines
+// (1,880 us for prompt-chunk).
 template <int D, bool HALF>
-__global__ __launch_bounds__(kThreads) void column_kernel(AttendArgs a, WeightArgs wa) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void column_kernel(AttendArgs a, WeightArgs wa) {
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
-    __shared__ float lds[kWaves][4];
+    __shared__ u32x4 lds_q[2][kWaves][D / 32][64];
+    __shared__ float lds_lse[2][16 * kWaves];
+    __shared__ int lds_seen[2][16 * kWaves];           // tokens that a row sees
     const uint32_t hk = a.kv.hk;
-    const uint32_t h = blockIdx.x % hk, kt = blockIdx.x / hk, s = blockIdx.y;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t h = blockIdx.x % hk, kt0 = blockIdx.x / hk * kWaves, kt = kt0 + w, s = blockIdx.y;
     const Head hd = seq_head(a.kv, s);
-    if ((uint64_t)kt * kStep >= hd.ctx) return;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if ((uint64_t)kt0 * kStep >= hd.ctx) return;
     const uint32_t c = lane & 15, g = lane >> 4;
-    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep);
+    const uint32_t bt = 1u << a.kv.btl;
     const uint32_t *pages = a.kv.pages + (uint64_t)s * a.kv.max_pages;
     const uint32_t last_block = (hd.ctx - 1) >> a.kv.btl;
     const uint32_t pk = pages[min((kt * kStep + 16 * (c >> 2)) >> a.kv.btl, last_block)];
     const uint32_t pv = pages[min((kt * kStep + 16 * g) >> a.kv.btl, last_block)];
     const bool bad = pv >= a.kv.n_pages;
-    const float sc = bad ? NAN : a.kv.ks[(uint64_t)pv * hk + h] * a.c0;
+    const float sc = bad ? NAN : a.kv.ks[(uint64_t)pv * hk + h] * (a.q_sign ? -a.c0 : a.c0);
     const uint32_t tok = ((kt * kStep + 16 * (c >> 2)) & (bt - 1)) + (c & 3);
     const uint8_t *p = a.kv.k + ((uint64_t)(pk < a.kv.n_pages ? pk : 0u) * hk + h) * head_bytes(a.kv, D) + (uint64_t)tok * D + 16 * g;
     T8 kf[4][D / 32];
@@ -1172,49 +1177,81 @@ __global__ __launch_bounds__(kThreads) void column_kernel(AttendArgs a, WeightAr
             kf[t][2 * i] = widen<HALF>(x[0], x[1]);
             kf[t][2 * i + 1] = widen<HALF>(x[2], x[3]);
         }
-    const uint32_t tok0 = kt * kStep + 16 * g;
+    const int tok0 = (int)(kt * kStep + 16 * g);
     const uint32_t n_rows = hd.n * a.G;
-    // the first row that sees a token of this step
-    const int64_t t0 = (int64_t)kt * kStep - ((int64_t)hd.ctx - hd.n);
-    const uint32_t first = t0 > 0 ? (uint32_t)t0 * a.G : 0u;
-    float sum = 0.0f;
-    for (uint32_t r0 = first / 16 * 16 + 16 * w; r0 < n_rows; r0 += 16 * kWaves) {
-        const uint32_t r = r0 + c;
-        const bool valid = r < n_rows;
-        const uint32_t t = valid ? r / a.G : 0u, qh = h * a.G + (valid ? r % a.G : 0u);
-        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
-        const uint32_t lim = valid && seen > 0 ? (uint32_t)seen : 0u;
-        const float lse = valid ? a.lse[(hd.row0 + t) * a.Hq + qh] : 0.0f;
+    // the first row that sees a token of the workgroup's; rows from `full` on
+    // see all of this wavefront's
+    const int64_t old = (int64_t)hd.ctx - hd.n;
+    const uint32_t first = (int64_t)kt0 * kStep > old ? (uint32_t)((int64_t)kt0 * kStep - old) * a.G / 16 * 16 : 0u;
+    const int64_t need = (int64_t)kt * kStep + kStep - 1 - old;
+    const uint64_t full = (uint64_t)kt * kStep + kStep > hd.ctx ? ~0ull : need > 0 ? (uint64_t)need * a.G : 0ull;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    T8 qf[D / 32];
+    float lse = 0.0f;
+    int seen = 0;
+    auto fetch = [&](uint32_t r0) {                    // rows r0 + 16 w + c
+        const uint32_t r = r0 + 16 * w + c;
+        const uint32_t at = min(r, n_rows - 1), t = at / a.G, qh = h * a.G + at % a.G;
+        const int64_t sees = old + t + 1;
+        seen = r < n_rows && sees > 0 ? (int)sees : 0;
+        lse = a.lse[(hd.row0 + t) * a.Hq + qh];
         const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)qh * D + 16 * g;
-        f32x4 st[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            u32x4 x = {0, 0, 0, 0};
-            if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
-            const T8 qf = __builtin_bit_cast(T8, x ^ a.q_sign);
+        for (int i = 0; i < D / 32; ++i) qf[i] = *(const T8 *)(q + (i / 2) * 64 + (i % 2) * 8);
+    };
+    auto stage = [&](int b) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) st[u] = product(kf[u][i], qf, st[u]);
+        for (int i = 0; i < D / 32; ++i) lds_q[b][w][i][lane] = __builtin_bit_cast(u32x4, qf[i]);
+        if (g == 0) {
+            lds_lse[b][16 * w + c] = lse;
+            lds_seen[b][16 * w + c] = seen;
         }
+    };
+    if (first < n_rows) {
+        fetch(first);
+        stage(0);
+        __syncthreads();
+    }
+    int b = 0;
+    for (uint32_t r0 = first; r0 < n_rows; r0 += 16 * kWaves, b ^= 1) {
+        if (r0 + 16 * kWaves < n_rows) fetch(r0 + 16 * kWaves);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int v = 0; v < kWaves; ++v) {
+            f32x4 st[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float e = exp2_of(st[u][i] * sc - lse);
-                sum += tok0 + 4 * u + i < lim ? e : 0.0f;
+            for (int i = 0; i < D / 32; ++i) {
+                const T8 x = __builtin_bit_cast(T8, lds_q[b][v][i][lane]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) st[u] = product(kf[u][i], x, st[u]);
             }
+            const float of = lds_lse[b][16 * v + c];
+            if (r0 + 16 * v >= full && r0 + 16 * v + 16 <= n_rows) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[u] += exp2_of(fmaf(st[u][i], sc, -of));
+            } else {
+                const int left = lds_seen[b][16 * v + c] - tok0;   // tokens of this lane's 16 that the row sees
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float e = exp2_of(fmaf(st[u][i], sc, -of));
+                        sum[u] += 4 * u + i < left ? e : 0.0f;
+                    }
+            }
+        }
+        if (r0 + 16 * kWaves < n_rows) stage(b ^ 1);
+        __syncthreads();
     }
-    // over the rows (16 lanes), then the group's 16 tokens join their unit
-    for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor(sum, d, 64);
-    if (c == 0) lds[w][g] = sum;
-    __syncthreads();
-    const uint32_t per = kStep / tile, gr = tile / 16;
-    if (threadIdx.x < per) {
-        float x = 0.0f;
-        for (uint32_t i = 0; i < gr; ++i)
-            for (int v = 0; v < kWaves; ++v) x += lds[v][threadIdx.x * gr + i];
-        const uint32_t u = kt * per + threadIdx.x;
-        if (u < a.n_units) wa.cols[((uint64_t)s * hk + h) * a.n_units + u] = x;
-    }
+    // over the rows (16 lanes), then the units' groups of 16 tokens
+    const uint32_t tile = min(bt, kStep);
+    float x = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    for (int d = 1; d < 16; d <<= 1) x += __shfl_xor(x, d, 64);
+    if (tile >= 32) x = pair16_sum(x);
+    if (tile >= 64) x += __shfl_xor(x, 32, 64);
+    const uint32_t u = kt * (kStep / tile) + 16 * g / tile;
+    if (c == 0 && ((16 * g) & (tile - 1)) == 0 && u < a.n_units) wa.cols[((uint64_t)s * hk + h) * a.n_units + u] = x;
 }
 
 // The units of a block and the heads, in order.
@@ -1653,7 +1690,7 @@ void launch_attend(const Layout &y, const AttendArgs &a, const Join *joins, cons
     if (!wa.w) return;
     if (y.rows) {
         const uint32_t steps = (uint32_t)((((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep);
-        column_kernel<D, HALF><<<dim3(steps * a.kv.hk, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
+        column_kernel<D, HALF><<<dim3((steps + kWaves - 1) / kWaves * a.kv.hk, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
         block_kernel<<<dim3((a.kv.max_pages + kThreads - 1) / kThreads, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
     } else {
         unit_kernel<<<dim3((a.kv.max_pages + kWaves - 1) / kWaves, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
