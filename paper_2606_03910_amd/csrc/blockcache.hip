@@ -167,18 +167,22 @@ struct PlanHead {
     uint32_t n_items, n_joins, n_slots, pad;
 };
 
+// How a call is split.  With up to kListed sequences every wavefront finds its
+// share by itself (Shares); beyond that plan_kernel writes the list.
 struct PlanArgs {
     Kv kv;
     uint32_t G, tile_rows, target, least, round;   // ranges of at least `least` steps, multiples of `round`
     uint32_t item_cap, slot_cap, join_cap;
     PlanHead *head;
-    Item *items;
+    Item *items;                                   // null: not listed
     Join *joins;
     // rows of sequences that cannot be answered
-    uint16_t *out;
+    uint16_t *bad_out;
     uint64_t out_stride;
     uint32_t row_elems, nan16;
 };
+
+constexpr uint32_t kListed = 256;
 
 constexpr int kPlanThreads = 1024;
 
@@ -216,6 +220,158 @@ __device__ inline uint32_t tile_end(const Head &h, uint32_t G, uint32_t tile, ui
     return seen <= 0 ? 0u : (uint32_t)((seen + kStep - 1) / kStep);
 }
 
+__device__ inline uint32_t tiles_of(const Head &h, const PlanArgs &a) {
+    return (uint32_t)(((uint64_t)h.n * a.G + a.tile_rows - 1) / a.tile_rows);
+}
+
+// Steps of a range: what spreads `work` steps over `target` ranges.
+__device__ inline uint32_t range_steps(const PlanArgs &a, unsigned long long work) {
+    unsigned long long len = (work + a.target - 1) / a.target;
+    if (len < a.least) len = a.least;
+    len = (len + a.round - 1) / a.round * a.round;
+    return len > 0x7FFFFFFFull ? 0x7FFFFFFFu : (uint32_t)len;
+}
+
+__device__ inline Item item_of(const PlanArgs &a, uint32_t seq, const Head &h, uint32_t C, uint32_t n, uint32_t p, uint32_t j, uint32_t slot0) {
+    const uint32_t tile = n - 1 - j / p, part = j % p;   // the tiles that see most first
+    const uint32_t end = tile_end(h, a.G, tile, a.tile_rows);
+    Item it;
+    it.seq = seq;
+    it.tile = tile;
+    it.k0 = part * C;
+    it.k1 = min(end, p > 1 ? (part + 1) * C : end);
+    it.slot = p > 1 ? slot0 + tile * p + part : kNoSlot;
+    return it;
+}
+
+// The rows of sequences that cannot be answered, by one workgroup.
+__device__ inline void fill_bad(const PlanArgs &a) {
+    for (uint32_t s = 0; s < a.kv.n_seq; ++s) {
+        const Head h = seq_head(a.kv, s);
+        if (h.ok) continue;
+        if (threadIdx.x == 0) report(a.kv);
+        if (!h.rows_ok) continue;
+        const uint64_t rows = a.kv.off[s + 1] - h.row0;
+        for (uint64_t i = threadIdx.x; i < rows * a.row_elems; i += blockDim.x)
+            a.bad_out[(h.row0 + i / a.row_elems) * a.out_stride + i % a.row_elems] = (uint16_t)a.nan16;
+    }
+}
+
+// The same list as a wavefront has it in its registers: each lane takes up to
+// four sequences in a row (n_seq <= kListed).
+struct Shares {
+    uint32_t rt[4], kt[4], C, per;
+    uint32_t items, slots, joins;      // inclusive sums up to this lane
+    uint32_t own_items, own_slots, own_joins;
+    bool bad;
+
+    __device__ explicit Shares(const PlanArgs &a) {
+        const uint32_t lane = threadIdx.x & 63;
+        per = (a.kv.n_seq + 63) / 64;
+        unsigned long long work = 0;
+        bad = false;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            rt[j] = kt[j] = 0;
+            const uint32_t s = lane * per + j;
+            if (j < per && s < a.kv.n_seq) {
+                const Head h = seq_head(a.kv, s);
+                rt[j] = tiles_of(h, a);
+                kt[j] = (h.ctx + kStep - 1) / kStep;
+                work += (unsigned long long)rt[j] * kt[j];
+                bad |= !h.ok;
+            }
+        }
+        for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d, 64);
+        C = range_steps(a, work);
+        own_items = own_slots = own_joins = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t p = parts(j);
+            own_items += rt[j] * p;
+            own_slots += p > 1 ? rt[j] * p : 0u;
+            own_joins += p > 1 ? rt[j] : 0u;
+        }
+        items = own_items;
+        slots = own_slots;
+        joins = own_joins;
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t x = __shfl_up(items, d, 64), y = __shfl_up(slots, d, 64), z = __shfl_up(joins, d, 64);
+            if ((int)lane >= d) {
+                items += x;
+                slots += y;
+                joins += z;
+            }
+        }
+    }
+    __device__ uint32_t parts(uint32_t j) const { return kt[j] > C ? (kt[j] + C - 1) / C : 1u; }
+
+    // false: there are not so many
+    __device__ bool item(const PlanArgs &a, uint32_t i, Item &it) const {
+        const uint64_t past = __ballot(items > i);
+        if (!past) return false;
+        const int l = __ffsll((unsigned long long)past) - 1;
+        uint32_t at = items - own_items, slot = slots - own_slots, seq = 0, n = 0, p = 1, rest = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t q = parts(j), x = rt[j] * q;
+            if (i >= at && i < at + x) {
+                seq = (threadIdx.x & 63) * per + j;
+                n = rt[j];
+                p = q;
+                rest = i - at;
+                break;
+            }
+            at += x;
+            slot += q > 1 ? x : 0u;
+        }
+        auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
+        seq = of(seq);
+        it = item_of(a, seq, seq_head(a.kv, seq), C, of(n), of(p), of(rest), of(slot));
+        return true;
+    }
+    __device__ uint32_t n_joins() const { return (uint32_t)__builtin_amdgcn_readlane((int)joins, 63); }
+    __device__ Join join(uint32_t i) const {
+        const int l = __ffsll((unsigned long long)__ballot(joins > i)) - 1;
+        uint32_t at = joins - own_joins, slot = slots - own_slots, seq = 0, tile = 0, p = 1;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t q = parts(j), x = q > 1 ? rt[j] : 0u;
+            if (i >= at && i < at + x) {
+                seq = (threadIdx.x & 63) * per + j;
+                tile = i - at;
+                p = q;
+                slot += tile * q;
+                break;
+            }
+            at += x;
+            slot += x * q;
+        }
+        auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
+        return Join{of(seq), of(tile), of(slot), of(p)};
+    }
+};
+
+// This workgroup's share and its sequence; false if there is none.  What every
+// lane has the same of goes to scalar registers.
+__device__ inline bool find_item(const PlanArgs &a, uint32_t i, Item &it, Head &hd) {
+    if (a.items) {
+        if (i >= a.head->n_items) return false;
+        it = a.items[i];
+    } else {
+        const Shares sh(a);
+        if (blockIdx.x == 0 && __any(sh.bad)) fill_bad(a);
+        if (!sh.item(a, i, it)) return false;
+    }
+    auto one = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+    it = Item{one(it.seq), one(it.tile), one(it.k0), one(it.k1), one(it.slot), {0, 0, 0}};
+    hd = seq_head(a.kv, it.seq);
+    hd.row0 = (uint64_t)one((uint32_t)(hd.row0 >> 32)) << 32 | one((uint32_t)hd.row0);
+    hd.n = one(hd.n);
+    hd.ctx = one(hd.ctx);
+    return true;
+}
+
 // One workgroup.  Ranges are as long as spreads the call's steps over
 // `target` of them, so a batch of unequal sequences fills the card evenly; a
 // sequence no longer than one range is not split and writes its rows itself.
@@ -228,23 +384,18 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     unsigned long long mine = 0;
     for (uint32_t s = threadIdx.x; s < a.kv.n_seq; s += kPlanThreads) {
         const Head h = seq_head(a.kv, s);
-        const uint64_t rt = ((uint64_t)h.n * a.G + a.tile_rows - 1) / a.tile_rows;
-        mine += rt * ((h.ctx + kStep - 1) / kStep);
-        if (!h.ok) report(a.kv);
+        mine += (unsigned long long)tiles_of(h, a) * ((h.ctx + kStep - 1) / kStep);
     }
     atomicAdd(&work, mine);
     __syncthreads();
-    unsigned long long len = (work + a.target - 1) / a.target;
-    if (len < a.least) len = a.least;
-    len = (len + a.round - 1) / a.round * a.round;
-    const uint32_t C = len > 0x7FFFFFFFull ? 0x7FFFFFFFu : (uint32_t)len;
+    const uint32_t C = range_steps(a, work);
     uint32_t at[3] = {0, 0, 0};   // items, slots, joins so far
     for (uint32_t s0 = 0; s0 < a.kv.n_seq; s0 += kPlanThreads) {
         const uint32_t s = s0 + threadIdx.x;
         uint32_t x[3] = {0, 0, 0}, rt = 0, sp = 1;
         if (s < a.kv.n_seq) {
             const Head h = seq_head(a.kv, s);
-            rt = (uint32_t)(((uint64_t)h.n * a.G + a.tile_rows - 1) / a.tile_rows);
+            rt = tiles_of(h, a);
             const uint32_t kt = (h.ctx + kStep - 1) / kStep;
             sp = kt > C ? (kt + C - 1) / C : 1u;
             x[0] = rt * sp;
@@ -265,54 +416,35 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
                 if (base[mid][0] <= i) lo = mid; else hi = mid;
             }
             const uint32_t j = i - base[lo][0], n = geo[lo][0], p = geo[lo][1];
-            const uint32_t tile = n - 1 - j / p, part = j % p;   // the tiles that see most first
-            const Head h = seq_head(a.kv, s0 + lo);
-            const uint32_t end = tile_end(h, a.G, tile, a.tile_rows);
-            Item it;
-            it.seq = s0 + lo;
-            it.tile = tile;
-            it.k0 = part * C;
-            it.k1 = min(end, p > 1 ? (part + 1) * C : end);
-            const uint32_t slot = at[1] + base[lo][1] + tile * p + part;
-            it.slot = p > 1 ? slot : kNoSlot;
+            const Item it = item_of(a, s0 + lo, seq_head(a.kv, s0 + lo), C, n, p, j, at[1] + base[lo][1]);
             const uint32_t idx = at[0] + i;
-            if (idx < a.item_cap && (p == 1 || slot < a.slot_cap)) a.items[idx] = it;
-            if (p > 1 && part == 0) {
-                const uint32_t q = at[2] + base[lo][2] + tile;
-                if (q < a.join_cap) a.joins[q] = Join{s0 + lo, tile, slot, p};
+            if (idx < a.item_cap && (p == 1 || it.slot < a.slot_cap)) a.items[idx] = it;
+            if (p > 1 && j % p == 0) {
+                const uint32_t q = at[2] + base[lo][2] + it.tile;
+                if (q < a.join_cap) a.joins[q] = Join{it.seq, it.tile, it.slot, p};
             }
         }
         for (int i = 0; i < 3; ++i) at[i] += tot[i];
         __syncthreads();
     }
     if (threadIdx.x == 0) *a.head = PlanHead{min(at[0], a.item_cap), min(at[2], a.join_cap), at[1], 0};
-    // rows of the sequences that cannot be answered
-    for (uint32_t s = 0; s < a.kv.n_seq; ++s) {
-        const Head h = seq_head(a.kv, s);
-        if (h.ok || !h.rows_ok) continue;
-        const uint64_t rows = a.kv.off[s + 1] - h.row0;
-        for (uint64_t i = threadIdx.x; i < rows * a.row_elems; i += kPlanThreads)
-            a.out[(h.row0 + i / a.row_elems) * a.out_stride + i % a.row_elems] = (uint16_t)a.nan16;
-    }
+    fill_bad(a);
 }
 
 // ------------------------------------------------------------------ attention
 
-struct AttendArgs {
-    Kv kv;
-    uint32_t G, Hq, tile_rows;
-    uint64_t q_stride, out_stride;   // elements between tokens
+struct AttendArgs : PlanArgs {
+    uint32_t Hq;
+    uint64_t q_stride;               // elements between tokens, as out_stride
     const void *q;
     void *out;
     float c0;                        // |scale| * log2(e)
     uint32_t q_sign;                 // flips the queries' signs where scale < 0
-    const PlanHead *head;
-    const Item *items;
     float *part;                     // [slot][head][tile_rows][D]
     f32x4 *part_ml;                  // [slot][head][tile_rows] m, l, y
     float *lse;                      // [row][query head] log2 of the row's sum, or null
-    float *units;                    // [seq][head][unit][tile_rows] log2 of the unit's sum, or null
-    uint32_t n_units;
+    float *units;                    // [seq][head][unit][unit_rows] log2 of the unit's sum, or null
+    uint32_t n_units, unit_rows;
 };
 
 // What a part with maximum m counts for beside the maximum of all; a part
@@ -349,7 +481,7 @@ struct ValRegs {
 // The four wavefronts take the same rows and every fourth step each, joined
 // through LDS.
 template <int D, int NT, bool HALF, bool UNITS>
-__global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : NT == 1 && !(UNITS && D == 128) ? 3 : 2) void attend_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
     constexpr int kDT = D / 16;
@@ -359,9 +491,9 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
 
     const uint32_t hk = a.kv.hk;
     const uint32_t h = blockIdx.x % hk, item = blockIdx.x / hk;
-    if (item >= a.head->n_items) return;
-    const Item it = a.items[item];
-    const Head hd = seq_head(a.kv, it.seq);
+    Item it;
+    Head hd;
+    if (!find_item(a, item, it, hd)) return;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
     const uint32_t c = lane & 15, g = lane >> 4;
     const uint32_t n_rows = hd.n * a.G;
@@ -521,7 +653,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(AttendArgs a) {
                 const uint32_t per = kStep / tile;
                 const uint32_t u = kt * per + 16 * g / tile;
                 if (((16 * g) & (tile - 1)) == 0 && u < a.n_units)
-                    a.units[(((uint64_t)it.seq * hk + h) * a.n_units + u) * a.tile_rows + n * 16 + c] =
+                    a.units[(((uint64_t)it.seq * hk + h) * a.n_units + u) * a.unit_rows + row0 + n * 16 + c] =
                         mm + log2_of(sum);
             }
         }
@@ -688,9 +820,9 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 
     const uint32_t hk = a.kv.hk;
     const uint32_t h = blockIdx.x % hk, item = blockIdx.x / hk;
-    if (item >= a.head->n_items) return;
-    const Item it = a.items[item];
-    const Head hd = seq_head(a.kv, it.seq);
+    Item it;
+    Head hd;
+    if (!find_item(a, item, it, hd)) return;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
     const bool second = w >= 4;
     const uint32_t c = lane & 15, g = lane >> 4;
@@ -1055,20 +1187,17 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 // O = sum 2^(y - Y) O_i, l = sum 2^(m - M) l_i.  A workgroup a row, its
 // threads the row's columns by four times a share of the ranges.
 template <int D, bool HALF>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, const Join *joins) {
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
     constexpr int kCols = D / 4, kGroups = kThreads / kCols;
     __shared__ f32x4 lo[kGroups][kCols];
     __shared__ float ll[kGroups];
     const uint32_t hk = a.kv.hk, rows = a.tile_rows;
     const uint32_t col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
-    const uint64_t all = (uint64_t)a.head->n_joins * hk * rows;
-    for (uint64_t task = blockIdx.x; task < all; task += gridDim.x) {
-        const uint32_t tr = (uint32_t)(task % rows), h = (uint32_t)(task / rows % hk);
-        const Join j = joins[task / rows / hk];
+    auto join_row = [&](const Join &j, uint32_t h, uint32_t tr) {
         const Head hd = seq_head(a.kv, j.seq);
         const uint32_t r = j.tile * rows + tr;
-        if (r >= hd.n * a.G) continue;
+        if (r >= hd.n * a.G) return;
         auto at = [&](uint32_t i) { return ((uint64_t)(j.slot + i) * hk + h) * rows + tr; };
         float M = -INFINITY, Y = -INFINITY;
         for (uint32_t i = 0; i < j.n; ++i) {
@@ -1107,6 +1236,14 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, const Join
             if (a.lse && col == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
         }
         __syncthreads();
+    };
+    if (a.joins) {
+        const uint64_t all = (uint64_t)a.head->n_joins * hk * rows;
+        for (uint64_t task = blockIdx.x; task < all; task += gridDim.x) join_row(a.joins[task / rows / hk], (uint32_t)(task / rows % hk), (uint32_t)(task % rows));
+    } else {
+        const Shares sh(a);
+        const uint64_t all = (uint64_t)sh.n_joins() * hk * rows;
+        for (uint64_t task = blockIdx.x; task < all; task += gridDim.x) join_row(sh.join((uint32_t)(task / rows / hk)), (uint32_t)(task / rows % hk), (uint32_t)(task % rows));
     }
 }
 
@@ -1132,8 +1269,8 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
         for (uint32_t i = lane; i < hd.n * a.Hq; i += 64) {
             const uint32_t h = i / (hd.n * a.G), row = i % (hd.n * a.G);
             const float lse = a.lse[(hd.row0 + row / a.G) * a.Hq + h * a.G + row % a.G];
-            const float *p = a.units + (((uint64_t)s * a.kv.hk + h) * a.n_units + u0) * a.tile_rows + row;
-            for (uint32_t u = u0; u < u1; ++u, p += a.tile_rows) sum += exp2_of(*p - lse);
+            const float *p = a.units + (((uint64_t)s * a.kv.hk + h) * a.n_units + u0) * a.unit_rows + row;
+            for (uint32_t u = u0; u < u1; ++u, p += a.unit_rows) sum += exp2_of(*p - lse);
         }
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
     if (lane == 0) wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? sum : NAN;
@@ -1617,7 +1754,7 @@ constexpr uint64_t align256(uint64_t x) { return (x + 255) & ~255ull; }
 struct Layout {
     int NT;
     bool rows;             // prompt_kernel
-    uint32_t G, tile_rows, target, item_cap, slot_cap, join_cap, n_units;
+    uint32_t G, tile_rows, target, item_cap, slot_cap, join_cap, n_units, unit_rows;
     uint64_t head, items, joins, ml, part, lse, units, cols, total;
 };
 
@@ -1627,9 +1764,10 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     if (y.G > 64) return invalid(h, "n_heads / n_kv_heads must be <= 64");
     const uint64_t most = (uint64_t)a.max_tok * y.G;   // rows of the longest sequence's head
     if (most > 0xFFFFFFFFull - 1024) return invalid(h, "max_tok * n_heads / n_kv_heads must be < 2^32 - 1024");
-    y.rows = most > (D == 256 ? 32u : 64u);
-    y.NT = most <= 16 ? 1 : most <= 32 ? 2 : 4;
+    y.rows = most > 64;
+    y.NT = most <= 16 || D == 256 ? 1 : 2;   // 64 rows: tiles side by side, their cache lines shared in L2
     y.tile_rows = y.rows ? (D == 256 ? 128u : 256u) : 16u * y.NT;
+    y.unit_rows = (uint32_t)((most + y.tile_rows - 1) / y.tile_rows * y.tile_rows);
     y.target = ((y.rows ? 512u : 1024u) + a.hk - 1) / a.hk;
     const uint64_t tiles = a.n_tok * y.G / y.tile_rows + a.n_seq;
     const uint64_t items = 2ull * y.target + tiles;
@@ -1659,14 +1797,14 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
         if (y.rows)
             y.cols = take(4 * u);
         else
-            y.units = take(4 * u * y.tile_rows);
+            y.units = take(4 * u * y.unit_rows);
     }
     y.total = at;
     return NETKV_OK;
 }
 
 template <int D, bool HALF>
-void launch_attend(const Layout &y, const AttendArgs &a, const Join *joins, const WeightArgs &wa, hipStream_t s) {
+void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, hipStream_t s) {
     const dim3 grid(y.item_cap * a.kv.hk);
 #define NETKV_ATTEND(NT, UNITS) attend_kernel<D, NT, HALF, UNITS><<<grid, kThreads, 0, s>>>(a)
     if (y.rows) {
@@ -1674,19 +1812,18 @@ void launch_attend(const Layout &y, const AttendArgs &a, const Join *joins, cons
             prompt_kernel<D, D == 256 ? 1 : 2, HALF, true><<<grid, kPromptThreads, 0, s>>>(a);
         else
             prompt_kernel<D, D == 256 ? 1 : 2, HALF, false><<<grid, kPromptThreads, 0, s>>>(a);
-    } else if (y.NT == 1) {
+    } else if (D == 256 || y.NT == 1) {
         if (wa.w) NETKV_ATTEND(1, true);
         else NETKV_ATTEND(1, false);
-    } else if (y.NT == 2) {
+    } else if constexpr (D != 256) {
         if (wa.w) NETKV_ATTEND(2, true);
         else NETKV_ATTEND(2, false);
-    } else if constexpr (D != 256) {
-        if (wa.w) NETKV_ATTEND(4, true);
-        else NETKV_ATTEND(4, false);
     }
 #undef NETKV_ATTEND
+    // nothing is split where no sequence can be longer than the shortest range
+    const uint64_t steps_most = (((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep;
     const uint64_t joins_most = (uint64_t)y.join_cap * a.kv.hk * y.tile_rows;
-    join_kernel<D, HALF><<<(uint32_t)(joins_most < 2048 ? joins_most : 2048), kThreads, 0, s>>>(a, joins);
+    if (steps_most > a.least) join_kernel<D, HALF><<<(uint32_t)(joins_most < 2048 ? joins_most : 2048), kThreads, 0, s>>>(a);
     if (!wa.w) return;
     if (y.rows) {
         const uint32_t steps = (uint32_t)((((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep);
@@ -1747,49 +1884,45 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     hipStream_t s = (hipStream_t)stream;
     uint8_t *ws = (uint8_t *)work;
     const bool half = dtype == NETKV_FP16;
-    PlanArgs p{};
-    p.kv = a;
-    p.G = y.G;
-    p.tile_rows = y.tile_rows;
-    p.target = y.target;
-    p.least = y.rows ? 8 : kWaves;
-    p.round = y.rows ? 1 : kWaves;
-    p.item_cap = y.item_cap;
-    p.slot_cap = y.slot_cap;
-    p.join_cap = y.join_cap;
-    p.head = (PlanHead *)(ws + y.head);
-    p.items = (Item *)(ws + y.items);
-    p.joins = (Join *)(ws + y.joins);
-    p.out = (uint16_t *)out;
-    p.out_stride = out_stride;
-    p.row_elems = (uint32_t)width;
-    p.nan16 = half ? 0x7E00u : 0x7FC0u;
-    plan_kernel<<<1, kPlanThreads, 0, s>>>(p);
     AttendArgs t{};
     t.kv = a;
     t.G = y.G;
-    t.Hq = n_heads;
     t.tile_rows = y.tile_rows;
-    t.q_stride = q_stride;
+    t.target = y.target;
+    t.least = y.rows ? 8 : kWaves;
+    t.round = y.rows ? 1 : kWaves;
+    t.item_cap = y.item_cap;
+    t.slot_cap = y.slot_cap;
+    t.join_cap = y.join_cap;
+    t.bad_out = (uint16_t *)out;
     t.out_stride = out_stride;
+    t.row_elems = (uint32_t)width;
+    t.nan16 = half ? 0x7E00u : 0x7FC0u;
+    if (a.n_seq > kListed) {
+        t.head = (PlanHead *)(ws + y.head);
+        t.items = (Item *)(ws + y.items);
+        t.joins = (Join *)(ws + y.joins);
+        plan_kernel<<<1, kPlanThreads, 0, s>>>(t);
+    }
+    t.Hq = n_heads;
+    t.q_stride = q_stride;
     t.q = q;
     t.out = out;
     t.c0 = std::fabs(scale) * kLog2e;
     t.q_sign = scale < 0.0f ? 0x80008000u : 0u;
-    t.head = p.head;
-    t.items = p.items;
     t.part = (float *)(ws + y.part);
     t.part_ml = (f32x4 *)(ws + y.ml);
     t.lse = block_weight ? (float *)(ws + y.lse) : nullptr;
     t.units = block_weight && !y.rows ? (float *)(ws + y.units) : nullptr;
     t.n_units = y.n_units;
+    t.unit_rows = y.unit_rows;
     WeightArgs wa{};
     wa.w = block_weight;
     wa.cols = y.rows ? (float *)(ws + y.cols) : nullptr;
     switch (kv->head_dim) {
-        case 64: half ? launch_attend<64, true>(y, t, p.joins, wa, s) : launch_attend<64, false>(y, t, p.joins, wa, s); break;
-        case 128: half ? launch_attend<128, true>(y, t, p.joins, wa, s) : launch_attend<128, false>(y, t, p.joins, wa, s); break;
-        default: half ? launch_attend<256, true>(y, t, p.joins, wa, s) : launch_attend<256, false>(y, t, p.joins, wa, s); break;
+        case 64: half ? launch_attend<64, true>(y, t, wa, s) : launch_attend<64, false>(y, t, wa, s); break;
+        case 128: half ? launch_attend<128, true>(y, t, wa, s) : launch_attend<128, false>(y, t, wa, s); break;
+        default: half ? launch_attend<256, true>(y, t, wa, s) : launch_attend<256, false>(y, t, wa, s); break;
     }
     return launched(h, "attention launch failed");
 }
