@@ -1184,48 +1184,74 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 }
 
 // Joins the ranges of one row: with M and Y the largest of their maxima,
-// O = sum 2^(y - Y) O_i, l = sum 2^(m - M) l_i.  A workgroup a row, its
-// threads the row's columns by four times a share of the ranges.
+// O = sum 2^(y - Y) O_i, l = sum 2^(m - M) l_i.  A workgroup a row: its threads
+// first take a range each for the factors, then the row's columns by four
+// times a share of the ranges (loads that wait for nothing).
 template <int D, bool HALF>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
     constexpr int kCols = D / 4, kGroups = kThreads / kCols;
     __shared__ f32x4 lo[kGroups][kCols];
-    __shared__ float ll[kGroups];
+    __shared__ float factor[kThreads], red[3][kWaves];
     const uint32_t hk = a.kv.hk, rows = a.tile_rows;
     const uint32_t col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     auto join_row = [&](const Join &j, uint32_t h, uint32_t tr) {
         const Head hd = seq_head(a.kv, j.seq);
         const uint32_t r = j.tile * rows + tr;
         if (r >= hd.n * a.G) return;
-        auto at = [&](uint32_t i) { return ((uint64_t)(j.slot + i) * hk + h) * rows + tr; };
+        const uint64_t at = ((uint64_t)j.slot * hk + h) * rows + tr, by = (uint64_t)hk * rows;
         float M = -INFINITY, Y = -INFINITY;
-        for (uint32_t i = 0; i < j.n; ++i) {
-            const f32x4 ml = a.part_ml[at(i)];
+        for (uint32_t i = threadIdx.x; i < j.n; i += kThreads) {
+            const f32x4 ml = a.part_ml[at + i * by];
             M = fmaxf(M, ml[0]);
             Y = fmaxf(Y, ml[2]);
         }
+        for (int d = 32; d; d >>= 1) {
+            M = fmaxf(M, __shfl_xor(M, d, 64));
+            Y = fmaxf(Y, __shfl_xor(Y, d, 64));
+        }
+        if (lane == 0) {
+            red[0][w] = M;
+            red[1][w] = Y;
+        }
+        __syncthreads();
+        for (int v = 0; v < kWaves; ++v) {
+            M = fmaxf(M, red[0][v]);
+            Y = fmaxf(Y, red[1][v]);
+        }
         float L = 0.0f;
         f32x4 o = {0, 0, 0, 0};
-        for (uint32_t i = grp; i < j.n; i += kGroups) {
-            const f32x4 ml = a.part_ml[at(i)];
-            const f32x4 x = *(const f32x4 *)(a.part + at(i) * D + col * 4);
-            const float f = joined(ml[2], Y);
-            L += joined(ml[0], M) * ml[1];
+        for (uint32_t i0 = 0; i0 < j.n; i0 += kThreads) {
+            const uint32_t i = i0 + threadIdx.x;
+            if (i < j.n) {
+                const f32x4 ml = a.part_ml[at + i * by];
+                factor[threadIdx.x] = joined(ml[2], Y);
+                L += joined(ml[0], M) * ml[1];
+            }
+            __syncthreads();
+            const uint32_t n = min(j.n - i0, (uint32_t)kThreads);
+            const float *p = a.part + (at + i0 * by) * D + col * 4;
+#pragma unroll 4
+            for (uint32_t q = grp; q < n; q += kGroups) {
+                const f32x4 x = *(const f32x4 *)(p + q * by * D);
+                const float f = factor[q];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += f * x[e];
+                for (int e = 0; e < 4; ++e) o[e] += f * x[e];
+            }
+            __syncthreads();
         }
+        for (int d = 32; d; d >>= 1) L += __shfl_xor(L, d, 64);
+        if (lane == 0) red[2][w] = L;
         lo[grp][col] = o;
-        if (col == 0) ll[grp] = L;
         __syncthreads();
         if (grp == 0) {
             L = 0.0f;
+            for (int v = 0; v < kWaves; ++v) L += red[2][v];
             o = f32x4{0, 0, 0, 0};
-            for (int i = 0; i < kGroups; ++i) {
-                L += ll[i];
+            for (int i = 0; i < kGroups; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] += lo[i][col][e];
-            }
             const uint64_t t = hd.row0 + r / a.G;
             const uint32_t qh = h * a.G + r % a.G;
             const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
