@@ -1794,7 +1794,12 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     y.NT = most <= 16 || D == 256 ? 1 : 2;   // 64 rows: tiles side by side, their cache lines shared in L2
     y.tile_rows = y.rows ? (D == 256 ? 128u : 256u) : 16u * y.NT;
     y.unit_rows = (uint32_t)((most + y.tile_rows - 1) / y.tile_rows * y.tile_rows);
-    y.target = ((y.rows ? 512u : 1024u) + a.hk - 1) / a.hk;
+    // ranges a head: what fills the card's workgroup slots (768 of them where
+    // few registers are used, else 512 and fewer) once or twice over.  512, 768,
+    // 1,024, 1,536 and 2,048 in all, 128 dimensions: 64 ragged sequences of up
+    // to 16,384 tokens 159, 162, 154, 152, 153 us, one of 131,072 54, 55, 54, 58,
+    // 60; 256 dimensions, 32 of 16,384: 124, 136, 141, 152, 170.
+    y.target = ((y.rows || y.NT == 2 || D == 256 ? 512u : 1024u) + a.hk - 1) / a.hk;
     const uint64_t tiles = a.n_tok * y.G / y.tile_rows + a.n_seq;
     const uint64_t items = 2ull * y.target + tiles;
     if (items * a.hk > (1ull << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
