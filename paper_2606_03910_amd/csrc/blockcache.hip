@@ -232,8 +232,8 @@ __device__ inline uint32_t range_steps(const PlanArgs &a, unsigned long long wor
     return len > 0x7FFFFFFFull ? 0x7FFFFFFFu : (uint32_t)len;
 }
 
-__device__ inline Item item_of(const PlanArgs &a, uint32_t seq, const Head &h, uint32_t C, uint32_t n, uint32_t p, uint32_t j, uint32_t slot0) {
-    const uint32_t tile = n - 1 - j / p, part = j % p;   // the tiles that see most first
+// Range `part` of `p` of a row tile.
+__device__ inline Item item_of(const PlanArgs &a, uint32_t seq, const Head &h, uint32_t C, uint32_t p, uint32_t tile, uint32_t part, uint32_t slot0) {
     const uint32_t end = tile_end(h, a.G, tile, a.tile_rows);
     Item it;
     it.seq = seq;
@@ -258,11 +258,12 @@ __device__ inline void fill_bad(const PlanArgs &a) {
 }
 
 // The same list as a wavefront has it in its registers: each lane takes up to
-// four sequences in a row (n_seq <= kListed).
+// four sequences in a row (n_seq <= kListed).  The ranges of full length come
+// first, then every tile's last one, tiles that see most before others.
 struct Shares {
     uint32_t rt[4], kt[4], C, per;
-    uint32_t items, slots, joins;      // inclusive sums up to this lane
-    uint32_t own_items, own_slots, own_joins;
+    uint32_t fulls, lasts, slots, joins;      // inclusive sums up to this lane
+    uint32_t own_fulls, own_lasts, own_slots, own_joins;
     bool bad;
 
     __device__ explicit Shares(const PlanArgs &a) {
@@ -284,21 +285,24 @@ struct Shares {
         }
         for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d, 64);
         C = range_steps(a, work);
-        own_items = own_slots = own_joins = 0;
+        own_fulls = own_lasts = own_slots = own_joins = 0;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
             const uint32_t p = parts(j);
-            own_items += rt[j] * p;
+            own_fulls += rt[j] * (p - 1);
+            own_lasts += rt[j];
             own_slots += p > 1 ? rt[j] * p : 0u;
             own_joins += p > 1 ? rt[j] : 0u;
         }
-        items = own_items;
+        fulls = own_fulls;
+        lasts = own_lasts;
         slots = own_slots;
         joins = own_joins;
         for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t x = __shfl_up(items, d, 64), y = __shfl_up(slots, d, 64), z = __shfl_up(joins, d, 64);
+            const uint32_t v = __shfl_up(fulls, d, 64), x = __shfl_up(lasts, d, 64), y = __shfl_up(slots, d, 64), z = __shfl_up(joins, d, 64);
             if ((int)lane >= d) {
-                items += x;
+                fulls += v;
+                lasts += x;
                 slots += y;
                 joins += z;
             }
@@ -308,13 +312,16 @@ struct Shares {
 
     // false: there are not so many
     __device__ bool item(const PlanArgs &a, uint32_t i, Item &it) const {
-        const uint64_t past = __ballot(items > i);
+        const uint32_t all_fulls = (uint32_t)__builtin_amdgcn_readlane((int)fulls, 63);
+        const bool last = i >= all_fulls;
+        if (last) i -= all_fulls;
+        const uint64_t past = __ballot((last ? lasts : fulls) > i);
         if (!past) return false;
         const int l = __ffsll((unsigned long long)past) - 1;
-        uint32_t at = items - own_items, slot = slots - own_slots, seq = 0, n = 0, p = 1, rest = 0;
+        uint32_t at = last ? lasts - own_lasts : fulls - own_fulls, slot = slots - own_slots, seq = 0, n = 0, p = 1, rest = 0;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t q = parts(j), x = rt[j] * q;
+            const uint32_t q = parts(j), x = rt[j] * (last ? 1u : q - 1);
             if (i >= at && i < at + x) {
                 seq = (threadIdx.x & 63) * per + j;
                 n = rt[j];
@@ -323,11 +330,14 @@ struct Shares {
                 break;
             }
             at += x;
-            slot += q > 1 ? x : 0u;
+            slot += q > 1 ? rt[j] * q : 0u;
         }
         auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
         seq = of(seq);
-        it = item_of(a, seq, seq_head(a.kv, seq), C, of(n), of(p), of(rest), of(slot));
+        p = of(p);
+        rest = of(rest);
+        const uint32_t tile = of(n) - 1 - (last ? rest : rest / (p - 1)), part = last ? p - 1 : rest % (p - 1);
+        it = item_of(a, seq, seq_head(a.kv, seq), C, p, tile, part, of(slot));
         return true;
     }
     __device__ uint32_t n_joins() const { return (uint32_t)__builtin_amdgcn_readlane((int)joins, 63); }
@@ -416,7 +426,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
                 if (base[mid][0] <= i) lo = mid; else hi = mid;
             }
             const uint32_t j = i - base[lo][0], n = geo[lo][0], p = geo[lo][1];
-            const Item it = item_of(a, s0 + lo, seq_head(a.kv, s0 + lo), C, n, p, j, at[1] + base[lo][1]);
+            const Item it = item_of(a, s0 + lo, seq_head(a.kv, s0 + lo), C, p, n - 1 - j / p, j % p, at[1] + base[lo][1]);
             const uint32_t idx = at[0] + i;
             if (idx < a.item_cap && (p == 1 || it.slot < a.slot_cap)) a.items[idx] = it;
             if (p > 1 && j % p == 0) {
@@ -652,7 +662,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : NT == 1 && !(UNITS && D ==
                 }
                 const uint32_t per = kStep / tile;
                 const uint32_t u = kt * per + 16 * g / tile;
-                if (((16 * g) & (tile - 1)) == 0 && u < a.n_units)
+                if (((16 * g) & (tile - 1)) == 0 && u < a.n_units && row0 + n * 16 + c < n_rows)
                     a.units[(((uint64_t)it.seq * hk + h) * a.n_units + u) * a.unit_rows + row0 + n * 16 + c] =
                         mm + log2_of(sum);
             }
@@ -1184,92 +1194,115 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 }
 
 // Joins the ranges of one row: with M and Y the largest of their maxima,
-// O = sum 2^(y - Y) O_i, l = sum 2^(m - M) l_i.  A workgroup a row: its threads
-// first take a range each for the factors, then the row's columns by four
-// times a share of the ranges (loads that wait for nothing).
-template <int D, bool HALF>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a) {
+// O = sum 2^(y - Y) O_i, l = sum 2^(m - M) l_i, by WAVES wavefronts: their
+// lanes first take a range each for the factors, then the row's columns by
+// four times a share of the ranges (loads that wait for nothing).
+template <int D, bool HALF, int WAVES>
+__device__ inline void join_row(const AttendArgs &a, const Join &j, uint32_t h, uint32_t tr, f32x4 *lo, float *factor, float (*red)[kWaves]) {
     typedef typename Elem<HALF>::T T;
-    constexpr int kCols = D / 4, kGroups = kThreads / kCols;
-    __shared__ f32x4 lo[kGroups][kCols];
-    __shared__ float factor[kThreads], red[3][kWaves];
+    constexpr uint32_t kLanes = 64 * WAVES, kCols = D / 4, kGroups = kLanes / kCols;
+    auto meet = [&]() {
+        if constexpr (WAVES > 1) __syncthreads();
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
     const uint32_t hk = a.kv.hk, rows = a.tile_rows;
-    const uint32_t col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    auto join_row = [&](const Join &j, uint32_t h, uint32_t tr) {
-        const Head hd = seq_head(a.kv, j.seq);
-        const uint32_t r = j.tile * rows + tr;
-        if (r >= hd.n * a.G) return;
-        const uint64_t at = ((uint64_t)j.slot * hk + h) * rows + tr, by = (uint64_t)hk * rows;
-        float M = -INFINITY, Y = -INFINITY;
-        for (uint32_t i = threadIdx.x; i < j.n; i += kThreads) {
-            const f32x4 ml = a.part_ml[at + i * by];
-            M = fmaxf(M, ml[0]);
-            Y = fmaxf(Y, ml[2]);
-        }
-        for (int d = 32; d; d >>= 1) {
-            M = fmaxf(M, __shfl_xor(M, d, 64));
-            Y = fmaxf(Y, __shfl_xor(Y, d, 64));
-        }
+    const uint32_t me = threadIdx.x % kLanes, lane = threadIdx.x & 63, w = me >> 6;
+    const uint32_t col = me % kCols, grp = me / kCols;
+    const Head hd = seq_head(a.kv, j.seq);
+    const uint32_t r = j.tile * rows + tr;
+    if (r >= hd.n * a.G) return;
+    const uint64_t at = ((uint64_t)j.slot * hk + h) * rows + tr, by = (uint64_t)hk * rows;
+    float M = -INFINITY, Y = -INFINITY;
+    for (uint32_t i = me; i < j.n; i += kLanes) {
+        const f32x4 ml = a.part_ml[at + i * by];
+        M = fmaxf(M, ml[0]);
+        Y = fmaxf(Y, ml[2]);
+    }
+    for (int d = 32; d; d >>= 1) {
+        M = fmaxf(M, __shfl_xor(M, d, 64));
+        Y = fmaxf(Y, __shfl_xor(Y, d, 64));
+    }
+    if constexpr (WAVES > 1) {
         if (lane == 0) {
             red[0][w] = M;
             red[1][w] = Y;
         }
         __syncthreads();
-        for (int v = 0; v < kWaves; ++v) {
+        for (int v = 0; v < WAVES; ++v) {
             M = fmaxf(M, red[0][v]);
             Y = fmaxf(Y, red[1][v]);
         }
-        float L = 0.0f;
-        f32x4 o = {0, 0, 0, 0};
-        for (uint32_t i0 = 0; i0 < j.n; i0 += kThreads) {
-            const uint32_t i = i0 + threadIdx.x;
-            if (i < j.n) {
-                const f32x4 ml = a.part_ml[at + i * by];
-                factor[threadIdx.x] = joined(ml[2], Y);
-                L += joined(ml[0], M) * ml[1];
-            }
-            __syncthreads();
-            const uint32_t n = min(j.n - i0, (uint32_t)kThreads);
-            const float *p = a.part + (at + i0 * by) * D + col * 4;
+    }
+    float L = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
+    for (uint32_t i0 = 0; i0 < j.n; i0 += kLanes) {
+        const uint32_t i = i0 + me;
+        if (i < j.n) {
+            const f32x4 ml = a.part_ml[at + i * by];
+            factor[me] = joined(ml[2], Y);
+            L += joined(ml[0], M) * ml[1];
+        }
+        meet();
+        const uint32_t n = min(j.n - i0, kLanes);
+        const float *p = a.part + (at + i0 * by) * D + col * 4;
 #pragma unroll 4
-            for (uint32_t q = grp; q < n; q += kGroups) {
-                const f32x4 x = *(const f32x4 *)(p + q * by * D);
-                const float f = factor[q];
+        for (uint32_t q = grp; q < n; q += kGroups) {
+            const f32x4 x = *(const f32x4 *)(p + q * by * D);
+            const float f = factor[q];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += f * x[e];
-            }
-            __syncthreads();
+            for (int e = 0; e < 4; ++e) o[e] += f * x[e];
         }
-        for (int d = 32; d; d >>= 1) L += __shfl_xor(L, d, 64);
-        if (lane == 0) red[2][w] = L;
-        lo[grp][col] = o;
-        __syncthreads();
-        if (grp == 0) {
+        meet();
+    }
+    for (int d = 32; d; d >>= 1) L += __shfl_xor(L, d, 64);
+    if (WAVES > 1 && lane == 0) red[2][w] = L;
+    lo[grp * kCols + col] = o;
+    meet();
+    if (grp == 0) {
+        if constexpr (WAVES > 1) {
             L = 0.0f;
-            for (int v = 0; v < kWaves; ++v) L += red[2][v];
-            o = f32x4{0, 0, 0, 0};
-            for (int i = 0; i < kGroups; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += lo[i][col][e];
-            const uint64_t t = hd.row0 + r / a.G;
-            const uint32_t qh = h * a.G + r % a.G;
-            const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
-            T z[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = (T)(o[e] * inv);
-            *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + col * 4) = *(u32x2 *)z;
-            if (a.lse && col == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
+            for (int v = 0; v < WAVES; ++v) L += red[2][v];
         }
-        __syncthreads();
+        o = f32x4{0, 0, 0, 0};
+        for (uint32_t i = 0; i < kGroups; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += lo[i * kCols + col][e];
+        const uint64_t t = hd.row0 + r / a.G;
+        const uint32_t qh = h * a.G + r % a.G;
+        const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
+        T z[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = (T)(o[e] * inv);
+        *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + col * 4) = *(u32x2 *)z;
+        if (a.lse && col == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
+    }
+    meet();
+}
+
+// A workgroup a row as long as there are no more rows than workgroups, else a
+// wavefront a row.
+template <int D, bool HALF>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, uint32_t rows) {
+    __shared__ f32x4 lo[kThreads];
+    __shared__ float factor[kThreads], red[3][kWaves];
+    const uint32_t hk = a.kv.hk, w = threadIdx.x >> 6;
+    auto all = [&](uint64_t n_joins, auto join) {
+        const uint64_t n = n_joins * hk * rows;
+        auto row = [&](uint64_t task, auto waves, uint32_t at) {
+            join_row<D, HALF, decltype(waves)::value>(a, join((uint32_t)(task / rows / hk)), (uint32_t)(task / rows % hk), (uint32_t)(task % rows),
+                                                      lo + at, factor + at, red);
+        };
+        if (n <= gridDim.x) {
+            if (blockIdx.x < n) row(blockIdx.x, std::integral_constant<int, kWaves>(), 0);
+        } else {
+            for (uint64_t task = blockIdx.x * kWaves + w; task < n; task += gridDim.x * kWaves) row(task, std::integral_constant<int, 1>(), 64 * w);
+        }
     };
     if (a.joins) {
-        const uint64_t all = (uint64_t)a.head->n_joins * hk * rows;
-        for (uint64_t task = blockIdx.x; task < all; task += gridDim.x) join_row(a.joins[task / rows / hk], (uint32_t)(task / rows % hk), (uint32_t)(task % rows));
+        all(a.head->n_joins, [&](uint32_t i) { return a.joins[i]; });
     } else {
         const Shares sh(a);
-        const uint64_t all = (uint64_t)sh.n_joins() * hk * rows;
-        for (uint64_t task = blockIdx.x; task < all; task += gridDim.x) join_row(sh.join((uint32_t)(task / rows / hk)), (uint32_t)(task / rows % hk), (uint32_t)(task % rows));
+        all(sh.n_joins(), [&](uint32_t i) { return sh.join(i); });
     }
 }
 
@@ -1793,7 +1826,7 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     y.rows = most > 64;
     y.NT = most <= 16 || D == 256 ? 1 : 2;   // 64 rows: tiles side by side, their cache lines shared in L2
     y.tile_rows = y.rows ? (D == 256 ? 128u : 256u) : 16u * y.NT;
-    y.unit_rows = (uint32_t)((most + y.tile_rows - 1) / y.tile_rows * y.tile_rows);
+    y.unit_rows = (uint32_t)(most / 4 * 4 + 4);
     // ranges a head: what fills the card's workgroup slots (768 of them where
     // few registers are used, else 512 and fewer) once or twice over.  512, 768,
     // 1,024, 1,536 and 2,048 in all, 128 dimensions: 64 ragged sequences of up
@@ -1853,8 +1886,9 @@ void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, h
 #undef NETKV_ATTEND
     // nothing is split where no sequence can be longer than the shortest range
     const uint64_t steps_most = (((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep;
-    const uint64_t joins_most = (uint64_t)y.join_cap * a.kv.hk * y.tile_rows;
-    if (steps_most > a.least) join_kernel<D, HALF><<<(uint32_t)(joins_most < 2048 ? joins_most : 2048), kThreads, 0, s>>>(a);
+    const uint32_t rows = y.unit_rows < y.tile_rows ? y.unit_rows : y.tile_rows;   // that a tile can have
+    const uint64_t joins_most = (uint64_t)y.join_cap * a.kv.hk * rows;
+    if (steps_most > a.least) join_kernel<D, HALF><<<(uint32_t)(joins_most < 2048 ? joins_most : 2048), kThreads, 0, s>>>(a, rows);
     if (!wa.w) return;
     if (y.rows) {
         const uint32_t steps = (uint32_t)((((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep);
