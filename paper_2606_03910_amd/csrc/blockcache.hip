@@ -43,8 +43,7 @@ constexpr int kWaves = 4;
 constexpr int kPromptThreads = 512;
 constexpr uint32_t kStep = 64;        // tokens a wavefront takes at a time
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kMaxGrow = 8.0f;      // how far (in powers of two) a row's maximum may be passed before it is raised
-constexpr float kMaxSum = 1024.0f;    // ... and how large 16 weights' sum may become instead
+constexpr float kMaxSum = 1024.0f;    // how large 16 weights' sum may become before a row's maximum is raised
 constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
 
 struct Kv {
@@ -457,6 +456,31 @@ struct AttendArgs : PlanArgs {
     uint32_t n_units, unit_rows;
 };
 
+// 2^(x + by) of 16 scores, as the operand of the product with the values, and
+// their sum.  (The empty statement: the weights are rounded here, not where
+// they are used, which would keep them in twice the registers.)
+__device__ __forceinline__ float weights_of(const f32x4 (&st)[4], float sc, float by, f16x8 (&pf)[2]) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = exp2_of(fmaf(st[t][i], sc, by));
+            sum += p[i];
+        }
+        const f16x2 u = __builtin_convertvector((f32x2{p[0], p[1]}), f16x2);
+        const f16x2 v = __builtin_convertvector((f32x2{p[2], p[3]}), f16x2);
+        const int j = 4 * (t & 1);
+        pf[t >> 1][j] = u[0];
+        pf[t >> 1][j + 1] = u[1];
+        pf[t >> 1][j + 2] = v[0];
+        pf[t >> 1][j + 3] = v[1];
+    }
+    asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(sum));
+    return sum;
+}
+
 // What a part with maximum m counts for beside the maximum of all; a part
 // that saw nothing finite holds zeros, or NaN.
 __device__ inline float joined(float m, float all) { return m == -INFINITY ? 1.0f : exp2_of(m - all); }
@@ -486,12 +510,12 @@ struct ValRegs {
 // bits for what is within 2^-14 of the largest (y is the maximum with s in it,
 // so that a block of small values that a row attends to keeps them).  l takes
 // the weights before that rounding.  A maximum is raised, and O rescaled, only
-// when it is passed by more than 2^8: P stays below 2^8.
+// when 16 weights' sum passes 2^10, which keeps them in fp16's range.
 //
 // The four wavefronts take the same rows and every fourth step each, joined
 // through LDS.
-template <int D, int NT, bool HALF, bool UNITS>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : NT == 1 && !(UNITS && D == 128) ? 3 : 2) void attend_kernel(AttendArgs a) {
+template <int D, int NT, bool HALF, bool UNITS, bool SMALL>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
     constexpr int kDT = D / 16;
@@ -535,7 +559,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : NT == 1 && !(UNITS && D ==
     const uint32_t row_last = min(row0 + a.tile_rows, n_rows) - 1;
     const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
     const int64_t see_any = (int64_t)hd.ctx - hd.n + row_last / a.G + 1;
-    const uint32_t all_lim = see_all > 0 ? (uint32_t)see_all : 0u;
+    const uint32_t all_lim = see_all > 0 ? (uint32_t)min(see_all, (int64_t)hd.ctx) : 0u;
     const uint32_t end = min(it.k1, see_any > 0 ? (uint32_t)((see_any + kStep - 1) / kStep) : 0u);
 
     f32x4 acc[NT][kDT];
@@ -548,40 +572,57 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : NT == 1 && !(UNITS && D ==
         for (int d = 0; d < kDT; ++d) acc[n][d] = f32x4{0, 0, 0, 0};
     }
 
+    // pages, scales and addresses are scalar where a step lies in one block
     auto page_at = [&](uint32_t kt, uint32_t group) {
-        const uint32_t b = min((kt * kStep + 16 * group) >> a.kv.btl, last_block);
-        return pages[b];
+        const uint32_t b = min((kt * kStep + (SMALL ? 16 * group : 0u)) >> a.kv.btl, last_block);
+        return SMALL ? pages[b] : scalar(pages)[b];
+    };
+    const uint64_t page_bytes = hk * hb;
+    const uint32_t key_in_page = (((SMALL ? (16 * (c >> 2)) & (tile - 1) : 16 * (c >> 2)) + (c & 3)) * D + 16 * g);
+    const uint32_t val_in_page = SMALL ? c * tile + ((16 * g) & (tile - 1)) : c * kStep + 16 * g;
+    const uint32_t val_piece = SMALL ? 16 * tile : 16 * kStep;
+    auto in_cache = [&](const uint8_t *x, uint32_t kt, uint32_t page) {
+        return x + h * hb + (page < a.kv.n_pages ? page : 0u) * page_bytes + (uint64_t)((kt * kStep) & (bt - 1)) * D;
     };
     auto load_keys = [&](KeyRegs<D> &x, uint32_t kt, uint32_t page) {
-        page = page < a.kv.n_pages ? page : 0u;
-        const uint32_t tok = ((kt * kStep + 16 * (c >> 2)) & (bt - 1)) + (c & 3);
-        const uint8_t *p = a.kv.k + ((uint64_t)page * hk + h) * hb + (uint64_t)tok * D + 16 * g;
+        const uint8_t *p = in_cache(a.kv.k, kt, page);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) x.f[t][i] = *(const u32x4 *)(p + 4 * t * D + 64 * i);
+            for (int i = 0; i < D / 64; ++i) x.f[t][i] = *(const u32x4 *)(p + key_in_page + 4 * t * D + 64 * i);
     };
     auto load_vals = [&](ValRegs<D> &x, uint32_t kt, uint32_t page) {
-        page = page < a.kv.n_pages ? page : 0u;
-        const uint32_t tok = (kt * kStep + 16 * g) & (bt - 1);
-        const uint8_t *p = a.kv.v + ((uint64_t)page * hk + h) * hb + (uint64_t)(tok & ~(tile - 1)) * D + c * tile + (tok & (tile - 1));
+        const uint8_t *p = in_cache(a.kv.v, kt, page);
 #pragma unroll
-        for (int d = 0; d < kDT; ++d) x.f[d] = *(const u32x4 *)(p + d * 16 * tile);
+        for (int d = 0; d < kDT; ++d) x.f[d] = *(const u32x4 *)(p + val_in_page + d * val_piece);
     };
 
+    // The next step's keys are asked for as soon as this one's have been
+    // multiplied, its values likewise; pages a step earlier.
     KeyRegs<D> kf;
     ValRegs<D> vf;
-    for (uint32_t kt = it.k0 + w; kt < end; kt += kWaves) {
-        const uint32_t pk = page_at(kt, c >> 2), pv = page_at(kt, g);
-        load_keys(kf, kt, pk);
-        load_vals(vf, kt, pv);
+    f32x4 st[NT][4];
+    f16x8 pf[NT][2];
+    float sc_next = 0.0f, vs_next = 0.0f, sc = 0.0f, vsl = 0.0f;
+    uint64_t nan_sums = 0;                             // sums of this lane that a NaN value belongs to
+    static_assert(4 * NT * kDT <= 64, "a bit a sum");
+    uint32_t pk = 0, pv = 0;
+    auto load_scales = [&]() {
         const bool bad = pv >= a.kv.n_pages;
         if (bad) report(a.kv);
         const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk + h;
-        const float sc = bad ? NAN : a.kv.ks[si] * a.c0;
-        const float vsl = bad ? NAN : a.kv.vs[si], vlog = log2_of(vsl);
-
-        f32x4 st[NT][4];
+        sc_next = SMALL ? a.kv.ks[si] : scalar(a.kv.ks)[si];
+        vs_next = SMALL ? a.kv.vs[si] : scalar(a.kv.vs)[si];
+        if (bad) sc_next = vs_next = NAN;
+    };
+    auto find_pages = [&](uint32_t kt) {
+        pk = page_at(kt, c >> 2);
+        pv = SMALL ? page_at(kt, g) : pk;
+    };
+    auto scores = [&](uint32_t kt) {
+        const float x = sc_next * a.c0;
+        sc = x == 0.0f ? 1.0e-30f : x;                 // not 0, which would turn a masked score's -inf into NaN
+        vsl = vs_next;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -598,119 +639,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : NT == 1 && !(UNITS && D ==
                     st[n][t] = product(hi, qf[n][2 * i + 1], st[n][t]);
                 }
             }
-        const uint32_t tok0 = kt * kStep + 16 * g;
-        const bool masked = kt * kStep + kStep > all_lim;
-        bool grow = false;
-        float mx[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            mx[n] = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = st[n][t][i] * sc;
-                    if (masked && tok0 + 4 * t + i >= lim[n]) x = -INFINITY;
-                    st[n][t][i] = x;
-                    mx[n] = fmaxf(mx[n], x);
-                }
-            grow |= mx[n] > m[n] + kMaxGrow || mx[n] + vlog > y[n] + kMaxGrow;
+        if (kt + kWaves < end) {
+            load_keys(kf, kt + kWaves, pk);
+            load_scales();
         }
-        if (__any(grow)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float mn = fmaxf(m[n], row_max(mx[n])), yn = fmaxf(y[n], row_max(mx[n] + vlog));
-                l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
-                const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
-                m[n] = mn;
-                y[n] = yn;
-#pragma unroll
-                for (int d = 0; d < kDT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
-            }
-        }
-        f16x8 pf[NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float sum = 0.0f;
-            const float mm = m[n] == -INFINITY ? 0.0f : m[n];
-            const float f = y[n] == -INFINITY ? 0.0f : fminf(vsl * exp2_of(mm - y[n]), 3.0e38f);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                float p[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[i] = exp2_of(st[n][t][i] - mm);
-                    sum += p[i];
-                }
-                const f16x2 x = __builtin_convertvector((f32x2{p[0] * f, p[1] * f}), f16x2);
-                const f16x2 y = __builtin_convertvector((f32x2{p[2] * f, p[3] * f}), f16x2);
-                const int j = 4 * (t & 1);
-                pf[n][t >> 1][j] = x[0];
-                pf[n][t >> 1][j + 1] = x[1];
-                pf[n][t >> 1][j + 2] = y[0];
-                pf[n][t >> 1][j + 3] = y[1];
-            }
-            l[n] += sum;
-            if constexpr (UNITS) {
-                // the unit's sum: 64 tokens are the row's four lanes, 32 two of them, 16 one
-                if (tile >= 32) sum = pair16_sum(sum);
-                if (tile >= 64) {
-                    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
-                    sum = __uint_as_float(b[0]) + __uint_as_float(b[1]);
-                }
-                const uint32_t per = kStep / tile;
-                const uint32_t u = kt * per + 16 * g / tile;
-                if (((16 * g) & (tile - 1)) == 0 && u < a.n_units && row0 + n * 16 + c < n_rows)
-                    a.units[(((uint64_t)it.seq * hk + h) * a.n_units + u) * a.unit_rows + row0 + n * 16 + c] =
-                        mm + log2_of(sum);
-            }
-        }
-        if (masked) {
-            // tokens that no row holds: their bytes may be anything
-            const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
-            u32x4 keep;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int b = have - 4 * i;
-                keep[i] = b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << (8 * b)) - 1u;
-            }
-            bool nan = false;
-#pragma unroll
-            for (int d = 0; d < kDT; ++d) {
-                vf.f[d] &= keep;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) nan |= nan_bytes(vf.f[d][i]) != 0;
-            }
-            if (__any(nan)) {
-                // A NaN among values that some rows see and others do not: a
-                // product with P = 0 would carry it to all.  The rows that see
-                // one are found by a product of the masks, and it is left out
-                // of the values.
-                f16x8 see[NT][2];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) see[n][j >> 3][j & 7] = tok0 + j < lim[n] ? (_Float16)1.0f : (_Float16)0.0f;
-#pragma unroll
-                for (int d = 0; d < kDT; ++d) {
-                    u32x4 y;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = nan_bytes(vf.f[d][i]);
-                    const u32x4 one = y * 0x38u;          // 1.0 per NaN
-                    vf.f[d] &= ~(y * 0xFFu);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        f32x4 hit = {0, 0, 0, 0};
-                        hit = product(widen_f16(one[0], one[1]), see[n][0], hit);
-                        hit = product(widen_f16(one[2], one[3]), see[n][1], hit);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[n][d][i] = hit[i] > 0.0f ? NAN : acc[n][d][i];
-                    }
-                }
-            }
-        }
+    };
+    auto values = [&](uint32_t kt) {
 #pragma unroll
         for (int d = 0; d < kDT; ++d) {
             const f16x8 lo = widen_f16(vf.f[d][0], vf.f[d][1]);
@@ -721,7 +655,152 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : NT == 1 && !(UNITS && D ==
                 acc[n][d] = product(hi, pf[n][1], acc[n][d]);
             }
         }
+        if (kt + kWaves < end) {
+            load_vals(vf, kt + kWaves, pv);
+            find_pages(kt + 2 * kWaves);
+        }
+    };
+    // log2 of the unit's sum, of which this lane has 2^base sum: 64 tokens are
+    // the row's four lanes, 32 two of them, 16 one
+    auto keep_unit = [&](uint32_t kt, int n, float sum, float base) {
+        if constexpr (UNITS) {
+            if (tile >= 32) sum = pair16_sum(sum);
+            if (tile >= 64) sum += __shfl_xor(sum, 32, 64);
+            const uint32_t u = kt * (kStep / tile) + 16 * g / tile;
+            if (((16 * g) & (tile - 1)) == 0 && u < a.n_units && row0 + n * 16 + c < n_rows)
+                a.units[(((uint64_t)it.seq * hk + h) * a.n_units + u) * a.unit_rows + row0 + n * 16 + c] = base + log2_of(sum);
+        }
+    };
+    // P in units of 2^y with y as it is, its sum in l's units of 2^m at once;
+    // false (and l as it was) where that will not do: a weight passes 2^y by
+    // too much (the first step, a larger score), scales are further apart than
+    // fp32 takes in one, NaN
+    auto softmax = [&](uint32_t kt) {
+        const float vlog = log2_of(vsl);
+        float up[NT], sum[NT];                         // up: log2 of a weight over its P
+        bool fits = true;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float by = vlog - y[n];
+            up[n] = -by - m[n];
+            sum[n] = weights_of(st[n], sc, by, pf[n]);
+            fits &= sum[n] <= kMaxSum && fabsf(up[n]) < 64.0f;
+        }
+        if (!__all(fits)) return false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            l[n] += sum[n] * exp2_of(up[n]);
+            // lanes of one row may have pages of their own, so one base for all: m
+            keep_unit(kt, n, sum[n] * exp2_of(up[n]), m[n]);
+        }
+        return true;
+    };
+    // any step: masks, NaN values, maxima raised
+    auto softmax_any = [&](uint32_t kt) {
+        const float vlog = log2_of(vsl);
+        const uint32_t tok0 = kt * kStep + 16 * g;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int left = (int)lim[n] - (int)tok0;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    st[n][t][i] = left > 4 * t + i ? st[n][t][i] : -INFINITY;
+                    mx = fmaxf(mx, st[n][t][i]);
+                }
+            mx = mx == -INFINITY ? -INFINITY : mx * sc;
+            const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog));
+            l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
+            const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
+            m[n] = mn;
+            y[n] = yn;
+#pragma unroll
+            for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
+            const float mm = mn == -INFINITY ? 0.0f : mn;
+            const float total = weights_of(st[n], sc, -mm, pf[n]);
+            l[n] += total;
+            keep_unit(kt, n, total, mm);
+            weights_of(st[n], sc, yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
+        }
+        if (kt * kStep + kStep <= all_lim) return;
+        // Tokens that not every row sees: bytes of slots that hold none may be
+        // anything.  A NaN among values that some rows see and others do not
+        // would come to all of them by a product with P = 0: the rows that see
+        // one are found by a product of the masks, and it is left out.
+        const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
+        u32x4 keep;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = have - 4 * i;
+            keep[i] = b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << (8 * b)) - 1u;
+        }
+        bool nan = false;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) {
+            vf.f[d] &= keep;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) nan |= nan_bytes(vf.f[d][i]) != 0;
+        }
+        if (!__any(nan)) return;
+        uint64_t found = 0;                            // four bits at a time, from the top (no constant for each sum)
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) {
+            u32x4 z;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = nan_bytes(vf.f[d][i]);
+            const u32x4 one = z * 0x38u;               // 1.0 per NaN
+            vf.f[d] &= ~(z * 0xFFu);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int left = (int)lim[n] - (int)tok0;
+                f16x8 see[2];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) see[j >> 3][j & 7] = left > j ? (_Float16)1.0f : (_Float16)0.0f;
+                f32x4 hit = {0, 0, 0, 0};
+                hit = product(widen_f16(one[0], one[1]), see[0], hit);
+                hit = product(widen_f16(one[2], one[3]), see[1], hit);
+                uint32_t bits = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bits |= hit[i] > 0.0f ? 1u << i : 0u;
+                found = found >> 4 | (uint64_t)bits << 60;
+            }
+        }
+        nan_sums |= found;
+    };
+    if (it.k0 + w < end) {
+        find_pages(it.k0 + w);
+        load_keys(kf, it.k0 + w, pk);
+        load_scales();
+        load_vals(vf, it.k0 + w, pv);
+        find_pages(it.k0 + w + kWaves);
     }
+    // the ordinary steps have a loop of their own (see prompt_kernel)
+    for (uint32_t kt = it.k0 + w; kt < end; kt += kWaves) {
+        bool done;
+        do {
+            scores(kt);
+            done = kt * kStep + kStep <= all_lim;
+            if (done) done = softmax(kt);
+            if (!done) break;
+            values(kt);
+            kt += kWaves;
+        } while (kt < end);
+        if (done) break;
+        softmax_any(kt);
+        values(kt);
+    }
+    if (nan_sums)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (nan_sums >> (64 - 4 * NT * kDT + 4 * (d * NT + n) + i) & 1) acc[n][d][i] = NAN;
 #pragma unroll
     for (int n = 0; n < NT; ++n) l[n] = row_sum(l[n]);
 
@@ -774,31 +853,6 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : NT == 1 && !(UNITS && D ==
             }
         }
     }
-}
-
-// 2^(x + by) of 16 scores, as the operand of the product with the values, and
-// their sum.  (The empty statement: the weights are rounded here, not where
-// they are used, which would keep them in twice the registers.)
-__device__ __forceinline__ float weights_of(const f32x4 (&st)[4], float sc, float by, f16x8 (&pf)[2]) {
-    float sum = 0.0f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        float p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i] = exp2_of(fmaf(st[t][i], sc, by));
-            sum += p[i];
-        }
-        const f16x2 u = __builtin_convertvector((f32x2{p[0], p[1]}), f16x2);
-        const f16x2 v = __builtin_convertvector((f32x2{p[2], p[3]}), f16x2);
-        const int j = 4 * (t & 1);
-        pf[t >> 1][j] = u[0];
-        pf[t >> 1][j + 1] = u[1];
-        pf[t >> 1][j + 2] = v[0];
-        pf[t >> 1][j + 3] = v[1];
-    }
-    asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(sum));
-    return sum;
 }
 
 // The same for prompts: eight wavefronts with 16 NT rows each go through the
@@ -1870,7 +1924,9 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
 template <int D, bool HALF>
 void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, hipStream_t s) {
     const dim3 grid(y.item_cap * a.kv.hk);
-#define NETKV_ATTEND(NT, UNITS) attend_kernel<D, NT, HALF, UNITS><<<grid, kThreads, 0, s>>>(a)
+#define NETKV_ATTEND(NT, UNITS)                                                             \
+    a.kv.btl < 6 ? attend_kernel<D, NT, HALF, UNITS, true><<<grid, kThreads, 0, s>>>(a)     \
+                 : attend_kernel<D, NT, HALF, UNITS, false><<<grid, kThreads, 0, s>>>(a)
     if (y.rows) {
         if (a.kv.btl < 6)
             prompt_kernel<D, D == 256 ? 1 : 2, HALF, true><<<grid, kPromptThreads, 0, s>>>(a);
