@@ -170,7 +170,9 @@ struct PlanHead {
 // share by itself (Shares); beyond that plan_kernel writes the list.
 struct PlanArgs {
     Kv kv;
-    uint32_t G, tile_rows, target, least, round;   // ranges of at least `least` steps, multiples of `round`
+    uint32_t G, tile_rows;
+    uint32_t target, fine;                         // ranges a head, with kEnough steps at most and with more
+    uint32_t least, round;                         // ranges of at least `least` steps, multiples of `round`
     uint32_t item_cap, slot_cap, join_cap;
     PlanHead *head;
     Item *items;                                   // null: not listed
@@ -223,9 +225,13 @@ __device__ inline uint32_t tiles_of(const Head &h, const PlanArgs &a) {
     return (uint32_t)(((uint64_t)h.n * a.G + a.tile_rows - 1) / a.tile_rows);
 }
 
-// Steps of a range: what spreads `work` steps over `target` ranges.
+// Steps of a range: what spreads `work` steps over `target` ranges, or from
+// kEnough steps on, where beginning a range costs little, over `fine`.
+constexpr uint32_t kEnough = 40;
 __device__ inline uint32_t range_steps(const PlanArgs &a, unsigned long long work) {
     unsigned long long len = (work + a.target - 1) / a.target;
+    const unsigned long long fine = (work + a.fine - 1) / a.fine;
+    if (len > kEnough) len = fine > kEnough ? fine : kEnough;
     if (len < a.least) len = a.least;
     len = (len + a.round - 1) / a.round * a.round;
     return len > 0x7FFFFFFFull ? 0x7FFFFFFFu : (uint32_t)len;
@@ -245,6 +251,9 @@ __device__ inline Item item_of(const PlanArgs &a, uint32_t seq, const Head &h, u
 
 // The rows of sequences that cannot be answered, by one workgroup.
 __device__ inline void fill_bad(const PlanArgs &a) {
+    bool bad = false;
+    for (uint32_t s = threadIdx.x; s < a.kv.n_seq; s += blockDim.x) bad |= !seq_head(a.kv, s).ok;
+    if (!__syncthreads_or(bad)) return;
     for (uint32_t s = 0; s < a.kv.n_seq; ++s) {
         const Head h = seq_head(a.kv, s);
         if (h.ok) continue;
@@ -1867,7 +1876,7 @@ constexpr uint64_t align256(uint64_t x) { return (x + 255) & ~255ull; }
 struct Layout {
     int NT;
     bool rows;             // prompt_kernel
-    uint32_t G, tile_rows, target, item_cap, slot_cap, join_cap, n_units, unit_rows;
+    uint32_t G, tile_rows, target, fine, item_cap, slot_cap, join_cap, n_units, unit_rows;
     uint64_t head, items, joins, ml, part, lse, units, cols, total;
 };
 
@@ -1881,18 +1890,18 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     y.NT = most <= 16 || D == 256 ? 1 : 2;   // 64 rows: tiles side by side, their cache lines shared in L2
     y.tile_rows = y.rows ? (D == 256 ? 128u : 256u) : 16u * y.NT;
     y.unit_rows = (uint32_t)(most / 4 * 4 + 4);
-    // ranges a head: what fills the card's workgroup slots (768 of them where
-    // few registers are used, else 512 and fewer) once or twice over.  512, 768,
-    // 1,024, 1,536 and 2,048 in all, 128 dimensions: 64 ragged sequences of up
-    // to 16,384 tokens 159, 162, 154, 152, 153 us, one of 131,072 54, 55, 54, 58,
-    // 60; 256 dimensions, 32 of 16,384: 124, 136, 141, 152, 170.
-    y.target = ((y.rows || y.NT == 2 || D == 256 ? 512u : 1024u) + a.hk - 1) / a.hk;
+    // ranges a head: what fills the card's 512 workgroup slots once, or where
+    // they stay long enough twice (unequal lengths even out).  512, 1,024, 1,536
+    // in all, 128 dimensions, us: 64 ragged sequences of up to 16,384 tokens
+    // 146, 136, 137; one of 131,072 51, 56, 60; 200 ragged of up to 700 50, 63, 70.
+    y.target = (512u + a.hk - 1) / a.hk;
+    y.fine = y.rows || y.NT == 2 || D == 256 ? y.target : (1024u + a.hk - 1) / a.hk;
     const uint64_t tiles = a.n_tok * y.G / y.tile_rows + a.n_seq;
-    const uint64_t items = 2ull * y.target + tiles;
+    const uint64_t items = 2ull * y.fine + tiles;
     if (items * a.hk > (1ull << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
     y.item_cap = (uint32_t)items;
-    y.slot_cap = 2 * y.target;
-    y.join_cap = y.target;
+    y.slot_cap = 2 * y.fine;
+    y.join_cap = y.fine;
     const uint32_t bt = 1u << a.btl;
     y.n_units = (uint32_t)(((uint64_t)a.max_pages << a.btl) / (bt < kStep ? bt : kStep)) + (uint32_t)(kStep / 16);
     if (weights && (((uint64_t)a.max_pages << a.btl) / kStep + 1) * a.hk > (1ull << 24))
@@ -2010,6 +2019,7 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     t.G = y.G;
     t.tile_rows = y.tile_rows;
     t.target = y.target;
+    t.fine = y.fine;
     t.least = y.rows ? 8 : kWaves;
     t.round = y.rows ? 1 : kWaves;
     t.item_cap = y.item_cap;
