@@ -1631,15 +1631,31 @@ __device__ inline uint32_t rescale4(uint32_t x, float ratio) {
     return narrow4(y, ratio);
 }
 
+// Four dwords of four bytes each, turned.
+__device__ inline void turn4(uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d) {
+    const uint32_t t0 = __builtin_amdgcn_perm(b, a, 0x05010400u), t1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
+    const uint32_t u0 = __builtin_amdgcn_perm(d, c, 0x05010400u), u1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+    a = __builtin_amdgcn_perm(u0, t0, 0x05040100u);
+    b = __builtin_amdgcn_perm(u0, t0, 0x07060302u);
+    c = __builtin_amdgcn_perm(u1, t1, 0x05040100u);
+    d = __builtin_amdgcn_perm(u1, t1, 0x07060302u);
+}
+
 // One workgroup quantises the keys (blockIdx.z = 0) or values of one head
 // that a call brings to one block.  The block's scale is the smallest power of
 // two that holds them, or the present one if the block was begun with a larger
 // one; where it grows, what the block holds is brought under the new scale
-// (exact but for values that become subnormal).
+// (exact but for values that become subnormal).  What fits the workgroup's
+// registers is read once, for the largest value and for the quantisation.
+// Values are turned through LDS: written byte by byte from the rows they came
+// in, a 512-token block took three times as long.
 template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
     constexpr int kEach = 8;                                  // 16-byte pieces a thread keeps
+    constexpr uint32_t kPass = THREADS * kEach * 8 / D;       // tokens that the workgroup keeps
+    constexpr uint32_t kPitch = D / 4 + 1;
     __shared__ float red[THREADS / 64];
+    __shared__ uint32_t rows[(kPass + 16) * kPitch];          // quantised values by token
     const Kv &kv = a.kv;
     const uint32_t bt = 1u << kv.btl;
     uint64_t rest;
@@ -1738,14 +1754,48 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
                 y = u32x2{narrow4(z, inv), narrow4(z + 4, inv)};
             }
             const uint32_t tok = p0 + e / (D / 8), d = e % (D / 8) * 8;
+            if (e >= pieces) continue;
             if (!vals) {
-                if (e < pieces) *(u32x2 *)(dst + (uint64_t)tok * D + d) = y;
-            } else if (e < pieces) {
-                uint8_t *p = dst + (uint64_t)(tok & ~(tile - 1)) * D + (uint64_t)d * tile + (tok & (tile - 1));
-#pragma unroll
-                for (int j = 0; j < 8; ++j) p[j * tile] = (uint8_t)(y[j >> 2] >> (8 * (j & 3)));
+                *(u32x2 *)(dst + (uint64_t)tok * D + d) = y;
+            } else {
+                uint32_t *q = rows + (tok - ((p0 + base / (D / 8)) & ~15u)) * kPitch + d / 4;
+                q[0] = y[0];
+                q[1] = y[1];
             }
         }
+        if (!vals) continue;
+        // four dimensions of 16 tokens a thread; groups that the call fills
+        // whole are written whole
+        __syncthreads();
+        const uint32_t t0 = p0 + base / (D / 8), t1 = min(p1, t0 + kPass), g0 = t0 & ~15u;
+        for (uint32_t i = threadIdx.x; i < (t1 - g0 + 63) / 64 * D; i += THREADS) {
+            // lanes: four groups, then the dimensions
+            const uint32_t dq = i / 4 % (D / 4), tg = i % 4 + i / D * 4, tok = g0 + 16 * tg;
+            if (tok >= t1) continue;
+            const uint32_t *q = rows + 16 * tg * kPitch + dq;
+            uint8_t *to = dst + (uint64_t)(tok & ~(tile - 1)) * D + (uint64_t)dq * 4 * tile + (tok & (tile - 1));
+            u32x4 o[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t x0 = q[(4 * j) * kPitch], x1 = q[(4 * j + 1) * kPitch], x2 = q[(4 * j + 2) * kPitch], x3 = q[(4 * j + 3) * kPitch];
+                turn4(x0, x1, x2, x3);
+                o[0][j] = x0;
+                o[1][j] = x1;
+                o[2][j] = x2;
+                o[3][j] = x3;
+            }
+            if (tok >= t0 && tok + 16 <= t1) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *(u32x4 *)(to + j * tile) = o[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (uint32_t e = 0; e < 16; ++e)
+                        if (tok + e >= t0 && tok + e < t1) to[j * tile + e] = (uint8_t)(o[j][e >> 2] >> (8 * (e & 3)));
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -1761,7 +1811,8 @@ __global__ __launch_bounds__(kThreads) void check_kernel(Kv kv) {
 // head: keys in rows as they lie, values turned through LDS.
 template <int D>
 __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
-    __shared__ uint32_t turn[D * (kStep + 4) / 4];
+    constexpr uint32_t kPitch = D / 4 + 1;
+    __shared__ uint32_t turn[kStep * kPitch];
     const Kv &kv = a.kv;
     uint64_t rest;
     const uint32_t s = locate(kv.n_seq, blockIdx.x, [&](uint32_t q) -> unsigned long long {
@@ -1795,24 +1846,31 @@ __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
         const u32x2 y = *(const u32x2 *)(kv.k + at * head_bytes(kv, D) + (uint64_t)(tok & (bt - 1)) * D + d);
         put8((void *)a.k, a.k_stride, tok, d, y, bad ? NAN : kv.ks[at]);
     }
-    // four tokens of a dimension a thread
-    uint8_t *tb = (uint8_t *)turn;
-    for (uint32_t e = threadIdx.x; e < D * (kStep / 4); e += kThreads) {
-        const uint32_t q = e % (tile / 4), d = e / (tile / 4) % D, tok = q0 + e / (tile / 4) / D * tile + q * 4;
-        if (tok >= t1 || tok + 4 <= t0) continue;
+    // 16 tokens of four dimensions a thread, turned
+    for (uint32_t e = threadIdx.x; e < D; e += kThreads) {
+        const uint32_t dq = e / 4, tok = q0 + e % 4 * 16;
+        if (tok >= t1 || tok + 16 <= t0) continue;
         const uint32_t page = pages[tok >> kv.btl];
         const uint64_t at = (uint64_t)(page < kv.n_pages ? page : 0u) * kv.hk + h;
         const uint32_t slot = tok & (bt - 1);
-        const uint32_t y = *(const uint32_t *)(kv.v + at * head_bytes(kv, D) + (uint64_t)(slot & ~(tile - 1)) * D + d * tile + (slot & (tile - 1)));
+        const uint8_t *p = kv.v + at * head_bytes(kv, D) + (uint64_t)(slot & ~(tile - 1)) * D + dq * 4 * tile + (slot & (tile - 1));
+        u32x4 x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) tb[(tok - q0 + j) * (D + 4) + d] = (uint8_t)(y >> (8 * j));
+        for (int j = 0; j < 4; ++j) x[j] = *(const u32x4 *)(p + j * tile);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t y[4] = {x[0][j], x[1][j], x[2][j], x[3][j]};
+            turn4(y[0], y[1], y[2], y[3]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) turn[(tok - q0 + 4 * j + q) * kPitch + dq] = y[q];
+        }
     }
     __syncthreads();
     for (uint32_t e = threadIdx.x; e < (t1 - t0) * (D / 8); e += kThreads) {
         const uint32_t tok = t0 + e / (D / 8), d = e % (D / 8) * 8;
         const uint32_t page = pages[tok >> kv.btl];
         const bool bad = page >= kv.n_pages;
-        const uint32_t *p = (const uint32_t *)(tb + (tok - q0) * (D + 4) + d);
+        const uint32_t *p = turn + (tok - q0) * kPitch + d / 4;
         put8((void *)a.v, a.v_stride, tok, d, u32x2{p[0], p[1]}, bad ? NAN : kv.vs[(uint64_t)page * kv.hk + h]);
     }
 }
