@@ -33,6 +33,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -1623,6 +1625,19 @@ __device__ inline uint32_t narrow4(const float *x, float inv) {
     return y;
 }
 
+// Four finite 16-bit values over a power of two to e4m3, nearest even.
+__device__ inline uint32_t narrow4_finite(uint32_t a, uint32_t b, float scale, bool half) {
+    i16x2 r = {0, 0};
+    if (half) {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(f16x2, a), scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(f16x2, b), scale, true);
+    } else {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, a), scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, b), scale, true);
+    }
+    return __builtin_bit_cast(uint32_t, r);
+}
+
 // Four e4m3 bytes under another scale (ratio <= 1, a power of two).
 __device__ inline uint32_t rescale4(uint32_t x, float ratio) {
     const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false);
@@ -1654,7 +1669,7 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
     constexpr int kEach = 8;                                  // 16-byte pieces a thread keeps
     constexpr uint32_t kPass = THREADS * kEach * 8 / D;       // tokens that the workgroup keeps
     constexpr uint32_t kPitch = D / 4 + 1;
-    __shared__ float red[THREADS / 64];
+    __shared__ uint32_t red[THREADS / 64];
     __shared__ uint32_t rows[(kPass + 16) * kPitch];          // quantised values by token
     const Kv &kv = a.kv;
     const uint32_t bt = 1u << kv.btl;
@@ -1693,24 +1708,38 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
             if (e < pieces) x[i] = *(const u32x4 *)(src + (row0 + e / (D / 8)) * stride + (uint64_t)h * D + e % (D / 8) * 8);
         }
     };
-    float amax = 0.0f;
-    for (uint32_t base = 0; base < pieces; base += THREADS * kEach) {
-        load(base);
+    // the largest of the values' bits without their signs, which order as the
+    // values do; infinities and NaN come last, and make a second look necessary
+    const uint32_t not_finite = half ? 0x7C00u : 0x7F80u;
+    auto largest = [&](bool all) {
+        u16x2 top = {0, 0};
+        for (uint32_t base = 0; base < pieces; base += THREADS * kEach) {
+            if (all || pieces > THREADS * kEach) load(base);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            if (base + i * THREADS + threadIdx.x < pieces)
+            for (int i = 0; i < kEach; ++i)
+                if (base + i * THREADS + threadIdx.x < pieces)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const float y = fabsf(to_f32(q ? x[i][j] >> 16 : x[i][j] & 0xFFFFu, half));
-                        amax = y < INFINITY ? fmaxf(amax, y) : amax;
+                    for (int j = 0; j < 4; ++j) {
+                        u16x2 z = __builtin_bit_cast(u16x2, x[i][j] & 0x7FFF7FFFu);
+                        if (!all) {
+                            z[0] = z[0] < not_finite ? z[0] : (uint16_t)0;
+                            z[1] = z[1] < not_finite ? z[1] : (uint16_t)0;
+                        }
+                        top = __builtin_elementwise_max(top, z);
                     }
-    }
-    for (int d = 32; d; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d, 64));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = amax;
-    __syncthreads();
-    for (int i = 0; i < THREADS / 64; ++i) amax = fmaxf(amax, red[i]);
+        }
+        uint32_t t = top[0] > top[1] ? top[0] : top[1];
+        for (int d = 32; d; d >>= 1) t = max(t, (uint32_t)__shfl_xor(t, d, 64));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
+        __syncthreads();
+        for (int i = 0; i < THREADS / 64; ++i) t = max(t, red[i]);
+        return t;
+    };
+    uint32_t top = largest(true);
+    const bool finite = top < not_finite;
+    if (!finite) top = largest(false);
+    const float amax = to_f32(top, half);
     float sc = scale_for(amax);
     if (p0) {
         const float was = *scale;
@@ -1745,13 +1774,17 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
             const uint32_t e = base + i * THREADS + threadIdx.x;
             u32x2 y = {0, 0};
             if (e < pieces) {
-                float z[8];
+                if (finite) {
+                    y = u32x2{narrow4_finite(x[i][0], x[i][1], sc, half), narrow4_finite(x[i][2], x[i][3], sc, half)};
+                } else {
+                    float z[8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    z[2 * j] = to_f32(x[i][j] & 0xFFFFu, half);
-                    z[2 * j + 1] = to_f32(x[i][j] >> 16, half);
+                    for (int j = 0; j < 4; ++j) {
+                        z[2 * j] = to_f32(x[i][j] & 0xFFFFu, half);
+                        z[2 * j + 1] = to_f32(x[i][j] >> 16, half);
+                    }
+                    y = u32x2{narrow4(z, inv), narrow4(z + 4, inv)};
                 }
-                y = u32x2{narrow4(z, inv), narrow4(z + 4, inv)};
             }
             const uint32_t tok = p0 + e / (D / 8), d = e % (D / 8) * 8;
             if (e >= pieces) continue;
