@@ -1599,6 +1599,14 @@ struct MoveArgs {
     uint64_t k_stride, v_stride;
 };
 
+// Reports the sequences that a store or a read leaves out: by the first head's workgroups.
+__device__ inline void report_bad(const Kv &kv, uint32_t task) {
+    for (uint32_t s = task * blockDim.x + threadIdx.x; s < kv.n_seq; s += gridDim.x * blockDim.x) {
+        const Head h = seq_head(kv, s);
+        if (!h.ok || h.n > h.ctx) report(kv);
+    }
+}
+
 // The smallest power of two s >= 2^-126 with amax <= 448 s: 448 = 1.75 * 2^8.
 __device__ inline float scale_for(float amax) {
     const uint32_t b = __float_as_uint(amax);
@@ -1665,7 +1673,7 @@ __device__ inline void turn4(uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d)
 // Values are turned through LDS: written byte by byte from the rows they came
 // in, a 512-token block took three times as long.
 template <int D, int THREADS>
-__global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
+__global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel(MoveArgs a, bool half) {
     constexpr int kEach = 8;                                  // 16-byte pieces a thread keeps
     constexpr uint32_t kPass = THREADS * kEach * 8 / D;       // tokens that the workgroup keeps
     constexpr uint32_t kPitch = D / 4 + 1;
@@ -1673,8 +1681,10 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
     __shared__ uint32_t rows[(kPass + 16) * kPitch];          // quantised values by token
     const Kv &kv = a.kv;
     const uint32_t bt = 1u << kv.btl;
+    const uint32_t task = blockIdx.x, h = blockIdx.y;
+    if (h == 0 && blockIdx.z == 0) report_bad(kv, task);
     uint64_t rest;
-    const uint32_t s = locate(kv.n_seq, blockIdx.x, [&](uint32_t q) -> unsigned long long {
+    const uint32_t s = locate(kv.n_seq, task, [&](uint32_t q) -> unsigned long long {
         const Head h = seq_head(kv, q);
         if (!h.n || h.n > h.ctx) return 0;
         return ((h.ctx - 1) >> kv.btl) - ((h.ctx - h.n) >> kv.btl) + 1;
@@ -1689,7 +1699,6 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
         return;
     }
     const bool vals = blockIdx.z;
-    const uint32_t h = blockIdx.y;
     const uint32_t p0 = max(start, blk << kv.btl) - (blk << kv.btl);     // slots [p0, p1) are new
     const uint32_t p1 = min(hd.ctx - (blk << kv.btl), bt);
     const uint64_t row0 = hd.row0 + ((blk << kv.btl) + p0 - start);
@@ -1701,11 +1710,13 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
     const uint32_t pieces = (p1 - p0) * (D / 8);
 
     u32x4 x[kEach];
+    const uint16_t *own = src + (row0 + threadIdx.x / (D / 8)) * stride + (uint64_t)h * D + threadIdx.x % (D / 8) * 8;
     auto load = [&](uint32_t base) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const uint32_t e = base + i * THREADS + threadIdx.x;
-            if (e < pieces) x[i] = *(const u32x4 *)(src + (row0 + e / (D / 8)) * stride + (uint64_t)h * D + e % (D / 8) * 8);
+            const uint32_t e = base + i * THREADS;
+            x[i] = u32x4{0, 0, 0, 0};
+            if (e + threadIdx.x < pieces) x[i] = *(const u32x4 *)(own + e / (D / 8) * stride);
         }
     };
     // the largest of the values' bits without their signs, which order as the
@@ -1717,16 +1728,15 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
             if (all || pieces > THREADS * kEach) load(base);
 #pragma unroll
             for (int i = 0; i < kEach; ++i)
-                if (base + i * THREADS + threadIdx.x < pieces)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        u16x2 z = __builtin_bit_cast(u16x2, x[i][j] & 0x7FFF7FFFu);
-                        if (!all) {
-                            z[0] = z[0] < not_finite ? z[0] : (uint16_t)0;
-                            z[1] = z[1] < not_finite ? z[1] : (uint16_t)0;
-                        }
-                        top = __builtin_elementwise_max(top, z);
+                for (int j = 0; j < 4; ++j) {
+                    u16x2 z = __builtin_bit_cast(u16x2, x[i][j] & 0x7FFF7FFFu);
+                    if (!all) {
+                        z[0] = z[0] < not_finite ? z[0] : (uint16_t)0;
+                        z[1] = z[1] < not_finite ? z[1] : (uint16_t)0;
                     }
+                    top = __builtin_elementwise_max(top, z);
+                }
         }
         uint32_t t = top[0] > top[1] ? top[0] : top[1];
         for (int d = 32; d; d >>= 1) t = max(t, (uint32_t)__shfl_xor(t, d, 64));
@@ -1767,8 +1777,8 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
     if (threadIdx.x == 0) *scale = sc;
     const float inv = 1.0f / sc;
     const uint32_t tile = min(bt, kStep);
-    for (uint32_t base = 0; base < pieces; base += THREADS * kEach) {
-        if (pieces > THREADS * kEach) load(base);
+    if (pieces > THREADS * kEach) load(0);
+    for (uint32_t base = 0;;) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t e = base + i * THREADS + threadIdx.x;
@@ -1796,48 +1806,44 @@ __global__ __launch_bounds__(THREADS) void store_kernel(MoveArgs a, bool half) {
                 q[1] = y[1];
             }
         }
-        if (!vals) continue;
-        // four dimensions of 16 tokens a thread; groups that the call fills
-        // whole are written whole
-        __syncthreads();
-        const uint32_t t0 = p0 + base / (D / 8), t1 = min(p1, t0 + kPass), g0 = t0 & ~15u;
-        for (uint32_t i = threadIdx.x; i < (t1 - g0 + 63) / 64 * D; i += THREADS) {
-            // lanes: four groups, then the dimensions
-            const uint32_t dq = i / 4 % (D / 4), tg = i % 4 + i / D * 4, tok = g0 + 16 * tg;
-            if (tok >= t1) continue;
-            const uint32_t *q = rows + 16 * tg * kPitch + dq;
-            uint8_t *to = dst + (uint64_t)(tok & ~(tile - 1)) * D + (uint64_t)dq * 4 * tile + (tok & (tile - 1));
-            u32x4 o[4];
+        if (vals) {
+            // four dimensions of 16 tokens a thread; groups that the call fills
+            // whole are written whole
+            __syncthreads();
+            const uint32_t t0 = p0 + base / (D / 8), t1 = min(p1, t0 + kPass), g0 = t0 & ~15u;
+            for (uint32_t i = threadIdx.x; i < (t1 - g0 + 63) / 64 * D; i += THREADS) {
+                // lanes: four groups, then the dimensions
+                const uint32_t dq = i / 4 % (D / 4), tg = i % 4 + i / D * 4, tok = g0 + 16 * tg;
+                if (tok >= t1) continue;
+                const uint32_t *q = rows + 16 * tg * kPitch + dq;
+                uint8_t *to = dst + (uint64_t)(tok & ~(tile - 1)) * D + (uint64_t)dq * 4 * tile + (tok & (tile - 1));
+                u32x4 o[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t x0 = q[(4 * j) * kPitch], x1 = q[(4 * j + 1) * kPitch], x2 = q[(4 * j + 2) * kPitch], x3 = q[(4 * j + 3) * kPitch];
-                turn4(x0, x1, x2, x3);
-                o[0][j] = x0;
-                o[1][j] = x1;
-                o[2][j] = x2;
-                o[3][j] = x3;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t x0 = q[(4 * j) * kPitch], x1 = q[(4 * j + 1) * kPitch], x2 = q[(4 * j + 2) * kPitch], x3 = q[(4 * j + 3) * kPitch];
+                    turn4(x0, x1, x2, x3);
+                    o[0][j] = x0;
+                    o[1][j] = x1;
+                    o[2][j] = x2;
+                    o[3][j] = x3;
+                }
+                if (tok >= t0 && tok + 16 <= t1) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) *(u32x4 *)(to + j * tile) = o[j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (uint32_t e = 0; e < 16; ++e)
+                            if (tok + e >= t0 && tok + e < t1) to[j * tile + e] = (uint8_t)(o[j][e >> 2] >> (8 * (e & 3)));
+                }
             }
-            if (tok >= t0 && tok + 16 <= t1) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *(u32x4 *)(to + j * tile) = o[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (uint32_t e = 0; e < 16; ++e)
-                        if (tok + e >= t0 && tok + e < t1) to[j * tile + e] = (uint8_t)(o[j][e >> 2] >> (8 * (e & 3)));
-            }
+            __syncthreads();
         }
-        __syncthreads();
+        base += THREADS * kEach;
+        if (base >= pieces) break;
+        load(base);
     }
-}
-
-// Reports the sequences that a store or a read leaves out.
-__global__ __launch_bounds__(kThreads) void check_kernel(Kv kv) {
-    const uint32_t s = blockIdx.x * kThreads + threadIdx.x;
-    if (s >= kv.n_seq) return;
-    const Head h = seq_head(kv, s);
-    if (!h.ok || h.n > h.ctx) report(kv);
 }
 
 // One workgroup gives back up to 64 tokens (one tile of positions) of one
@@ -1847,15 +1853,17 @@ __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
     constexpr uint32_t kPitch = D / 4 + 1;
     __shared__ uint32_t turn[kStep * kPitch];
     const Kv &kv = a.kv;
+    const uint32_t task = blockIdx.x, h = blockIdx.y;
+    if (h == 0) report_bad(kv, task);
     uint64_t rest;
-    const uint32_t s = locate(kv.n_seq, blockIdx.x, [&](uint32_t q) -> unsigned long long {
+    const uint32_t s = locate(kv.n_seq, task, [&](uint32_t q) -> unsigned long long {
         const Head h = seq_head(kv, q);
         if (!h.n || h.n > h.ctx) return 0;
         return (h.ctx - 1) / kStep - (h.ctx - h.n) / kStep + 1;
     }, &rest);
     if (s >= kv.n_seq) return;
     const Head hd = seq_head(kv, s);
-    const uint32_t start = hd.ctx - hd.n, h = blockIdx.y, bt = 1u << kv.btl, tile = min(bt, kStep);
+    const uint32_t start = hd.ctx - hd.n, bt = 1u << kv.btl, tile = min(bt, kStep);
     const uint32_t q0 = (start / kStep + (uint32_t)rest) * kStep;
     const uint32_t t0 = max(start, q0), t1 = min(hd.ctx, q0 + kStep);
     const uint32_t *pages = kv.pages + (uint64_t)s * kv.max_pages;
@@ -2210,7 +2218,6 @@ extern "C" netkv_status netkv_kv_store(netkv_handle h, const netkv_kv_t *kv, con
     hipStream_t s = (hipStream_t)stream;
     const bool half = dtype == NETKV_FP16;
     const uint32_t rows = a.kv.max_tok < kv->block_tokens ? a.kv.max_tok : kv->block_tokens;
-    check_kernel<<<(a.kv.n_seq + kThreads - 1) / kThreads, kThreads, 0, s>>>(a.kv);
     switch (kv->head_dim) {
         case 64: launch_store<64>(a, half, (uint32_t)tasks, rows, s); break;
         case 128: launch_store<128>(a, half, (uint32_t)tasks, rows, s); break;
@@ -2242,7 +2249,6 @@ extern "C" netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, cons
     hipStream_t s = (hipStream_t)stream;
     const bool half = dtype == NETKV_FP16;
     const dim3 grid((uint32_t)tasks, kv->n_kv_heads);
-    check_kernel<<<(a.kv.n_seq + kThreads - 1) / kThreads, kThreads, 0, s>>>(a.kv);
     switch (kv->head_dim) {
         case 64: read_kernel<64><<<grid, kThreads, 0, s>>>(a, half); break;
         case 128: read_kernel<128><<<grid, kThreads, 0, s>>>(a, half); break;
