@@ -39,8 +39,6 @@ constexpr uint32_t kGather = 4;                    // and of eight bins each
 constexpr uint32_t kListed = 1024;                 // segments that every workgroup looks through itself
 constexpr uint32_t kTile = 1024;                   // segments a workgroup of plan_kernel places
 constexpr uint32_t kMaxSeg = 0x7FFFFFu;
-constexpr int kThrThreads = 1024;
-constexpr int kThrWaves = kThrThreads / 64;
 
 struct Seg {
     uint64_t first;      // entry
@@ -557,7 +555,7 @@ __global__ __launch_bounds__(kThreads) void count_kernel(EvictArgs a) {
 #pragma unroll
         for (uint32_t j = 0; j < kBatch; ++j) {
             const uint32_t i = i0 + j * kThreads + threadIdx.x;
-            k[j] = i < end ? wt[i] : 0ull;
+            k[j] = i < end ? __builtin_nontemporal_load(wt + i) : 0ull;
         }
 #pragma unroll
         for (uint32_t j = 0; j < kBatch; ++j) {
@@ -600,23 +598,33 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictArgs a) {
             x[j] = make_uint4(0, 0, 0, 0);
             if (i0 + 512 * j < end) x[j] = *(const uint4 *)(bins + i0 + 512 * j);
         }
+        uint32_t is = 0;   // the lane's entries of the bin
 #pragma unroll
         for (uint32_t j = 0; j < kGather; ++j) {
             const uint32_t y[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
 #pragma unroll
             for (uint32_t q = 0; q < 8; ++q) {
-                const uint32_t i = i0 + 512 * j + q, b = q & 1 ? y[q / 2] >> 16 : y[q / 2] & 0xFFFFu;
-                above += i < end && b > bin;
-                const bool is = i < end && b == bin;
-                const uint64_t m = __ballot(is);
-                if (is) {
-                    const uint64_t k = key_of(a, n, keep, i, wt[i]);
-                    cand[in + __popcll(m & ((1ull << lane) - 1))] = k;
-                    every &= k;
-                    some |= k;
-                }
-                in += __popcll(m);
+                const uint32_t b = q & 1 ? y[q / 2] >> 16 : y[q / 2] & 0xFFFFu;
+                const bool in = i0 + 512 * j + q < end;
+                above += in && b > bin;
+                is |= in && b == bin ? 1u << (8 * j + q) : 0u;
             }
+        }
+        const uint32_t mine = __popc(is);
+        uint32_t to = mine;
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t z = __shfl_up(to, d, 64);
+            if (lane >= d) to += z;
+        }
+        const uint32_t all = __shfl(to, 63, 64);
+        to += in - mine;
+        in += all;
+        for (is = bin < 32 ? 0u : is; is; is &= is - 1) {
+            const uint32_t q = __builtin_ctz(is), i = i0 + 512 * (q / 8) + q % 8;
+            const uint64_t k = key_of(a, n, keep, i, wt[i]);
+            cand[to++] = k;
+            every &= k;
+            some |= k;
         }
     }
     for (int d = 32; d; d >>= 1) {
@@ -626,6 +634,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictArgs a) {
     }
     if (lane == 0) {
         a.parts[(uint64_t)blockIdx.x * kWaves + w] = make_uint2(above, in);
+        if (bin < 32 && in) every = some = bin;   // such a bin holds one weight: none is looked at
         a.bits[(uint64_t)blockIdx.x * kWaves + w] = make_ulonglong2(every, some);
     }
     if (threadIdx.x == 0 && blockIdx.x == l.chunk0) {
@@ -634,10 +643,10 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictArgs a) {
     }
 }
 
-__global__ __launch_bounds__(kThrThreads) void threshold_kernel(EvictArgs a) {
+__global__ __launch_bounds__(kThreads) void threshold_kernel(EvictArgs a) {
     __shared__ __align__(16) uint32_t hist[256];
-    __shared__ uint32_t found[3], cw[kThrWaves][2], n_list, n_need;
-    __shared__ uint64_t value, bw[kThrWaves][2];
+    __shared__ uint32_t found[3], cw[kWaves][2], n_list, n_need;
+    __shared__ uint64_t value, bw[kWaves][2];
     __shared__ unsigned long long list[64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const uint32_t part = a.chunk / kWaves;
@@ -649,7 +658,7 @@ __global__ __launch_bounds__(kThrThreads) void threshold_kernel(EvictArgs a) {
         const uint64_t *cand = a.cand + l.first;
         uint32_t need = l.need, among = 0;
         uint64_t every = ~0ull, some = 0;
-        for (uint32_t c = threadIdx.x; c < n_part; c += kThrThreads) {
+        for (uint32_t c = threadIdx.x; c < n_part; c += kThreads) {
             const ulonglong2 b = a.bits[(uint64_t)l.chunk0 * kWaves + c];
             among += parts[c].y;
             every &= b.x;
@@ -669,7 +678,7 @@ __global__ __launch_bounds__(kThrThreads) void threshold_kernel(EvictArgs a) {
         if (threadIdx.x == 0) n_list = 0;
         __syncthreads();
         among = 0;
-        for (int v = 0; v < kThrWaves; ++v) {
+        for (int v = 0; v < kWaves; ++v) {
             among += cw[v][0];
             every &= bw[v][0];
             some |= bw[v][1];
@@ -680,7 +689,7 @@ __global__ __launch_bounds__(kThrThreads) void threshold_kernel(EvictArgs a) {
         uint64_t prefix = some >> shift;
         // as many lanes a part as parts have weights on average, at most a wavefront
         const uint32_t lg = among > n_part ? min(32 - __clz((among - 1) / n_part), 6) : 0;
-        const uint32_t c_own = threadIdx.x >> lg, c_step = kThrThreads >> lg, i_own = threadIdx.x & ((1u << lg) - 1);
+        const uint32_t c_own = threadIdx.x >> lg, c_step = kThreads >> lg, i_own = threadIdx.x & ((1u << lg) - 1);
         auto each = [&](auto f) {
             for (uint32_t c = c_own; c < n_part; c += c_step) {
                 const uint32_t m = parts[c].y;
@@ -689,7 +698,7 @@ __global__ __launch_bounds__(kThrThreads) void threshold_kernel(EvictArgs a) {
         };
         while (shift && need != among && among > 64) {
             const uint32_t by = min(shift, 8u);
-            if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+            hist[threadIdx.x] = 0;
             __syncthreads();
             each([&](uint64_t k) {
                 if (k >> shift == prefix) atomicAdd(&hist[(uint32_t)(k >> (shift - by)) & ((1u << by) - 1)], 1u);
@@ -746,7 +755,7 @@ __global__ __launch_bounds__(kThrThreads) void threshold_kernel(EvictArgs a) {
             }
             __syncthreads();
             uint32_t g0 = bg, e0 = be;
-            for (int v = 0; v < kThrWaves; ++v) {
+            for (int v = 0; v < kWaves; ++v) {
                 if (v < w) {
                     g0 += cw[v][0];
                     e0 += cw[v][1];
@@ -795,8 +804,8 @@ __global__ __launch_bounds__(kThreads) void write_kernel(EvictArgs a) {
 #pragma unroll
         for (uint32_t j = 0; j < kBatch; ++j) {
             const uint32_t i = i0 + j * 64 + lane;
-            bool up = i < end && b[j] > bin, tie = false;
-            if (i < end && b[j] == bin) {
+            bool up = i < end && b[j] > bin, tie = i < end && b[j] == bin;
+            if (tie && bin >= 32) {
                 const uint64_t p = key_of(a, n, keep, i, wt[i]) >> shift;
                 up = p > prefix;
                 tie = p == prefix;
@@ -805,7 +814,7 @@ __global__ __launch_bounds__(kThreads) void write_kernel(EvictArgs a) {
             const uint32_t e = ne + __popcll(me & below);
             const bool stays = up || (tie && e < need);
             b[j] = stays ? ng + __popcll(mg & below) + min(e, need) : ~0u;
-            x[j] = stays && a.out_hashes ? hashes[i] : 0ull;
+            x[j] = stays && a.out_hashes ? __builtin_nontemporal_load(hashes + i) : 0ull;
             ng += __popcll(mg);
             ne += __popcll(me);
         }
@@ -918,7 +927,7 @@ extern "C" netkv_status netkv_cache_evict(netkv_handle h, uint32_t n_seg, const 
     if (n_seg && y.long_cap) {
         count_kernel<<<y.chunk_cap, kThreads, 0, s>>>(a);
         gather_kernel<<<y.chunk_cap, kThreads, 0, s>>>(a);
-        threshold_kernel<<<y.long_cap < 1024 ? y.long_cap : 1024, kThrThreads, 0, s>>>(a);
+        threshold_kernel<<<y.long_cap < 1024 ? y.long_cap : 1024, kThreads, 0, s>>>(a);
         write_kernel<<<y.chunk_cap, kThreads, 0, s>>>(a);
     }
     const hipError_t e = hipGetLastError();
