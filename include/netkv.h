@@ -508,7 +508,7 @@ typedef struct {
  * nothing outside the arrays is read or written for it. */
 typedef struct {
     uint32_t n_seq;                 /* <= 65535 */
-    uint32_t max_pages;             /* >= 1, max_pages * block_tokens <= 2^31 */
+    uint32_t max_pages;             /* >= 1, max_pages * block_tokens < 2^31 */
     uint64_t n_tok, max_tok;        /* n_tok <= 2^31 */
     const uint64_t *tok_off;        /* [n_seq + 1] */
     const uint32_t *ctx_len;        /* [n_seq] */
@@ -525,8 +525,8 @@ enum { NETKV_BF16 = 1, NETKV_FP16 = 2 };
  * and that is larger; if it grows, those tokens are brought under the new
  * scale.  Rounding is to nearest even: at most half a step, 2^-4 of a value
  * down to 2^-6 s and 2^-10 s below.  What is not finite is stored as NaN.  A
- * page that the call writes must be in no other sequence of the call that
- * writes it.  An invalid sequence, or one with more rows than tokens, is left
+ * page that the call writes must be one block of one sequence (the same page
+ * twice, and which of the two remains is not said).  An invalid sequence, or one with more rows than tokens, is left
  * out.  Asynchronous; allocates nothing. */
 netkv_status netkv_kv_store(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *k,
                             uint64_t k_stride, const void *v, uint64_t v_stride, int dtype, void *stream);

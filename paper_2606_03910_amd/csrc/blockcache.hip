@@ -1949,7 +1949,7 @@ netkv_status make_kv(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t
     if (q->n_seq && (!q->tok_off || !q->ctx_len || !q->pages)) return invalid(h, "a sequence array is NULL");
     if (q->n_seq > 65535) return invalid(h, "n_seq must be <= 65535");
     if (q->n_seq && q->max_pages < 1) return invalid(h, "max_pages must be >= 1");
-    if (((uint64_t)q->max_pages << btl) > (1ull << 31)) return invalid(h, "max_pages * block_tokens must be <= 2^31");
+    if (((uint64_t)q->max_pages << btl) >= (1ull << 31)) return invalid(h, "max_pages * block_tokens must be < 2^31");
     if (q->n_tok > (1ull << 31)) return invalid(h, "n_tok must be <= 2^31");
     a.k = (uint8_t *)kv->k;
     a.v = (uint8_t *)kv->v;
