@@ -465,6 +465,8 @@ struct AttendArgs : PlanArgs {
     float *lse;                      // [row][query head] log2 of the row's sum, or null
     float *units;                    // [seq][head][unit][unit_rows] log2 of the unit's sum, or null
     uint32_t n_units, unit_rows;
+    float *sums;                     // [head][block][row] log2 of the block's sum for each row of the call, or null
+    uint64_t sum_rows;               // rows of a head
 };
 
 // 2^(x + by) of 16 scores, as the operand of the product with the values, and
@@ -881,7 +883,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
 //
 // SMALL: blocks of less than 64 tokens, so a step's four groups of 16 tokens
 // may be in different pages; else pages, scales and addresses are scalar.
-template <int D, int NT, bool HALF, bool SMALL>
+//
+// SUMS: every row's sum over each block is kept for the blocks' weights (a
+// block is whole steps then, and ranges are whole blocks).
+template <int D, int NT, bool HALF, bool SMALL, bool SUMS>
 __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
@@ -935,13 +940,13 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
 
     f32x4 acc[NT][kDT], st[NT][4];
     f16x8 pf[NT][2];
-    float m[NT], l[NT], y[NT];
+    float m[NT], l[NT], y[NT], lb[NT];                // lb: the share of l that is the present block's
     uint64_t nan_sums = 0;                            // sums of this lane that a NaN value belongs to
     static_assert(4 * NT * kDT <= 64, "a bit a sum");
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         m[n] = y[n] = -INFINITY;
-        l[n] = 0.0f;
+        l[n] = lb[n] = 0.0f;
         pf[n][0] = pf[n][1] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
         for (int d = 0; d < kDT; ++d) acc[n][d] = f32x4{0, 0, 0, 0};
@@ -1096,7 +1101,11 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
         }
         if (!__all(fits)) return false;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) l[n] += sum[n] * exp2_of(up[n]);
+        for (int n = 0; n < NT; ++n) {
+            const float add = sum[n] * exp2_of(up[n]);
+            l[n] += add;
+            if constexpr (SUMS) lb[n] += add;
+        }
         return true;
     };
     // any step: masks, NaN values among those that not every row sees, maxima
@@ -1149,7 +1158,9 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
                 }
             mx = mx == -INFINITY ? -INFINITY : mx * sc;
             const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog));
-            l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
+            const float ml = m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
+            l[n] *= ml;
+            if constexpr (SUMS) lb[n] *= ml;
             const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
             m[n] = mn;
             y[n] = yn;
@@ -1157,11 +1168,26 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
             for (int d = 0; d < kDT; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
-            l[n] += weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
+            const float add = weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
+            l[n] += add;
+            if constexpr (SUMS) lb[n] += add;
             weights_of(st[n], sc, yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
         }
     };
 
+    const uint32_t per = SUMS ? bt / kStep : 1u;
+    auto keep_sums = [&](uint32_t kt) {
+        if constexpr (SUMS) {
+            if (((kt + 1) & (per - 1)) != 0 && kt + 1 < it.k1) return;
+            float *to = a.sums + ((uint64_t)h * a.kv.max_pages + ((kt * kStep) >> a.kv.btl)) * a.sum_rows + hd.row0 * a.G + row0 + c;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float sum = row_sum(lb[n]);
+                if (g == 0 && row0 + n * 16 + c < n_rows) to[n * 16] = m[n] + log2_of(sum);
+                lb[n] = 0.0f;
+            }
+        }
+    };
     // pages of the step after next and the one after it
     uint32_t po = 0, pv = 0, po_on = 0, pv_on = 0;
     float sc_on = 0.0f, vs_on = 0.0f;                 // scales of the step after next
@@ -1216,11 +1242,13 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
             look_ahead(kt);
             if (done) done = softmax();
             if (!done) break;
+            keep_sums(kt);
             pass_on(kt);
             ++kt;
         } while (kt < it.k1);
         if (done) break;
         softmax_any(kt);
+        keep_sums(kt);
         pass_on(kt);
     }
     if (!second) meet();
@@ -1376,6 +1404,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, uint32_t r
 struct WeightArgs {
     float *w;            // [seq][max_pages]
     float *cols;         // [seq][head][unit], or null
+    uint32_t tile;       // tokens of a unit of cols
 };
 
 // Block weights of a call of few rows: a wavefront a block, lanes over (head,
@@ -1400,7 +1429,27 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
     if (lane == 0) wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? sum : NAN;
 }
 
-// Block weights of a call of many rows: with every row's lse known, the
+// Block weights of a call of many rows that kept its rows' sums: a workgroup
+// a block and head adds 2^(sum - lse) over the rows that see it.
+__global__ __launch_bounds__(kThreads) void row_kernel(AttendArgs a, WeightArgs wa) {
+    __shared__ float red[kWaves];
+    const uint32_t b = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+    const Head hd = seq_head(a.kv, s);
+    const uint64_t from = (uint64_t)b << a.kv.btl;
+    if (!hd.ok || from >= hd.ctx) return;
+    // rows before the block's first token do not see it (and kept nothing)
+    const int64_t first = (int64_t)from - ((int64_t)hd.ctx - hd.n);
+    const float *p = a.sums + ((uint64_t)h * a.kv.max_pages + b) * a.sum_rows + hd.row0 * a.G;
+    float sum = 0.0f;
+    for (uint32_t r = (first > 0 ? (uint32_t)first * a.G : 0u) + threadIdx.x; r < hd.n * a.G; r += kThreads)
+        sum += exp2_of(p[r] - a.lse[(hd.row0 + r / a.G) * a.Hq + h * a.G + r % a.G]);
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) wa.cols[((uint64_t)s * a.kv.hk + h) * a.n_units + b] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// The same without such sums: with every row's lse known, the
 // scores are formed once more, 256 tokens a workgroup (64 a wavefront, their
 // keys in registers) against all rows, and 2^(x - lse) is summed over them (a
 // prompt's partial sums of every row would be larger than its cache).  Rows
@@ -1520,8 +1569,7 @@ __global__ __launch_bounds__(kThreads) void block_kernel(AttendArgs a, WeightArg
     const uint32_t s = blockIdx.y, b = blockIdx.x * kThreads + threadIdx.x;
     if (b >= a.kv.max_pages) return;
     const Head hd = seq_head(a.kv, s);
-    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep), per = bt / tile;
-    const uint32_t have = (hd.ctx + tile - 1) / tile;
+    const uint32_t per = (1u << a.kv.btl) / wa.tile, have = (hd.ctx + wa.tile - 1) / wa.tile;
     const uint32_t u0 = b * per, u1 = min(u0 + per, have);
     float sum = 0.0f;
     if (hd.n)
@@ -1975,8 +2023,9 @@ constexpr uint64_t align256(uint64_t x) { return (x + 255) & ~255ull; }
 struct Layout {
     int NT;
     bool rows;             // prompt_kernel
+    bool sums;             // and its rows' sums over the blocks
     uint32_t G, tile_rows, target, fine, item_cap, slot_cap, join_cap, n_units, unit_rows;
-    uint64_t head, items, joins, ml, part, lse, units, cols, total;
+    uint64_t head, items, joins, ml, part, lse, units, cols, sums_at, total;
 };
 
 netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads, bool weights, Layout &y) {
@@ -2016,7 +2065,13 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     y.joins = take(sizeof(Join) * y.join_cap);
     y.ml = take(16ull * y.slot_cap * a.hk * y.tile_rows);
     y.part = take(4ull * y.slot_cap * a.hk * y.tile_rows * D);
-    y.lse = y.units = y.cols = 0;
+    // A prompt's weights come from every row's sum over each block where a
+    // block is whole steps and a row has at most 256 of them (1 KB; a row's
+    // query and output are 512 bytes at 128 dimensions), else from a second
+    // pass over the keys.
+    y.sums = weights && y.rows && bt >= kStep && a.max_pages <= 256;
+    if (y.sums) y.n_units = a.max_pages;
+    y.lse = y.units = y.cols = y.sums_at = 0;
     if (weights) {
         y.lse = take(4ull * a.n_tok * heads);
         const uint64_t u = (uint64_t)a.n_seq * a.hk * y.n_units;
@@ -2024,6 +2079,7 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
             y.cols = take(4 * u);
         else
             y.units = take(4 * u * y.unit_rows);
+        if (y.sums) y.sums_at = take(4ull * a.n_tok * heads * a.max_pages);
     }
     y.total = at;
     return NETKV_OK;
@@ -2037,9 +2093,11 @@ void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, h
                  : attend_kernel<D, NT, HALF, UNITS, false><<<grid, kThreads, 0, s>>>(a)
     if (y.rows) {
         if (a.kv.btl < 6)
-            prompt_kernel<D, D == 256 ? 1 : 2, HALF, true><<<grid, kPromptThreads, 0, s>>>(a);
+            prompt_kernel<D, D == 256 ? 1 : 2, HALF, true, false><<<grid, kPromptThreads, 0, s>>>(a);
+        else if (y.sums)
+            prompt_kernel<D, D == 256 ? 1 : 2, HALF, false, true><<<grid, kPromptThreads, 0, s>>>(a);
         else
-            prompt_kernel<D, D == 256 ? 1 : 2, HALF, false><<<grid, kPromptThreads, 0, s>>>(a);
+            prompt_kernel<D, D == 256 ? 1 : 2, HALF, false, false><<<grid, kPromptThreads, 0, s>>>(a);
     } else if (D == 256 || y.NT == 1) {
         if (wa.w) NETKV_ATTEND(1, true);
         else NETKV_ATTEND(1, false);
@@ -2056,7 +2114,10 @@ void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, h
     if (!wa.w) return;
     if (y.rows) {
         const uint32_t steps = (uint32_t)((((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep);
-        column_kernel<D, HALF><<<dim3((steps + kWaves - 1) / kWaves * a.kv.hk, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
+        if (y.sums)
+            row_kernel<<<dim3(a.kv.max_pages, a.kv.hk, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
+        else
+            column_kernel<D, HALF><<<dim3((steps + kWaves - 1) / kWaves * a.kv.hk, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
         block_kernel<<<dim3((a.kv.max_pages + kThreads - 1) / kThreads, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
     } else {
         unit_kernel<<<dim3((a.kv.max_pages + kWaves - 1) / kWaves, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
@@ -2120,7 +2181,8 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     t.target = y.target;
     t.fine = y.fine;
     t.least = y.rows ? 8 : kWaves;
-    t.round = y.rows ? 1 : kWaves;
+    // whole blocks for a prompt (its sums), with and without weights the same
+    t.round = !y.rows ? kWaves : kv->block_tokens > kStep ? kv->block_tokens / kStep : 1;
     t.item_cap = y.item_cap;
     t.slot_cap = y.slot_cap;
     t.join_cap = y.join_cap;
@@ -2146,7 +2208,10 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     t.units = block_weight && !y.rows ? (float *)(ws + y.units) : nullptr;
     t.n_units = y.n_units;
     t.unit_rows = y.unit_rows;
+    t.sums = y.sums ? (float *)(ws + y.sums_at) : nullptr;
+    t.sum_rows = (uint64_t)a.n_tok * y.G;
     WeightArgs wa{};
+    wa.tile = y.sums ? kv->block_tokens : kv->block_tokens < kStep ? kv->block_tokens : kStep;
     wa.w = block_weight;
     wa.cols = y.rows ? (float *)(ws + y.cols) : nullptr;
     switch (kv->head_dim) {

@@ -97,8 +97,9 @@ def attend(cache, table, ctx, n_new, q, heads, scale):
     The bounds, for exact products summed in fp32 over D terms: a score is off
     by at most D 2^-24 sum |q k| scale, a weight relatively by that plus the
     exponential's and the sum's few 2^-23 (delta); the weights are rounded to
-    11 bits, 2^-12 each, or by 2^-25 of the largest (weight times value scale)
-    below 2^-14 of it, with |value| <= 448."""
+    11 bits, 2^-11 each (their steps are 2^-10 of their power of two, and half
+    a step of a weight just above it is 2^-11 of it), or by 2^-25 of the largest
+    (weight times value scale) below 2^-14 of it, with |value| <= 448."""
     p, hk, D, b = cache.shape
     g = heads // hk
     out = np.zeros(q.shape)
@@ -123,7 +124,7 @@ def attend(cache, table, ctx, n_new, q, heads, scale):
                     pr = e / e.sum(1, keepdims=True)
                     a = np.abs(v[:seen])
                     out[row + t, h * g:(h + 1) * g] = pr @ v[:seen]
-                    tol[row + t, h * g:(h + 1) * g] = ((2.0 ** -12 + 2 * delta)[:, None] * (pr @ a)
+                    tol[row + t, h * g:(h + 1) * g] = ((2.0 ** -11 + 2 * delta)[:, None] * (pr @ a)
                                                       + seen * 2.0 ** -25 * 448 * (pr * sv[:seen]).max(1)[:, None])
                     blocks = np.arange(seen) // b
                     for j in range(g):

@@ -258,3 +258,20 @@ def test_evict_weights_of_every_width(nk, sel, kind):
         w = np.uint64(1) << rng.integers(0, 64, m).astype(np.uint64)
     for f in (0.0, 0.3, 0.97, 1.0):
         run(nk, sel, n, w, [max(1, int(f * x)) for x in n], 2 if f == 0.3 else 0)
+
+
+@pytest.mark.parametrize("block", [64, 256, 1024])
+def test_prompt_weights_both_ways(nk, sel, block):
+    """A prompt's block weights from its rows' sums (at most 256 blocks a
+    sequence) and from the second pass (more), whole and split, with rows that
+    see nothing."""
+    ctx, n_new = [9000, 600, 3, 64, 129], [40, 600, 70, 64, 1]
+    c, table, q = case(nk, sel, 38, ctx, n_new, 6, 2, 64, block, "fp16")
+    cache, qd = upload(nk, sel, c), q.cuda()
+    wide = np.concatenate([table, np.full((5, 257), 1 << 30)], 1)     # never read
+    for t in (table, wide):
+        o, w = cache.attend(sequences(nk, n_new, ctx, t), qd, weights=True)
+        sel.sync_errors()
+        _say(check_attend(c, t, ctx, n_new, q, o, w))
+        o2, w2 = cache.attend(sequences(nk, n_new, ctx, t), qd, weights=True)
+        assert torch.equal(o, o2) and torch.equal(w, w2)
