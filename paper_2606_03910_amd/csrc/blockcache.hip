@@ -284,8 +284,9 @@ struct Shares {
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
             rt[j] = kt[j] = 0;
+            if (j >= per) continue;
             const uint32_t s = lane * per + j;
-            if (j < per && s < a.kv.n_seq) {
+            if (s < a.kv.n_seq) {
                 const Head h = seq_head(a.kv, s);
                 rt[j] = tiles_of(h, a);
                 kt[j] = (h.ctx + kStep - 1) / kStep;
@@ -298,6 +299,7 @@ struct Shares {
         own_fulls = own_lasts = own_slots = own_joins = 0;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
+            if (j >= per) continue;
             const uint32_t p = parts(j);
             own_fulls += rt[j] * (p - 1);
             own_lasts += rt[j];
@@ -935,8 +937,9 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
     // without a branch around the products their sums stay where they are.
     const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
     const uint32_t all_lim = see_all > 0 ? (uint32_t)min(see_all, (int64_t)hd.ctx) : 0u;
-    // tokens that every row of the sequence sees
-    const uint32_t own_from = hd.ctx > hd.n ? hd.ctx - hd.n : 0u;
+    // tokens that every row of the tile sees
+    const int64_t see_tile = (int64_t)hd.ctx - hd.n + it.tile * a.tile_rows / a.G + 1;
+    const uint32_t tile_lim = see_tile > 0 ? (uint32_t)min(see_tile, (int64_t)hd.ctx) : 0u;
 
     f32x4 acc[NT][kDT], st[NT][4];
     f16x8 pf[NT][2];
@@ -991,7 +994,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
             }
             return;
         }
-        if (kt * kStep + kStep > own_from) {
+        if (kt * kStep + kStep > tile_lim) {
             // bytes of slots that hold no token are cleared, a NaN is taken out
             // and noted
             const uint32_t tok0 = kt * kStep + 16 * g;
@@ -1113,7 +1116,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
     auto softmax_any = [&](uint32_t kt) {
         const float sc = scale_of(), vlog = log2_of(vs_at[0]);
         const uint32_t tok0 = kt * kStep + 16 * g;
-        if (kt * kStep + kStep > own_from) {
+        if (kt * kStep + kStep > tile_lim) {
             const uint32_t noted = lds_nan[kt & 1];
             // as in attend_kernel: the rows that see a NaN value are found by
             // a product of the masks
@@ -1237,8 +1240,8 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
             scores(kt);
             interleave(std::integral_constant<int, D / 4>());
             meet();
-            done = kt * kStep + kStep <= all_lim;
-            if (kt * kStep + kStep > own_from) done = done && __builtin_amdgcn_readfirstlane(lds_nan[kt & 1]) == 0;
+            done = kt * kStep + kStep <= all_lim && kt > it.k0;   // the first step sets the maxima
+            if (kt * kStep + kStep > tile_lim) done = done && __builtin_amdgcn_readfirstlane(lds_nan[kt & 1]) == 0;
             look_ahead(kt);
             if (done) done = softmax();
             if (!done) break;
