@@ -4,10 +4,10 @@
 //   store_kernel    -- new keys and values quantised into their blocks.
 //   read_kernel     -- tokens given back in 16 bits.
 //   plan_kernel     -- a call's work list: (sequence, row tile, token range).
-//   attend_kernel   -- attention of up to 64 rows over a token range.
+//   attend_kernel   -- attention of up to 32 rows over a token range.
 //   prompt_kernel   -- the same of up to 256 rows.
 //   join_kernel     -- joins the ranges of the rows that were split.
-//   unit_kernel, column_kernel, block_kernel -- block weights.
+//   unit_kernel, row_kernel, column_kernel, block_kernel -- block weights.
 //   weigh_kernel    -- block weights summed over pages in fixed point.
 //
 // A block ("page") holds block_tokens tokens of every head.  An element is
@@ -1426,7 +1426,10 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
             const uint32_t h = i / (hd.n * a.G), row = i % (hd.n * a.G);
             const float lse = a.lse[(hd.row0 + row / a.G) * a.Hq + h * a.G + row % a.G];
             const float *p = a.units + (((uint64_t)s * a.kv.hk + h) * a.n_units + u0) * a.unit_rows + row;
-            for (uint32_t u = u0; u < u1; ++u, p += a.unit_rows) sum += exp2_of(*p - lse);
+            // only units that the row sees: its tile may have ended before the others
+            const int64_t seen = (int64_t)hd.ctx - hd.n + row / a.G + 1;
+            const uint32_t end = seen <= 0 ? 0u : min(u1, (uint32_t)((seen + tile - 1) / tile));
+            for (uint32_t u = u0; u < end; ++u, p += a.unit_rows) sum += exp2_of(*p - lse);
         }
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
     if (lane == 0) wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? sum : NAN;
@@ -2037,8 +2040,16 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     if (y.G > 64) return invalid(h, "n_heads / n_kv_heads must be <= 64");
     const uint64_t most = (uint64_t)a.max_tok * y.G;   // rows of the longest sequence's head
     if (most > 0xFFFFFFFFull - 1024) return invalid(h, "max_tok * n_heads / n_kv_heads must be < 2^32 - 1024");
-    y.rows = most > 64;
-    y.NT = most <= 16 || D == 256 ? 1 : 2;   // 64 rows: tiles side by side, their cache lines shared in L2
+    // Rows of the longest sequence from which prompt_kernel pays, whose tile
+    // takes as long with one row as with all.  The row tiles of attend_kernel
+    // lie side by side, and the cache's lines reach them from L2.  64 sequences
+    // of 8,192 tokens, attend_kernel against prompt_kernel, us: 64 dimensions,
+    // 192 rows 205, 258, 256 rows 268, 265; 128 dimensions, 128 rows 520, 609,
+    // 160 rows 626, 673, 192 rows 794, 701; 256 dimensions, 32 rows 81, 84, 64
+    // rows 162, 84.
+    y.rows = most > (D == 64 ? 240u : D == 128 ? 160u : 32u);
+    // 16 rows a tile or 32: 16 rows 79, 85; 32 rows 100, 89; 64 rows 177, 131
+    y.NT = most <= 16 || D == 256 ? 1 : 2;
     y.tile_rows = y.rows ? (D == 256 ? 128u : 256u) : 16u * y.NT;
     y.unit_rows = (uint32_t)(most / 4 * 4 + 4);
     // ranges a head: what fills the card's 512 workgroup slots once, or where

@@ -275,3 +275,89 @@ def test_prompt_weights_both_ways(nk, sel, block):
         _say(check_attend(c, t, ctx, n_new, q, o, w))
         o2, w2 = cache.attend(sequences(nk, n_new, ctx, t), qd, weights=True)
         assert torch.equal(o, o2) and torch.equal(w, w2)
+
+
+@pytest.mark.parametrize("block", [16, 64, 512])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_prompt_nan_in_what_a_row_does_not_see(nk, sel, dim, block):
+    """As for few rows: a NaN key or value reaches the rows that see its token
+    and no others (360 rows a head)."""
+    ctx, n_new = [100], 90
+    c, table, q = case(nk, sel, 40, ctx, [n_new], 8, 2, dim, block, "bf16")
+    tok, kt = 100 - n_new // 2, 100 - n_new // 4
+    c.v[table[0, tok // block], 1, tok % block, 5] = 0xFF
+    c.k[table[0, kt // block], 0, kt % block, 9] = 0x7F
+    o, w = upload(nk, sel, c).attend(sequences(nk, [n_new], ctx, table), q.cuda(), weights=True)
+    sel.sync_errors()
+    check_attend(c, table, ctx, [n_new], q, o)
+    nan = torch.isnan(o.float())
+    first = tok - (100 - n_new)                            # the row whose own token it is
+    assert not nan[:first, 4:].any() and nan[first:, 4:, 5].all() and nan[:, 4:].sum() == (n_new - first) * 4
+    first = kt - (100 - n_new)
+    assert not nan[:first, :4].any() and nan[first:, :4].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("block", [16, 128])
+def test_prompt_large_scores_and_unequal_scales(nk, sel, block, dtype):
+    ctx, n_new = [400, 130], [80, 1]
+    c, table, q = case(nk, sel, 41, ctx, n_new, 8, 2, 128, block, dtype, qstd=60.0)
+    c.vs = c.vs * 2.0 ** c.rng.integers(-28, 28, c.vs.shape)
+    if dtype == "fp16":
+        c.vs = np.clip(c.vs, 2.0 ** -12, 2.0 ** 5)
+    o, w = upload(nk, sel, c).attend(sequences(nk, n_new, ctx, table), q.cuda(), weights=True)
+    sel.sync_errors()
+    _say(check_attend(c, table, ctx, n_new, q, o, w))
+
+
+@pytest.mark.parametrize("block", [16, 64])
+def test_prompt_rows_that_see_nothing(nk, sel, block):
+    ctx, n_new = [2, 0, 1], [70, 66, 1]
+    c, table, q = case(nk, sel, 42, ctx, n_new, 12, 2, 128, block, "bf16")
+    o, w = upload(nk, sel, c).attend(sequences(nk, n_new, ctx, table), q.cuda(), weights=True)
+    sel.sync_errors()
+    check_attend(c, table, ctx, n_new, q, o, w)
+    assert not o[:68].any() and not o[70:136].any()
+
+
+@pytest.mark.parametrize("block", [16, 64])
+def test_prompt_invalid_sequences(nk, sel, block):
+    ctx, n_new = [100, 200, 300], [80] * 3
+    c, table, q = case(nk, sel, 43, ctx, n_new, 12, 2, 64, block, "bf16")
+    cache, qd = upload(nk, sel, c), q.cuda()
+    good, gw = cache.attend(sequences(nk, n_new, ctx, table), qd, weights=True)
+    sel.sync_errors()
+    bad = table.copy()
+    bad[1, 1] = c.shape[0]
+    long = [100, table.shape[1] * block + 1, 300]
+    for lens, tab in ((ctx, bad), (long, table)):
+        o, w = cache.attend(sequences(nk, n_new, lens, tab), qd, weights=True)
+        with pytest.raises(nk.NetKVError, match="block cache"):
+            sel.sync_errors()
+        assert torch.isnan(o[80:160]).all() and torch.equal(o[:80], good[:80]) and torch.equal(o[160:], good[160:])
+        assert torch.isnan(w[1, :2]).all() and torch.equal(w[[0, 2]], gw[[0, 2]])
+
+
+@pytest.mark.parametrize("dim,rows", [(64, 240), (64, 241), (128, 160), (128, 161), (256, 32), (256, 33)])
+def test_rows_at_the_forms_border(nk, sel, dim, rows):
+    """The most rows that the form for few takes, and one more."""
+    ctx, n_new = [rows + 150, 40, 700], [rows, 3, 1]
+    c, table, q = case(nk, sel, 44, ctx, n_new, 2, 2, dim, 64, "fp16")
+    o, w = upload(nk, sel, c).attend(sequences(nk, n_new, ctx, table), q.cuda(), weights=True)
+    sel.sync_errors()
+    _say(check_attend(c, table, ctx, n_new, q, o, w))
+
+
+@pytest.mark.parametrize("dim,block,heads,hk,ctx,n_new", [
+    (128, 64, 16, 1, [66, 130], [4, 4]), (64, 16, 24, 2, [70, 65], [5, 3]), (128, 512, 16, 2, [700, 515], [64, 40]),
+    (256, 64, 8, 2, [129, 66], [4, 8]), (64, 16, 8, 2, [400, 100], [90, 66])])
+def test_weights_do_not_read_what_was_not_written(nk, sel, dim, block, heads, hk, ctx, n_new):
+    """A workspace full of large numbers: row tiles that end at different
+    steps give the weights of the tokens they see."""
+    c, table, q = case(nk, sel, 45, ctx, n_new, heads, hk, dim, block, "bf16")
+    cache, seqs, qd = upload(nk, sel, c), sequences(nk, n_new, ctx, table), q.cuda()
+    work = torch.full((nk.netkv_kv_attend_workspace(sel.h, cache.c, seqs, heads, True),), 0x7E, dtype=torch.uint8, device="cuda")
+    o, w = torch.empty_like(qd), torch.empty(table.shape, dtype=torch.float32, device="cuda")
+    nk.netkv_kv_attend(sel.h, cache.c, seqs, qd, dim ** -0.5, o, w, work, sel.device)
+    sel.sync_errors()
+    _say(check_attend(c, table, ctx, n_new, q, o, w))
