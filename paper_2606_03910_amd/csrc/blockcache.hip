@@ -528,7 +528,13 @@ struct ValRegs {
 // when 16 weights' sum passes 2^10, which keeps them in fp16's range.
 //
 // The four wavefronts take the same rows and every fourth step each, joined
-// through LDS.
+// through LDS.  Long calls are bound by the cache's bytes: 8 sequences of
+// 131,071 tokens and 8 heads of 128 dimensions (2.15 GB) take 358 us, 6.0 TB/s,
+// 64 of up to 16,384 with block weights (0.61 GB) 132 us, 4.6 TB/s.  Short ones
+// by latency: one of 700 tokens takes 10 us, three of its 11 steps one after the
+// other.  A step's loads go out as the registers of the one before come free,
+// two workgroups a CU.  A static partition into equal pieces of all steps, which
+// needs no ranges of its own, took 166 us where these take 150.
 template <int D, int NT, bool HALF, bool UNITS, bool SMALL>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
@@ -885,6 +891,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
 //
 // SMALL: blocks of less than 64 tokens, so a step's four groups of 16 tokens
 // may be in different pages; else pages, scales and addresses are scalar.
+//
+// Bound by the matrix units and the vector units beside them: two chunks of
+// 1,024 rows of 64 heads after 31,744 tokens (128 dimensions, 2.16 TFLOP) take
+// 1,990 us, 1.09 PFLOP/s, where a product of 8,192 x 8,192 matrices reaches
+// 1.17.  An ordinary step of 256 rows takes 1.9 us, the first and the masked
+// ones 5, finding the tile, its first loads and its output 9: six prompts of up
+// to 2,777 tokens (0.31 TFLOP, 17 steps a tile) take 520 us.
 //
 // SUMS: every row's sum over each block is kept for the blocks' weights (a
 // block is whole steps then, and ranges are whole blocks).
@@ -1376,7 +1389,8 @@ __device__ inline void join_row(const AttendArgs &a, const Join &j, uint32_t h, 
 }
 
 // A workgroup a row as long as there are no more rows than workgroups, else a
-// wavefront a row.
+// wavefront a row: latency, 5 us for the 8 rows of one sequence, 10 us for the
+// 512 of 64 sequences.
 template <int D, bool HALF>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, uint32_t rows) {
     __shared__ f32x4 lo[kThreads];
@@ -1412,7 +1426,8 @@ struct WeightArgs {
 
 // Block weights of a call of few rows: a wavefront a block, lanes over (head,
 // row); every unit's sum was kept as its log2, so
-// w = sum over rows and units of 2^(unit - lse).
+// w = sum over rows and units of 2^(unit - lse).  64 sequences of up to 32
+// blocks, 64 heads: 6 us.
 __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs wa) {
     const uint32_t s = blockIdx.y, b = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (b >= a.kv.max_pages) return;
@@ -1436,7 +1451,9 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
 }
 
 // Block weights of a call of many rows that kept its rows' sums: a workgroup
-// a block and head adds 2^(sum - lse) over the rows that see it.
+// a block and head adds 2^(sum - lse) over the rows that see it: 15 us for
+// 131,072 rows and 64 blocks (34 MB).  prompt_kernel takes 3 to 14 % longer
+// for it with blocks of 512 and 64 tokens, the second pass 54 %.
 __global__ __launch_bounds__(kThreads) void row_kernel(AttendArgs a, WeightArgs wa) {
     __shared__ float red[kWaves];
     const uint32_t b = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
@@ -1461,7 +1478,8 @@ __global__ __launch_bounds__(kThreads) void row_kernel(AttendArgs a, WeightArgs 
 // prompt's partial sums of every row would be larger than its cache).  Rows
 // come 64 at a time, 16 by each wavefront, through LDS: read by each wavefront
 // for itself, every CU of a head's XCD asked its cache for the same lines
-// (1,880 us for prompt-chunk).
+// (two chunks of 1,024 rows of 64 heads and 32,768 tokens, 1.08 TFLOP: 1,030 us
+// against 1,880).
 template <int D, bool HALF>
 __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void column_kernel(AttendArgs a, WeightArgs wa) {
     typedef typename Elem<HALF>::T T;
@@ -1570,7 +1588,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void column_kernel(Atte
     if (c == 0 && ((16 * g) & (tile - 1)) == 0 && u < a.n_units) wa.cols[((uint64_t)s * hk + h) * a.n_units + u] = x;
 }
 
-// The units of a block and the heads, in order.
+// The units of a block and the heads, in order: 4 us, a launch's latency.
 __global__ __launch_bounds__(kThreads) void block_kernel(AttendArgs a, WeightArgs wa) {
     const uint32_t s = blockIdx.y, b = blockIdx.x * kThreads + threadIdx.x;
     if (b >= a.kv.max_pages) return;
@@ -1585,7 +1603,8 @@ __global__ __launch_bounds__(kThreads) void block_kernel(AttendArgs a, WeightArg
 }
 
 // A page's weight is the sum over the sequences that hold it, in fixed point
-// (2^-24 of one row's whole attention) so that their order does not matter.
+// (2^-24 of one row's whole attention) so that their order does not matter.  64
+// sequences of 1,024 blocks: 4 us.
 __global__ __launch_bounds__(kThreads) void weigh_kernel(Kv a, const float *w, unsigned long long *page_weight) {
     const uint32_t s = blockIdx.y, b = blockIdx.x * kThreads + threadIdx.x;
     const uint32_t held = a.ctx[s];
@@ -1725,7 +1744,9 @@ __device__ inline void turn4(uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d)
 // (exact but for values that become subnormal).  What fits the workgroup's
 // registers is read once, for the largest value and for the quantisation.
 // Values are turned through LDS: written byte by byte from the rows they came
-// in, a 512-token block took three times as long.
+// in, a 512-token block took three times as long.  Bound by memory: 16 prompts
+// of up to 16,384 tokens, 8 heads of 128 dimensions (537 MB in, 269 MB out)
+// take 226 us, 3.6 TB/s; 64 single tokens 8 us, latency.
 template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel(MoveArgs a, bool half) {
     constexpr int kEach = 8;                                  // 16-byte pieces a thread keeps
@@ -1901,7 +1922,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel
 }
 
 // One workgroup gives back up to 64 tokens (one tile of positions) of one
-// head: keys in rows as they lie, values turned through LDS.
+// head: keys in rows as they lie, values turned through LDS.  Bound by memory:
+// the same prompts (269 MB in, 537 MB out) take 170 us, 4.7 TB/s.
 template <int D>
 __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
     constexpr uint32_t kPitch = D / 4 + 1;
@@ -2264,7 +2286,9 @@ namespace {
 template <int D>
 void launch_store(const MoveArgs &a, bool half, uint32_t tasks, uint32_t rows, hipStream_t s) {
     const dim3 grid(tasks, a.kv.hk, 2);
-    // one pass over the data where the workgroup's registers hold a block's rows
+    // one pass over the data where the workgroup's registers hold a block's rows.
+    // 256 threads against 1,024, us: 64 times 64 rows of 128 dimensions 13, 27;
+    // single rows 9, 20; prompts in 512-token blocks 267, 226.
     if (rows * (uint32_t)D <= 256 * 64)
         store_kernel<D, 256><<<grid, 256, 0, s>>>(a, half);
     else
