@@ -1418,6 +1418,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, uint32_t r
 
 // ------------------------------------------------------------------ block weights
 
+// Weights are sums of many equal shares, so they are added in 64 bits (fp32
+// one after the other loses 2^-24 of the sum each time: 2e-6 after 14,000 rows).
 struct WeightArgs {
     float *w;            // [seq][max_pages]
     float *cols;         // [seq][head][unit], or null
@@ -1435,7 +1437,7 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
     const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep), per = bt / tile;
     const uint32_t have = (hd.ctx + tile - 1) / tile;   // units that hold tokens
     const uint32_t u0 = b * per, u1 = min(u0 + per, have);
-    float sum = 0.0f;
+    double sum = 0.0;
     if (u0 < u1)
         for (uint32_t i = lane; i < hd.n * a.Hq; i += 64) {
             const uint32_t h = i / (hd.n * a.G), row = i % (hd.n * a.G);
@@ -1447,7 +1449,7 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
             for (uint32_t u = u0; u < end; ++u, p += a.unit_rows) sum += exp2_of(*p - lse);
         }
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
-    if (lane == 0) wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? sum : NAN;
+    if (lane == 0) wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? (float)sum : NAN;
 }
 
 // Block weights of a call of many rows that kept its rows' sums: a workgroup
@@ -1455,7 +1457,7 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
 // 131,072 rows and 64 blocks (34 MB).  prompt_kernel takes 3 to 14 % longer
 // for it with blocks of 512 and 64 tokens, the second pass 54 %.
 __global__ __launch_bounds__(kThreads) void row_kernel(AttendArgs a, WeightArgs wa) {
-    __shared__ float red[kWaves];
+    __shared__ double red[kWaves];
     const uint32_t b = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
     const Head hd = seq_head(a.kv, s);
     const uint64_t from = (uint64_t)b << a.kv.btl;
@@ -1463,13 +1465,13 @@ __global__ __launch_bounds__(kThreads) void row_kernel(AttendArgs a, WeightArgs 
     // rows before the block's first token do not see it (and kept nothing)
     const int64_t first = (int64_t)from - ((int64_t)hd.ctx - hd.n);
     const float *p = a.sums + ((uint64_t)h * a.kv.max_pages + b) * a.sum_rows + hd.row0 * a.G;
-    float sum = 0.0f;
+    double sum = 0.0;
     for (uint32_t r = (first > 0 ? (uint32_t)first * a.G : 0u) + threadIdx.x; r < hd.n * a.G; r += kThreads)
         sum += exp2_of(p[r] - a.lse[(hd.row0 + r / a.G) * a.Hq + h * a.G + r % a.G]);
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) wa.cols[((uint64_t)s * a.kv.hk + h) * a.n_units + b] = (red[0] + red[1]) + (red[2] + red[3]);
+    if (threadIdx.x == 0) wa.cols[((uint64_t)s * a.kv.hk + h) * a.n_units + b] = (float)((red[0] + red[1]) + (red[2] + red[3]));
 }
 
 // The same without such sums: with every row's lse known, the
@@ -1519,7 +1521,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void column_kernel(Atte
     const uint32_t first = (int64_t)kt0 * kStep > old ? (uint32_t)((int64_t)kt0 * kStep - old) * a.G / 16 * 16 : 0u;
     const int64_t need = (int64_t)kt * kStep + kStep - 1 - old;
     const uint64_t full = (uint64_t)kt * kStep + kStep > hd.ctx ? ~0ull : need > 0 ? (uint64_t)need * a.G : 0ull;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    double total = 0.0;
     T8 qf[D / 32];
     float lse = 0.0f;
     int seen = 0;
@@ -1549,6 +1551,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void column_kernel(Atte
     int b = 0;
     for (uint32_t r0 = first; r0 < n_rows; r0 += 16 * kWaves, b ^= 1) {
         if (r0 + 16 * kWaves < n_rows) fetch(r0 + 16 * kWaves);
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) {
             f32x4 st[4] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -1575,17 +1578,18 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void column_kernel(Atte
                     }
             }
         }
+        total += (double)((sum[0] + sum[1]) + (sum[2] + sum[3]));
         if (r0 + 16 * kWaves < n_rows) stage(b ^ 1);
         __syncthreads();
     }
     // over the rows (16 lanes), then the units' groups of 16 tokens
     const uint32_t tile = min(bt, kStep);
-    float x = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    double x = total;
     for (int d = 1; d < 16; d <<= 1) x += __shfl_xor(x, d, 64);
-    if (tile >= 32) x = pair16_sum(x);
+    if (tile >= 32) x += __shfl_xor(x, 16, 64);
     if (tile >= 64) x += __shfl_xor(x, 32, 64);
     const uint32_t u = kt * (kStep / tile) + 16 * g / tile;
-    if (c == 0 && ((16 * g) & (tile - 1)) == 0 && u < a.n_units) wa.cols[((uint64_t)s * hk + h) * a.n_units + u] = x;
+    if (c == 0 && ((16 * g) & (tile - 1)) == 0 && u < a.n_units) wa.cols[((uint64_t)s * hk + h) * a.n_units + u] = (float)x;
 }
 
 // The units of a block and the heads, in order: 4 us, a launch's latency.
@@ -1595,11 +1599,11 @@ __global__ __launch_bounds__(kThreads) void block_kernel(AttendArgs a, WeightArg
     const Head hd = seq_head(a.kv, s);
     const uint32_t per = (1u << a.kv.btl) / wa.tile, have = (hd.ctx + wa.tile - 1) / wa.tile;
     const uint32_t u0 = b * per, u1 = min(u0 + per, have);
-    float sum = 0.0f;
+    double sum = 0.0;
     if (hd.n)
         for (uint32_t h = 0; h < a.kv.hk; ++h)
             for (uint32_t u = u0; u < u1; ++u) sum += wa.cols[((uint64_t)s * a.kv.hk + h) * a.n_units + u];
-    wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? sum : NAN;
+    wa.w[(uint64_t)s * a.kv.max_pages + b] = hd.ok ? (float)sum : NAN;
 }
 
 // A page's weight is the sum over the sequences that hold it, in fixed point
