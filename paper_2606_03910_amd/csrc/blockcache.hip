@@ -899,8 +899,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
 // ones 5, finding the tile, its first loads and its output 9: six prompts of up
 // to 2,777 tokens (0.31 TFLOP, 17 steps a tile) take 520 us.
 //
-// SUMS: every row's sum over each block is kept for the blocks' weights (a
-// block is whole steps then, and ranges are whole blocks).
+// SUMS: every row's sum over each block is kept for the blocks' weights (ranges
+// are whole blocks).
 template <int D, int NT, bool HALF, bool SMALL, bool SUMS>
 __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
@@ -1191,15 +1191,18 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
         }
     };
 
-    const uint32_t per = SUMS ? bt / kStep : 1u;
+    // a lane has the sum of its own 16 tokens
+    const uint32_t per = SMALL ? 1u : bt / kStep;
     auto keep_sums = [&](uint32_t kt) {
         if constexpr (SUMS) {
             if (((kt + 1) & (per - 1)) != 0 && kt + 1 < it.k1) return;
-            float *to = a.sums + ((uint64_t)h * a.kv.max_pages + ((kt * kStep) >> a.kv.btl)) * a.sum_rows + hd.row0 * a.G + row0 + c;
+            const uint32_t block = (kt * kStep + (SMALL ? 16 * g : 0u)) >> a.kv.btl;
+            const bool keeps = SMALL ? ((16 * g) & (bt - 1)) == 0 && block < a.kv.max_pages : g == 0;
+            float *to = a.sums + ((uint64_t)h * a.kv.max_pages + block) * a.sum_rows + hd.row0 * a.G + row0 + c;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const float sum = row_sum(lb[n]);
-                if (g == 0 && row0 + n * 16 + c < n_rows) to[n * 16] = m[n] + log2_of(sum);
+                const float sum = !SMALL ? row_sum(lb[n]) : bt == 32 ? pair16_sum(lb[n]) : lb[n];
+                if (keeps && row0 + n * 16 + c < n_rows) to[n * 16] = m[n] + log2_of(sum);
                 lb[n] = 0.0f;
             }
         }
@@ -1454,8 +1457,8 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
 
 // Block weights of a call of many rows that kept its rows' sums: a workgroup
 // a block and head adds 2^(sum - lse) over the rows that see it: 15 us for
-// 131,072 rows and 64 blocks (34 MB).  prompt_kernel takes 3 to 14 % longer
-// for it with blocks of 512 and 64 tokens, the second pass 54 %.
+// 131,072 rows and 64 blocks (34 MB).  prompt_kernel takes 3 % longer for it
+// with blocks of 512 tokens and 9 to 14 % with smaller ones.
 __global__ __launch_bounds__(kThreads) void row_kernel(AttendArgs a, WeightArgs wa) {
     __shared__ double red[kWaves];
     const uint32_t b = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
@@ -2105,11 +2108,13 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     y.joins = take(sizeof(Join) * y.join_cap);
     y.ml = take(16ull * y.slot_cap * a.hk * y.tile_rows);
     y.part = take(4ull * y.slot_cap * a.hk * y.tile_rows * D);
-    // A prompt's weights come from every row's sum over each block where a
-    // block is whole steps and a row has at most 256 of them (1 KB; a row's
-    // query and output are 512 bytes at 128 dimensions), else from a second
-    // pass over the keys.
-    y.sums = weights && y.rows && bt >= kStep && a.max_pages <= 256;
+    // A prompt's weights come from every row's sum over each block where a row
+    // has at most 256 of them (1 KB; a row's query and output are 512 bytes at
+    // 128 dimensions), else from a second pass over the keys, which takes
+    // longer but no memory: two chunks of 1,024 rows of 64 heads in 8,192 tokens
+    // of 32-token blocks 704 us against 921, in 16,384 of 64-token blocks 1,320
+    // against 1,750.
+    y.sums = weights && y.rows && a.max_pages <= 256;
     if (y.sums) y.n_units = a.max_pages;
     y.lse = y.units = y.cols = y.sums_at = 0;
     if (weights) {
@@ -2132,12 +2137,12 @@ void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, h
     a.kv.btl < 6 ? attend_kernel<D, NT, HALF, UNITS, true><<<grid, kThreads, 0, s>>>(a)     \
                  : attend_kernel<D, NT, HALF, UNITS, false><<<grid, kThreads, 0, s>>>(a)
     if (y.rows) {
-        if (a.kv.btl < 6)
-            prompt_kernel<D, D == 256 ? 1 : 2, HALF, true, false><<<grid, kPromptThreads, 0, s>>>(a);
-        else if (y.sums)
-            prompt_kernel<D, D == 256 ? 1 : 2, HALF, false, true><<<grid, kPromptThreads, 0, s>>>(a);
+        if (y.sums)
+            a.kv.btl < 6 ? prompt_kernel<D, D == 256 ? 1 : 2, HALF, true, true><<<grid, kPromptThreads, 0, s>>>(a)
+                         : prompt_kernel<D, D == 256 ? 1 : 2, HALF, false, true><<<grid, kPromptThreads, 0, s>>>(a);
         else
-            prompt_kernel<D, D == 256 ? 1 : 2, HALF, false, false><<<grid, kPromptThreads, 0, s>>>(a);
+            a.kv.btl < 6 ? prompt_kernel<D, D == 256 ? 1 : 2, HALF, true, false><<<grid, kPromptThreads, 0, s>>>(a)
+                         : prompt_kernel<D, D == 256 ? 1 : 2, HALF, false, false><<<grid, kPromptThreads, 0, s>>>(a);
     } else if (D == 256 || y.NT == 1) {
         if (wa.w) NETKV_ATTEND(1, true);
         else NETKV_ATTEND(1, false);

@@ -361,3 +361,21 @@ def test_weights_do_not_read_what_was_not_written(nk, sel, dim, block, heads, hk
     nk.netkv_kv_attend(sel.h, cache.c, seqs, qd, dim ** -0.5, o, w, work, sel.device)
     sel.sync_errors()
     _say(check_attend(c, table, ctx, n_new, q, o, w))
+
+
+@pytest.mark.parametrize("block,dim", [(16, 128), (32, 128), (16, 256), (32, 64)])
+def test_prompt_weights_of_small_blocks_both_ways(nk, sel, block, dim):
+    """Blocks of less than a step: the last ones of a table, groups past the
+    last token, two sequences and a split one."""
+    ctx, n_new = [256 * block, 600, 3, 64, 129 + block], [400, 600, 70, 64, 100]
+    c, table, q = case(nk, sel, 46, ctx, n_new, 4, 2, dim, block, "bf16")
+    cache, qd = upload(nk, sel, c), q.cuda()
+    wide = np.concatenate([table, np.full((5, 3), 1 << 30)], 1)       # never read
+    for t in (table, wide):
+        seqs = sequences(nk, n_new, ctx, t)
+        work = torch.full((nk.netkv_kv_attend_workspace(sel.h, cache.c, seqs, 4, True),), 0x7E, dtype=torch.uint8, device="cuda")
+        o, w = torch.empty_like(qd), torch.empty(t.shape, dtype=torch.float32, device="cuda")
+        nk.netkv_kv_attend(sel.h, cache.c, seqs, qd, dim ** -0.5, o, w, work, sel.device)
+        sel.sync_errors()
+        _say(check_attend(c, t, ctx, n_new, q, o, w))
+        assert torch.equal(o, cache.attend(seqs, qd))
