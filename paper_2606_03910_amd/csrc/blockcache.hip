@@ -2059,7 +2059,7 @@ struct Layout {
     int NT;
     bool rows;             // prompt_kernel
     bool sums;             // and its rows' sums over the blocks
-    uint32_t G, tile_rows, target, fine, item_cap, slot_cap, join_cap, n_units, unit_rows;
+    uint32_t G, tile_rows, target, fine, least, item_cap, slot_cap, join_cap, n_units, unit_rows;
     uint64_t head, items, joins, ml, part, lse, units, cols, sums_at, total;
 };
 
@@ -2088,11 +2088,14 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     y.target = (512u + a.hk - 1) / a.hk;
     y.fine = y.rows || y.NT == 2 || D == 256 ? y.target : (1024u + a.hk - 1) / a.hk;
     const uint64_t tiles = a.n_tok * y.G / y.tile_rows + a.n_seq;
-    const uint64_t items = 2ull * y.fine + tiles;
+    // at most so many ranges a tile, none shorter than `least` steps
+    y.least = y.rows ? 8 : kWaves;
+    const uint64_t steps = (((uint64_t)a.max_pages << a.btl) + kStep - 1) / kStep, parts = (steps + y.least - 1) / y.least;
+    const uint64_t items = 2ull * y.fine + tiles < tiles * parts ? 2ull * y.fine + tiles : tiles * parts;
     if (items * a.hk > (1ull << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
     y.item_cap = (uint32_t)items;
-    y.slot_cap = 2 * y.fine;
-    y.join_cap = y.fine;
+    y.slot_cap = items < 2 * y.fine ? (uint32_t)items : 2 * y.fine;
+    y.join_cap = tiles < y.fine ? (uint32_t)tiles : y.fine;
     const uint32_t bt = 1u << a.btl;
     y.n_units = (uint32_t)(((uint64_t)a.max_pages << a.btl) / (bt < kStep ? bt : kStep)) + (uint32_t)(kStep / 16);
     if (weights && (((uint64_t)a.max_pages << a.btl) / kStep + 1) * a.hk > (1ull << 24))
@@ -2225,7 +2228,7 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     t.tile_rows = y.tile_rows;
     t.target = y.target;
     t.fine = y.fine;
-    t.least = y.rows ? 8 : kWaves;
+    t.least = y.least;
     // whole blocks for a prompt (its sums), with and without weights the same
     t.round = !y.rows ? kWaves : kv->block_tokens > kStep ? kv->block_tokens / kStep : 1;
     t.item_cap = y.item_cap;
