@@ -180,6 +180,9 @@ def _check(h, st: int):
 
 
 def _stream(dev) -> int:
+    # its address without the Stream object around it, which takes 3 us a call
+    if isinstance(dev, torch.device) and dev.index is not None and torch.cuda.is_initialized():
+        return torch._C._cuda_getCurrentRawStream(dev.index)
     return torch.cuda.current_stream(dev).cuda_stream
 
 
@@ -429,14 +432,15 @@ def _rows(t: torch.Tensor, n_tok: int, heads: int, dim: int, device, name: str):
     if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPE or not t.is_cuda:
         raise TypeError(f"{name} must be a bfloat16 or float16 CUDA tensor")
     _on(t, device, name)
-    if t.dim() != 3 or t.shape[0] < n_tok or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"{name} must be [{n_tok}][{heads}][{dim}], not {list(t.shape)}")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+    shape, strides, at = t.shape, t.stride(), t.data_ptr()
+    if len(shape) != 3 or shape[0] < n_tok or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"{name} must be [{n_tok}][{heads}][{dim}], not {list(shape)}")
+    if strides[2] != 1 or (heads > 1 and strides[1] != dim):
         raise ValueError(f"{name} must be dense within a token")
-    stride = t.stride(0) if t.shape[0] > 1 else heads * dim
-    if t.data_ptr() % 16 or stride % 8 or stride < heads * dim:
+    stride = strides[0] if shape[0] > 1 else heads * dim
+    if at % 16 or stride % 8 or stride < heads * dim:
         raise ValueError(f"{name} must be 16-byte aligned with a token stride of a multiple of 8 elements")
-    return t.data_ptr(), stride
+    return at, stride
 
 
 def _on_all(device, **tensors) -> None:
