@@ -531,8 +531,7 @@ struct ValRegs {
 // through LDS.  Long calls are bound by the cache's bytes: 8 sequences of
 // 131,071 tokens and 8 heads of 128 dimensions (2.15 GB) take 358 us, 6.0 TB/s,
 // 64 of up to 16,384 with block weights (0.61 GB) 132 us, 4.6 TB/s.  Short ones
-// by latency: one of 700 tokens takes 10 us, three of its 11 steps one after the
-// other.  A step's loads go out as the registers of the one before come free,
+// by latency: one of 700 tokens takes 8 us, a wavefront one step of its 11.  A step's loads go out as the registers of the one before come free,
 // two workgroups a CU.  A static partition into equal pieces of all steps, which
 // needs no ranges of its own, took 166 us where these take 150.
 template <int D, int NT, bool HALF, bool UNITS, bool SMALL>

@@ -582,7 +582,7 @@ __global__ __launch_bounds__(kThreads) void count_kernel(EvictArgs a) {
 }
 
 // 101 MB of bins in 35 us, and the few weights of one bin.
-__global__ __launch_bounds__(kThreads) void gather_kernel(EvictArgs a) {
+__global__ __launch_bounds__(kThreads, 6) void gather_kernel(EvictArgs a) {
     __shared__ uint32_t found[3];
     if (blockIdx.x >= a.counts[0]) return;
     const uint32_t at = find_long(a, blockIdx.x);
@@ -631,14 +631,35 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictArgs a) {
         }
         const uint32_t all = __shfl(to, 63, 64);
         to += in - mine;
-        in += all;
-        for (is = bin < 32 ? 0u : is; is; is &= is - 1) {
-            const uint32_t q = __builtin_ctz(is), i = i0 + 512 * (q / 8) + q % 8;
-            const uint64_t k = key_of(a, n, keep, i, wt[i]);
-            cand[to++] = k;
-            every &= k;
-            some |= k;
+        if (bin < 32) {
+            // such a bin holds one weight: none is looked at
+        } else if (all <= 512) {
+            for (; is; is &= is - 1) {
+                const uint32_t q = __builtin_ctz(is), i = i0 + 512 * (q / 8) + q % 8;
+                const uint64_t k = key_of(a, n, keep, i, wt[i]);
+                cand[to++] = k;
+                every &= k;
+                some |= k;
+            }
+        } else {
+            // a lane's entries are lines apart: where every fourth is of the bin the
+            // lanes take them side by side (768 segments of 65,536 weights within 3 %
+            // of each other 233 us against 328, within 0.3 % 219 against 658)
+            uint32_t next = in;
+            for (uint32_t q = 0; q < 8 * kGather; ++q) {
+                const uint32_t i = i0 - 8 * lane + 64 * q + lane;
+                const bool own = i < end && bins[i] == bin;
+                const uint64_t m = __ballot(own);
+                if (own) {
+                    const uint64_t k = key_of(a, n, keep, i, wt[i]);
+                    cand[next + __popcll(m & ((1ull << lane) - 1))] = k;
+                    every &= k;
+                    some |= k;
+                }
+                next += __popcll(m);
+            }
         }
+        in += all;
     }
     for (int d = 32; d; d >>= 1) {
         above += __shfl_xor(above, d, 64);
@@ -647,7 +668,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(EvictArgs a) {
     }
     if (lane == 0) {
         a.parts[(uint64_t)blockIdx.x * kWaves + w] = make_uint2(above, in);
-        if (bin < 32 && in) every = some = bin;   // such a bin holds one weight: none is looked at
+        if (bin < 32 && in) every = some = bin;
         a.bits[(uint64_t)blockIdx.x * kWaves + w] = make_ulonglong2(every, some);
     }
     if (threadIdx.x == 0 && blockIdx.x == l.chunk0) {
