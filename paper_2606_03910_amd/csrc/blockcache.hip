@@ -1391,23 +1391,23 @@ __device__ inline void join_row(const AttendArgs &a, const Join &j, uint32_t h, 
 }
 
 // A workgroup a row as long as there are no more rows than workgroups, else a
-// wavefront a row: latency, 5 us for the 8 rows of one sequence, 10 us for the
-// 512 of 64 sequences.
+// wavefront a row: latency, 5 us for the 64 rows of one sequence's heads, 9 us
+// for the 4,096 of 64 sequences.
 template <int D, bool HALF>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, uint32_t rows) {
     __shared__ f32x4 lo[kThreads];
     __shared__ float factor[kThreads], red[3][kWaves];
     const uint32_t hk = a.kv.hk, w = threadIdx.x >> 6;
-    auto all = [&](uint64_t n_joins, auto join) {
-        const uint64_t n = n_joins * hk * rows;
-        auto row = [&](uint64_t task, auto waves, uint32_t at) {
-            join_row<D, HALF, decltype(waves)::value>(a, join((uint32_t)(task / rows / hk)), (uint32_t)(task / rows % hk), (uint32_t)(task % rows),
-                                                      lo + at, factor + at, red);
+    auto all = [&](uint32_t n_joins, auto join) {
+        const uint32_t n = n_joins * hk * rows;   // at most 2,048 joins and heads, 256 rows
+        auto row = [&](uint32_t task, auto waves, uint32_t at) {
+            const uint32_t jh = task / rows;
+            join_row<D, HALF, decltype(waves)::value>(a, join(jh / hk), jh % hk, task % rows, lo + at, factor + at, red);
         };
         if (n <= gridDim.x) {
             if (blockIdx.x < n) row(blockIdx.x, std::integral_constant<int, kWaves>(), 0);
         } else {
-            for (uint64_t task = blockIdx.x * kWaves + w; task < n; task += gridDim.x * kWaves) row(task, std::integral_constant<int, 1>(), 64 * w);
+            for (uint32_t task = blockIdx.x * kWaves + w; task < n; task += gridDim.x * kWaves) row(task, std::integral_constant<int, 1>(), 64 * w);
         }
     };
     if (a.joins) {
@@ -2087,13 +2087,14 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     y.target = (512u + a.hk - 1) / a.hk;
     y.fine = y.rows || y.NT == 2 || D == 256 ? y.target : (1024u + a.hk - 1) / a.hk;
     const uint64_t tiles = a.n_tok * y.G / y.tile_rows + a.n_seq;
-    // at most so many ranges a tile, none shorter than `least` steps
+    // full ranges of the whole call and a last one a tile; no more a tile than
+    // there are of the shortest length
     y.least = y.rows ? 8 : kWaves;
     const uint64_t steps = (((uint64_t)a.max_pages << a.btl) + kStep - 1) / kStep, parts = (steps + y.least - 1) / y.least;
-    const uint64_t items = 2ull * y.fine + tiles < tiles * parts ? 2ull * y.fine + tiles : tiles * parts;
+    const uint64_t items = y.fine + tiles < tiles * parts ? y.fine + tiles : tiles * parts;
     if (items * a.hk > (1ull << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
     y.item_cap = (uint32_t)items;
-    y.slot_cap = items < 2 * y.fine ? (uint32_t)items : 2 * y.fine;
+    y.slot_cap = items < 2 * y.fine ? (uint32_t)items : 2 * y.fine;   // a split tile has a full one at least
     y.join_cap = tiles < y.fine ? (uint32_t)tiles : y.fine;
     const uint32_t bt = 1u << a.btl;
     y.n_units = (uint32_t)(((uint64_t)a.max_pages << a.btl) / (bt < kStep ? bt : kStep)) + (uint32_t)(kStep / 16);
@@ -2157,7 +2158,13 @@ void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, h
     const uint64_t steps_most = (((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep;
     const uint32_t rows = y.unit_rows < y.tile_rows ? y.unit_rows : y.tile_rows;   // that a tile can have
     const uint64_t joins_most = (uint64_t)y.join_cap * a.kv.hk * rows;
-    if (steps_most > a.least) join_kernel<D, HALF><<<(uint32_t)(joins_most < 2048 ? joins_most : 2048), kThreads, 0, s>>>(a, rows);
+    // a workgroup a row up to 512, else a wavefront a row, in at most 1,024
+    // workgroups: those without a row find that out first (2,048 against 855 for
+    // 37 sequences of 9 rows and 5 heads: 10.8 us, 6.3; against 1,024 for 200
+    // sequences of 32 rows and 8 heads: 11.6, 9.3)
+    const uint64_t quarter = (joins_most + 3) / 4;
+    const uint64_t join_groups = joins_most < 512 ? joins_most : quarter < 512 ? 512 : quarter < 1024 ? quarter : 1024;
+    if (steps_most > a.least) join_kernel<D, HALF><<<(uint32_t)join_groups, kThreads, 0, s>>>(a, rows);
     if (!wa.w) return;
     if (y.rows) {
         const uint32_t steps = (uint32_t)((((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep);
