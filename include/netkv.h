@@ -502,10 +502,11 @@ typedef struct {
  * sequences (shared prefixes).  Rows tok_off[s] .. tok_off[s+1] of a call's
  * token arrays are its last tokens, in order.  n_tok bounds tok_off, max_tok
  * one sequence's rows; both are host values, as large as needed or larger.
- * A sequence with offsets that decrease or pass n_tok, more than max_tok
- * rows, more tokens than max_pages pages hold, or a page >= n_pages among
- * those that a call reads is invalid and reported by netkv_sync_errors;
- * nothing outside the arrays is read or written for it. */
+ * A sequence with offsets that decrease or pass n_tok, a first row before the
+ * last one of an earlier sequence, more than max_tok rows, more tokens than
+ * max_pages pages hold, or a page >= n_pages among those that a call reads is
+ * invalid and reported by netkv_sync_errors; nothing outside the arrays is
+ * read or written for it, and the others are as without it. */
 typedef struct {
     uint32_t n_seq;                 /* <= 65535 */
     uint32_t max_pages;             /* >= 1, max_pages * block_tokens < 2^31 */
@@ -548,8 +549,8 @@ netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_
  * row that sees no token (c < n) is 0.  What a row does not see never reaches
  * it, be it NaN.  Products are exact and summed in fp32, the softmax is fp32,
  * and its weights are rounded to 11 bits before the product with the values.
- * Rows of invalid sequences become NaN; rows past the last sequence are left
- * as they were.
+ * Rows of invalid sequences become NaN (rows that an earlier sequence names as
+ * well are that one's); rows past the last sequence are left as they were.
  * block_weight (NULL: none; DEVICE f32[n_seq * max_pages], overwritten): the
  * sum over the sequence's rows and query heads of p over each block's
  * tokens, 0 past the last block; NaN for an invalid sequence.

@@ -24,10 +24,13 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "blockplan.h"
 #include "netkv.h"
 #include "netkv_internal.h"
 
 namespace {
+
+using namespace blockplan;
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -41,43 +44,36 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kWaves = 4;
 constexpr int kPromptThreads = 512;
-constexpr uint32_t kStep = 64;        // tokens a wavefront takes at a time
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMaxSum = 1024.0f;    // how large 16 weights' sum may become before a row's maximum is raised
 constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
 
-struct Kv {
-    uint8_t *k, *v;
-    float *ks, *vs;
-    uint32_t n_pages, hk, btl;        // 2^btl tokens a block
-    uint32_t n_seq, max_pages, max_tok;
-    const uint64_t *off;
-    const uint32_t *ctx, *pages;
-    uint64_t n_tok;
-    uint32_t *err;
-};
-
-struct Head {
-    uint64_t row0;       // first row of the token arrays
-    uint32_t n, ctx;     // rows, tokens held (rows included)
-    bool rows_ok, ok;
-};
-
-__device__ inline Head seq_head(const Kv &a, uint32_t s) {
-    const uint64_t b = a.off[s], e = a.off[s + 1];
-    Head h;
-    h.row0 = b;
-    h.ctx = a.ctx[s];
-    h.rows_ok = b <= e && e <= a.n_tok;
-    h.ok = h.rows_ok && e - b <= a.max_tok && (uint64_t)h.ctx <= ((uint64_t)a.max_pages << a.btl);
-    h.n = h.ok ? (uint32_t)(e - b) : 0u;
-    if (!h.ok) h.ctx = 0;
-    return h;
-}
-
 __device__ inline void report(const Kv &a) { atomicOr(a.err, kErrBlockBit); }
+
+// rows_before for every thread's sequence, from what each adds to it (rows_end,
+// 0 for none); `named` is that of the first thread's, and is moved on to the
+// one after the workgroup's last.
+__device__ inline uint32_t rows_before(uint32_t end, uint32_t &named, uint32_t *sh) {
+    const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x / 64;
+    uint32_t most = end;
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t v = __shfl_up(most, d, 64);
+        if ((int)lane >= d) most = max(most, v);
+    }
+    if (lane == 63) sh[w] = most;
+    __syncthreads();
+    uint32_t before = __shfl_up(most, 1, 64), all = named;
+    if (lane == 0) before = 0;
+    before = max(before, named);
+    for (uint32_t v = 0; v < waves; ++v) {
+        if (v < w) before = max(before, sh[v]);
+        all = max(all, sh[v]);
+    }
+    named = all;
+    __syncthreads();
+    return before;
+}
 
 // bytes of one head of one page
 __device__ inline uint64_t head_bytes(const Kv &a, int D) { return (uint64_t)D << a.btl; }
@@ -170,15 +166,12 @@ struct PlanHead {
 
 // How a call is split.  With up to kListed sequences every wavefront finds its
 // share by itself (Shares); beyond that plan_kernel writes the list.
-struct PlanArgs {
+struct PlanArgs : Split {
     Kv kv;
-    uint32_t G, tile_rows;
-    uint32_t target, fine;                         // ranges a head, with kEnough steps at most and with more
-    uint32_t least, round;                         // ranges of at least `least` steps, multiples of `round`
-    uint32_t item_cap, slot_cap, join_cap;
     PlanHead *head;
     Item *items;                                   // null: not listed
     Join *joins;
+    uint32_t *left_out;                            // [seq] 1: begins among rows of an earlier one; null: no weights
     // rows of sequences that cannot be answered
     uint16_t *bad_out;
     uint64_t out_stride;
@@ -223,22 +216,6 @@ __device__ inline uint32_t tile_end(const Head &h, uint32_t G, uint32_t tile, ui
     return seen <= 0 ? 0u : (uint32_t)((seen + kStep - 1) / kStep);
 }
 
-__device__ inline uint32_t tiles_of(const Head &h, const PlanArgs &a) {
-    return (uint32_t)(((uint64_t)h.n * a.G + a.tile_rows - 1) / a.tile_rows);
-}
-
-// Steps of a range: what spreads `work` steps over `target` ranges, or from
-// kEnough steps on, where beginning a range costs little, over `fine`.
-constexpr uint32_t kEnough = 40;
-__device__ inline uint32_t range_steps(const PlanArgs &a, unsigned long long work) {
-    unsigned long long len = (work + a.target - 1) / a.target;
-    const unsigned long long fine = (work + a.fine - 1) / a.fine;
-    if (len > kEnough) len = fine > kEnough ? fine : kEnough;
-    if (len < a.least) len = a.least;
-    len = (len + a.round - 1) / a.round * a.round;
-    return len > 0x7FFFFFFFull ? 0x7FFFFFFFu : (uint32_t)len;
-}
-
 // Range `part` of `p` of a row tile.
 __device__ inline Item item_of(const PlanArgs &a, uint32_t seq, const Head &h, uint32_t C, uint32_t p, uint32_t tile, uint32_t part, uint32_t slot0) {
     const uint32_t end = tile_end(h, a.G, tile, a.tile_rows);
@@ -251,19 +228,23 @@ __device__ inline Item item_of(const PlanArgs &a, uint32_t seq, const Head &h, u
     return it;
 }
 
-// The rows of sequences that cannot be answered, by one workgroup.
+// The rows of sequences that cannot be answered, by one workgroup; those that
+// an earlier sequence names as well are left to it.
 __device__ inline void fill_bad(const PlanArgs &a) {
     bool bad = false;
     for (uint32_t s = threadIdx.x; s < a.kv.n_seq; s += blockDim.x) bad |= !seq_head(a.kv, s).ok;
     if (!__syncthreads_or(bad)) return;
+    uint32_t before = 0;
     for (uint32_t s = 0; s < a.kv.n_seq; ++s) {
         const Head h = seq_head(a.kv, s);
-        if (h.ok) continue;
+        const uint64_t from = max(h.row0, (uint64_t)before);
+        before = max(before, rows_end(a.kv, s));
+        if (h.ok && from == h.row0) continue;
         if (threadIdx.x == 0) report(a.kv);
-        if (!h.rows_ok) continue;
-        const uint64_t rows = a.kv.off[s + 1] - h.row0;
+        if (!h.rows_ok || from >= a.kv.off[s + 1]) continue;
+        const uint64_t rows = a.kv.off[s + 1] - from;
         for (uint64_t i = threadIdx.x; i < rows * a.row_elems; i += blockDim.x)
-            a.bad_out[(h.row0 + i / a.row_elems) * a.out_stride + i % a.row_elems] = (uint16_t)a.nan16;
+            a.bad_out[(from + i / a.row_elems) * a.out_stride + i % a.row_elems] = (uint16_t)a.nan16;
     }
 }
 
@@ -274,12 +255,14 @@ struct Shares {
     uint32_t rt[4], kt[4], C, per;
     uint32_t fulls, lasts, slots, joins;      // inclusive sums up to this lane
     uint32_t own_fulls, own_lasts, own_slots, own_joins;
+    uint32_t left;                            // a bit for each of the lane's sequences that begin among rows of an earlier one
     bool bad;
 
     __device__ explicit Shares(const PlanArgs &a) {
         const uint32_t lane = threadIdx.x & 63;
         per = (a.kv.n_seq + 63) / 64;
-        unsigned long long work = 0;
+        bool rows_ok = true;
+        left = 0;
         bad = false;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
@@ -289,11 +272,15 @@ struct Shares {
             if (s < a.kv.n_seq) {
                 const Head h = seq_head(a.kv, s);
                 rt[j] = tiles_of(h, a);
-                kt[j] = (h.ctx + kStep - 1) / kStep;
-                work += (unsigned long long)rt[j] * kt[j];
+                kt[j] = steps_of(h);
                 bad |= !h.ok;
+                rows_ok &= h.rows_ok;
             }
         }
+        if (__any(!rows_ok)) leave_out(a);
+        unsigned long long work = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) work += (unsigned long long)rt[j] * kt[j];
         for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d, 64);
         C = range_steps(a, work);
         own_fulls = own_lasts = own_slots = own_joins = 0;
@@ -320,7 +307,31 @@ struct Shares {
             }
         }
     }
-    __device__ uint32_t parts(uint32_t j) const { return kt[j] > C ? (kt[j] + C - 1) / C : 1u; }
+    __device__ uint32_t parts(uint32_t j) const { return parts_of(kt[j], C); }
+
+    // Sequences that begin among rows of an earlier one.
+    __device__ void leave_out(const PlanArgs &a) {
+        const uint32_t lane = threadIdx.x & 63;
+        uint32_t end = 0;
+        for (uint32_t j = 0; j < per; ++j)
+            if (lane * per + j < a.kv.n_seq) end = max(end, rows_end(a.kv, lane * per + j));
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t v = __shfl_up(end, d, 64);
+            if ((int)lane >= d) end = max(end, v);
+        }
+        uint32_t before = __shfl_up(end, 1, 64);
+        if (lane == 0) before = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t s = lane * per + j;
+            if (j >= per || s >= a.kv.n_seq) continue;
+            if (a.kv.off[s] < before) {
+                rt[j] = kt[j] = 0;
+                left |= 1u << j;
+            }
+            before = max(before, rows_end(a.kv, s));
+        }
+    }
 
     // false: there are not so many
     __device__ bool item(const PlanArgs &a, uint32_t i, Item &it) const {
@@ -382,7 +393,14 @@ __device__ inline bool find_item(const PlanArgs &a, uint32_t i, Item &it, Head &
         it = a.items[i];
     } else {
         const Shares sh(a);
-        if (blockIdx.x == 0 && __any(sh.bad)) fill_bad(a);
+        if (blockIdx.x == 0) {
+            if (a.left_out)
+                for (uint32_t j = 0; j < sh.per; ++j) {
+                    const uint32_t s = (threadIdx.x & 63) * sh.per + j;
+                    if (s < a.kv.n_seq) a.left_out[s] = sh.left >> j & 1;
+                }
+            if (__any(sh.bad)) fill_bad(a);
+        }
         if (!sh.item(a, i, it)) return false;
     }
     auto one = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
@@ -400,26 +418,42 @@ __device__ inline bool find_item(const PlanArgs &a, uint32_t i, Item &it, Head &
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     __shared__ uint32_t wsum[kPlanThreads / 64][3];
     __shared__ uint32_t base[kPlanThreads + 1][3], geo[kPlanThreads][2];
+    __shared__ uint32_t ends[kPlanThreads / 64];
     __shared__ unsigned long long work;
     if (threadIdx.x == 0) work = 0;
-    __syncthreads();
+    bool rows_ok = true;
+    for (uint32_t s = threadIdx.x; s < a.kv.n_seq; s += kPlanThreads) rows_ok &= seq_head(a.kv, s).rows_ok;
+    const bool falls = __syncthreads_or(!rows_ok);
+    // this thread's sequence; without rows if it begins among an earlier one's
+    uint32_t named = 0;
+    bool early = false;
+    auto head_of = [&](uint32_t s) {
+        Head h{};
+        if (s < a.kv.n_seq) h = seq_head(a.kv, s);
+        if (falls) {
+            early = h.row0 < rows_before(s < a.kv.n_seq ? rows_end(a.kv, s) : 0u, named, ends);
+            if (early) h.n = h.ctx = 0;
+        }
+        return h;
+    };
     unsigned long long mine = 0;
-    for (uint32_t s = threadIdx.x; s < a.kv.n_seq; s += kPlanThreads) {
-        const Head h = seq_head(a.kv, s);
-        mine += (unsigned long long)tiles_of(h, a) * ((h.ctx + kStep - 1) / kStep);
+    for (uint32_t s0 = 0; s0 < a.kv.n_seq; s0 += kPlanThreads) {
+        const Head h = head_of(s0 + threadIdx.x);
+        mine += (unsigned long long)tiles_of(h, a) * steps_of(h);
     }
     atomicAdd(&work, mine);
     __syncthreads();
     const uint32_t C = range_steps(a, work);
     uint32_t at[3] = {0, 0, 0};   // items, slots, joins so far
+    named = 0;
     for (uint32_t s0 = 0; s0 < a.kv.n_seq; s0 += kPlanThreads) {
         const uint32_t s = s0 + threadIdx.x;
         uint32_t x[3] = {0, 0, 0}, rt = 0, sp = 1;
+        const Head h = head_of(s);
         if (s < a.kv.n_seq) {
-            const Head h = seq_head(a.kv, s);
+            if (a.left_out) a.left_out[s] = early;
             rt = tiles_of(h, a);
-            const uint32_t kt = (h.ctx + kStep - 1) / kStep;
-            sp = kt > C ? (kt + C - 1) / C : 1u;
+            sp = parts_of(steps_of(h), C);
             x[0] = rt * sp;
             x[1] = sp > 1 ? x[0] : 0u;
             x[2] = sp > 1 ? rt : 0u;
@@ -439,17 +473,13 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
             }
             const uint32_t j = i - base[lo][0], n = geo[lo][0], p = geo[lo][1];
             const Item it = item_of(a, s0 + lo, seq_head(a.kv, s0 + lo), C, p, n - 1 - j / p, j % p, at[1] + base[lo][1]);
-            const uint32_t idx = at[0] + i;
-            if (idx < a.item_cap && (p == 1 || it.slot < a.slot_cap)) a.items[idx] = it;
-            if (p > 1 && j % p == 0) {
-                const uint32_t q = at[2] + base[lo][2] + it.tile;
-                if (q < a.join_cap) a.joins[q] = Join{it.seq, it.tile, it.slot, p};
-            }
+            a.items[at[0] + i] = it;   // within caps_of, as its joins are
+            if (p > 1 && j % p == 0) a.joins[at[2] + base[lo][2] + it.tile] = Join{it.seq, it.tile, it.slot, p};
         }
         for (int i = 0; i < 3; ++i) at[i] += tot[i];
         __syncthreads();
     }
-    if (threadIdx.x == 0) *a.head = PlanHead{min(at[0], a.item_cap), min(at[2], a.join_cap), at[1], 0};
+    if (threadIdx.x == 0) *a.head = PlanHead{at[0], at[2], at[1], 0};
     fill_bad(a);
 }
 
@@ -1420,6 +1450,16 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttendArgs a, uint32_t r
 
 // ------------------------------------------------------------------ block weights
 
+// A sequence as the attention saw it.
+__device__ inline Head weight_head(const AttendArgs &a, uint32_t s) {
+    Head h = seq_head(a.kv, s);
+    if (a.left_out[s]) {
+        h.ok = false;
+        h.n = h.ctx = 0;
+    }
+    return h;
+}
+
 // Weights are sums of many equal shares, so they are added in 64 bits (fp32
 // one after the other loses 2^-24 of the sum each time: 2e-6 after 14,000 rows).
 struct WeightArgs {
@@ -1435,7 +1475,7 @@ struct WeightArgs {
 __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs wa) {
     const uint32_t s = blockIdx.y, b = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (b >= a.kv.max_pages) return;
-    const Head hd = seq_head(a.kv, s);
+    const Head hd = weight_head(a, s);
     const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep), per = bt / tile;
     const uint32_t have = (hd.ctx + tile - 1) / tile;   // units that hold tokens
     const uint32_t u0 = b * per, u1 = min(u0 + per, have);
@@ -1467,7 +1507,7 @@ __global__ __launch_bounds__(kThreads) void unit_kernel(AttendArgs a, WeightArgs
 __global__ __launch_bounds__(kThreads) void row_kernel(AttendArgs a, WeightArgs wa) {
     __shared__ double red[kWaves];
     const uint32_t b = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
-    const Head hd = seq_head(a.kv, s);
+    const Head hd = weight_head(a, s);
     const uint64_t from = (uint64_t)b << a.kv.btl;
     if (!hd.ok || from >= hd.ctx) return;
     // rows before the block's first token do not see it (and kept nothing)
@@ -1500,7 +1540,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void column_kernel(Atte
     const uint32_t hk = a.kv.hk;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t h = blockIdx.x % hk, kt0 = blockIdx.x / hk * kWaves, kt = kt0 + w, s = blockIdx.y;
-    const Head hd = seq_head(a.kv, s);
+    const Head hd = weight_head(a, s);
     if ((uint64_t)kt0 * kStep >= hd.ctx) return;
     const uint32_t c = lane & 15, g = lane >> 4;
     const uint32_t bt = 1u << a.kv.btl;
@@ -1604,7 +1644,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 2 : 3) void column_kernel(Atte
 __global__ __launch_bounds__(kThreads) void block_kernel(AttendArgs a, WeightArgs wa) {
     const uint32_t s = blockIdx.y, b = blockIdx.x * kThreads + threadIdx.x;
     if (b >= a.kv.max_pages) return;
-    const Head hd = seq_head(a.kv, s);
+    const Head hd = weight_head(a, s);
     const uint32_t per = (1u << a.kv.btl) / wa.tile, have = (hd.ctx + wa.tile - 1) / wa.tile;
     const uint32_t u0 = b * per, u1 = min(u0 + per, have);
     double sum = 0.0;
@@ -1637,28 +1677,46 @@ __global__ __launch_bounds__(kThreads) void weigh_kernel(Kv a, const float *w, u
 
 // ------------------------------------------------------------------ store and read
 
-// The `task`-th of the sequences' consecutive shares, where count(s) is
-// sequence s's: found by the whole workgroup, 256 sequences at a time.
+// The `task`-th of the sequences' consecutive shares, where count(h) is how
+// many sequence h has: found by the whole workgroup, 256 sequences at a time.
 // Returns the sequence (n_seq if there is none) and the share in `rest`.
 template <typename F>
-__device__ inline uint32_t locate(uint32_t n_seq, uint64_t task, F count, uint64_t *rest) {
+__device__ inline uint32_t locate(const Kv &a, uint64_t task, F count, uint64_t *rest) {
     __shared__ unsigned long long sums[kWaves];
-    __shared__ uint32_t found;
+    __shared__ uint32_t found, ends[16];
     __shared__ unsigned long long left;
     const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) & (kWaves - 1);
     const bool in = threadIdx.x < kThreads;
-    if (threadIdx.x == 0) found = n_seq;
-    unsigned long long before = 0;
-    for (uint32_t s0 = 0; s0 < n_seq; s0 += kThreads) {
-        const uint32_t s = s0 + threadIdx.x;
-        const unsigned long long x = in && s < n_seq ? count(s) : 0ull;
-        unsigned long long y = x;
+    if (threadIdx.x == 0) found = a.n_seq;
+    unsigned long long before = 0, x, y;
+    uint32_t named = 0;
+    bool falls = false;
+    constexpr unsigned long long kFalls = 1ull << 63;
+    unsigned long long fell;
+    auto scan = [&](bool mark) {                           // a sum's top bit: a sequence whose rows are not good
+        y = x;
         for (int d = 1; d < 64; d <<= 1) {
             const unsigned long long z = __shfl_up(y, d, 64);
             if (lane >= d) y += z;
         }
-        if (in && lane == 63) sums[w] = y;
+        mark = __any(mark);
+        if (in && lane == 63) sums[w] = y | (mark ? kFalls : 0ull);
         __syncthreads();
+        fell = 0;
+        for (int v = 0; v < kWaves; ++v) fell |= sums[v];
+    };
+    for (uint32_t s0 = 0; s0 < a.n_seq; s0 += kThreads) {
+        const uint32_t s = s0 + threadIdx.x;
+        Head h{};
+        if (in && s < a.n_seq) h = seq_head(a, s);
+        x = h.n ? count(h) : 0ull;
+        scan(in && s < a.n_seq && !h.rows_ok);
+        if (falls || fell & kFalls) {   // sequences that begin among rows of an earlier one do not count
+            if (!falls) named = s0 ? rows_end(a, s0 - 1) : 0u;   // none fell before these
+            falls = true;
+            if (h.row0 < rows_before(in && s < a.n_seq ? rows_end(a, s) : 0u, named, ends)) x = 0;
+            scan(false);
+        }
         unsigned long long base = before, all = 0;
         for (int v = 0; v < kWaves; ++v) {
             if (v < w) base += sums[v];
@@ -1671,7 +1729,7 @@ __device__ inline uint32_t locate(uint32_t n_seq, uint64_t task, F count, uint64
         }
         __syncthreads();
         before += all;
-        if (found < n_seq || task < before) break;
+        if (found < a.n_seq || task < before) break;
     }
     __syncthreads();
     *rest = left;
@@ -1771,9 +1829,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel
     const uint32_t task = blockIdx.x, h = blockIdx.y;
     if (h == 0 && blockIdx.z == 0) report_bad(kv, task);
     uint64_t rest;
-    const uint32_t s = locate(kv.n_seq, task, [&](uint32_t q) -> unsigned long long {
-        const Head h = seq_head(kv, q);
-        if (!h.n || h.n > h.ctx) return 0;
+    const uint32_t s = locate(kv, task, [&](const Head &h) -> unsigned long long {
+        if (h.n > h.ctx) return 0;
         return ((h.ctx - 1) >> kv.btl) - ((h.ctx - h.n) >> kv.btl) + 1;
     }, &rest);
     if (s >= kv.n_seq) return;
@@ -1944,9 +2001,8 @@ __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
     const uint32_t task = blockIdx.x, h = blockIdx.y;
     if (h == 0) report_bad(kv, task);
     uint64_t rest;
-    const uint32_t s = locate(kv.n_seq, task, [&](uint32_t q) -> unsigned long long {
-        const Head h = seq_head(kv, q);
-        if (!h.n || h.n > h.ctx) return 0;
+    const uint32_t s = locate(kv, task, [&](const Head &h) -> unsigned long long {
+        if (h.n > h.ctx) return 0;
         return (h.ctx - 1) / kStep - (h.ctx - h.n) / kStep + 1;
     }, &rest);
     if (s >= kv.n_seq) return;
@@ -2060,12 +2116,12 @@ netkv_status make_kv(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t
 constexpr uint64_t align256(uint64_t x) { return (x + 255) & ~255ull; }
 
 // How a call is split, and its workspace.
-struct Layout {
+struct Layout : Split {
     int NT;
     bool rows;             // prompt_kernel
     bool sums;             // and its rows' sums over the blocks
-    uint32_t G, tile_rows, target, fine, least, item_cap, slot_cap, join_cap, n_units, unit_rows;
-    uint64_t head, items, joins, ml, part, lse, units, cols, sums_at, total;
+    uint32_t item_cap, slot_cap, join_cap, n_units, unit_rows;
+    uint64_t head, items, joins, ml, part, lse, left_out, units, cols, sums_at, total;
 };
 
 netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads, bool weights, Layout &y) {
@@ -2092,17 +2148,15 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     // 146, 136, 137; one of 131,072 51, 56, 60; 200 ragged of up to 700 50, 63, 70.
     y.target = (512u + a.hk - 1) / a.hk;
     y.fine = y.rows || y.NT == 2 || D == 256 ? y.target : (1024u + a.hk - 1) / a.hk;
-    const uint64_t tiles = a.n_tok * y.G / y.tile_rows + a.n_seq;
-    // full ranges of the whole call and a last one a tile; no more a tile than
-    // there are of the shortest length
-    y.least = y.rows ? 8 : kWaves;
-    const uint64_t steps = (((uint64_t)a.max_pages << a.btl) + kStep - 1) / kStep, parts = (steps + y.least - 1) / y.least;
-    const uint64_t items = y.fine + tiles < tiles * parts ? y.fine + tiles : tiles * parts;
-    if (items * a.hk > (1ull << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
-    y.item_cap = (uint32_t)items;
-    y.slot_cap = items < 2 * y.fine ? (uint32_t)items : 2 * y.fine;   // a split tile has a full one at least
-    y.join_cap = tiles < y.fine ? (uint32_t)tiles : y.fine;
     const uint32_t bt = 1u << a.btl;
+    y.least = y.rows ? 8 : kWaves;
+    // whole blocks for a prompt (its sums), with and without weights the same
+    y.round = !y.rows ? kWaves : bt > kStep ? bt / kStep : 1;
+    const Caps caps = caps_of(a, y);
+    if (caps.items * a.hk > (1ull << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
+    y.item_cap = (uint32_t)caps.items;
+    y.slot_cap = (uint32_t)caps.slots;
+    y.join_cap = (uint32_t)caps.joins;
     y.n_units = (uint32_t)(((uint64_t)a.max_pages << a.btl) / (bt < kStep ? bt : kStep)) + (uint32_t)(kStep / 16);
     if (weights && (((uint64_t)a.max_pages << a.btl) / kStep + 1) * a.hk > (1ull << 24))
         return netkv_internal_fail(h, NETKV_ECAPACITY, "too many cache blocks for one call with weights");
@@ -2113,7 +2167,7 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
         return p;
     };
     y.head = take(sizeof(PlanHead));
-    y.items = take(sizeof(Item) * items);
+    y.items = take(sizeof(Item) * y.item_cap);
     y.joins = take(sizeof(Join) * y.join_cap);
     y.ml = take(16ull * y.slot_cap * a.hk * y.tile_rows);
     y.part = take(4ull * y.slot_cap * a.hk * y.tile_rows * D);
@@ -2125,9 +2179,10 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     // against 1,750.
     y.sums = weights && y.rows && a.max_pages <= 256;
     if (y.sums) y.n_units = a.max_pages;
-    y.lse = y.units = y.cols = y.sums_at = 0;
+    y.lse = y.left_out = y.units = y.cols = y.sums_at = 0;
     if (weights) {
         y.lse = take(4ull * a.n_tok * heads);
+        y.left_out = take(4ull * a.n_seq);
         const uint64_t u = (uint64_t)a.n_seq * a.hk * y.n_units;
         if (y.rows)
             y.cols = take(4 * u);
@@ -2236,16 +2291,8 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     const bool half = dtype == NETKV_FP16;
     AttendArgs t{};
     t.kv = a;
-    t.G = y.G;
-    t.tile_rows = y.tile_rows;
-    t.target = y.target;
-    t.fine = y.fine;
-    t.least = y.least;
-    // whole blocks for a prompt (its sums), with and without weights the same
-    t.round = !y.rows ? kWaves : kv->block_tokens > kStep ? kv->block_tokens / kStep : 1;
-    t.item_cap = y.item_cap;
-    t.slot_cap = y.slot_cap;
-    t.join_cap = y.join_cap;
+    (Split &)t = y;
+    t.left_out = block_weight ? (uint32_t *)(ws + y.left_out) : nullptr;
     t.bad_out = (uint16_t *)out;
     t.out_stride = out_stride;
     t.row_elems = (uint32_t)width;

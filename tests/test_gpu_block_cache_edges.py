@@ -1,0 +1,183 @@
+"""The block cache's operators on calls at the edge of what include/netkv.h
+allows: sequences that name the same rows.  Needs an MI355X and the built
+library."""
+import numpy as np
+import pytest
+
+from tests import blockcache_ref as R
+from tests.test_gpu_block_cache import case, check_attend, dev, ref_store, same_cache, sequences, upload
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+def _say(*a):
+    print("[gpu-case]", *a, flush=True)
+
+
+@pytest.fixture(scope="module")
+def nk():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2606_03910_amd import netkv
+    netkv.load_library()
+    return netkv
+
+
+@pytest.fixture(scope="module")
+def sel(nk):
+    s = nk.Selector(0)
+    yield s
+    s.close()
+
+
+# ------------------------------------------------------------------ rows of two sequences
+
+def counts(off, n_tok, max_tok):
+    """Which sequences count, and the rows that are NaN after an attention."""
+    before, ok, nan = 0, [], np.zeros(n_tok, bool)
+    for b, e in zip(off[:-1], off[1:]):
+        rows = b <= e <= n_tok
+        ok.append(bool(rows and e - b <= max_tok and b >= before))
+        if rows and not ok[-1]:
+            nan[max(b, before):e] = True
+        if rows:
+            before = max(before, e)
+    return ok, nan
+
+
+OVERLAPS = [
+    # offsets, max_tok, heads, kv heads, dim, block, tokens of every sequence
+    ([0, 128, 0, 128, 0, 128, 0, 128, 170], 128, 64, 8, 128, 512, 2048),   # 63 slots if all of them counted, of 44
+    ([0, 20, 0, 20, 0, 20, 21], 20, 64, 8, 128, 512, 512),
+    ([0, 1, 0, 1, 0, 1, 0, 1, 2], 1, 16, 2, 64, 16, 700),
+    ([3, 9, 1, 5, 40, 30, 33, 33, 44], 12, 4, 2, 256, 64, 130),
+    ([0, 4, 1 << 40, 4, 8], 4, 8, 2, 64, 32, 100),
+]
+
+
+@pytest.mark.parametrize("at", range(len(OVERLAPS)))
+def test_attend_rows_of_two_sequences(nk, sel, at):
+    """A sequence that begins among rows of an earlier one is invalid: NaN
+    where no other names the row, its block weights NaN; the others as without
+    it, and nothing past the workspace."""
+    off, max_tok, heads, hk, dim, block, held = OVERLAPS[at]
+    _say("overlap", at)
+    n_seq, n_tok = len(off) - 1, max(x for x in off if x < 1 << 30)
+    ok, nan = counts(off, n_tok, max_tok)
+    assert not all(ok) and any(ok)
+    ctx = [held - 3 * s for s in range(n_seq)]
+    c, table, q = case(nk, sel, 50 + at, ctx, [n_tok] + [0] * (n_seq - 1), heads, hk, dim, block, "bf16")
+    cache, qd = upload(nk, sel, c), q.cuda()
+    seqs = sequences(nk, None, ctx, table, n_tok=n_tok, max_tok=max_tok, off=np.array(off, np.int64))
+    for weights in (True, False):
+        size = nk.netkv_kv_attend_workspace(sel.h, cache.c, seqs, heads, weights)
+        work = torch.full((size + 4096,), 0x7E, dtype=torch.uint8, device="cuda")
+        out = torch.full_like(qd, 5.0)
+        w = torch.full(table.shape, 7.0, device="cuda") if weights else None
+        nk.netkv_kv_attend(sel.h, cache.c, seqs, qd, dim ** -0.5, out, w, work[:size], sel.device)
+        with pytest.raises(nk.NetKVError, match="block cache"):
+            sel.sync_errors()
+        assert (work[size:] == 0x7E).all()
+        for s in range(n_seq):
+            if ok[s]:
+                b, e = off[s], off[s + 1]
+                check_attend(c, table[s:s + 1], ctx[s:s + 1], [e - b], q[b:e], out[b:e], w[s:s + 1] if weights else None)
+            elif weights:
+                assert torch.isnan(w[s]).all()
+        named = nan.copy()
+        for s in range(n_seq):
+            if ok[s]:
+                named[off[s]:off[s + 1]] = True
+        assert torch.isnan(out[torch.from_numpy(nan).cuda()]).all()
+        assert (out[torch.from_numpy(~named).cuda()] == 5).all()
+
+
+def _fallen(n_seq, at, to):
+    off = np.arange(n_seq + 1, dtype=np.int64)
+    for a, t in zip(at, to):
+        off[a] = t
+    return off
+
+
+FALLS = [(600, [300], [290]), (600, [256], [3]), (600, [10, 400], [0, 255]), (1500, [1024, 1300], [1000, 5]),
+         (300, [299], [1 << 33]), (2000, [0, 1999], [1 << 50, 1])]
+
+
+@pytest.mark.parametrize("at", range(len(FALLS)))
+def test_many_sequences_with_offsets_that_fall(nk, sel, at):
+    """More sequences than a workgroup looks through at a time: attention,
+    store and read leave out the same ones."""
+    n, where, to = FALLS[at]
+    _say("falls", at)
+    off, max_tok = _fallen(n, where, to), 20
+    ok, nan = counts(off.tolist(), n, max_tok)
+    assert not all(ok)
+    rng = np.random.default_rng(60 + at)
+    hk, heads, dim, block = 2, 4, 64, 16
+    ctx = [int(x) for x in rng.integers(20, 40, n)]
+    c, table, q = case(nk, sel, 60 + at, ctx, [n] + [0] * (n - 1), heads, hk, dim, block, "bf16")
+    cache, qd = upload(nk, sel, c), q.cuda()
+    seqs = sequences(nk, None, ctx, table, n_tok=n, max_tok=max_tok, off=off)
+    out = torch.full_like(qd, 5.0)
+    _, w = cache.attend(seqs, qd, out=out, weights=True)
+    with pytest.raises(nk.NetKVError, match="block cache"):
+        sel.sync_errors()
+    good = [s for s in range(n) if ok[s]]
+    rows = np.concatenate([np.arange(off[s], off[s + 1]) for s in good]).astype(np.int64)
+    new = [int(off[s + 1] - off[s]) for s in good]
+    check_attend(c, table[good], [ctx[s] for s in good], new, q[rows], out[torch.from_numpy(rows).cuda()], w[good])
+    assert torch.isnan(w[[s for s in range(n) if not ok[s]]]).all()
+    assert torch.isnan(out[torch.from_numpy(nan).cuda()]).all()
+    left = ~nan
+    left[rows] = False
+    assert (out[torch.from_numpy(left).cuda()] == 5).all()
+    # store and read
+    x = torch.from_numpy(rng.standard_normal((n, 2 * hk, dim))).to(torch.bfloat16)
+    xd = x.cuda()
+    cache.store(seqs, xd[:, :hk], xd[:, hk:])
+    with pytest.raises(nk.NetKVError, match="block cache"):
+        sel.sync_errors()
+    f = x[rows].double().numpy()
+    ref_store(c, table[good], [ctx[s] for s in good], new, f[:, :hk], f[:, hk:])
+    same_cache(cache, c, table, ctx)                       # the others' pages as they were
+    k, v = (torch.full((n, hk, dim), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    nk.netkv_kv_read(sel.h, cache.c, seqs, k, v, sel.device)
+    with pytest.raises(nk.NetKVError, match="block cache"):
+        sel.sync_errors()
+    for s in good:
+        b, e = int(off[s]), int(off[s + 1])
+        for h in range(hk):
+            for got, which in ((k, "k"), (v, "v")):
+                assert np.array_equal(got[b:e, h].double().cpu().numpy(), c.held(table[s], ctx[s], h, which)[ctx[s] - (e - b):])
+    rest = np.ones(n, bool)
+    rest[rows] = False
+    assert (k[torch.from_numpy(rest).cuda()] == 9).all() and (v[torch.from_numpy(rest).cuda()] == 9).all()
+
+
+@pytest.mark.parametrize("n_new", [60, 200])
+def test_store_blocks_of_rows_named_twice(nk, sel, n_new):
+    """The rows that two sequences name are stored for the first; a later
+    sequence with rows of its own is stored whole."""
+    hk, dim, block = 2, 64, 16
+    rng = np.random.default_rng(70)
+    off = [0, n_new, 0, n_new, 0, n_new, 0, n_new, 2 * n_new]
+    ctx = [n_new + 5 * s for s in range(8)]
+    ok, _ = counts(off, 2 * n_new, n_new)
+    table, pages = R.tables(rng, ctx, block)
+    c = R.Cache(pages, hk, dim, block, rng)
+    for s, t in enumerate(ctx):
+        for i in range(-(-t // block)):
+            c.put(table[s, i], min(block, t - i * block))
+    cache = upload(nk, sel, c)
+    x = torch.from_numpy(rng.standard_normal((2 * n_new, 2 * hk, dim))).to(torch.float16)
+    xd = x.cuda()
+    seqs = sequences(nk, None, ctx, table, n_tok=2 * n_new, max_tok=n_new, off=off)
+    cache.store(seqs, xd[:, :hk], xd[:, hk:])
+    with pytest.raises(nk.NetKVError, match="block cache"):
+        sel.sync_errors()
+    good = [s for s in range(8) if ok[s]]
+    assert good == [0, 7]
+    f = x.double().numpy()
+    ref_store(c, table[good], [ctx[s] for s in good], [n_new, n_new], f[:, :hk], f[:, hk:])
+    same_cache(cache, c, table, ctx)
