@@ -545,8 +545,10 @@ netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_
  *     out = sum_i p_i v_i,  p = softmax_i(scale * q . k_i)
  * per query head; n_heads is a multiple of n_kv_heads (at most 64 times), and
  * query head j reads KV head j / (n_heads / n_kv_heads).  q and out
- * [n_tok][n_heads][head_dim] of dtype with strides as for netkv_kv_store.  A
- * row that sees no token (c < n) is 0.  What a row does not see never reaches
+ * [n_tok][n_heads][head_dim] of dtype with strides as for netkv_kv_store.  out
+ * may be q itself (the same address and stride) if block_weight is NULL, else
+ * they must not overlap (EINVAL); rows of one and the same stride may lie side
+ * by side.  A row that sees no token (c < n) is 0.  What a row does not see never reaches
  * it, be it NaN.  Products are exact and summed in fp32, the softmax is fp32,
  * and its weights are rounded to 11 bits before the product with the values.
  * Rows of invalid sequences become NaN (rows that an earlier sequence names as

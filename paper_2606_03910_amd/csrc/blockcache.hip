@@ -2283,6 +2283,10 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     const uint64_t width = (uint64_t)n_heads * kv->head_dim;
     if ((st = check_rows(h, q, q_stride, width, a.n_tok, "q must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
     if ((st = check_rows(h, out, out_stride, width, a.n_tok, "out must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    // a row is read by the one workgroup that writes it, or before a join does;
+    // but the second pass over the keys for a prompt's weights reads q again
+    if (rows_overlap(q, q_stride, out, out_stride, width, a.n_tok) && (q != out || q_stride != out_stride || block_weight))
+        return invalid(h, "out must not overlap q (without block weights it may be q itself)");
     if (a.n_seq == 0) return NETKV_OK;
     if (!work || ((uintptr_t)work & 255) || work_bytes < y.total) return invalid(h, "work must be 256-byte aligned and of at least netkv_kv_attend_workspace's bytes");
     DeviceScope scope(netkv_internal_device(h));

@@ -104,4 +104,15 @@ NETKV_BOTH inline Caps caps_of(const Kv &a, const Split &s) {
     return c;
 }
 
+// Whether two arrays of n rows of `width` 16-bit elements share one.  With
+// unlike strides: whether the memory from their first to their last does.
+inline bool rows_overlap(const void *p, uint64_t p_stride, const void *q, uint64_t q_stride, uint64_t width, uint64_t n) {
+    if (!n || !width) return false;
+    const uint64_t a = (uint64_t)(uintptr_t)p / 2, b = (uint64_t)(uintptr_t)q / 2;
+    if (a + (n - 1) * p_stride + width <= b || b + (n - 1) * q_stride + width <= a) return false;
+    if (p_stride != q_stride || n == 1) return true;
+    const uint64_t d = a < b ? b - a : a - b, rows = d / p_stride, rest = d % p_stride;
+    return (rest < width && rows < n) || (p_stride - rest < width && rows + 1 < n);
+}
+
 }  // namespace blockplan

@@ -41,17 +41,23 @@ extern "C" void plan(uint32_t n_seq, uint32_t max_pages, uint32_t btl, uint64_t 
     const Caps c = caps_of(a, y);
     out[3] = c.items; out[4] = c.slots; out[5] = c.joins; out[6] = rows;
 }
+extern "C" int overlap(uint64_t p, uint64_t ps, uint64_t q, uint64_t qs, uint64_t width, uint64_t n) {
+    return rows_overlap((void *)(uintptr_t)p, ps, (void *)(uintptr_t)q, qs, width, n);
+}
 """
 
 
 @pytest.fixture(scope="module")
-def plan(tmp_path_factory):
+def lib(tmp_path_factory):
     d = tmp_path_factory.mktemp("plan")
     (d / "plan.cpp").write_text(_SOURCE)
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I",
                            os.path.join(ROOT, "paper_2606_03910_amd", "csrc"), "-o", str(d / "plan.so"), str(d / "plan.cpp")])
-    lib = ctypes.CDLL(str(d / "plan.so"))
+    return ctypes.CDLL(str(d / "plan.so"))
 
+
+@pytest.fixture(scope="module")
+def plan(lib):
     def run(off, ctx, n_tok, max_tok, max_pages, btl, G, tile_rows, target, fine, least, rnd, look=True):
         off, ctx, out = np.asarray(off, np.uint64), np.asarray(ctx, np.uint32), np.zeros(7, np.uint64)
         lib.plan(ctypes.c_uint32(len(ctx)), ctypes.c_uint32(max_pages), ctypes.c_uint32(btl), ctypes.c_uint64(n_tok),
@@ -108,3 +114,24 @@ def test_capacities_hold_for_any_offsets(plan, seed):
         r = plan(off, ctx, n_tok, max_tok, max_pages, btl, int(rng.choice([1, 3, 8, 64])),
                  int(rng.choice([128, 256]) if prompt else rng.choice([16, 32])), target, fine, 8 if prompt else 4, rnd)
         assert within(r) and r[6] <= n_tok, (seed, off, r)
+
+
+def test_overlap_of_rows(lib):
+    """Against the elements themselves, for rows of one stride; the whole
+    ranges for others."""
+    rng = np.random.default_rng(0)
+    seen = [0, 0]
+    for _ in range(4000):
+        width, n = int(rng.integers(1, 12)), int(rng.integers(0, 6))
+        ps = width + int(rng.integers(0, 25))
+        qs = ps if rng.integers(0, 4) else width + int(rng.integers(0, 25))
+        p, q = (int(x) for x in rng.integers(0, 160, 2))
+        rows = [{a + i * s + e for i in range(n) for e in range(width)} for a, s in ((p, ps), (q, qs))]
+        if ps == qs:
+            want = bool(rows[0] & rows[1])
+        else:
+            want = n > 0 and max(p, q) <= min(max(rows[0]), max(rows[1]))
+        got = bool(lib.overlap(*(ctypes.c_uint64(x) for x in (2 * p, ps, 2 * q, qs, width, n))))
+        assert got == want, (p, ps, q, qs, width, n)
+        seen[got] += 1
+    assert min(seen) > 500

@@ -1,5 +1,5 @@
 """The block cache's operators on calls at the edge of what include/netkv.h
-allows: sequences that name the same rows.  Needs an MI355X and the built
+allows: sequences that name the same rows, outputs over the queries.  Needs an MI355X and the built
 library."""
 import numpy as np
 import pytest
@@ -181,3 +181,42 @@ def test_store_blocks_of_rows_named_twice(nk, sel, n_new):
     f = x.double().numpy()
     ref_store(c, table[good], [ctx[s] for s in good], [n_new, n_new], f[:, :hk], f[:, hk:])
     same_cache(cache, c, table, ctx)
+
+
+# ------------------------------------------------------------------ outputs over the queries
+
+@pytest.mark.parametrize("ctx,n_new,dim", [([700, 33], [1, 1], 128), ([9000, 40], [3, 4], 64), ([9000, 600], [40, 600], 64),
+                                           ([300, 200], [30, 70], 256)])
+def test_attend_in_place(nk, sel, ctx, n_new, dim):
+    """out may be q itself without weights, and lie beside it in wider rows."""
+    c, table, q = case(nk, sel, 80, ctx, n_new, 8, 2, dim, 64, "bf16")
+    cache, seqs = upload(nk, sel, c), sequences(nk, n_new, ctx, table)
+    qd = q.cuda()
+    want = cache.attend(seqs, qd)
+    x = qd.clone()
+    assert cache.attend(seqs, x, out=x) is x and torch.equal(x, want)
+    wide = torch.cat([qd, torch.zeros_like(qd), qd], 1)
+    cache.attend(seqs, wide[:, 16:], out=wide[:, 8:16], weights=True)
+    assert torch.equal(wide[:, 8:16], want) and torch.equal(wide[:, :8], qd) and torch.equal(wide[:, 16:], qd)
+    sel.sync_errors()
+
+
+@pytest.mark.parametrize("blocks", [3, 300])
+def test_attend_refuses_outputs_over_queries(nk, sel, blocks):
+    """With weights, where a prompt's second pass would read them, and any
+    other overlap."""
+    ctx, n_new = [170], [120]
+    c, table, q = case(nk, sel, 81, ctx, n_new, 8, 2, 128, 64, "bf16")
+    table = np.concatenate([table, np.zeros((1, blocks - 3), np.int64)], 1)
+    cache, seqs = upload(nk, sel, c), sequences(nk, n_new, ctx, table)
+    wide = torch.cat([q, q], 1).cuda()
+    a = wide[:, :8]
+    for out, weights in ((a, True), (wide[:, 4:12], False), (wide[:, 4:12], True)):
+        with pytest.raises(nk.NetKVError, match="overlap"):
+            cache.attend(seqs, a, out=out, weights=weights)
+    flat = torch.zeros(122 * 1024, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(nk.NetKVError, match="overlap"):
+        cache.attend(seqs, flat[:120 * 1024].view(120, 8, 128), out=flat[1024:121 * 1024].view(120, 8, 128))
+    o, w = cache.attend(seqs, a, weights=True)
+    sel.sync_errors()
+    check_attend(c, table, ctx, n_new, q, o, w)
