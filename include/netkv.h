@@ -550,7 +550,9 @@ netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_
  * they must not overlap (EINVAL); rows of one and the same stride may lie side
  * by side.  A row that sees no token (c < n) is 0.  What a row does not see never reaches
  * it, be it NaN.  Products are exact and summed in fp32, the softmax is fp32,
- * and its weights are rounded to 11 bits before the product with the values.
+ * and its weights times their values' scales are rounded to 11 bits before the
+ * product with the values; those below 2^-20 of the row's largest to a multiple
+ * of 2^-30 of that (so those below 2^-31 of it may count as 0).
  * Rows of invalid sequences become NaN (rows that an earlier sequence names as
  * well are that one's); rows past the last sequence are left as they were.
  * block_weight (NULL: none; DEVICE f32[n_seq * max_pages], overwritten): the

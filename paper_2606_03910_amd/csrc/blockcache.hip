@@ -46,7 +46,16 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 constexpr int kPromptThreads = 512;
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kMaxSum = 1024.0f;    // how large 16 weights' sum may become before a row's maximum is raised
+// A weight is held as P = 2^(x - y) s in fp16, with the row's largest 2^kLift
+// when y is set: what P loses below fp16's smallest steps is then 2^-(25 +
+// kLift) of the largest weight at most, 2^-14 of a row over 131,072 equal
+// tokens behind a dominant one (without the lift 2^-8).  From there y stays
+// until 16 weights' sum passes kMaxSum, fp16's largest.  A larger lift loses
+// less and raises y more often: 5, 6, 7, 8 and 10 take 469, 476, 484, 495 and
+// 521 us for six prompts of up to 2,777 tokens whose scores' deviation is up
+// to 3, 1,997 to 2,089 us for two chunks of 1,024 rows after 31,744.
+constexpr float kLift = 6.0f;
+constexpr float kMaxSum = 65504.0f;
 constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
 
 __device__ inline void report(const Kv &a) { atomicOr(a.err, kErrBlockBit); }
@@ -526,6 +535,18 @@ __device__ __forceinline__ float weights_of(const f32x4 (&st)[4], float sc, floa
     return sum;
 }
 
+// O to the row: 2^(y - m) / l in two factors, neither of them subnormal (y - m
+// is near log2(s) - kLift, and s may be 2^-126).
+struct Over {
+    float a, b;
+    __device__ Over(float y, float m, float l) {
+        const float t = l == 0.0f ? 0.0f : y - m, h = rintf(0.5f * t);
+        a = l == 0.0f ? 0.0f : exp2_of(h) / l;
+        b = exp2_of(t - h);
+    }
+    __device__ float operator()(float o) const { return o * a * b; }
+};
+
 // What a part with maximum m counts for beside the maximum of all; a part
 // that saw nothing finite holds zeros, or NaN.
 __device__ inline float joined(float m, float all) { return m == -INFINITY ? 1.0f : exp2_of(m - all); }
@@ -544,18 +565,18 @@ struct ValRegs {
 // Attention of one row tile over steps [k0, k1), the maximum and sum of its
 // softmax kept as they run: with x = q.k scale log2(e), m the maximum of x so
 // far and l = sum 2^(x - m); with s a block's value scale and v its e4m3
-// values, y the maximum of x + log2(s) so far and O = sum 2^(x - y) s v.  The
-// row is O 2^(y - m) / l.
+// values, y the maximum of x + log2(s) so far less kLift and O = sum 2^(x - y)
+// s v.  The row is O 2^(y - m) / l.
 //
 // A wavefront multiplies 16-row tiles of S^T = K Q^T and O^T = V^T P^T, so
 // that a lane of S^T (a query row, 16 tokens in a row) holds the very P^T
 // operand of the second product: the token that key row r of product t means
 // is 16 (r / 4) + 4 t + r % 4, and nothing moves between lanes.  P = 2^(x - y) s
 // is rounded to fp16 for both types of query, since e4m3 is exact in it: 11
-// bits for what is within 2^-14 of the largest (y is the maximum with s in it,
-// so that a block of small values that a row attends to keeps them).  l takes
-// the weights before that rounding.  A maximum is raised, and O rescaled, only
-// when 16 weights' sum passes 2^10, which keeps them in fp16's range.
+// bits for what is within 2^-20 of the largest, a step of 2^-30 of that below
+// (kLift; y is the maximum with s in it, so that a block of small values that a
+// row attends to keeps them).  l takes the weights before that rounding.  A
+// maximum is raised, and O rescaled, only when 16 weights' sum passes kMaxSum.
 //
 // The four wavefronts take the same rows and every fourth step each, joined
 // through LDS.  Long calls are bound by the cache's bytes: 8 sequences of
@@ -761,7 +782,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
                     mx = fmaxf(mx, st[n][t][i]);
                 }
             mx = mx == -INFINITY ? -INFINITY : mx * sc;
-            const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog));
+            const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog) - kLift);
             l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
             const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
             m[n] = mn;
@@ -894,10 +915,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
             } else {
                 const uint64_t t = hd.row0 + r / a.G;
                 const uint32_t qh = h * a.G + r % a.G;
-                const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
+                const Over over(Y, M, L);
                 T z[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[i] = (T)(o[i] * inv);
+                for (int i = 0; i < 4; ++i) z[i] = (T)over(o[i]);
                 *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + d4) = *(u32x2 *)z;
                 if (a.lse && d4 == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
             }
@@ -1202,7 +1223,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
                     mx = fmaxf(mx, st[n][t][i]);
                 }
             mx = mx == -INFINITY ? -INFINITY : mx * sc;
-            const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog));
+            const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog) - kLift);
             const float ml = m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
             l[n] *= ml;
             if constexpr (SUMS) lb[n] *= ml;
@@ -1320,13 +1341,13 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
         } else {
             const uint64_t t = hd.row0 + r / a.G;
             const uint32_t qh = h * a.G + r % a.G;
-            const float inv = l[n] == 0.0f ? 0.0f : exp2_of(y[n] - m[n]) / l[n];
+            const Over over(y[n], m[n], l[n]);
             T *out = (T *)a.out + t * a.out_stride + (uint64_t)qh * D + 4 * g;
 #pragma unroll
             for (int d = 0; d < kDT; ++d) {
                 T o[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = (T)(acc[n][d][i] * inv);
+                for (int i = 0; i < 4; ++i) o[i] = (T)over(acc[n][d][i]);
                 *(u32x2 *)(out + d * 16) = *(u32x2 *)o;
             }
             if (a.lse && g == 0) a.lse[t * a.Hq + qh] = l[n] == 0.0f ? INFINITY : m[n] + log2_of(l[n]);
@@ -1410,10 +1431,10 @@ __device__ inline void join_row(const AttendArgs &a, const Join &j, uint32_t h, 
             for (int e = 0; e < 4; ++e) o[e] += lo[i * kCols + col][e];
         const uint64_t t = hd.row0 + r / a.G;
         const uint32_t qh = h * a.G + r % a.G;
-        const float inv = L == 0.0f ? 0.0f : exp2_of(Y - M) / L;
+        const Over over(Y, M, L);
         T z[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = (T)(o[e] * inv);
+        for (int e = 0; e < 4; ++e) z[e] = (T)over(o[e]);
         *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + col * 4) = *(u32x2 *)z;
         if (a.lse && col == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
     }

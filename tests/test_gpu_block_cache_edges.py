@@ -1,5 +1,6 @@
 """The block cache's operators on calls at the edge of what include/netkv.h
-allows: sequences that name the same rows, outputs over the queries.  Needs an MI355X and the built
+allows: sequences that name the same rows, outputs over the
+queries, dominant tokens.  Needs an MI355X and the built
 library."""
 import numpy as np
 import pytest
@@ -220,3 +221,56 @@ def test_attend_refuses_outputs_over_queries(nk, sel, blocks):
     o, w = cache.attend(seqs, a, weights=True)
     sel.sync_errors()
     check_attend(c, table, ctx, n_new, q, o, w)
+
+
+# ------------------------------------------------------------------ dominant tokens
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("dim,n_new,ctx,block", [(128, 1, 32768, 512), (64, 7, 5000, 16), (256, 2, 9000, 64),
+                                                 (128, 40, 32768, 512), (64, 70, 5000, 16), (256, 20, 3000, 64)])
+def test_attend_dominant_token(nk, sel, dim, n_new, ctx, block, where, dtype):
+    """One token far above many equal ones whose values alone are not zero:
+    the output is what those keep of the weight.
+
+    Relative limit: a weight e^-S of the largest is rounded by half of the
+    larger of 2^-10 of itself and 2^-30 of the largest, so relatively by
+    max(2^-11, 2^-31 e^S); the others' values are 1, so all of them may be off
+    to the same side.  Scores are exact (ones and zeros, one product with the
+    scale) up to S 2^-23 by that product and S log2(e) 2^-23 by the exponential's
+    argument, twice; the exponential and sums in fp32, at most 2^9 one after
+    the other, 2^-15 in all; and the output's own half step."""
+    heads, hk = 16, 2
+    rng = np.random.default_rng(90)
+    table, pages = R.tables(rng, [ctx], block)
+    c = R.Cache(pages, hk, dim, block, rng)
+    c.ks[:], c.vs[:] = 1.0, 1.0
+    c.k[:], c.v[:] = 0, 0x38                               # 0 and 1.0
+    tok = dict(first=0, middle=ctx // 2 + 5, last=ctx - n_new)[where]
+    c.k[table[0, tok // block], :, tok % block] = 0x38
+    c.v[table[0, tok // block], :, tok % block] = 0
+    cache, seqs = upload(nk, sel, c), sequences(nk, [n_new], [ctx], table)
+    q = torch.ones((n_new, heads, dim), dtype=torch.bfloat16 if dtype == "bf16" else torch.float16, device="cuda")
+    for S in (0.0, 9.0, 14.0, 17.5, 19.0):
+        o = cache.attend(seqs, q, S / dim).double().cpu().numpy()
+        s = dim * float(np.float32(S / dim))
+        for t in range(n_new):
+            others = ctx - n_new + t
+            want = others / (others + np.exp(s))
+            rel = max(2.0 ** -11, 2.0 ** -31 * np.exp(s)) + s * 2.0 ** -21 + 2.0 ** -15 + torch.finfo(q.dtype).eps / 2
+            assert (np.abs(o[t] - want) <= rel * want).all(), (S, t, o[t].min() / want, o[t].max() / want)
+    sel.sync_errors()
+
+
+@pytest.mark.parametrize("n_new", [1, 90])
+@pytest.mark.parametrize("e", [-126, 119])
+def test_attend_smallest_and_largest_scales(nk, sel, n_new, e):
+    """Values of the smallest and of very large scales (448 * 2^119 is the
+    format's largest scale's), in bf16, whole and split."""
+    ctx, new = [200, 3000], [n_new, 1]
+    c, table, q = case(nk, sel, 91, ctx, new, 8, 2, 128, 64, "bf16")
+    c.vs[:] = 2.0 ** e
+    c.v[:] = np.where((c.v & 127) < 0x20, 0x40, c.v)       # no value below 2^-3: none of the outputs is subnormal
+    o = upload(nk, sel, c).attend(sequences(nk, new, ctx, table), q.cuda())
+    sel.sync_errors()
+    _say(check_attend(c, table, ctx, new, q, o))
