@@ -548,8 +548,8 @@ netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_
  * [n_tok][n_heads][head_dim] of dtype with strides as for netkv_kv_store.  out
  * may be q itself (the same address and stride) if block_weight is NULL, else
  * they must not overlap (EINVAL); rows of one and the same stride may lie side
- * by side.  A row that sees no token (c < n) is 0.  What a row does not see never reaches
- * it, be it NaN.  Products are exact and summed in fp32, the softmax is fp32,
+ * by side.  A row that sees no token (c < n) is 0, one whose scores are all
+ * infinite NaN.  What a row does not see never reaches it, be it NaN.  Products are exact and summed in fp32, the softmax is fp32,
  * and its weights times their values' scales are rounded to 11 bits before the
  * product with the values; those below 2^-20 of the row's largest to a multiple
  * of 2^-30 of that (so those below 2^-31 of it may count as 0).

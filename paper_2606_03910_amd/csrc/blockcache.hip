@@ -503,7 +503,7 @@ struct AttendArgs : PlanArgs {
     uint32_t q_sign;                 // flips the queries' signs where scale < 0
     float *part;                     // [slot][head][tile_rows][D]
     f32x4 *part_ml;                  // [slot][head][tile_rows] m, l, y
-    float *lse;                      // [row][query head] log2 of the row's sum, or null
+    float *lse;                      // [row][query head] log2 of the row's sum (inf if it sees no token), or null
     float *units;                    // [seq][head][unit][unit_rows] log2 of the unit's sum, or null
     uint32_t n_units, unit_rows;
     float *sums;                     // [head][block][row] log2 of the block's sum for each row of the call, or null
@@ -536,12 +536,13 @@ __device__ __forceinline__ float weights_of(const f32x4 (&st)[4], float sc, floa
 }
 
 // O to the row: 2^(y - m) / l in two factors, neither of them subnormal (y - m
-// is near log2(s) - kLift, and s may be 2^-126).
+// is near log2(s) - kLift, and s may be 2^-126).  A row that sees no token is 0;
+// one whose scores are all -inf is no number.
 struct Over {
     float a, b;
-    __device__ Over(float y, float m, float l) {
+    __device__ Over(float y, float m, float l, bool sees) {
         const float t = l == 0.0f ? 0.0f : y - m, h = rintf(0.5f * t);
-        a = l == 0.0f ? 0.0f : exp2_of(h) / l;
+        a = l != 0.0f ? exp2_of(h) / l : sees ? NAN : 0.0f;
         b = exp2_of(t - h);
     }
     __device__ float operator()(float o) const { return o * a * b; }
@@ -915,12 +916,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
             } else {
                 const uint64_t t = hd.row0 + r / a.G;
                 const uint32_t qh = h * a.G + r % a.G;
-                const Over over(Y, M, L);
+                const bool sees = (int64_t)hd.ctx - hd.n + r / a.G + 1 > 0;
+                const Over over(Y, M, L, sees);
                 T z[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) z[i] = (T)over(o[i]);
                 *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + d4) = *(u32x2 *)z;
-                if (a.lse && d4 == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
+                if (a.lse && d4 == 0) a.lse[t * a.Hq + qh] = sees ? M + log2_of(L) : INFINITY;
             }
         }
     }
@@ -1341,7 +1343,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
         } else {
             const uint64_t t = hd.row0 + r / a.G;
             const uint32_t qh = h * a.G + r % a.G;
-            const Over over(y[n], m[n], l[n]);
+            const Over over(y[n], m[n], l[n], lim[n] > 0);
             T *out = (T *)a.out + t * a.out_stride + (uint64_t)qh * D + 4 * g;
 #pragma unroll
             for (int d = 0; d < kDT; ++d) {
@@ -1350,7 +1352,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void prompt_kernel(AttendArgs a)
                 for (int i = 0; i < 4; ++i) o[i] = (T)over(acc[n][d][i]);
                 *(u32x2 *)(out + d * 16) = *(u32x2 *)o;
             }
-            if (a.lse && g == 0) a.lse[t * a.Hq + qh] = l[n] == 0.0f ? INFINITY : m[n] + log2_of(l[n]);
+            if (a.lse && g == 0) a.lse[t * a.Hq + qh] = lim[n] > 0 ? m[n] + log2_of(l[n]) : INFINITY;
         }
     }
 }
@@ -1431,12 +1433,13 @@ __device__ inline void join_row(const AttendArgs &a, const Join &j, uint32_t h, 
             for (int e = 0; e < 4; ++e) o[e] += lo[i * kCols + col][e];
         const uint64_t t = hd.row0 + r / a.G;
         const uint32_t qh = h * a.G + r % a.G;
-        const Over over(Y, M, L);
+        const bool sees = (int64_t)hd.ctx - hd.n + r / a.G + 1 > 0;
+        const Over over(Y, M, L, sees);
         T z[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = (T)over(o[e]);
         *(u32x2 *)((T *)a.out + t * a.out_stride + (uint64_t)qh * D + col * 4) = *(u32x2 *)z;
-        if (a.lse && col == 0) a.lse[t * a.Hq + qh] = L == 0.0f ? INFINITY : M + log2_of(L);
+        if (a.lse && col == 0) a.lse[t * a.Hq + qh] = sees ? M + log2_of(L) : INFINITY;
     }
     meet();
 }

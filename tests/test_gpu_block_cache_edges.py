@@ -274,3 +274,28 @@ def test_attend_smallest_and_largest_scales(nk, sel, n_new, e):
     o = upload(nk, sel, c).attend(sequences(nk, new, ctx, table), q.cuda())
     sel.sync_errors()
     _say(check_attend(c, table, ctx, new, q, o))
+
+
+@pytest.mark.parametrize("n_new", [1, 90])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_attend_scores_that_are_all_infinite(nk, sel, n_new, sign):
+    """An infinite query over keys of one sign has scores of one infinity: the
+    row and its block weights are no numbers, as with any other query that is
+    not finite."""
+    ctx, new, heads, hk = [70, 3000, 2], [n_new, 1, 4], 8, 2
+    c, table, q = case(nk, sel, 92, ctx, new, heads, hk, 128, 64, "fp16")
+    c.k[..., 3] = np.clip(c.k[..., 3] & 127, 1, 0x7E)               # positive
+    inf = np.zeros((sum(new), heads), bool)
+    for row, head in ((n_new // 2, 1), (n_new, 6), (n_new + 4, 0)):
+        q[row, head, 3] = sign * float("inf")
+        inf[row, head] = True
+    cache, seqs = upload(nk, sel, c), sequences(nk, new, ctx, table)
+    o, w = cache.attend(seqs, q.cuda(), weights=True)
+    sel.sync_errors()
+    nan = torch.isnan(o.float()).cpu().numpy()
+    assert nan[inf].all() and not nan[~inf].any()
+    seen = np.zeros(table.shape, bool)
+    seen[0, :-(-(70 - n_new + n_new // 2 + 1) // 64)] = seen[1, :-(-3000 // 64)] = seen[2, :1] = True
+    assert np.array_equal(torch.isnan(w).cpu().numpy(), seen)
+    # rows that see nothing are still 0
+    assert not o[n_new + 1:n_new + 3].any()
