@@ -426,11 +426,18 @@ def _on(t: torch.Tensor, device, name: str) -> None:
         raise ValueError(f"{name} is on {t.device}, the handle on {device}")
 
 
+def _no_gradient(t: torch.Tensor, name: str) -> None:
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which this call does not give: pass {name}.detach(), "
+                         "or call it under torch.no_grad()")
+
+
 def _rows(t: torch.Tensor, n_tok: int, heads: int, dim: int, device, name: str):
     """Address and token stride of rows [n_tok][heads][dim] of 16-bit values,
-    dense within a token."""
+    dense within a token.  The cache's operators have no gradient."""
     if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPE or not t.is_cuda:
         raise TypeError(f"{name} must be a bfloat16 or float16 CUDA tensor")
+    _no_gradient(t, name)
     _on(t, device, name)
     shape, strides, at = t.shape, t.stride(), t.data_ptr()
     if len(shape) != 3 or shape[0] < n_tok or shape[1] != heads or shape[2] != dim:

@@ -59,6 +59,17 @@ def test_evict_by_hand():
     assert o.tolist() == [0, 3, 3, 5] and pos.tolist() == [1, 2, 4, 0, 2] and hs.tolist() == [11, 12, 14, 15, 17]
 
 
+def test_binding_refuses_a_gradient():
+    """It would be lost without a word."""
+    from paper_2606_03910_amd import netkv as nk
+    q = torch.zeros((1, 2, 64), dtype=torch.bfloat16, requires_grad=True)
+    with pytest.raises(ValueError, match="gradient"):
+        nk._no_gradient(q, "q")
+    with torch.no_grad():
+        nk._no_gradient(q, "q")
+    nk._no_gradient(q.detach(), "q")
+
+
 def test_binding_refuses_without_a_gpu():
     from paper_2606_03910_amd import netkv as nk
     off, ctx = torch.zeros(2, dtype=torch.int64).view(torch.uint64), torch.zeros(1, dtype=torch.int32).view(torch.uint32)

@@ -1,6 +1,6 @@
 """The block cache's operators on calls at the edge of what include/netkv.h
 allows: sequences that name the same rows, outputs over the
-queries, dominant tokens.  Needs an MI355X and the built
+queries, dominant tokens, tensors that require a gradient.  Needs an MI355X and the built
 library."""
 import numpy as np
 import pytest
@@ -299,3 +299,26 @@ def test_attend_scores_that_are_all_infinite(nk, sel, n_new, sign):
     assert np.array_equal(torch.isnan(w).cpu().numpy(), seen)
     # rows that see nothing are still 0
     assert not o[n_new + 1:n_new + 3].any()
+
+
+# ------------------------------------------------------------------ gradients
+
+def test_tensors_that_require_a_gradient(nk, sel):
+    """Refused where a gradient would be lost; as ever without one."""
+    ctx, n_new = [30, 50], [1, 2]
+    c, table, q = case(nk, sel, 93, ctx, n_new, 8, 2, 128, 16, "bf16")
+    cache, seqs = upload(nk, sel, c), sequences(nk, n_new, ctx, table)
+    qd = q.cuda()
+    want = cache.attend(seqs, qd)
+    x = qd.clone().requires_grad_()
+    with pytest.raises(ValueError, match="q requires a gradient"):
+        cache.attend(seqs, x)
+    with pytest.raises(ValueError, match="q requires a gradient"):
+        cache.attend(seqs, x * 1)
+    assert torch.equal(cache.attend(seqs, x.detach()), want)
+    with torch.no_grad():
+        assert torch.equal(cache.attend(seqs, x), want)
+    k = torch.zeros((3, 2, 128), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="v requires a gradient"):
+        cache.store(seqs, k, k.clone().requires_grad_())
+    sel.sync_errors()
