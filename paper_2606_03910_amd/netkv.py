@@ -179,10 +179,14 @@ def _check(h, st: int):
         raise NetKVError(st, msg.decode() if msg else "")
 
 
+# the current stream's address without the Stream object around it, which takes
+# 3 us a call; not a public name, so it may be missing
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(dev) -> int:
-    # its address without the Stream object around it, which takes 3 us a call
-    if isinstance(dev, torch.device) and dev.index is not None and torch.cuda.is_initialized():
-        return torch._C._cuda_getCurrentRawStream(dev.index)
+    if _raw_stream and isinstance(dev, torch.device) and dev.index is not None and torch.cuda.is_initialized():
+        return _raw_stream(dev.index)
     return torch.cuda.current_stream(dev).cuda_stream
 
 

@@ -59,6 +59,19 @@ def test_evict_by_hand():
     assert o.tolist() == [0, 3, 3, 5] and pos.tolist() == [1, 2, 4, 0, 2] and hs.tolist() == [11, 12, 14, 15, 17]
 
 
+def test_stream_without_the_short_way(monkeypatch):
+    """A torch without the name that is not public still gives its stream."""
+    from types import SimpleNamespace
+
+    from paper_2606_03910_amd import netkv as nk
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev: SimpleNamespace(cuda_stream=40 + dev.index))
+    monkeypatch.setattr(nk, "_raw_stream", None)
+    assert nk._stream(torch.device("cuda:2")) == 42
+    monkeypatch.setattr(nk, "_raw_stream", lambda i: 70 + i)
+    assert nk._stream(torch.device("cuda:2")) == 72
+
+
 def test_binding_refuses_a_gradient():
     """It would be lost without a word."""
     from paper_2606_03910_amd import netkv as nk

@@ -322,3 +322,13 @@ def test_tensors_that_require_a_gradient(nk, sel):
     with pytest.raises(ValueError, match="v requires a gradient"):
         cache.store(seqs, k, k.clone().requires_grad_())
     sel.sync_errors()
+
+
+def test_stream_both_ways(nk, sel, monkeypatch):
+    s = torch.cuda.Stream()
+    for stream in (torch.cuda.current_stream(), s):
+        with torch.cuda.stream(stream):
+            got = nk._stream(sel.device)
+            with monkeypatch.context() as m:
+                m.setattr(nk, "_raw_stream", None)
+                assert nk._stream(sel.device) == got == stream.cuda_stream
