@@ -563,8 +563,9 @@ netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_
  * that may overlap need their own.  Results do not depend on other sequences
  * of the batch except through how a long one is split (fp32 sums in another
  * order); the same call gives the same bytes.  Asynchronous; allocates
- * nothing.  ECAPACITY: more than 2^24 workgroups (tens of millions of
- * query rows). */
+ * nothing.  ECAPACITY: more than 2^32 - 1 threads, in workgroups of 512 or 256
+ * for up to 256 or 16 query rows of a KV head (tens of millions of query
+ * rows). */
 netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *q,
                              int dtype, uint32_t n_heads, uint64_t q_stride, float scale, void *out,
                              uint64_t out_stride, float *block_weight, void *work, uint64_t work_bytes,

@@ -1733,7 +1733,7 @@ __device__ inline uint32_t locate(const Kv &a, uint64_t task, F count, uint64_t 
         const uint32_t s = s0 + threadIdx.x;
         Head h{};
         if (in && s < a.n_seq) h = seq_head(a, s);
-        x = h.n ? count(h) : 0ull;
+        x = count(h);
         scan(in && s < a.n_seq && !h.rows_ok);
         if (falls || fell & kFalls) {   // sequences that begin among rows of an earlier one do not count
             if (!falls) named = s0 ? rows_end(a, s0 - 1) : 0u;   // none fell before these
@@ -1853,10 +1853,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel
     const uint32_t task = blockIdx.x, h = blockIdx.y;
     if (h == 0 && blockIdx.z == 0) report_bad(kv, task);
     uint64_t rest;
-    const uint32_t s = locate(kv, task, [&](const Head &h) -> unsigned long long {
-        if (h.n > h.ctx) return 0;
-        return ((h.ctx - 1) >> kv.btl) - ((h.ctx - h.n) >> kv.btl) + 1;
-    }, &rest);
+    const uint32_t s = locate(kv, task, [&](const Head &h) { return stored_blocks(kv, h); }, &rest);
     if (s >= kv.n_seq) return;
     const Head hd = seq_head(kv, s);
     const uint32_t start = hd.ctx - hd.n;                     // the first new token
@@ -2025,10 +2022,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
     const uint32_t task = blockIdx.x, h = blockIdx.y;
     if (h == 0) report_bad(kv, task);
     uint64_t rest;
-    const uint32_t s = locate(kv, task, [&](const Head &h) -> unsigned long long {
-        if (h.n > h.ctx) return 0;
-        return (h.ctx - 1) / kStep - (h.ctx - h.n) / kStep + 1;
-    }, &rest);
+    const uint32_t s = locate(kv, task, [&](const Head &h) { return read_steps(h); }, &rest);
     if (s >= kv.n_seq) return;
     const Head hd = seq_head(kv, s);
     const uint32_t start = hd.ctx - hd.n, bt = 1u << kv.btl, tile = min(bt, kStep);
@@ -2177,7 +2171,7 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     // whole blocks for a prompt (its sums), with and without weights the same
     y.round = !y.rows ? kWaves : bt > kStep ? bt / kStep : 1;
     const Caps caps = caps_of(a, y);
-    if (caps.items * a.hk > (1ull << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
+    if (!grid_fits(caps.items * a.hk, y.rows ? kPromptThreads : kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
     y.item_cap = (uint32_t)caps.items;
     y.slot_cap = (uint32_t)caps.slots;
     y.join_cap = (uint32_t)caps.joins;
@@ -2382,13 +2376,15 @@ extern "C" netkv_status netkv_kv_weigh(netkv_handle h, const netkv_kv_seqs_t *q,
 
 namespace {
 
+// One pass over the data where a workgroup's registers hold a block's rows.
+// 256 threads against 1,024, us: 64 times 64 rows of 128 dimensions 13, 27;
+// single rows 9, 20; prompts in 512-token blocks 267, 226.
+uint32_t store_threads(uint32_t rows, uint32_t D) { return rows * D <= 256 * 64 ? 256 : 1024; }
+
 template <int D>
-void launch_store(const MoveArgs &a, bool half, uint32_t tasks, uint32_t rows, hipStream_t s) {
+void launch_store(const MoveArgs &a, bool half, uint32_t tasks, uint32_t threads, hipStream_t s) {
     const dim3 grid(tasks, a.kv.hk, 2);
-    // one pass over the data where the workgroup's registers hold a block's rows.
-    // 256 threads against 1,024, us: 64 times 64 rows of 128 dimensions 13, 27;
-    // single rows 9, 20; prompts in 512-token blocks 267, 226.
-    if (rows * (uint32_t)D <= 256 * 64)
+    if (threads == 256)
         store_kernel<D, 256><<<grid, 256, 0, s>>>(a, half);
     else
         store_kernel<D, 1024><<<grid, 1024, 0, s>>>(a, half);
@@ -2412,18 +2408,16 @@ extern "C" netkv_status netkv_kv_store(netkv_handle h, const netkv_kv_t *kv, con
     a.v = v;
     a.k_stride = k_stride;
     a.v_stride = v_stride;
-    // blocks that the rows can touch: n rows of a sequence at most n / bt + 2, and at most n
-    uint64_t tasks = (a.kv.n_tok >> a.kv.btl) + 2ull * a.kv.n_seq;
-    if (tasks > a.kv.n_tok) tasks = a.kv.n_tok;
-    if (tasks > (1u << 22)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many blocks for one call");
+    const uint64_t tasks = store_groups(a.kv);
+    const uint32_t threads = store_threads(a.kv.max_tok < kv->block_tokens ? a.kv.max_tok : kv->block_tokens, kv->head_dim);
+    if (!grid_fits(tasks, threads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many blocks for one call");
     DeviceScope scope(netkv_internal_device(h));
     hipStream_t s = (hipStream_t)stream;
     const bool half = dtype == NETKV_FP16;
-    const uint32_t rows = a.kv.max_tok < kv->block_tokens ? a.kv.max_tok : kv->block_tokens;
     switch (kv->head_dim) {
-        case 64: launch_store<64>(a, half, (uint32_t)tasks, rows, s); break;
-        case 128: launch_store<128>(a, half, (uint32_t)tasks, rows, s); break;
-        default: launch_store<256>(a, half, (uint32_t)tasks, rows, s); break;
+        case 64: launch_store<64>(a, half, (uint32_t)tasks, threads, s); break;
+        case 128: launch_store<128>(a, half, (uint32_t)tasks, threads, s); break;
+        default: launch_store<256>(a, half, (uint32_t)tasks, threads, s); break;
     }
     return launched(h, "store launch failed");
 }
@@ -2444,9 +2438,8 @@ extern "C" netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, cons
     a.v = v;
     a.k_stride = k_stride;
     a.v_stride = v_stride;
-    uint64_t tasks = a.kv.n_tok / kStep + 2ull * a.kv.n_seq;
-    if (tasks > a.kv.n_tok) tasks = a.kv.n_tok;
-    if (tasks > (1u << 24)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many tokens for one call");
+    const uint64_t tasks = read_groups(a.kv);
+    if (!grid_fits(tasks, kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many tokens for one call");
     DeviceScope scope(netkv_internal_device(h));
     hipStream_t s = (hipStream_t)stream;
     const bool half = dtype == NETKV_FP16;

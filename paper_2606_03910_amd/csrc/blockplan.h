@@ -104,6 +104,27 @@ NETKV_BOTH inline Caps caps_of(const Kv &a, const Split &s) {
     return c;
 }
 
+// Workgroups a head of a store, one a block that the rows touch (n rows of a
+// sequence touch at most n / block + 2, and at most n), and of a read, one for
+// up to kStep tokens.
+NETKV_BOTH inline uint32_t stored_blocks(const Kv &a, const Head &h) {
+    return h.n && h.n <= h.ctx ? ((h.ctx - 1) >> a.btl) - ((h.ctx - h.n) >> a.btl) + 1 : 0u;
+}
+NETKV_BOTH inline uint32_t read_steps(const Head &h) {
+    return h.n && h.n <= h.ctx ? (h.ctx - 1) / kStep - (h.ctx - h.n) / kStep + 1 : 0u;
+}
+inline uint64_t store_groups(const Kv &a) {
+    const uint64_t n = (a.n_tok >> a.btl) + 2ull * a.n_seq;
+    return n < a.n_tok ? n : a.n_tok;
+}
+inline uint64_t read_groups(const Kv &a) {
+    const uint64_t n = a.n_tok / kStep + 2ull * a.n_seq;
+    return n < a.n_tok ? n : a.n_tok;
+}
+
+// A launch has less than 2^32 threads along a grid's axis.
+inline bool grid_fits(uint64_t groups, uint32_t threads) { return groups <= 0xFFFFFFFFull / threads; }
+
 // Whether two arrays of n rows of `width` 16-bit elements share one.  With
 // unlike strides: whether the memory from their first to their last does.
 inline bool rows_overlap(const void *p, uint64_t p_stride, const void *q, uint64_t q_stride, uint64_t width, uint64_t n) {

@@ -40,7 +40,18 @@ extern "C" void plan(uint32_t n_seq, uint32_t max_pages, uint32_t btl, uint64_t 
     }
     const Caps c = caps_of(a, y);
     out[3] = c.items; out[4] = c.slots; out[5] = c.joins; out[6] = rows;
+    uint32_t before = 0;
+    for (uint32_t s = 0; s < n_seq; ++s) {
+        Head h = seq_head(a, s);
+        if (look && h.row0 < before) h.n = h.ctx = 0;
+        const uint32_t e = rows_end(a, s);
+        if (e > before) before = e;
+        out[7] += stored_blocks(a, h);
+        out[8] += read_steps(h);
+    }
+    out[9] = store_groups(a); out[10] = read_groups(a);
 }
+extern "C" int fits(uint64_t groups, uint32_t threads) { return grid_fits(groups, threads); }
 extern "C" int overlap(uint64_t p, uint64_t ps, uint64_t q, uint64_t qs, uint64_t width, uint64_t n) {
     return rows_overlap((void *)(uintptr_t)p, ps, (void *)(uintptr_t)q, qs, width, n);
 }
@@ -59,7 +70,7 @@ def lib(tmp_path_factory):
 @pytest.fixture(scope="module")
 def plan(lib):
     def run(off, ctx, n_tok, max_tok, max_pages, btl, G, tile_rows, target, fine, least, rnd, look=True):
-        off, ctx, out = np.asarray(off, np.uint64), np.asarray(ctx, np.uint32), np.zeros(7, np.uint64)
+        off, ctx, out = np.asarray(off, np.uint64), np.asarray(ctx, np.uint32), np.zeros(11, np.uint64)
         lib.plan(ctypes.c_uint32(len(ctx)), ctypes.c_uint32(max_pages), ctypes.c_uint32(btl), ctypes.c_uint64(n_tok),
                  ctypes.c_uint64(max_tok), ctypes.c_void_p(off.ctypes.data), ctypes.c_void_p(ctx.ctypes.data),
                  *(ctypes.c_uint32(x) for x in (G, tile_rows, target, fine, least, rnd)), ctypes.c_int(look),
@@ -70,7 +81,7 @@ def plan(lib):
 
 
 def within(r):
-    return r[0] <= r[3] and r[1] <= r[4] and r[2] <= r[5]
+    return r[0] <= r[3] and r[1] <= r[4] and r[2] <= r[5] and r[7] <= r[9] and r[8] <= r[10]
 
 
 @pytest.mark.parametrize("off,ctx,args", [
@@ -135,3 +146,11 @@ def test_overlap_of_rows(lib):
         assert got == want, (p, ps, q, qs, width, n)
         seen[got] += 1
     assert min(seen) > 500
+
+
+def test_grids_of_less_than_2_32_threads(lib):
+    for threads in (256, 512, 1024):
+        most = (1 << 32) // threads - 1                    # 2^32 threads are one workgroup more
+        assert lib.fits(ctypes.c_uint64(most), ctypes.c_uint32(threads))
+        assert not lib.fits(ctypes.c_uint64(most + 1), ctypes.c_uint32(threads))
+        assert not lib.fits(ctypes.c_uint64(1 << 40), ctypes.c_uint32(threads))

@@ -332,3 +332,19 @@ def test_stream_both_ways(nk, sel, monkeypatch):
             with monkeypatch.context() as m:
                 m.setattr(nk, "_raw_stream", None)
                 assert nk._stream(sel.device) == got == stream.cuda_stream
+
+
+# ------------------------------------------------------------------ capacities
+
+@pytest.mark.parametrize("n_tok,max_tok,n_heads,fits", [
+    (200000, 200000, 8192, True), (300000, 300000, 8192, False),          # 512 threads: 2^23 workgroups
+    (32764, 2, 8192, True), (32766, 2, 8192, False)])                     # 256 threads: 2^24
+def test_grids_that_no_launch_takes(nk, sel, n_tok, max_tok, n_heads, fits):
+    """Refused as documented, from the host's values alone."""
+    kv = nk.netkv_kv_t(n_pages=1, block_tokens=16, n_kv_heads=1024, head_dim=64, k=256, v=256, k_scale=256, v_scale=256)
+    seqs = sequences(nk, None, [1], np.zeros((1, 1)), n_tok=n_tok, max_tok=max_tok, off=[0, 1])
+    if fits:
+        assert nk.netkv_kv_attend_workspace(sel.h, kv, seqs, n_heads, False) > 0
+    else:
+        with pytest.raises(nk.NetKVError, match="ECAPACITY"):
+            nk.netkv_kv_attend_workspace(sel.h, kv, seqs, n_heads, False)
