@@ -286,7 +286,7 @@ struct Shares {
                 rows_ok &= h.rows_ok;
             }
         }
-        if (__any(!rows_ok)) leave_out(a);
+        if (__builtin_expect(__any(!rows_ok), 0)) leave_out(a);
         unsigned long long work = 0;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) work += (unsigned long long)rt[j] * kt[j];
@@ -408,7 +408,7 @@ __device__ inline bool find_item(const PlanArgs &a, uint32_t i, Item &it, Head &
                     const uint32_t s = (threadIdx.x & 63) * sh.per + j;
                     if (s < a.kv.n_seq) a.left_out[s] = sh.left >> j & 1;
                 }
-            if (__any(sh.bad)) fill_bad(a);
+            if (__builtin_expect(__any(sh.bad), 0)) fill_bad(a);
         }
         if (!sh.item(a, i, it)) return false;
     }
@@ -916,7 +916,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
             } else {
                 const uint64_t t = hd.row0 + r / a.G;
                 const uint32_t qh = h * a.G + r % a.G;
-                const bool sees = (int64_t)hd.ctx - hd.n + r / a.G + 1 > 0;
+                const bool sees = hd.ctx + r / a.G >= hd.n;   // both below 2^31
                 const Over over(Y, M, L, sees);
                 T z[4];
 #pragma unroll
@@ -1433,7 +1433,7 @@ __device__ inline void join_row(const AttendArgs &a, const Join &j, uint32_t h, 
             for (int e = 0; e < 4; ++e) o[e] += lo[i * kCols + col][e];
         const uint64_t t = hd.row0 + r / a.G;
         const uint32_t qh = h * a.G + r % a.G;
-        const bool sees = (int64_t)hd.ctx - hd.n + r / a.G + 1 > 0;
+        const bool sees = hd.ctx + r / a.G >= hd.n;   // both below 2^31
         const Over over(Y, M, L, sees);
         T z[4];
 #pragma unroll
