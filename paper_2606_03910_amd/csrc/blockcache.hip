@@ -2138,6 +2138,7 @@ struct Layout : Split {
     int NT;
     bool rows;             // prompt_kernel
     bool sums;             // and its rows' sums over the blocks
+    bool kept;             // attend_kernel's sums of every unit
     uint32_t item_cap, slot_cap, join_cap, n_units, unit_rows;
     uint64_t head, items, joins, ml, part, lse, left_out, units, cols, sums_at, total;
 };
@@ -2194,19 +2195,19 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     // 128 dimensions), else from a second pass over the keys, which takes
     // longer but no memory: two chunks of 1,024 rows of 64 heads in 8,192 tokens
     // of 32-token blocks 704 us against 921, in 16,384 of 64-token blocks 1,320
-    // against 1,750.
-    y.sums = weights && y.rows && a.max_pages <= 256;
+    // against 1,750.  Either form's sums are kept up to kMostKept.
+    y.sums = weights && y.rows && a.max_pages <= 256 && row_sum_bytes(a, y.G) <= kMostKept;
+    y.kept = weights && !y.rows && unit_bytes(a, y.n_units, y.unit_rows) <= kMostKept;
     if (y.sums) y.n_units = a.max_pages;
     y.lse = y.left_out = y.units = y.cols = y.sums_at = 0;
     if (weights) {
         y.lse = take(4ull * a.n_tok * heads);
         y.left_out = take(4ull * a.n_seq);
-        const uint64_t u = (uint64_t)a.n_seq * a.hk * y.n_units;
-        if (y.rows)
-            y.cols = take(4 * u);
+        if (y.kept)
+            y.units = take(unit_bytes(a, y.n_units, y.unit_rows));
         else
-            y.units = take(4 * u * y.unit_rows);
-        if (y.sums) y.sums_at = take(4ull * a.n_tok * heads * a.max_pages);
+            y.cols = take(4ull * a.n_seq * a.hk * y.n_units);
+        if (y.sums) y.sums_at = take(row_sum_bytes(a, y.G));
     }
     y.total = at;
     return NETKV_OK;
@@ -2226,10 +2227,10 @@ void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, h
             a.kv.btl < 6 ? prompt_kernel<D, D == 256 ? 1 : 2, HALF, true, false><<<grid, kPromptThreads, 0, s>>>(a)
                          : prompt_kernel<D, D == 256 ? 1 : 2, HALF, false, false><<<grid, kPromptThreads, 0, s>>>(a);
     } else if (D == 256 || y.NT == 1) {
-        if (wa.w) NETKV_ATTEND(1, true);
+        if (y.kept) NETKV_ATTEND(1, true);
         else NETKV_ATTEND(1, false);
     } else if constexpr (D != 256) {
-        if (wa.w) NETKV_ATTEND(2, true);
+        if (y.kept) NETKV_ATTEND(2, true);
         else NETKV_ATTEND(2, false);
     }
 #undef NETKV_ATTEND
@@ -2245,7 +2246,7 @@ void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, h
     const uint64_t join_groups = joins_most < 512 ? joins_most : quarter < 512 ? 512 : quarter < 1024 ? quarter : 1024;
     if (steps_most > a.least) join_kernel<D, HALF><<<(uint32_t)join_groups, kThreads, 0, s>>>(a, rows);
     if (!wa.w) return;
-    if (y.rows) {
+    if (!y.kept) {
         const uint32_t steps = (uint32_t)((((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep);
         if (y.sums)
             row_kernel<<<dim3(a.kv.max_pages, a.kv.hk, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
@@ -2302,7 +2303,7 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     if ((st = check_rows(h, q, q_stride, width, a.n_tok, "q must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
     if ((st = check_rows(h, out, out_stride, width, a.n_tok, "out must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
     // a row is read by the one workgroup that writes it, or before a join does;
-    // but the second pass over the keys for a prompt's weights reads q again
+    // but the second pass over the keys for block weights reads q again
     if (rows_overlap(q, q_stride, out, out_stride, width, a.n_tok) && (q != out || q_stride != out_stride || block_weight))
         return invalid(h, "out must not overlap q (without block weights it may be q itself)");
     if (a.n_seq == 0) return NETKV_OK;
@@ -2334,7 +2335,7 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     t.part = (float *)(ws + y.part);
     t.part_ml = (f32x4 *)(ws + y.ml);
     t.lse = block_weight ? (float *)(ws + y.lse) : nullptr;
-    t.units = block_weight && !y.rows ? (float *)(ws + y.units) : nullptr;
+    t.units = y.kept ? (float *)(ws + y.units) : nullptr;
     t.n_units = y.n_units;
     t.unit_rows = y.unit_rows;
     t.sums = y.sums ? (float *)(ws + y.sums_at) : nullptr;
@@ -2342,7 +2343,7 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
     WeightArgs wa{};
     wa.tile = y.sums ? kv->block_tokens : kv->block_tokens < kStep ? kv->block_tokens : kStep;
     wa.w = block_weight;
-    wa.cols = y.rows ? (float *)(ws + y.cols) : nullptr;
+    wa.cols = block_weight && !y.kept ? (float *)(ws + y.cols) : nullptr;
     switch (kv->head_dim) {
         case 64: half ? launch_attend<64, true>(y, t, wa, s) : launch_attend<64, false>(y, t, wa, s); break;
         case 128: half ? launch_attend<128, true>(y, t, wa, s) : launch_attend<128, false>(y, t, wa, s); break;

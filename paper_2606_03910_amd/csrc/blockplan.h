@@ -104,6 +104,17 @@ NETKV_BOTH inline Caps caps_of(const Kv &a, const Split &s) {
     return c;
 }
 
+// What a call with block weights may keep of its rows for them: a sum for each
+// row and block (prompts) or row and unit (few rows).  Both are as wide as the
+// call's longest table, whatever the sequences hold; beyond kMostKept a second
+// pass over the keys takes their place, which needs a number for each row and
+// each head's unit only.
+constexpr uint64_t kMostKept = 1ull << 30;
+inline uint64_t row_sum_bytes(const Kv &a, uint32_t G) { return 4ull * a.n_tok * G * a.hk * a.max_pages; }
+inline uint64_t unit_bytes(const Kv &a, uint32_t n_units, uint32_t unit_rows) {
+    return 4ull * a.n_seq * a.hk * n_units * unit_rows;
+}
+
 // Workgroups a head of a store, one a block that the rows touch (n rows of a
 // sequence touch at most n / block + 2, and at most n), and of a read, one for
 // up to kStep tokens.

@@ -348,3 +348,49 @@ def test_grids_that_no_launch_takes(nk, sel, n_tok, max_tok, n_heads, fits):
     else:
         with pytest.raises(nk.NetKVError, match="ECAPACITY"):
             nk.netkv_kv_attend_workspace(sel.h, kv, seqs, n_heads, False)
+
+
+@pytest.mark.parametrize("n_seq,n_tok,max_tok,max_pages,block,heads,hk,dim", [
+    (256, 256, 1, 8192, 16, 64, 8, 128), (256, 1792, 7, 8192, 16, 64, 8, 128), (512, 15360, 30, 8192, 16, 64, 8, 64),
+    (64, 64, 1, 32, 512, 64, 8, 128), (16, 131072, 16384, 256, 512, 64, 8, 128), (2, 2048, 1024, 64, 512, 64, 8, 128)])
+def test_workspace_is_bounded(nk, sel, n_seq, n_tok, max_tok, max_pages, block, heads, hk, dim):
+    """One long sequence among many does not make the others' sums as wide:
+    2^30 bytes of them, parts of split rows (2 x 512 workgroups' slots of 256
+    rows of 128 dimensions and their sums), the work list, a number a row and
+    head, and one a head's unit."""
+    kv = nk.netkv_kv_t(n_pages=1, block_tokens=block, n_kv_heads=hk, head_dim=dim, k=256, v=256, k_scale=256, v_scale=256)
+    seqs = sequences(nk, None, np.ones(n_seq), np.zeros((n_seq, max_pages)), n_tok=n_tok, max_tok=max_tok,
+                     off=np.arange(n_seq + 1))
+    tiles = n_tok * heads // hk // 16 + n_seq
+    without = nk.netkv_kv_attend_workspace(sel.h, kv, seqs, heads, False)
+    assert without <= (1024 + hk) * 256 * (4 * 128 + 16) + 48 * (tiles + 1024) + 4096
+    units = n_seq * hk * (max_pages * block // min(block, 64) + 4)
+    _say(without, nk.netkv_kv_attend_workspace(sel.h, kv, seqs, heads, True) - without)
+    assert nk.netkv_kv_attend_workspace(sel.h, kv, seqs, heads, True) - without <= (1 << 30) + 4 * (n_tok * heads + n_seq + units) + 4096
+
+
+@pytest.mark.parametrize("dim,block,heads,hk,ctx,n_new,pages", [
+    (64, 16, 60, 1, [700, 4, 65, 0], [4, 4, 1, 0], 300000),      # 240 rows a sequence, of few
+    (128, 64, 128, 2, [3000, 64, 1], [2, 1, 1], 400000), (256, 32, 64, 2, [100, 3, 70], [1, 1, 1], 1300000),
+    (64, 512, 8, 2, [900, 600, 3], [600, 100, 5], 250)])
+def test_weights_without_kept_sums(nk, sel, dim, block, heads, hk, ctx, n_new, pages):
+    """Few rows over tables too wide for every unit's sum, and a prompt whose
+    rows' sums would be too many: the second pass over the keys gives the same
+    weights."""
+    c, table, q = case(nk, sel, 94, ctx, n_new, heads, hk, dim, block, "bf16")
+    cache, qd = upload(nk, sel, c), q.cuda()
+    wide = np.concatenate([table, np.full((len(ctx), pages - table.shape[1]), 1 << 30)], 1)     # never read
+    # a bound of rows that makes the prompt's sums too many; the rows that there are stay the same
+    n_tok = 300000 if max(n_new) > 100 else sum(n_new)
+    if n_tok > sum(n_new):
+        qd = torch.cat([qd, torch.zeros((n_tok - sum(n_new), heads, dim), dtype=qd.dtype, device="cuda")])
+    seqs = sequences(nk, n_new, ctx, wide, n_tok=n_tok)
+    size = nk.netkv_kv_attend_workspace(sel.h, cache.c, seqs, heads, True)
+    assert size < 1 << 30
+    work = torch.full((size,), 0x7E, dtype=torch.uint8, device="cuda")
+    o, w = torch.empty_like(qd), torch.empty(wide.shape, dtype=torch.float32, device="cuda")
+    nk.netkv_kv_attend(sel.h, cache.c, seqs, qd, dim ** -0.5, o, w, work, sel.device)
+    sel.sync_errors()
+    assert not w[:, table.shape[1]:].any()
+    _say(check_attend(c, table, ctx, n_new, q, o, w[:, :table.shape[1]]))
+    assert torch.equal(o[:sum(n_new)], cache.attend(sequences(nk, n_new, ctx, table), qd)[:sum(n_new)])
