@@ -1703,57 +1703,57 @@ __global__ __launch_bounds__(kThreads) void weigh_kernel(Kv a, const float *w, u
 
 // The `task`-th of the sequences' consecutive shares, where count(h) is how
 // many sequence h has: found by the whole workgroup, 256 sequences at a time.
-// Returns the sequence (n_seq if there is none) and the share in `rest`.
+// Returns the sequence (n_seq if there is none) and the share in `rest`.  Those
+// that count have less than 2^32 (store_groups, read_groups).
 template <typename F>
-__device__ inline uint32_t locate(const Kv &a, uint64_t task, F count, uint64_t *rest) {
-    __shared__ unsigned long long sums[kWaves];
-    __shared__ uint32_t found, ends[16];
-    __shared__ unsigned long long left;
+__device__ inline uint32_t locate(const Kv &a, uint32_t task, F count, uint32_t *rest) {
+    constexpr uint32_t kFalls = ~0u;      // a sequence whose rows are not good: every sum after it stays this
+    __shared__ uint32_t sums[kWaves], found, left, ends[16];
     const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) & (kWaves - 1);
     const bool in = threadIdx.x < kThreads;
     if (threadIdx.x == 0) found = a.n_seq;
-    unsigned long long before = 0, x, y;
-    uint32_t named = 0;
-    bool falls = false;
-    constexpr unsigned long long kFalls = 1ull << 63;
-    unsigned long long fell;
-    auto scan = [&](bool mark) {                           // a sum's top bit: a sequence whose rows are not good
-        y = x;
+    uint32_t before = 0;
+    auto look = [&](uint32_t s, uint32_t x) {              // whether that was the last chunk to look at
+        uint32_t y = x;
         for (int d = 1; d < 64; d <<= 1) {
-            const unsigned long long z = __shfl_up(y, d, 64);
-            if (lane >= d) y += z;
+            const uint32_t z = __shfl_up(y, d, 64);
+            if (lane >= d) y = __builtin_elementwise_add_sat(y, z);
         }
-        mark = __any(mark);
-        if (in && lane == 63) sums[w] = y | (mark ? kFalls : 0ull);
+        if (in && lane == 63) sums[w] = y;
         __syncthreads();
-        fell = 0;
-        for (int v = 0; v < kWaves; ++v) fell |= sums[v];
-    };
-    for (uint32_t s0 = 0; s0 < a.n_seq; s0 += kThreads) {
-        const uint32_t s = s0 + threadIdx.x;
-        Head h{};
-        if (in && s < a.n_seq) h = seq_head(a, s);
-        x = count(h);
-        scan(in && s < a.n_seq && !h.rows_ok);
-        if (falls || fell & kFalls) {   // sequences that begin among rows of an earlier one do not count
-            if (!falls) named = s0 ? rows_end(a, s0 - 1) : 0u;   // none fell before these
-            falls = true;
-            if (h.row0 < rows_before(in && s < a.n_seq ? rows_end(a, s) : 0u, named, ends)) x = 0;
-            scan(false);
-        }
-        unsigned long long base = before, all = 0;
+        uint32_t base = before;
         for (int v = 0; v < kWaves; ++v) {
-            if (v < w) base += sums[v];
-            all += sums[v];
+            if (v < w) base = __builtin_elementwise_add_sat(base, sums[v]);
+            before = __builtin_elementwise_add_sat(before, sums[v]);
         }
-        y += base;   // inclusive
+        y = __builtin_elementwise_add_sat(y, base);   // inclusive
         if (in && x && task >= y - x && task < y) {
             found = s;
             left = task - (y - x);
         }
         __syncthreads();
-        before += all;
-        if (found < a.n_seq || task < before) break;
+        return found < a.n_seq || task < before;
+    };
+    uint32_t named = 0;
+    for (bool again = false;; again = true) {
+        for (uint32_t s0 = 0; s0 < a.n_seq; s0 += kThreads) {
+            const uint32_t s = s0 + threadIdx.x;
+            const bool is = in && s < a.n_seq;
+            uint32_t x = 0;
+            if (is) {
+                const Head h = seq_head(a, s);
+                x = h.rows_ok ? count(h) : again ? 0u : kFalls;
+            }
+            if (__builtin_expect(again, 0)) {
+                const uint32_t earlier = rows_before(is ? rows_end(a, s) : 0u, named, ends);
+                if (x && a.off[s] < earlier) x = 0;
+            }
+            if (look(s, x)) break;
+        }
+        if (__builtin_expect(before != kFalls, 1)) break;
+        __syncthreads();
+        if (threadIdx.x == 0) found = a.n_seq;
+        before = 0;
     }
     __syncthreads();
     *rest = left;
@@ -1852,12 +1852,12 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel
     const uint32_t bt = 1u << kv.btl;
     const uint32_t task = blockIdx.x, h = blockIdx.y;
     if (h == 0 && blockIdx.z == 0) report_bad(kv, task);
-    uint64_t rest;
+    uint32_t rest;
     const uint32_t s = locate(kv, task, [&](const Head &h) { return stored_blocks(kv, h); }, &rest);
     if (s >= kv.n_seq) return;
     const Head hd = seq_head(kv, s);
     const uint32_t start = hd.ctx - hd.n;                     // the first new token
-    const uint32_t blk = (start >> kv.btl) + (uint32_t)rest;
+    const uint32_t blk = (start >> kv.btl) + rest;
     const uint32_t page = kv.pages[(uint64_t)s * kv.max_pages + blk];
     if (page >= kv.n_pages) {
         if (threadIdx.x == 0) report(kv);
@@ -2021,12 +2021,12 @@ __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
     const Kv &kv = a.kv;
     const uint32_t task = blockIdx.x, h = blockIdx.y;
     if (h == 0) report_bad(kv, task);
-    uint64_t rest;
+    uint32_t rest;
     const uint32_t s = locate(kv, task, [&](const Head &h) { return read_steps(h); }, &rest);
     if (s >= kv.n_seq) return;
     const Head hd = seq_head(kv, s);
     const uint32_t start = hd.ctx - hd.n, bt = 1u << kv.btl, tile = min(bt, kStep);
-    const uint32_t q0 = (start / kStep + (uint32_t)rest) * kStep;
+    const uint32_t q0 = (start / kStep + rest) * kStep;
     const uint32_t t0 = max(start, q0), t1 = min(hd.ctx, q0 + kStep);
     const uint32_t *pages = kv.pages + (uint64_t)s * kv.max_pages;
     auto put8 = [&](void *base, uint64_t stride, uint32_t tok, uint32_t d, u32x2 y, float sc) {
