@@ -575,7 +575,7 @@ netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, const netkv_k
  * gives block weights).  Depends on the host values only: n_seq, max_pages,
  * n_tok, max_tok, the cache's shape and n_heads.  At most 140 MB without weights
  * (parts of split rows; 280 with 1,024 KV heads).  With them 4 bytes more a row and
- * query head, and up to 1 GiB of partial sums, as wide as max_pages for every
+ * query head, and up to 4 GiB of partial sums, as wide as max_pages for every
  * sequence; where more would be needed, the weights come from a second pass
  * over the keys, with 4 bytes for every sequence, KV head and 64 tokens of
  * max_pages blocks (or block, if that is smaller). */
