@@ -2356,7 +2356,11 @@ extern "C" netkv_status netkv_kv_weigh(netkv_handle h, const netkv_kv_seqs_t *q,
                                        uint32_t n_pages, uint64_t *page_weight, void *stream) {
     if (!h) return NETKV_EINVAL;
     netkv_internal_clear(h);
-    // the cache itself is not touched: any address stands for it in the checks
+    if (!q) return invalid(h, "seqs must not be NULL");
+    // neither the cache nor the rows are touched: any address stands for them in the checks
+    netkv_kv_seqs_t seqs = *q;
+    seqs.n_tok = seqs.max_tok = 0;
+    seqs.tok_off = (const uint64_t *)16;
     netkv_kv_t kv{};
     kv.n_pages = n_pages;
     kv.block_tokens = block_tokens;
@@ -2365,7 +2369,7 @@ extern "C" netkv_status netkv_kv_weigh(netkv_handle h, const netkv_kv_seqs_t *q,
     kv.k = kv.v = (uint8_t *)16;
     kv.k_scale = kv.v_scale = (float *)16;
     Kv a{};
-    netkv_status st = make_kv(h, &kv, q, a);
+    netkv_status st = make_kv(h, &kv, &seqs, a);
     if (st != NETKV_OK) return st;
     if (a.n_seq == 0) return NETKV_OK;
     if (!block_weight || !page_weight) return invalid(h, "block_weight and page_weight must not be NULL");

@@ -2,6 +2,8 @@
 allows: sequences that name the same rows, outputs over the
 queries, dominant tokens, tensors that require a gradient.  Needs an MI355X and the built
 library."""
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -299,6 +301,26 @@ def test_attend_scores_that_are_all_infinite(nk, sel, n_new, sign):
     assert np.array_equal(torch.isnan(w).cpu().numpy(), seen)
     # rows that see nothing are still 0
     assert not o[n_new + 1:n_new + 3].any()
+
+
+# ------------------------------------------------------------------ weigh
+
+def test_weigh_reads_only_what_it_says(nk, sel):
+    """ctx_len, pages, n_seq and max_pages: offsets may be NULL, the bounds of
+    the rows anything."""
+    ctx, table = [40, 5], np.array([[1, 0, 2], [3, 0, 0]])
+    seqs = sequences(nk, [0, 0], ctx, table)
+    w = torch.tensor([[0.5, 0.25, 2.0], [1.0, 9.0, 9.0]], device="cuda")
+    got = [torch.zeros(4, dtype=torch.int64, device="cuda") for _ in range(2)]
+    nk.netkv_kv_weigh(sel.h, seqs, 16, w, got[0].view(torch.uint64), sel.device)
+    bare = nk.netkv_kv_seqs_t.from_buffer_copy(seqs.c)
+    bare.tok_off, bare.n_tok, bare.max_tok = None, 1 << 40, 1 << 50
+    lib = nk.load_library()
+    assert lib.netkv_kv_weigh(sel.h, ctypes.byref(bare), 16, w.data_ptr(), 4, got[1].data_ptr(), nk._stream(sel.device)) == 0
+    with pytest.raises(nk.NetKVError, match="EINVAL.*seqs must not be NULL"):
+        nk._check(sel.h, lib.netkv_kv_weigh(sel.h, None, 16, w.data_ptr(), 4, got[1].data_ptr(), nk._stream(sel.device)))
+    sel.sync_errors()
+    assert torch.equal(*got) and (got[0] / 2 ** 24).tolist() == [0.25, 0.5, 2.0, 1.0]
 
 
 # ------------------------------------------------------------------ gradients
