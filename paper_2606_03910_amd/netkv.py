@@ -653,7 +653,8 @@ class Selector:
         if n_keep is None:
             size = off.view(torch.int64)[1:] - off.view(torch.int64)[:-1]
             most = keep.view(torch.int32).to(torch.int64) & 0xFFFFFFFF
-            n_keep = int(torch.minimum(most, size).sum()) if len(size) else 0
+            # bad offsets are for the call to report: no size below zero, no more than there are
+            n_keep = min(int(torch.minimum(most, size).clamp_(min=0).sum()), int(weight.numel())) if len(size) else 0
         out = dict(hash_off=torch.empty_like(off), pos=torch.empty(n_keep, dtype=torch.uint32, device=dev),
                    hashes=None if hs is None else torch.empty(n_keep, dtype=torch.uint64, device=dev))
         work = torch.empty(netkv_cache_evict_workspace(self.h, int(weight.numel())), dtype=torch.uint8, device=dev)

@@ -323,6 +323,17 @@ def test_weigh_reads_only_what_it_says(nk, sel):
     assert torch.equal(*got) and (got[0] / 2 ** 24).tolist() == [0.25, 0.5, 2.0, 1.0]
 
 
+@pytest.mark.parametrize("off", [[7, 6, 5, 4], [0, 600, 500, 900], [0, 1 << 60, 1 << 61, 1 << 62], [900, 0, 0, 0]])
+def test_evict_bad_offsets_without_a_count(nk, sel, off):
+    """Reported by the call, whatever their sizes add up to."""
+    cache = dict(hash_off=dev(off, np.int64).view(torch.uint64), hashes=torch.arange(900, device="cuda").view(torch.uint64))
+    weight = torch.arange(900, device="cuda").view(torch.uint64)
+    r = sel.evict(cache, weight, torch.full((3,), -1, dtype=torch.int32, device="cuda").view(torch.uint32))
+    with pytest.raises(nk.NetKVError, match="eviction"):
+        sel.sync_errors()
+    assert not r["hash_off"].view(torch.int64).any()
+
+
 # ------------------------------------------------------------------ gradients
 
 def test_tensors_that_require_a_gradient(nk, sel):
