@@ -502,6 +502,11 @@ typedef struct {
  * sequences (shared prefixes).  Rows tok_off[s] .. tok_off[s+1] of a call's
  * token arrays are its last tokens, in order.  n_tok bounds tok_off, max_tok
  * one sequence's rows; both are host values, as large as needed or larger.
+ * Work is laid out by them: attention takes one form for all sequences of a
+ * call, by max_tok * n_heads / n_kv_heads rows (more than 240, 160 or 32 at
+ * head_dim 64, 128 or 256: the form for prompts, in which sequences of single
+ * tokens take up to three times as long), so give prompts and single tokens a
+ * call each, and a max_tok that is not much too large.
  * A sequence with offsets that decrease or pass n_tok, a first row before the
  * last one of an earlier sequence, more than max_tok rows, more tokens than
  * max_pages pages hold, or a page >= n_pages among those that a call reads is
@@ -526,16 +531,20 @@ enum { NETKV_BF16 = 1, NETKV_FP16 = 2 };
  * and that is larger; if it grows, those tokens are brought under the new
  * scale.  Rounding is to nearest even: at most half a step, 2^-4 of a value
  * down to 2^-6 s and 2^-10 s below.  What is not finite is stored as NaN.  A
- * page that the call writes must be one block of one sequence (the same page
- * twice, and which of the two remains is not said).  An invalid sequence, or one with more rows than tokens, is left
- * out.  Asynchronous; allocates nothing. */
+ * page that the call writes must be one block of one sequence (written for two,
+ * it holds some of both).  An invalid sequence, or one with more rows than
+ * tokens, is left out.  The time grows with the square of n_seq from some
+ * thousands of sequences on.  Asynchronous; allocates nothing.  ECAPACITY: more
+ * than 2^32 - 1 threads, in workgroups of 256 or 1,024 for every block that the
+ * rows touch. */
 netkv_status netkv_kv_store(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *k,
                             uint64_t k_stride, const void *v, uint64_t v_stride, int dtype, void *stream);
 
 /* The reverse: the sequences' last rows as held (value times scale, rounded
  * to dtype: exact in bf16 wherever it is normal) into k and v, laid out as
  * for netkv_kv_store.  Rows of invalid sequences and rows past the last
- * sequence are left as they were; a row on an invalid page is NaN. */
+ * sequence are left as they were; a row on an invalid page is NaN.  Time and
+ * capacity as for netkv_kv_store, in workgroups of 256 for up to 64 tokens. */
 netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, void *k,
                            uint64_t k_stride, void *v, uint64_t v_stride, int dtype, void *stream);
 
@@ -563,9 +572,9 @@ netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_
  * that may overlap need their own.  Results do not depend on other sequences
  * of the batch except through how a long one is split (fp32 sums in another
  * order); the same call gives the same bytes.  Asynchronous; allocates
- * nothing.  ECAPACITY: more than 2^32 - 1 threads, in workgroups of 512 or 256
- * for up to 256 or 16 query rows of a KV head (tens of millions of query
- * rows). */
+ * nothing.  No gradient.  ECAPACITY: more than 2^32 - 1 threads, in workgroups
+ * of 512 or 256 for up to 256 or 16 query rows of a KV head (tens of millions of
+ * query rows). */
 netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *q,
                              int dtype, uint32_t n_heads, uint64_t q_stride, float scale, void *out,
                              uint64_t out_stride, float *block_weight, void *work, uint64_t work_bytes,

@@ -581,11 +581,13 @@ struct ValRegs {
 //
 // The four wavefronts take the same rows and every fourth step each, joined
 // through LDS.  Long calls are bound by the cache's bytes: 8 sequences of
-// 131,071 tokens and 8 heads of 128 dimensions (2.15 GB) take 358 us, 6.0 TB/s,
-// 64 of up to 16,384 with block weights (0.61 GB) 132 us, 4.6 TB/s.  Short ones
-// by latency: one of 700 tokens takes 8 us, a wavefront one step of its 11.  A step's loads go out as the registers of the one before come free,
-// two workgroups a CU.  A static partition into equal pieces of all steps, which
-// needs no ranges of its own, took 166 us where these take 150.
+// 131,071 tokens and 8 heads of 128 dimensions (2.15 GB) take 361 us, 6.0 TB/s,
+// 64 of up to 16,384 with block weights (0.61 GB) 136 us, 4.5 TB/s.  Short ones
+// by latency: one of 700 tokens takes 8 us, a wavefront one step of its 11.  A
+// step's loads go out as the registers of the one before come free, two
+// workgroups a CU.  With a static partition into equal pieces of all steps,
+// which needs no ranges of its own, the whole call of the 64 sequences took 166
+// us, with ranges as they were then 150 (147 now).
 template <int D, int NT, bool HALF, bool UNITS, bool SMALL>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
     typedef typename Elem<HALF>::T T;
@@ -949,7 +951,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attend_kernel(Atte
 // 1,990 us, 1.09 PFLOP/s, where a product of 8,192 x 8,192 matrices reaches
 // 1.17.  An ordinary step of 256 rows takes 1.9 us, the first and the masked
 // ones 5, finding the tile, its first loads and its output 9: six prompts of up
-// to 2,777 tokens (0.31 TFLOP, 17 steps a tile) take 520 us.
+// to 2,777 tokens (0.31 TFLOP, 17 steps a tile) take 514 us under the profiler
+// (the whole call without it 463).
 //
 // SUMS: every row's sum over each block is kept for the blocks' weights (ranges
 // are whole blocks).
@@ -1704,7 +1707,11 @@ __global__ __launch_bounds__(kThreads) void weigh_kernel(Kv a, const float *w, u
 // The `task`-th of the sequences' consecutive shares, where count(h) is how
 // many sequence h has: found by the whole workgroup, 256 sequences at a time.
 // Returns the sequence (n_seq if there is none) and the share in `rest`.  Those
-// that count have less than 2^32 (store_groups, read_groups).
+// that count have less than 2^32 (store_groups, read_groups).  Every workgroup
+// goes through the sequences before its own, so a call's time grows with their
+// square from some thousands on: single tokens of 1,024, 4,096, 16,384 and 65,535
+// sequences (8 heads of 128 dimensions) are stored in 66 us, 399 us, 4.3 ms and
+// 58 ms and read in 23 us, 164 us, 2.0 ms and 26 ms.
 template <typename F>
 __device__ inline uint32_t locate(const Kv &a, uint32_t task, F count, uint32_t *rest) {
     constexpr uint32_t kFalls = ~0u;      // a sequence whose rows are not good: every sum after it stays this
@@ -1840,7 +1847,7 @@ __device__ inline void turn4(uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d)
 // Values are turned through LDS: written byte by byte from the rows they came
 // in, a 512-token block took three times as long.  Bound by memory: 16 prompts
 // of up to 16,384 tokens, 8 heads of 128 dimensions (537 MB in, 269 MB out)
-// take 226 us, 3.6 TB/s; 64 single tokens 8 us, latency.
+// take 228 us, 3.5 TB/s; 64 single tokens 8 us, latency.
 template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel(MoveArgs a, bool half) {
     constexpr int kEach = 8;                                  // 16-byte pieces a thread keeps
@@ -2013,7 +2020,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel
 
 // One workgroup gives back up to 64 tokens (one tile of positions) of one
 // head: keys in rows as they lie, values turned through LDS.  Bound by memory:
-// the same prompts (269 MB in, 537 MB out) take 170 us, 4.7 TB/s.
+// the same prompts (269 MB in, 537 MB out) take 178 us, 4.5 TB/s.
 template <int D>
 __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
     constexpr uint32_t kPitch = D / 4 + 1;
@@ -2155,7 +2162,9 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     // of 8,192 tokens, attend_kernel against prompt_kernel, us: 64 dimensions,
     // 192 rows 205, 258, 256 rows 268, 265; 128 dimensions, 128 rows 520, 609,
     // 160 rows 626, 673, 192 rows 794, 701; 256 dimensions, 32 rows 81, 84, 64
-    // rows 162, 84.
+    // rows 162, 84.  One form for the whole call: beside a chunk of 21 rows (168 a
+    // head) 255 such sequences with single tokens take 1,861 us, beside one of 20
+    // rows 779, alone 710.
     y.rows = most > (D == 64 ? 240u : D == 128 ? 160u : 32u);
     // 16 rows a tile or 32: 16 rows 79, 85; 32 rows 100, 89; 64 rows 177, 131
     y.NT = most <= 16 || D == 256 ? 1 : 2;
@@ -2168,6 +2177,13 @@ netkv_status make_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads
     y.target = (512u + a.hk - 1) / a.hk;
     y.fine = y.rows || y.NT == 2 || D == 256 ? y.target : (1024u + a.hk - 1) / a.hk;
     const uint32_t bt = 1u << a.btl;
+    // The shortest range, steps: one a wavefront (4, 8, 12, 16; single tokens, 64
+    // heads of 128 dimensions, the whole call, us: one sequence of 8 steps 14.6,
+    // 11.9, 11.7, 11.7, of 16 14.0, 14.7, 15.9, 11.7, of 64 14.3, 14.7, 16.1, 17.2;
+    // 64 sequences of 8 steps 22.7, 16.6, 16.5, 16.4, of 16 32.0, 31.0, 31.2, 25.1,
+    // of 32 49.7, 50.2, 50.1, 49.2): it pays where a join's 6 us are less than the
+    // steps it saves, from some 20 on.  Prompts (4, 8, 16, 32; 64 rows after that
+    // many steps): 8 steps 31, 28, 28, 28, 16 37, 37, 41, 41, 64 41, 41, 53, 77.
     y.least = y.rows ? 8 : kWaves;
     // whole blocks for a prompt (its sums), with and without weights the same
     y.round = !y.rows ? kWaves : bt > kStep ? bt / kStep : 1;

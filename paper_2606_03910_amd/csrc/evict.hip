@@ -21,9 +21,10 @@
 //
 // 768 segments of 65,536 entries, half of them kept, have to read 805 MB (all
 // weights, and with half of the hashes every line of them) and write 302 MB:
-// 221 us at 5 TB/s.  They take 362 us (9, 126, 35, 11 and 176 us in the order
-// above).  One segment of 65,536 takes 27 us and 48 of 4,096 24 us, launches
-// and the latency of their chains of loads.
+// 221 us at 5 TB/s (181 if the kept hashes could be read alone).  The call takes
+// 359 us, its kernels under the profiler 9, 129, 36, 12 and 178 in the order
+// above.  One segment of 65,536 takes 30 us and 48 of 4,096 32 us, launches and
+// the latency of their chains of loads.
 
 #include <hip/hip_runtime.h>
 
@@ -313,8 +314,10 @@ __device__ inline void rank64(const unsigned long long *list, uint32_t n, uint32
 }
 
 // A segment of at most kTiny entries by one wavefront: the threshold bit by
-// bit, from counts of ballots.  100,000 of up to 200 entries take 190 us; a
-// workgroup each, as for larger ones, 616.
+// bit, from counts of ballots.  100,000 of up to 200 entries take 220 us under
+// the profiler (190 without it; a workgroup each, as for larger ones, 616), 40
+// of memory: bound by the vector units, 820 instructions a segment, which at 4
+// cycles each are 134 us, and shifts and comparisons of 64 bits take more.
 __device__ inline void tiny_segment(const EvictArgs &a, const Seg &g, uint64_t out) {
     constexpr uint32_t kMine = kTiny / 64;
     const uint32_t lane = threadIdx.x & 63;
@@ -549,8 +552,8 @@ __device__ inline uint32_t find_long(const EvictArgs &a, uint32_t c) {
     return lo;
 }
 
-// Bound by the weights' bytes: 402 MB in and 101 MB of bins out take 126 us,
-// 4.0 TB/s.  Weights and hashes are read once, past the cache, which keeps the
+// Bound by the weights' bytes: 402 MB in and 101 MB of bins out take 129 us,
+// 3.9 TB/s.  Weights and hashes are read once, past the cache, which keeps the
 // bins (145 us through it).
 __global__ __launch_bounds__(kThreads) void count_kernel(EvictArgs a) {
     __shared__ uint32_t hist[kBins];
@@ -581,7 +584,7 @@ __global__ __launch_bounds__(kThreads) void count_kernel(EvictArgs a) {
         if (hist[i]) atomicAdd(&a.hist[(uint64_t)at * kBins + i], hist[i]);
 }
 
-// 101 MB of bins in 35 us, and the few weights of one bin.
+// 101 MB of bins in 36 us, and the few weights of one bin.
 __global__ __launch_bounds__(kThreads, 6) void gather_kernel(EvictArgs a) {
     __shared__ uint32_t found[3];
     if (blockIdx.x >= a.counts[0]) return;
@@ -677,7 +680,7 @@ __global__ __launch_bounds__(kThreads, 6) void gather_kernel(EvictArgs a) {
     }
 }
 
-// A workgroup a long segment, latency: 768 of them take 11 us (26 with 1,024
+// A workgroup a long segment, latency: 768 of them take 12 us (26 with 1,024
 // threads each, three rounds in place of one).
 __global__ __launch_bounds__(kThreads) void threshold_kernel(EvictArgs a) {
     __shared__ __align__(16) uint32_t hist[256];
@@ -810,7 +813,7 @@ __global__ __launch_bounds__(kThreads) void threshold_kernel(EvictArgs a) {
 }
 
 // Bound by memory: bins, all lines of the hashes and the outputs, 805 MB, take
-// 176 us, 4.6 TB/s.
+// 178 us, 4.5 TB/s.
 __global__ __launch_bounds__(kThreads) void write_kernel(EvictArgs a) {
     if (blockIdx.x >= a.counts[0]) return;
     const uint32_t at = find_long(a, blockIdx.x);

@@ -804,7 +804,8 @@ class BlockCache:
         """Causal attention of the sequences' last tokens q
         [n_tok][n_heads][head_dim] over their blocks (scale: 1 /
         sqrt(head_dim)); with weights=True (out, block weights
-        [n_seq][max_pages])."""
+        [n_seq][max_pages]).  out may be q itself without weights.  Prompts
+        and single tokens go faster as two calls.  No gradient."""
         if scale is None:
             scale = self.c.head_dim ** -0.5
         if out is None:
