@@ -541,7 +541,7 @@ __device__ __forceinline__ float weights_of(const f32x4 (&st)[4], float sc, floa
 struct Over {
     float a, b;
     __device__ Over(float y, float m, float l, bool sees) {
-        const float t = l == 0.0f ? 0.0f : y - m, h = rintf(0.5f * t);
+        const float t = l == 0.0f ? 0.0f : y - m, h = rintf(0.5f * fmaxf(t, -256.0f));   // -inf where every s is 0
         a = l != 0.0f ? exp2_of(h) / l : sees ? NAN : 0.0f;
         b = exp2_of(t - h);
     }

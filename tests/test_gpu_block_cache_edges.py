@@ -279,6 +279,19 @@ def test_attend_smallest_and_largest_scales(nk, sel, n_new, e):
 
 
 @pytest.mark.parametrize("n_new", [1, 90])
+def test_attend_scales_of_zero(nk, sel, n_new):
+    """Blocks of zeros whose scale says so."""
+    ctx, new = [200, 3000], [n_new, 1]
+    c, table, q = case(nk, sel, 95, ctx, new, 8, 2, 128, 64, "bf16")
+    c.vs[:, 0] = 0.0
+    c.vs[table[0, 1], 1] = 0.0
+    o = upload(nk, sel, c).attend(sequences(nk, new, ctx, table), q.cuda())
+    sel.sync_errors()
+    check_attend(c, table, ctx, new, q, o)
+    assert not o[:, :4].any() and (o[:, 4:] != 0).any(2).all()
+
+
+@pytest.mark.parametrize("n_new", [1, 90])
 @pytest.mark.parametrize("sign", [1.0, -1.0])
 def test_attend_scores_that_are_all_infinite(nk, sel, n_new, sign):
     """An infinite query over keys of one sign has scores of one infinity: the
