@@ -507,8 +507,8 @@ typedef struct {
  * head_dim 64, 128 or 256: the form for prompts, in which sequences of single
  * tokens take up to three times as long), so give prompts and single tokens a
  * call each, and a max_tok that is not much too large.
- * A sequence with offsets that decrease or pass n_tok, a first row before the
- * last one of an earlier sequence, more than max_tok rows, more tokens than
+ * A sequence with offsets that decrease or pass n_tok, a start before the end
+ * of an earlier sequence's rows, more than max_tok rows, more tokens than
  * max_pages pages hold, or a page >= n_pages among those that a call reads is
  * invalid and reported by netkv_sync_errors; nothing outside the arrays is
  * read or written for it, and the others are as without it. */
