@@ -20,406 +20,12 @@
 
 #include <hip/hip_runtime.h>
 
-#include <cmath>
-#include <cstdint>
-#include <type_traits>
-
-#include "blockplan.h"
-#include "netkv.h"
-#include "netkv_internal.h"
+#include "blockdev.h"
+#include "blockstore.h"
 
 namespace {
 
-using namespace blockplan;
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-typedef short i16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kThreads = 256;
-constexpr int kPromptThreads = 512;
-constexpr float kLog2e = 1.44269504088896340736f;
-// A weight is held as P = 2^(x - y) s in fp16, with the row's largest 2^kLift
-// when y is set: what P loses below fp16's smallest steps is then 2^-(25 +
-// kLift) of the largest weight at most, 2^-14 of a row over 131,072 equal
-// tokens behind a dominant one (without the lift 2^-8).  From there y stays
-// until 16 weights' sum passes kMaxSum, fp16's largest.  A larger lift loses
-// less and raises y more often: 5, 6, 7, 8 and 10 take 469, 476, 484, 495 and
-// 521 us for six prompts of up to 2,777 tokens whose scores' deviation is up
-// to 3, 1,997 to 2,089 us for two chunks of 1,024 rows after 31,744.
-constexpr float kLift = 6.0f;
-constexpr float kMaxSum = 65504.0f;
-constexpr uint32_t kNoSlot = 0xFFFFFFFFu;
-
-__device__ inline void report(const Kv &a) { atomicOr(a.err, kErrBlockBit); }
-
-// rows_before for every thread's sequence, from what each adds to it (rows_end,
-// 0 for none); `named` is that of the first thread's, and is moved on to the
-// one after the workgroup's last.
-__device__ inline uint32_t rows_before(uint32_t end, uint32_t &named, uint32_t *sh) {
-    const uint32_t lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x / 64;
-    uint32_t most = end;
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t v = __shfl_up(most, d, 64);
-        if ((int)lane >= d) most = max(most, v);
-    }
-    if (lane == 63) sh[w] = most;
-    __syncthreads();
-    uint32_t before = __shfl_up(most, 1, 64), all = named;
-    if (lane == 0) before = 0;
-    before = max(before, named);
-    for (uint32_t v = 0; v < waves; ++v) {
-        if (v < w) before = max(before, sh[v]);
-        all = max(all, sh[v]);
-    }
-    named = all;
-    __syncthreads();
-    return before;
-}
-
-// bytes of one head of one page
-__device__ inline uint64_t head_bytes(const Kv &a, int D) { return (uint64_t)D << a.btl; }
-
-template <bool HALF>
-struct Elem;
-template <>
-struct Elem<true> {
-    typedef _Float16 T;
-    typedef f16x2 T2;
-    typedef f16x8 T8;
-};
-template <>
-struct Elem<false> {
-    typedef __bf16 T;
-    typedef bf16x2 T2;
-    typedef bf16x8 T8;
-};
-
-// 8 e4m3 bytes to 16 bits, exactly (4 significant bits, exponents -9 to 8)
-__device__ inline f16x8 widen_f16(uint32_t a, uint32_t b) {
-    const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
-    const f16x2 q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
-    const f16x2 r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false);
-    const f16x2 s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
-    return f16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
-}
-
-__device__ inline bf16x8 widen_bf16(uint32_t a, uint32_t b) {
-    const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false);
-    const bf16x2 q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
-    const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false);
-    const bf16x2 s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
-    return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
-}
-
-template <bool HALF>
-__device__ inline typename Elem<HALF>::T8 widen(uint32_t a, uint32_t b) {
-    if constexpr (HALF)
-        return widen_f16(a, b);
-    else
-        return widen_bf16(a, b);
-}
-
-__device__ inline f32x4 product(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-__device__ inline f32x4 product(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-// 1 in the lowest bit of each byte that is a NaN
-__device__ inline uint32_t nan_bytes(uint32_t x) { return (((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7; }
-
-// over the four lanes of a row (lanes l, l ^ 16, l ^ 32, l ^ 48)
-__device__ inline float row_max(float x) {
-    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ inline float pair16_sum(float x) {   // lanes l, l ^ 16
-    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-__device__ inline float row_sum(float x) {
-    x = pair16_sum(x);
-    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-// Memory that no kernel writes while this one runs, at an address that is the
-// same for the whole wavefront: loads go through the scalar cache.
-template <typename T>
-__device__ inline const __attribute__((address_space(4))) T *scalar(const T *p) {
-    return (const __attribute__((address_space(4))) T *)p;
-}
-
-__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ inline float log2_of(float x) { return __builtin_amdgcn_logf(x); }
-
-// ------------------------------------------------------------------ work list
-
-struct Item {
-    uint32_t seq, tile, k0, k1;   // row tile, steps [k0, k1)
-    uint32_t slot, pad[3];        // partial result, or kNoSlot
-};
-struct Join {
-    uint32_t seq, tile, slot, n;  // ranges slot .. slot + n - 1
-};
-struct PlanHead {
-    uint32_t n_items, n_joins, n_slots, pad;
-};
-
-// How a call is split.  With up to kListed sequences every wavefront finds its
-// share by itself (Shares); beyond that plan_kernel writes the list.
-struct PlanArgs : Split {
-    Kv kv;
-    PlanHead *head;
-    Item *items;                                   // null: not listed
-    Join *joins;
-    uint32_t *left_out;                            // [seq] 1: begins among rows of an earlier one; null: no weights
-    // rows of sequences that cannot be answered
-    uint16_t *bad_out;
-    uint64_t out_stride;
-    uint32_t row_elems, nan16;
-};
-
-constexpr uint32_t kListed = 256;
-
-constexpr int kPlanThreads = 1024;
-
-// Exclusive scan of three counts over the workgroup; totals in tot.
-__device__ inline void scan3(uint32_t (&x)[3], uint32_t (&tot)[3], uint32_t (*wsum)[3]) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint32_t in[3];
-    for (int i = 0; i < 3; ++i) {
-        uint32_t y = x[i];
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t z = __shfl_up(y, d, 64);
-            if (lane >= d) y += z;
-        }
-        in[i] = y;
-        if (lane == 63) wsum[w][i] = y;
-    }
-    __syncthreads();
-    for (int i = 0; i < 3; ++i) {
-        uint32_t before = 0, all = 0;
-        for (int v = 0; v < kPlanThreads / 64; ++v) {
-            const uint32_t z = wsum[v][i];
-            if (v < w) before += z;
-            all += z;
-        }
-        x[i] = before + in[i] - x[i];
-        tot[i] = all;
-    }
-    __syncthreads();
-}
-
-// The last step (exclusive) that a row tile of a sequence sees.
-__device__ inline uint32_t tile_end(const Head &h, uint32_t G, uint32_t tile, uint32_t rows) {
-    const uint64_t last = min((uint64_t)(tile + 1) * rows, (uint64_t)h.n * G) - 1;
-    const int64_t seen = (int64_t)h.ctx - h.n + (int64_t)(last / G) + 1;
-    return seen <= 0 ? 0u : (uint32_t)((seen + kStep - 1) / kStep);
-}
-
-// Range `part` of `p` of a row tile.
-__device__ inline Item item_of(const PlanArgs &a, uint32_t seq, const Head &h, uint32_t C, uint32_t p, uint32_t tile, uint32_t part, uint32_t slot0) {
-    const uint32_t end = tile_end(h, a.G, tile, a.tile_rows);
-    Item it;
-    it.seq = seq;
-    it.tile = tile;
-    it.k0 = part * C;
-    it.k1 = min(end, p > 1 ? (part + 1) * C : end);
-    it.slot = p > 1 ? slot0 + tile * p + part : kNoSlot;
-    return it;
-}
-
-// The rows of sequences that cannot be answered, by one workgroup; those that
-// an earlier sequence names as well are left to it.
-__device__ inline void fill_bad(const PlanArgs &a) {
-    bool bad = false;
-    for (uint32_t s = threadIdx.x; s < a.kv.n_seq; s += blockDim.x) bad |= !seq_head(a.kv, s).ok;
-    if (!__syncthreads_or(bad)) return;
-    uint32_t before = 0;
-    for (uint32_t s = 0; s < a.kv.n_seq; ++s) {
-        const Head h = seq_head(a.kv, s);
-        const uint64_t from = max(h.row0, (uint64_t)before);
-        before = max(before, rows_end(a.kv, s));
-        if (h.ok && from == h.row0) continue;
-        if (threadIdx.x == 0) report(a.kv);
-        if (!h.rows_ok || from >= a.kv.off[s + 1]) continue;
-        const uint64_t rows = a.kv.off[s + 1] - from;
-        for (uint64_t i = threadIdx.x; i < rows * a.row_elems; i += blockDim.x)
-            a.bad_out[(from + i / a.row_elems) * a.out_stride + i % a.row_elems] = (uint16_t)a.nan16;
-    }
-}
-
-// The same list as a wavefront has it in its registers: each lane takes up to
-// four sequences in a row (n_seq <= kListed).  The ranges of full length come
-// first, then every tile's last one, tiles that see most before others.
-struct Shares {
-    uint32_t rt[4], kt[4], C, per;
-    uint32_t fulls, lasts, slots, joins;      // inclusive sums up to this lane
-    uint32_t own_fulls, own_lasts, own_slots, own_joins;
-    uint32_t left;                            // a bit for each of the lane's sequences that begin among rows of an earlier one
-    bool bad;
-
-    __device__ explicit Shares(const PlanArgs &a) {
-        const uint32_t lane = threadIdx.x & 63;
-        per = (a.kv.n_seq + 63) / 64;
-        bool rows_ok = true;
-        left = 0;
-        bad = false;
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            rt[j] = kt[j] = 0;
-            if (j >= per) continue;
-            const uint32_t s = lane * per + j;
-            if (s < a.kv.n_seq) {
-                const Head h = seq_head(a.kv, s);
-                rt[j] = tiles_of(h, a);
-                kt[j] = steps_of(h);
-                bad |= !h.ok;
-                rows_ok &= h.rows_ok;
-            }
-        }
-        if (__builtin_expect(__any(!rows_ok), 0)) leave_out(a);
-        unsigned long long work = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) work += (unsigned long long)rt[j] * kt[j];
-        for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d, 64);
-        C = range_steps(a, work);
-        own_fulls = own_lasts = own_slots = own_joins = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            if (j >= per) continue;
-            const uint32_t p = parts(j);
-            own_fulls += rt[j] * (p - 1);
-            own_lasts += rt[j];
-            own_slots += p > 1 ? rt[j] * p : 0u;
-            own_joins += p > 1 ? rt[j] : 0u;
-        }
-        fulls = own_fulls;
-        lasts = own_lasts;
-        slots = own_slots;
-        joins = own_joins;
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t v = __shfl_up(fulls, d, 64), x = __shfl_up(lasts, d, 64), y = __shfl_up(slots, d, 64), z = __shfl_up(joins, d, 64);
-            if ((int)lane >= d) {
-                fulls += v;
-                lasts += x;
-                slots += y;
-                joins += z;
-            }
-        }
-    }
-    __device__ uint32_t parts(uint32_t j) const { return parts_of(kt[j], C); }
-
-    // Sequences that begin among rows of an earlier one.
-    __device__ void leave_out(const PlanArgs &a) {
-        const uint32_t lane = threadIdx.x & 63;
-        uint32_t end = 0;
-        for (uint32_t j = 0; j < per; ++j)
-            if (lane * per + j < a.kv.n_seq) end = max(end, rows_end(a.kv, lane * per + j));
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t v = __shfl_up(end, d, 64);
-            if ((int)lane >= d) end = max(end, v);
-        }
-        uint32_t before = __shfl_up(end, 1, 64);
-        if (lane == 0) before = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t s = lane * per + j;
-            if (j >= per || s >= a.kv.n_seq) continue;
-            if (a.kv.off[s] < before) {
-                rt[j] = kt[j] = 0;
-                left |= 1u << j;
-            }
-            before = max(before, rows_end(a.kv, s));
-        }
-    }
-
-    // false: there are not so many
-    __device__ bool item(const PlanArgs &a, uint32_t i, Item &it) const {
-        const uint32_t all_fulls = (uint32_t)__builtin_amdgcn_readlane((int)fulls, 63);
-        const bool last = i >= all_fulls;
-        if (last) i -= all_fulls;
-        const uint64_t past = __ballot((last ? lasts : fulls) > i);
-        if (!past) return false;
-        const int l = __ffsll((unsigned long long)past) - 1;
-        uint32_t at = last ? lasts - own_lasts : fulls - own_fulls, slot = slots - own_slots, seq = 0, n = 0, p = 1, rest = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t q = parts(j), x = rt[j] * (last ? 1u : q - 1);
-            if (i >= at && i < at + x) {
-                seq = (threadIdx.x & 63) * per + j;
-                n = rt[j];
-                p = q;
-                rest = i - at;
-                break;
-            }
-            at += x;
-            slot += q > 1 ? rt[j] * q : 0u;
-        }
-        auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
-        seq = of(seq);
-        p = of(p);
-        rest = of(rest);
-        const uint32_t tile = of(n) - 1 - (last ? rest : rest / (p - 1)), part = last ? p - 1 : rest % (p - 1);
-        it = item_of(a, seq, seq_head(a.kv, seq), C, p, tile, part, of(slot));
-        return true;
-    }
-    __device__ uint32_t n_joins() const { return (uint32_t)__builtin_amdgcn_readlane((int)joins, 63); }
-    __device__ Join join(uint32_t i) const {
-        const int l = __ffsll((unsigned long long)__ballot(joins > i)) - 1;
-        uint32_t at = joins - own_joins, slot = slots - own_slots, seq = 0, tile = 0, p = 1;
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t q = parts(j), x = q > 1 ? rt[j] : 0u;
-            if (i >= at && i < at + x) {
-                seq = (threadIdx.x & 63) * per + j;
-                tile = i - at;
-                p = q;
-                slot += tile * q;
-                break;
-            }
-            at += x;
-            slot += x * q;
-        }
-        auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
-        return Join{of(seq), of(tile), of(slot), of(p)};
-    }
-};
-
-// This workgroup's share and its sequence; false if there is none.  What every
-// lane has the same of goes to scalar registers.
-__device__ inline bool find_item(const PlanArgs &a, uint32_t i, Item &it, Head &hd) {
-    if (a.items) {
-        if (i >= a.head->n_items) return false;
-        it = a.items[i];
-    } else {
-        const Shares sh(a);
-        if (blockIdx.x == 0) {
-            if (a.left_out)
-                for (uint32_t j = 0; j < sh.per; ++j) {
-                    const uint32_t s = (threadIdx.x & 63) * sh.per + j;
-                    if (s < a.kv.n_seq) a.left_out[s] = sh.left >> j & 1;
-                }
-            if (__builtin_expect(__any(sh.bad), 0)) fill_bad(a);
-        }
-        if (!sh.item(a, i, it)) return false;
-    }
-    auto one = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
-    it = Item{one(it.seq), one(it.tile), one(it.k0), one(it.k1), one(it.slot), {0, 0, 0}};
-    hd = seq_head(a.kv, it.seq);
-    hd.row0 = (uint64_t)one((uint32_t)(hd.row0 >> 32)) << 32 | one((uint32_t)hd.row0);
-    hd.n = one(hd.n);
-    hd.ctx = one(hd.ctx);
-    return true;
-}
+using namespace blockdev;
 
 // One workgroup.  Ranges are as long as spreads the call's steps over
 // `target` of them, so a batch of unequal sequences fills the card evenly; a
@@ -508,59 +114,6 @@ struct AttendArgs : PlanArgs {
     uint32_t n_units, unit_rows;
     float *sums;                     // [head][block][row] log2 of the block's sum for each row of the call, or null
     uint64_t sum_rows;               // rows of a head
-};
-
-// 2^(x + by) of 16 scores, as the operand of the product with the values, and
-// their sum.  (The empty statement: the weights are rounded here, not where
-// they are used, which would keep them in twice the registers.)
-__device__ __forceinline__ float weights_of(const f32x4 (&st)[4], float sc, float by, f16x8 (&pf)[2]) {
-    float sum = 0.0f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        float p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            p[i] = exp2_of(fmaf(st[t][i], sc, by));
-            sum += p[i];
-        }
-        const f16x2 u = __builtin_convertvector((f32x2{p[0], p[1]}), f16x2);
-        const f16x2 v = __builtin_convertvector((f32x2{p[2], p[3]}), f16x2);
-        const int j = 4 * (t & 1);
-        pf[t >> 1][j] = u[0];
-        pf[t >> 1][j + 1] = u[1];
-        pf[t >> 1][j + 2] = v[0];
-        pf[t >> 1][j + 3] = v[1];
-    }
-    asm volatile("" : "+v"(pf[0]), "+v"(pf[1]), "+v"(sum));
-    return sum;
-}
-
-// O to the row: 2^(y - m) / l in two factors, neither of them subnormal (y - m
-// is near log2(s) - kLift, and s may be 2^-126).  A row that sees no token is 0;
-// one whose scores are all -inf is no number.
-struct Over {
-    float a, b;
-    __device__ Over(float y, float m, float l, bool sees) {
-        const float t = l == 0.0f ? 0.0f : y - m, h = rintf(0.5f * fmaxf(t, -256.0f));   // -inf where every s is 0
-        a = l != 0.0f ? exp2_of(h) / l : sees ? NAN : 0.0f;
-        b = exp2_of(t - h);
-    }
-    __device__ float operator()(float o) const { return o * a * b; }
-};
-
-// What a part with maximum m counts for beside the maximum of all; a part
-// that saw nothing finite holds zeros, or NaN.
-__device__ inline float joined(float m, float all) { return m == -INFINITY ? 1.0f : exp2_of(m - all); }
-
-// One step's operands: keys of 64 tokens (lane: key row token, 16 dimensions)
-// and values (lane: dimension, 16 tokens).
-template <int D>
-struct KeyRegs {
-    u32x4 f[4][D / 64];
-};
-template <int D>
-struct ValRegs {
-    u32x4 f[D / 16];
 };
 
 // Attention of one row tile over steps [k0, k1), the maximum and sum of its
@@ -1704,318 +1257,10 @@ __global__ __launch_bounds__(kThreads) void weigh_kernel(Kv a, const float *w, u
 
 // ------------------------------------------------------------------ store and read
 
-// The `task`-th of the sequences' consecutive shares, where count(h) is how
-// many sequence h has: found by the whole workgroup, 256 sequences at a time.
-// Returns the sequence (n_seq if there is none) and the share in `rest`.  Those
-// that count have less than 2^32 (store_groups, read_groups).  Every workgroup
-// goes through the sequences before its own, so a call's time grows with their
-// square from some thousands on: single tokens of 1,024, 4,096, 16,384 and 65,535
-// sequences (8 heads of 128 dimensions) are stored in 66 us, 399 us, 4.3 ms and
-// 58 ms and read in 23 us, 164 us, 2.0 ms and 26 ms.
-template <typename F>
-__device__ inline uint32_t locate(const Kv &a, uint32_t task, F count, uint32_t *rest) {
-    constexpr uint32_t kFalls = ~0u;      // a sequence whose rows are not good: every sum after it stays this
-    __shared__ uint32_t sums[kWaves], found, left, ends[16];
-    const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) & (kWaves - 1);
-    const bool in = threadIdx.x < kThreads;
-    if (threadIdx.x == 0) found = a.n_seq;
-    uint32_t before = 0;
-    auto look = [&](uint32_t s, uint32_t x) {              // whether that was the last chunk to look at
-        uint32_t y = x;
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t z = __shfl_up(y, d, 64);
-            if (lane >= d) y = __builtin_elementwise_add_sat(y, z);
-        }
-        if (in && lane == 63) sums[w] = y;
-        __syncthreads();
-        uint32_t base = before;
-        for (int v = 0; v < kWaves; ++v) {
-            if (v < w) base = __builtin_elementwise_add_sat(base, sums[v]);
-            before = __builtin_elementwise_add_sat(before, sums[v]);
-        }
-        y = __builtin_elementwise_add_sat(y, base);   // inclusive
-        if (in && x && task >= y - x && task < y) {
-            found = s;
-            left = task - (y - x);
-        }
-        __syncthreads();
-        return found < a.n_seq || task < before;
-    };
-    uint32_t named = 0;
-    for (bool again = false;; again = true) {
-        for (uint32_t s0 = 0; s0 < a.n_seq; s0 += kThreads) {
-            const uint32_t s = s0 + threadIdx.x;
-            const bool is = in && s < a.n_seq;
-            uint32_t x = 0;
-            if (is) {
-                const Head h = seq_head(a, s);
-                x = h.rows_ok ? count(h) : again ? 0u : kFalls;
-            }
-            if (__builtin_expect(again, 0)) {
-                const uint32_t earlier = rows_before(is ? rows_end(a, s) : 0u, named, ends);
-                if (x && a.off[s] < earlier) x = 0;
-            }
-            if (look(s, x)) break;
-        }
-        if (__builtin_expect(before != kFalls, 1)) break;
-        __syncthreads();
-        if (threadIdx.x == 0) found = a.n_seq;
-        before = 0;
-    }
-    __syncthreads();
-    *rest = left;
-    return found;
-}
-
-struct MoveArgs {
-    Kv kv;
-    const void *k, *v;            // store: the new rows; read: the outputs
-    uint64_t k_stride, v_stride;
-};
-
-// Reports the sequences that a store or a read leaves out: by the first head's workgroups.
-__device__ inline void report_bad(const Kv &kv, uint32_t task) {
-    for (uint32_t s = task * blockDim.x + threadIdx.x; s < kv.n_seq; s += gridDim.x * blockDim.x) {
-        const Head h = seq_head(kv, s);
-        if (!h.ok || h.n > h.ctx) report(kv);
-    }
-}
-
-// The smallest power of two s >= 2^-126 with amax <= 448 s: 448 = 1.75 * 2^8.
-__device__ inline float scale_for(float amax) {
-    const uint32_t b = __float_as_uint(amax);
-    int e = (int)(b >> 23) - 127;
-    if (e < -126) return 1.17549435e-38f;
-    e += (b & 0x7FFFFFu) <= 0x600000u ? -8 : -7;
-    e = e < -126 ? -126 : e;
-    return __uint_as_float((uint32_t)(e + 127) << 23);
-}
-
-__device__ inline float to_f32(uint32_t bits16, bool half) {
-    return half ? (float)__builtin_bit_cast(_Float16, (uint16_t)bits16) : __uint_as_float(bits16 << 16);
-}
-
-// Four values to e4m3, nearest even; what is not finite becomes NaN.
-__device__ inline uint32_t narrow4(const float *x, float inv) {
-    int r = 0;
-    r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, r, false);
-    r = __builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, r, true);
-    uint32_t y = (uint32_t)r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (!(fabsf(x[i]) < INFINITY)) y = (y & ~(0xFFu << (8 * i))) | (0x7Fu << (8 * i));
-    return y;
-}
-
-// Four finite 16-bit values over a power of two to e4m3, nearest even.
-__device__ inline uint32_t narrow4_finite(uint32_t a, uint32_t b, float scale, bool half) {
-    i16x2 r = {0, 0};
-    if (half) {
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(f16x2, a), scale, false);
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(f16x2, b), scale, true);
-    } else {
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, a), scale, false);
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, b), scale, true);
-    }
-    return __builtin_bit_cast(uint32_t, r);
-}
-
-// Four e4m3 bytes under another scale (ratio <= 1, a power of two).
-__device__ inline uint32_t rescale4(uint32_t x, float ratio) {
-    const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false);
-    const f16x2 q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true);
-    const float y[4] = {(float)p[0], (float)p[1], (float)q[0], (float)q[1]};
-    return narrow4(y, ratio);
-}
-
-// Four dwords of four bytes each, turned.
-__device__ inline void turn4(uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d) {
-    const uint32_t t0 = __builtin_amdgcn_perm(b, a, 0x05010400u), t1 = __builtin_amdgcn_perm(b, a, 0x07030602u);
-    const uint32_t u0 = __builtin_amdgcn_perm(d, c, 0x05010400u), u1 = __builtin_amdgcn_perm(d, c, 0x07030602u);
-    a = __builtin_amdgcn_perm(u0, t0, 0x05040100u);
-    b = __builtin_amdgcn_perm(u0, t0, 0x07060302u);
-    c = __builtin_amdgcn_perm(u1, t1, 0x05040100u);
-    d = __builtin_amdgcn_perm(u1, t1, 0x07060302u);
-}
-
-// One workgroup quantises the keys (blockIdx.z = 0) or values of one head
-// that a call brings to one block.  The block's scale is the smallest power of
-// two that holds them, or the present one if the block was begun with a larger
-// one; where it grows, what the block holds is brought under the new scale
-// (exact but for values that become subnormal).  What fits the workgroup's
-// registers is read once, for the largest value and for the quantisation.
-// Values are turned through LDS: written byte by byte from the rows they came
-// in, a 512-token block took three times as long.  Bound by memory: 16 prompts
-// of up to 16,384 tokens, 8 heads of 128 dimensions (537 MB in, 269 MB out)
-// take 228 us, 3.5 TB/s; 64 single tokens 8 us, latency.
 template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 8 : 1) void store_kernel(MoveArgs a, bool half) {
-    constexpr int kEach = 8;                                  // 16-byte pieces a thread keeps
-    constexpr uint32_t kPass = THREADS * kEach * 8 / D;       // tokens that the workgroup keeps
-    constexpr uint32_t kPitch = D / 4 + 1;
-    __shared__ uint32_t red[THREADS / 64];
-    __shared__ uint32_t rows[(kPass + 16) * kPitch];          // quantised values by token
-    const Kv &kv = a.kv;
-    const uint32_t bt = 1u << kv.btl;
-    const uint32_t task = blockIdx.x, h = blockIdx.y;
-    if (h == 0 && blockIdx.z == 0) report_bad(kv, task);
-    uint32_t rest;
-    const uint32_t s = locate(kv, task, [&](const Head &h) { return stored_blocks(kv, h); }, &rest);
-    if (s >= kv.n_seq) return;
-    const Head hd = seq_head(kv, s);
-    const uint32_t start = hd.ctx - hd.n;                     // the first new token
-    const uint32_t blk = (start >> kv.btl) + rest;
-    const uint32_t page = kv.pages[(uint64_t)s * kv.max_pages + blk];
-    if (page >= kv.n_pages) {
-        if (threadIdx.x == 0) report(kv);
-        return;
-    }
-    const bool vals = blockIdx.z;
-    const uint32_t p0 = max(start, blk << kv.btl) - (blk << kv.btl);     // slots [p0, p1) are new
-    const uint32_t p1 = min(hd.ctx - (blk << kv.btl), bt);
-    const uint64_t row0 = hd.row0 + ((blk << kv.btl) + p0 - start);
-    const uint16_t *src = (const uint16_t *)(vals ? a.v : a.k);
-    const uint64_t stride = vals ? a.v_stride : a.k_stride;
-    const uint64_t at = (uint64_t)page * kv.hk + h;
-    uint8_t *dst = (vals ? kv.v : kv.k) + at * head_bytes(kv, D);
-    float *scale = (vals ? kv.vs : kv.ks) + at;
-    const uint32_t pieces = (p1 - p0) * (D / 8);
-
-    u32x4 x[kEach];
-    const uint16_t *own = src + (row0 + threadIdx.x / (D / 8)) * stride + (uint64_t)h * D + threadIdx.x % (D / 8) * 8;
-    auto load = [&](uint32_t base) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const uint32_t e = base + i * THREADS;
-            x[i] = u32x4{0, 0, 0, 0};
-            if (e + threadIdx.x < pieces) x[i] = *(const u32x4 *)(own + e / (D / 8) * stride);
-        }
-    };
-    // the largest of the values' bits without their signs, which order as the
-    // values do; infinities and NaN come last, and make a second look necessary
-    const uint32_t not_finite = half ? 0x7C00u : 0x7F80u;
-    auto largest = [&](bool all) {
-        u16x2 top = {0, 0};
-        for (uint32_t base = 0; base < pieces; base += THREADS * kEach) {
-            if (all || pieces > THREADS * kEach) load(base);
-#pragma unroll
-            for (int i = 0; i < kEach; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    u16x2 z = __builtin_bit_cast(u16x2, x[i][j] & 0x7FFF7FFFu);
-                    if (!all) {
-                        z[0] = z[0] < not_finite ? z[0] : (uint16_t)0;
-                        z[1] = z[1] < not_finite ? z[1] : (uint16_t)0;
-                    }
-                    top = __builtin_elementwise_max(top, z);
-                }
-        }
-        uint32_t t = top[0] > top[1] ? top[0] : top[1];
-        for (int d = 32; d; d >>= 1) t = max(t, (uint32_t)__shfl_xor(t, d, 64));
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = t;
-        __syncthreads();
-        for (int i = 0; i < THREADS / 64; ++i) t = max(t, red[i]);
-        return t;
-    };
-    uint32_t top = largest(true);
-    const bool finite = top < not_finite;
-    if (!finite) top = largest(false);
-    const float amax = to_f32(top, half);
-    float sc = scale_for(amax);
-    if (p0) {
-        const float was = *scale;
-        sc = was > sc ? was : sc;
-        if (was != sc) {
-            const float ratio = was / sc;
-            if (!vals) {
-                for (uint32_t i = threadIdx.x; i < p0 * (D / 4); i += THREADS) ((uint32_t *)dst)[i] = rescale4(((uint32_t *)dst)[i], ratio);
-            } else {
-                // by 4 tokens of a dimension; a group that the new tokens share with old ones by bytes
-                const uint32_t tile = min(bt, kStep), quads = (p0 + 3) / 4;
-                for (uint32_t i = threadIdx.x; i < quads * D; i += THREADS) {
-                    const uint32_t d = i % D, tok = i / D * 4;
-                    uint8_t *p = dst + (uint64_t)(tok & ~(tile - 1)) * D + d * tile + (tok & (tile - 1));
-                    const uint32_t y = rescale4(*(uint32_t *)p, ratio);
-                    if (tok + 4 <= p0)
-                        *(uint32_t *)p = y;
-                    else
-                        for (uint32_t j = 0; tok + j < p0; ++j) p[j] = (uint8_t)(y >> (8 * j));
-                }
-            }
-        }
-    }
-    __syncthreads();   // every thread has read the old scale
-    if (threadIdx.x == 0) *scale = sc;
-    const float inv = 1.0f / sc;
-    const uint32_t tile = min(bt, kStep);
-    if (pieces > THREADS * kEach) load(0);
-    for (uint32_t base = 0;;) {
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const uint32_t e = base + i * THREADS + threadIdx.x;
-            u32x2 y = {0, 0};
-            if (e < pieces) {
-                if (finite) {
-                    y = u32x2{narrow4_finite(x[i][0], x[i][1], sc, half), narrow4_finite(x[i][2], x[i][3], sc, half)};
-                } else {
-                    float z[8];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        z[2 * j] = to_f32(x[i][j] & 0xFFFFu, half);
-                        z[2 * j + 1] = to_f32(x[i][j] >> 16, half);
-                    }
-                    y = u32x2{narrow4(z, inv), narrow4(z + 4, inv)};
-                }
-            }
-            const uint32_t tok = p0 + e / (D / 8), d = e % (D / 8) * 8;
-            if (e >= pieces) continue;
-            if (!vals) {
-                *(u32x2 *)(dst + (uint64_t)tok * D + d) = y;
-            } else {
-                uint32_t *q = rows + (tok - ((p0 + base / (D / 8)) & ~15u)) * kPitch + d / 4;
-                q[0] = y[0];
-                q[1] = y[1];
-            }
-        }
-        if (vals) {
-            // four dimensions of 16 tokens a thread; groups that the call fills
-            // whole are written whole
-            __syncthreads();
-            const uint32_t t0 = p0 + base / (D / 8), t1 = min(p1, t0 + kPass), g0 = t0 & ~15u;
-            for (uint32_t i = threadIdx.x; i < (t1 - g0 + 63) / 64 * D; i += THREADS) {
-                // lanes: four groups, then the dimensions
-                const uint32_t dq = i / 4 % (D / 4), tg = i % 4 + i / D * 4, tok = g0 + 16 * tg;
-                if (tok >= t1) continue;
-                const uint32_t *q = rows + 16 * tg * kPitch + dq;
-                uint8_t *to = dst + (uint64_t)(tok & ~(tile - 1)) * D + (uint64_t)dq * 4 * tile + (tok & (tile - 1));
-                u32x4 o[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t x0 = q[(4 * j) * kPitch], x1 = q[(4 * j + 1) * kPitch], x2 = q[(4 * j + 2) * kPitch], x3 = q[(4 * j + 3) * kPitch];
-                    turn4(x0, x1, x2, x3);
-                    o[0][j] = x0;
-                    o[1][j] = x1;
-                    o[2][j] = x2;
-                    o[3][j] = x3;
-                }
-                if (tok >= t0 && tok + 16 <= t1) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) *(u32x4 *)(to + j * tile) = o[j];
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (uint32_t e = 0; e < 16; ++e)
-                            if (tok + e >= t0 && tok + e < t1) to[j * tile + e] = (uint8_t)(o[j][e >> 2] >> (8 * (e & 3)));
-                }
-            }
-            __syncthreads();
-        }
-        base += THREADS * kEach;
-        if (base >= pieces) break;
-        load(base);
-    }
+    if (blockIdx.y == 0 && blockIdx.z == 0) report_bad(a.kv, blockIdx.x, gridDim.x);
+    store_block<D, THREADS>(a, half, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 // One workgroup gives back up to 64 tokens (one tile of positions) of one
@@ -2027,7 +1272,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
     __shared__ uint32_t turn[kStep * kPitch];
     const Kv &kv = a.kv;
     const uint32_t task = blockIdx.x, h = blockIdx.y;
-    if (h == 0) report_bad(kv, task);
+    if (h == 0) report_bad(kv, task, gridDim.x);
     uint32_t rest;
     const uint32_t s = locate(kv, task, [&](const Head &h) { return read_steps(h); }, &rest);
     if (s >= kv.n_seq) return;
@@ -2086,59 +1331,6 @@ __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
 }
 
 // ------------------------------------------------------------------ host
-
-struct DeviceScope {
-    int prev = -1;
-    explicit DeviceScope(int dev) {
-        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-        if (prev == dev) prev = -1;
-        else (void)hipSetDevice(dev);
-    }
-    ~DeviceScope() {
-        if (prev >= 0) (void)hipSetDevice(prev);
-    }
-};
-
-netkv_status invalid(netkv_handle h, const char *msg) { return netkv_internal_fail(h, NETKV_EINVAL, msg); }
-
-bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
-
-// Checks what the host can and fills the kernels' view of it.
-netkv_status make_kv(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *q, Kv &a) {
-    if (!kv || !q) return invalid(h, "kv and seqs must not be NULL");
-    uint32_t btl = 0;
-    while (btl < 31 && (1u << btl) < kv->block_tokens) ++btl;
-    if (kv->block_tokens < 16 || kv->block_tokens > 1024 || (1u << btl) != kv->block_tokens)
-        return invalid(h, "block_tokens must be a power of two from 16 to 1024");
-    if (kv->head_dim != 64 && kv->head_dim != 128 && kv->head_dim != 256) return invalid(h, "head_dim must be 64, 128 or 256");
-    if (kv->n_kv_heads < 1 || kv->n_kv_heads > 1024) return invalid(h, "n_kv_heads must be in [1, 1024]");
-    if (kv->n_pages < 1 || kv->n_pages > 0x7FFFFFFFu) return invalid(h, "n_pages must be in [1, 2^31)");
-    if (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale) return invalid(h, "a cache array is NULL");
-    if (!aligned16(kv->k) || !aligned16(kv->v)) return invalid(h, "k and v must be 16-byte aligned");
-    if (q->n_seq && (!q->tok_off || !q->ctx_len || !q->pages)) return invalid(h, "a sequence array is NULL");
-    if (q->n_seq > 65535) return invalid(h, "n_seq must be <= 65535");
-    if (q->n_seq && q->max_pages < 1) return invalid(h, "max_pages must be >= 1");
-    if (((uint64_t)q->max_pages << btl) >= (1ull << 31)) return invalid(h, "max_pages * block_tokens must be < 2^31");
-    if (q->n_tok > (1ull << 31)) return invalid(h, "n_tok must be <= 2^31");
-    a.k = (uint8_t *)kv->k;
-    a.v = (uint8_t *)kv->v;
-    a.ks = kv->k_scale;
-    a.vs = kv->v_scale;
-    a.n_pages = kv->n_pages;
-    a.hk = kv->n_kv_heads;
-    a.btl = btl;
-    a.n_seq = q->n_seq;
-    a.max_pages = q->max_pages;
-    a.max_tok = (uint32_t)(q->max_tok < q->n_tok ? q->max_tok : q->n_tok);
-    a.off = q->tok_off;
-    a.ctx = q->ctx_len;
-    a.pages = q->pages;
-    a.n_tok = q->n_tok;
-    a.err = netkv_internal_errword(h);
-    return NETKV_OK;
-}
-
-constexpr uint64_t align256(uint64_t x) { return (x + 255) & ~255ull; }
 
 // How a call is split, and its workspace.
 struct Layout : Split {
@@ -2272,16 +1464,6 @@ void launch_attend(const Layout &y, const AttendArgs &a, const WeightArgs &wa, h
     } else {
         unit_kernel<<<dim3((a.kv.max_pages + kWaves - 1) / kWaves, a.kv.n_seq), kThreads, 0, s>>>(a, wa);
     }
-}
-
-netkv_status launched(netkv_handle h, const char *what) {
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? NETKV_OK : netkv_internal_fail(h, NETKV_EDEVICE, what);
-}
-
-netkv_status check_rows(netkv_handle h, const void *p, uint64_t stride, uint64_t width, uint64_t n_tok, const char *msg) {
-    if (n_tok && (!p || !aligned16(p) || stride % 8 || stride < width)) return invalid(h, msg);
-    return NETKV_OK;
 }
 
 }  // namespace

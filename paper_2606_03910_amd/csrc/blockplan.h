@@ -138,15 +138,19 @@ inline uint64_t read_groups(const Kv &a) {
 // A launch has less than 2^32 threads along a grid's axis.
 inline bool grid_fits(uint64_t groups, uint32_t threads) { return groups <= 0xFFFFFFFFull / threads; }
 
-// Whether two arrays of n rows of `width` 16-bit elements share one.  With
-// unlike strides: whether the memory from their first to their last does.
-inline bool rows_overlap(const void *p, uint64_t p_stride, const void *q, uint64_t q_stride, uint64_t width, uint64_t n) {
-    if (!n || !width) return false;
+// Whether two arrays of n rows of p_width and q_width 16-bit elements share one.
+// With unlike strides: whether the memory from their first to their last does.
+inline bool rows_overlap(const void *p, uint64_t p_stride, uint64_t p_width, const void *q, uint64_t q_stride, uint64_t q_width, uint64_t n) {
+    if (!n || !p_width || !q_width) return false;
     const uint64_t a = (uint64_t)(uintptr_t)p / 2, b = (uint64_t)(uintptr_t)q / 2;
-    if (a + (n - 1) * p_stride + width <= b || b + (n - 1) * q_stride + width <= a) return false;
+    if (a > b) return rows_overlap(q, q_stride, q_width, p, p_stride, p_width, n);
+    if (a + (n - 1) * p_stride + p_width <= b || b + (n - 1) * q_stride + q_width <= a) return false;
     if (p_stride != q_stride || n == 1) return true;
-    const uint64_t d = a < b ? b - a : a - b, rows = d / p_stride, rest = d % p_stride;
-    return (rest < width && rows < n) || (p_stride - rest < width && rows + 1 < n);
+    const uint64_t rows = (b - a) / p_stride, rest = (b - a) % p_stride;
+    return (rest < p_width && rows < n) || (p_stride - rest < q_width && rows + 1 < n);
+}
+inline bool rows_overlap(const void *p, uint64_t p_stride, const void *q, uint64_t q_stride, uint64_t width, uint64_t n) {
+    return rows_overlap(p, p_stride, width, q, q_stride, width, n);
 }
 
 }  // namespace blockplan
