@@ -548,6 +548,56 @@ netkv_status netkv_kv_store(netkv_handle h, const netkv_kv_t *kv, const netkv_kv
 netkv_status netkv_kv_read(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, void *k,
                            uint64_t k_stride, void *v, uint64_t v_stride, int dtype, void *stream);
 
+/* Rotary positions: of a head's first rot_dim elements, pair i -- elements i and
+ * i + rot_dim / 2, or 2 i and 2 i + 1 if interleaved -- turns by the angle that
+ * the table has for it at its axis's position:
+ *     (a, b) -> (a cos - b sin, b cos + a sin).
+ * The other elements stay as they are.  With several axes (text 1; an image's
+ * rows and columns; a video's time, height and width) axis[i] is pair i's. */
+typedef struct {
+    uint32_t rot_dim;               /* a multiple of 16, 16 .. 256, at most the head's dimension */
+    uint32_t n_pos;                 /* positions 0 .. n_pos - 1 have a row of the table, >= 1 */
+    uint32_t n_axes;                /* 1 .. 4 */
+    uint32_t interleaved;           /* 0 or 1 */
+    const float *table;             /* DEVICE [n_pos][rot_dim]: rot_dim / 2 cosines, then as many
+                                       sines (any factors: a scaled rotation has them scaled);
+                                       16-byte aligned */
+    const uint8_t *axis;            /* HOST [rot_dim / 2], each < n_axes; NULL: all 0 (one axis) */
+} netkv_rope_t;
+
+/* Rotate the heads of n_rows rows x ([n_rows][n_heads][head_dim] of dtype, strides
+ * in elements and alignment as for netkv_kv_store) into out, which may be x
+ * itself (the same address and stride), else they must not overlap (EINVAL).
+ * Row r's position on axis i is pos[i * pos_stride + r] (DEVICE, pos_stride >=
+ * n_rows with several axes); a position >= n_pos makes its pairs NaN and is
+ * reported by netkv_sync_errors.  transpose: by the negative angles, which is the
+ * gradient of the rotation for x from that for out.  Each output is
+ * a c +- b s to 2^-23 of it, rounded once to dtype, also where the products
+ * cancel (down to 2^-149).  head_dim: a multiple of 8 from 16 to 1024.  Any order
+ * of pos; needs no loads.  Asynchronous; allocates nothing.  ECAPACITY: more than
+ * 2^32 - 1 threads, in workgroups of 256. */
+netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *rope, uint64_t n_rows, const uint32_t *pos,
+                               uint64_t pos_stride, const void *x, uint64_t x_stride, void *out,
+                               uint64_t out_stride, uint32_t n_heads, uint32_t head_dim, int dtype, int transpose,
+                               void *stream);
+
+/* A step's rows into the cache with the rotation on the way: q rotated into
+ * q_out as by netkv_rope_rotate ([n_tok][n_heads][head_dim]; n_heads 0: none, q and q_out are
+ * not looked at), k rotated and v as it is stored as by netkv_kv_store.  A rotated
+ * key is rounded once, from a c +- b s in 64 bits to its 8 bits, and the scale is
+ * that of the unrounded keys.  pos as for netkv_rope_rotate, for the rows of the
+ * token arrays; NULL: a row's position on every axis is its token's place in its
+ * sequence (0 for the first).  A position >= n_pos is reported, and its pairs are
+ * NaN in q_out and in the cache.  q_out may be q itself; else it must not
+ * overlap q, k or v (EINVAL).  Sequences that netkv_kv_store leaves out are left
+ * out, their rows of q_out and those past the last sequence left as they were.
+ * Time, capacity and all else as for netkv_kv_store, and a workgroup of 256 or
+ * more threads for each of up to 16 query rows. */
+netkv_status netkv_kv_append(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
+                             const netkv_rope_t *rope, const uint32_t *pos, uint64_t pos_stride, const void *q,
+                             uint32_t n_heads, uint64_t q_stride, void *q_out, uint64_t q_out_stride, const void *k,
+                             uint64_t k_stride, const void *v, uint64_t v_stride, int dtype, void *stream);
+
 /* Attention of the sequences' last rows over their cached tokens, the rows'
  * own tokens among them (store first): row t of the n rows of a sequence
  * with c tokens sees tokens 0 .. c - n + t (causal), and

@@ -1,0 +1,436 @@
+// Rotary positions on MI355X (gfx950): rows of heads rotated, and a step's
+// queries, keys and values taken into the block cache with the rotation on the
+// way.
+//
+//   rotate_kernel  -- rows of heads, each pair turned by its position's angle.
+//   append_kernel  -- the sequences' new queries rotated, their keys rotated and
+//                     quantised into their blocks, their values quantised.
+//
+// A pair (a, b) of a head becomes (a cos - b sin, b cos + a sin); the cosines
+// and sines come from a table with a row for every position, and a pair's
+// position is that of its axis.  The work is in units of 16 elements: eight
+// pairs, in two pieces of eight elements, which lie half of the rotated
+// elements apart or, interleaved, side by side.
+
+#include <hip/hip_runtime.h>
+
+#include "blockstore.h"
+#include "ropeplan.h"
+
+namespace {
+
+using namespace blockdev;
+using namespace ropeplan;
+
+// What a rotation is made of, as the kernels see it.
+struct Turn {
+    const float *table;               // [n_pos][2 pairs]: cosines, sines
+    const uint32_t *pos;              // [axis][row]; null: a row's place in its sequence
+    uint64_t pos_stride;
+    uint32_t n_pos, pairs;
+    uint32_t interleaved;
+    uint32_t sign;                    // flips the sines' signs: the transposed rotation
+    uint32_t axes[kMaxPairs / 16];    // two bits a pair
+    uint32_t *err;
+};
+
+// cos and sin of a unit's eight pairs
+struct Angles {
+    float c[8], s[8];
+};
+
+// Positions past the table make their pairs NaN.
+__device__ inline void load_angles(const Turn &t, uint64_t row, uint32_t place, uint32_t u, Angles &a) {
+    const uint32_t which = t.axes[u >> 1] >> (16 * (u & 1)) & 0xFFFFu;
+    auto position = [&](uint32_t axis) { return t.pos ? t.pos[axis * t.pos_stride + row] : place; };
+    const uint32_t first = which & 3;
+    bool bad = false;
+    if (which == first * 0x5555u) {
+        const uint32_t p = position(first);
+        bad = p >= t.n_pos;
+        const float *at = t.table + (uint64_t)(bad ? 0u : p) * 2 * t.pairs + 8 * u;
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const f32x4 x = *(const f32x4 *)(at + i), y = *(const f32x4 *)(at + t.pairs + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                a.c[i + j] = bad ? NAN : x[j];
+                a.s[i + j] = bad ? NAN : y[j];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t p = position(which >> (2 * i) & 3);
+            const bool out = p >= t.n_pos;
+            const float *at = t.table + (uint64_t)(out ? 0u : p) * 2 * t.pairs + 8 * u + i;
+            a.c[i] = out ? NAN : at[0];
+            a.s[i] = out ? NAN : at[t.pairs];
+            bad |= out;
+        }
+    }
+    if (bad) atomicOr(t.err, kErrBlockBit);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a.s[i] = __uint_as_float(__float_as_uint(a.s[i]) ^ t.sign);
+}
+
+// The 16 elements of a unit's two pieces as eight pairs, and back.
+__device__ inline uint32_t half_of(const u32x4 &x, int i) { return x[i / 2] >> (16 * (i & 1)) & 0xFFFFu; }
+
+struct Pairs {
+    float a[8], b[8];
+};
+
+__device__ inline void to_pairs(const u32x4 &lo, const u32x4 &hi, bool half, bool interleaved, Pairs &p) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const u32x4 &x = i < 4 ? lo : hi;
+        const uint32_t a = interleaved ? x[i & 3] & 0xFFFFu : half_of(lo, i), b = interleaved ? x[i & 3] >> 16 : half_of(hi, i);
+        p.a[i] = to_f32(a, half);
+        p.b[i] = to_f32(b, half);
+    }
+}
+
+__device__ inline uint32_t pack16(float x, float y, bool half) {
+    const f32x2 p = {x, y};
+    return half ? __builtin_bit_cast(uint32_t, __builtin_convertvector(p, f16x2)) : __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2));
+}
+
+// a c - b s of 16-bit a, b to 1.5 units of fp32's last place, also where the
+// products cancel: what the first product loses comes back.
+__device__ inline float cross(float a, float c, float b, float s) {
+    const float w = b * s, e = fmaf(b, s, -w), t = fmaf(a, c, -w);
+    return e == e ? t - e : t;        // w not finite
+}
+
+// A double to fp32, to odd where it is not exact: what is rounded from there to
+// 8 bits is as if rounded once.
+__device__ inline float to_odd(double x) {
+    const float f = (float)x;
+    uint32_t u = __float_as_uint(f);
+    if ((double)f != x) {
+        if (fabs((double)f) > fabs(x)) --u;
+        u |= 1;
+    }
+    return __uint_as_float(u);
+}
+
+// ------------------------------------------------------------------ rows
+
+struct RowArgs {
+    Turn turn;
+    const uint16_t *x;
+    uint16_t *out;
+    uint64_t x_stride, out_stride;
+    uint32_t heads, dim;
+    uint32_t units;                   // a head's: those that turn, and those copied
+    uint32_t part;                    // heads a thread takes, one after the other
+    uint32_t half;
+};
+
+// Rows [row, row + n) of the arrays; a row's position is `place` and on if the
+// turn has none of its own.
+__device__ inline void rotate_rows(const RowArgs &a, uint64_t row, uint32_t n, uint32_t place) {
+    const uint32_t parts = (a.heads + a.part - 1) / a.part;
+    const uint32_t each = parts * a.units;
+    for (uint32_t i = threadIdx.x; i < n * each; i += blockDim.x) {
+        const uint32_t t = i / each, u = i % each % a.units, h0 = i % each / a.units * a.part;
+        const uint32_t heads = min(a.part, a.heads - h0);
+        const Unit p = unit_of(u, a.turn.pairs, a.turn.interleaved, a.dim);
+        const uint16_t *x = a.x + (row + t) * a.x_stride + (uint64_t)h0 * a.dim;
+        uint16_t *out = a.out + (row + t) * a.out_stride + (uint64_t)h0 * a.dim;
+        if (!p.turns) {
+            for (uint32_t h = 0; h < heads; ++h) {
+                *(u32x4 *)(out + h * a.dim + p.lo) = *(const u32x4 *)(x + h * a.dim + p.lo);
+                if (p.both) *(u32x4 *)(out + h * a.dim + p.hi) = *(const u32x4 *)(x + h * a.dim + p.hi);
+            }
+            continue;
+        }
+        Angles g;
+        load_angles(a.turn, row + t, place + t, u, g);
+        for (uint32_t h = 0; h < heads; ++h) {
+            const u32x4 xl = *(const u32x4 *)(x + h * a.dim + p.lo), xh = *(const u32x4 *)(x + h * a.dim + p.hi);
+            Pairs e;
+            to_pairs(xl, xh, a.half, a.turn.interleaved, e);
+            float y[8], z[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                y[j] = cross(e.a[j], g.c[j], e.b[j], g.s[j]);
+                z[j] = cross(e.b[j], g.c[j], e.a[j], -g.s[j]);
+            }
+            u32x4 yl, yh;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (a.turn.interleaved) {
+                    yl[j] = pack16(y[j], z[j], a.half);
+                    yh[j] = pack16(y[4 + j], z[4 + j], a.half);
+                } else {
+                    yl[j] = pack16(y[2 * j], y[2 * j + 1], a.half);
+                    yh[j] = pack16(z[2 * j], z[2 * j + 1], a.half);
+                }
+            }
+            *(u32x4 *)(out + h * a.dim + p.lo) = yl;
+            *(u32x4 *)(out + h * a.dim + p.hi) = yh;
+        }
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void rotate_kernel(RowArgs a, uint32_t rows, uint32_t chunk) {
+    const uint32_t row = blockIdx.x * chunk;
+    rotate_rows(a, row, min(chunk, rows - row), 0);
+}
+
+// ------------------------------------------------------------------ append
+
+struct AppendArgs {
+    MoveArgs move;
+    RowArgs rows;                     // the queries
+    uint32_t chunk;                   // of rows that a workgroup rotates
+    uint32_t row_tasks, store_tasks;  // workgroups for the queries, for each head's keys and values
+};
+
+// One workgroup rotates the keys of one head that a call brings to one block
+// and quantises them, as store_block does values.  A rotated key is computed in
+// 64 bits, where the products of 16-bit elements and 32-bit cosines are exact,
+// and rounded once, to 8 bits: in fp32 one in some hundred thousand would
+// come out a step off, and a block's scale by a factor of two.
+template <int D, int THREADS>
+__device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, uint32_t h) {
+    constexpr int kEach = 4;                                  // units a thread keeps
+    constexpr uint32_t kUnits = D / 16;                       // of a token
+    __shared__ uint32_t red[THREADS / 64];
+    const Kv &kv = g.move.kv;
+    const Turn &turn = g.rows.turn;
+    Place pl;
+    if (!find_place(kv, task, pl)) return;
+    const uint64_t at = (uint64_t)pl.page * kv.hk + h;
+    uint8_t *dst = kv.k + at * head_bytes(kv, D);
+    const uint16_t *src = (const uint16_t *)g.move.k + (uint64_t)h * D;
+    const uint32_t units = (pl.p1 - pl.p0) * kUnits, turning = turn.pairs / 8, half = g.rows.half;
+
+    float x[kEach][16];
+    auto unit = [&](uint32_t e) { return unit_of(e % kUnits, turn.pairs, turn.interleaved, D); };
+    auto load = [&](uint32_t base) {
+        u32x4 lo[kEach], hi[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t e = base + i * THREADS + threadIdx.x;
+            lo[i] = hi[i] = u32x4{0, 0, 0, 0};
+            if (e >= units) continue;
+            const uint16_t *p = src + (pl.row0 + e / kUnits) * g.move.k_stride;
+            const Unit w = unit(e);
+            lo[i] = *(const u32x4 *)(p + w.lo);
+            hi[i] = *(const u32x4 *)(p + w.hi);
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t e = base + i * THREADS + threadIdx.x, t = e / kUnits, u = e % kUnits;
+            if (e >= units || u >= turning) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x[i][j] = to_f32(half_of(lo[i], j), half);
+                    x[i][8 + j] = to_f32(half_of(hi[i], j), half);
+                }
+                continue;
+            }
+            Angles a;
+            Pairs p;
+            load_angles(turn, pl.row0 + t, pl.token + t, u, a);
+            to_pairs(lo[i], hi[i], half, turn.interleaved, p);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const double c = a.c[j], s = a.s[j], pa = p.a[j], pb = p.b[j];
+                const float y = to_odd(fma(pa, c, -(pb * s))), z = to_odd(fma(pb, c, pa * s));
+                if (turn.interleaved) {
+                    x[i][2 * j] = y;
+                    x[i][2 * j + 1] = z;
+                } else {
+                    x[i][j] = y;
+                    x[i][8 + j] = z;
+                }
+            }
+        }
+    };
+    // the largest finite value, by its bits
+    uint32_t top = 0;
+    for (uint32_t base = 0; base < units; base += THREADS * kEach) {
+        load(base);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const uint32_t z = __float_as_uint(x[i][j]) & 0x7FFFFFFFu;
+                top = max(top, z < 0x7F800000u ? z : 0u);
+            }
+    }
+    for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor(top, d, 64));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int i = 0; i < THREADS / 64; ++i) top = max(top, red[i]);
+
+    float *scale = kv.ks + at;
+    float sc = scale_for(__uint_as_float(top));
+    if (pl.p0) {
+        const float was = *scale;
+        sc = was > sc ? was : sc;
+        if (was != sc) {
+            const float ratio = was / sc;
+            for (uint32_t i = threadIdx.x; i < pl.p0 * (D / 4); i += THREADS) ((uint32_t *)dst)[i] = rescale4(((uint32_t *)dst)[i], ratio);
+        }
+    }
+    __syncthreads();   // every thread has read the old scale
+    if (threadIdx.x == 0) *scale = sc;
+    const float inv = 1.0f / sc;
+    for (uint32_t base = 0; base < units; base += THREADS * kEach) {
+        if (units > THREADS * kEach) load(base);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t e = base + i * THREADS + threadIdx.x;
+            if (e >= units) continue;
+            uint8_t *p = dst + (uint64_t)(pl.p0 + e / kUnits) * D;
+            const Unit w = unit(e);
+            *(u32x2 *)(p + w.lo) = u32x2{narrow4(x[i], inv), narrow4(x[i] + 4, inv)};
+            *(u32x2 *)(p + w.hi) = u32x2{narrow4(x[i] + 8, inv), narrow4(x[i] + 12, inv)};
+        }
+    }
+}
+
+// The queries of up to `chunk` rows of one sequence.
+__device__ inline void append_queries(const AppendArgs &a, uint32_t task) {
+    const Kv &kv = a.move.kv;
+    uint32_t rest;
+    const uint32_t s = locate(kv, task, [&](const Head &h) { return row_chunks(h, a.chunk); }, &rest);
+    if (s >= kv.n_seq) return;
+    const Head h = seq_head(kv, s);
+    const uint32_t t = rest * a.chunk;
+    rotate_rows(a.rows, h.row0 + t, min(a.chunk, h.n - t), h.ctx - h.n + t);
+}
+
+template <int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a) {
+    if (blockIdx.x < a.row_tasks) {
+        append_queries(a, blockIdx.x);
+        return;
+    }
+    const uint32_t i = blockIdx.x - a.row_tasks, task = i % a.store_tasks, r = i / a.store_tasks, h = r % a.move.kv.hk;
+    const bool vals = r >= a.move.kv.hk;
+    if (r == 0) report_bad(a.move.kv, task, a.store_tasks);
+    if (vals)
+        store_block<D, THREADS>(a.move, a.rows.half, task, h, true);
+    else
+        append_keys<D, THREADS>(a, task, h);
+}
+
+// ------------------------------------------------------------------ host
+
+netkv_status make_turn(netkv_handle h, const netkv_rope_t *rope, uint32_t head_dim, const uint32_t *pos, uint64_t pos_stride,
+                       uint64_t rows, bool need_pos, Turn &t) {
+    if (const char *why = rope_error(rope, head_dim, pos, pos_stride, rows, need_pos)) return invalid(h, why);
+    t.table = rope->table;
+    t.pos = pos;
+    t.pos_stride = pos_stride;
+    t.n_pos = rope->n_pos;
+    t.pairs = rope->rot_dim / 2;
+    t.interleaved = rope->interleaved;
+    for (uint32_t i = 0; rope->axis && i < t.pairs; ++i) t.axes[i / 16] |= (uint32_t)rope->axis[i] << (2 * (i % 16));
+    t.err = netkv_internal_errword(h);
+    return NETKV_OK;
+}
+
+}  // namespace
+
+extern "C" netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *rope, uint64_t n_rows, const uint32_t *pos,
+                                          uint64_t pos_stride, const void *x, uint64_t x_stride, void *out, uint64_t out_stride,
+                                          uint32_t n_heads, uint32_t head_dim, int dtype, int transpose, void *stream) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    if (dtype != NETKV_BF16 && dtype != NETKV_FP16) return invalid(h, "dtype must be NETKV_BF16 or NETKV_FP16");
+    if (head_dim < 16 || head_dim % 8 || head_dim > 1024) return invalid(h, "head_dim must be a multiple of 8 from 16 to 1024");
+    if (n_heads < 1 || n_heads > 65535) return invalid(h, "n_heads must be in [1, 65535]");
+    if (n_rows > (1ull << 31)) return invalid(h, "n_rows must be <= 2^31");
+    RowArgs a{};
+    netkv_status st = make_turn(h, rope, head_dim, pos, pos_stride, n_rows, true, a.turn);
+    if (st != NETKV_OK) return st;
+    const uint64_t width = (uint64_t)n_heads * head_dim;
+    if ((st = check_rows(h, x, x_stride, width, n_rows, "x must be 16-byte aligned, its stride a multiple of 8 and at least a row's elements")) != NETKV_OK) return st;
+    if ((st = check_rows(h, out, out_stride, width, n_rows, "out must be 16-byte aligned, its stride a multiple of 8 and at least a row's elements")) != NETKV_OK) return st;
+    const bool in_place = x == out && x_stride == out_stride;
+    if (!in_place && rows_overlap(x, x_stride, out, out_stride, width, n_rows)) return invalid(h, "out must not overlap x (it may be x itself)");
+    if (n_rows == 0) return NETKV_OK;
+    a.turn.sign = transpose ? 0x80000000u : 0u;
+    a.x = (const uint16_t *)x;
+    a.out = (uint16_t *)out;
+    a.x_stride = x_stride;
+    a.out_stride = out_stride;
+    a.heads = n_heads;
+    a.dim = head_dim;
+    a.half = dtype == NETKV_FP16;
+    a.units = units_of(a.turn.pairs, head_dim, in_place);
+    a.part = part_of(n_rows, n_heads, a.units);
+    const uint64_t each = (uint64_t)((n_heads + a.part - 1) / a.part) * a.units;
+    const uint32_t chunk = (uint32_t)(each >= kThreads ? 1 : kThreads / each);
+    const uint64_t groups = (n_rows + chunk - 1) / chunk;
+    if (!grid_fits(groups, kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many rows for one call");
+    DeviceScope scope(netkv_internal_device(h));
+    rotate_kernel<<<(uint32_t)groups, kThreads, 0, (hipStream_t)stream>>>(a, (uint32_t)n_rows, chunk);
+    return launched(h, "rotation launch failed");
+}
+
+extern "C" netkv_status netkv_kv_append(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const netkv_rope_t *rope,
+                                        const uint32_t *pos, uint64_t pos_stride, const void *q, uint32_t n_heads,
+                                        uint64_t q_stride, void *q_out, uint64_t q_out_stride, const void *k, uint64_t k_stride,
+                                        const void *v, uint64_t v_stride, int dtype, void *stream) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    AppendArgs a{};
+    Kv &kv_ = a.move.kv;
+    netkv_status st = make_kv(h, kv, seqs, kv_);
+    if (st != NETKV_OK) return st;
+    if (dtype != NETKV_BF16 && dtype != NETKV_FP16) return invalid(h, "dtype must be NETKV_BF16 or NETKV_FP16");
+    if ((st = make_turn(h, rope, kv->head_dim, pos, pos_stride, kv_.n_tok, false, a.rows.turn)) != NETKV_OK) return st;
+    const uint64_t width = (uint64_t)kv->n_kv_heads * kv->head_dim, q_width = (uint64_t)n_heads * kv->head_dim;
+    if ((st = check_rows(h, k, k_stride, width, kv_.n_tok, "k must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    if ((st = check_rows(h, v, v_stride, width, kv_.n_tok, "v must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    bool in_place = false;
+    if (n_heads) {
+        if (n_heads > 65535) return invalid(h, "n_heads must be <= 65535");
+        if ((st = check_rows(h, q, q_stride, q_width, kv_.n_tok, "q must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+        if ((st = check_rows(h, q_out, q_out_stride, q_width, kv_.n_tok, "q_out must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+        in_place = q == q_out && q_stride == q_out_stride;
+        if (!in_place && rows_overlap(q, q_stride, q_out, q_out_stride, q_width, kv_.n_tok)) return invalid(h, "q_out must not overlap q (it may be q itself)");
+        if (rows_overlap(k, k_stride, width, q_out, q_out_stride, q_width, kv_.n_tok) || rows_overlap(v, v_stride, width, q_out, q_out_stride, q_width, kv_.n_tok))
+            return invalid(h, "q_out must not overlap k or v");
+    }
+    if (kv_.n_seq == 0 || kv_.n_tok == 0) return NETKV_OK;
+    a.move.k = k;
+    a.move.v = v;
+    a.move.k_stride = k_stride;
+    a.move.v_stride = v_stride;
+    RowArgs &r = a.rows;
+    r.half = dtype == NETKV_FP16;
+    uint64_t row_tasks = 0;
+    if (n_heads) {
+        r.x = (const uint16_t *)q;
+        r.out = (uint16_t *)q_out;
+        r.x_stride = q_stride;
+        r.out_stride = q_out_stride;
+        r.heads = n_heads;
+        r.dim = kv->head_dim;
+        r.units = units_of(r.turn.pairs, kv->head_dim, in_place);
+        r.part = part_of(kv_.n_tok, n_heads, r.units);
+        a.chunk = kv_.max_tok < 16 ? 1 : 16;
+        row_tasks = row_groups(kv_, a.chunk);
+    }
+    const uint64_t tasks = store_groups(kv_), groups = row_tasks + tasks * kv_.hk * 2;
+    if (!grid_fits(groups, kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many rows for one call");
+    a.row_tasks = (uint32_t)row_tasks;
+    a.store_tasks = (uint32_t)tasks;
+    DeviceScope scope(netkv_internal_device(h));
+    hipStream_t s = (hipStream_t)stream;
+    switch (kv->head_dim) {
+        case 64: append_kernel<64, kThreads><<<(uint32_t)groups, kThreads, 0, s>>>(a); break;
+        case 128: append_kernel<128, kThreads><<<(uint32_t)groups, kThreads, 0, s>>>(a); break;
+        default: append_kernel<256, kThreads><<<(uint32_t)groups, kThreads, 0, s>>>(a); break;
+    }
+    return launched(h, "append launch failed");
+}

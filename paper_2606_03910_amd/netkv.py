@@ -13,7 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, Optional
+from typing import Dict, Iterable, Optional
 
 import numpy as np
 import torch
@@ -60,6 +60,11 @@ class netkv_kv_t(C.Structure):
 class netkv_kv_seqs_t(C.Structure):
     _fields_ = [("n_seq", C.c_uint32), ("max_pages", C.c_uint32), ("n_tok", C.c_uint64), ("max_tok", C.c_uint64),
                 ("tok_off", C.c_void_p), ("ctx_len", C.c_void_p), ("pages", C.c_void_p)]
+
+
+class netkv_rope_t(C.Structure):
+    _fields_ = [("rot_dim", C.c_uint32), ("n_pos", C.c_uint32), ("n_axes", C.c_uint32), ("interleaved", C.c_uint32),
+                ("table", C.c_void_p), ("axis", C.c_void_p)]
 
 
 class netkv_pairs_t(C.Structure):
@@ -119,6 +124,13 @@ _SIGS = {
                                     C.c_uint64, C.c_void_p]),
     "netkv_kv_attend_workspace": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_t), C.POINTER(netkv_kv_seqs_t),
                                               C.c_uint32, C.c_int, C.POINTER(C.c_uint64)]),
+    "netkv_rope_rotate": (C.c_int32, [C.c_void_p, C.POINTER(netkv_rope_t), C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p,
+                                      C.c_uint64, C.c_void_p, C.c_uint64, C.c_uint32, C.c_uint32, C.c_int, C.c_int,
+                                      C.c_void_p]),
+    "netkv_kv_append": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_t), C.POINTER(netkv_kv_seqs_t),
+                                    C.POINTER(netkv_rope_t), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint32, C.c_uint64,
+                                    C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_int,
+                                    C.c_void_p]),
     "netkv_kv_weigh": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_seqs_t), C.c_uint32, C.c_void_p, C.c_uint32,
                                    C.c_void_p, C.c_void_p]),
     "netkv_cache_evict": (C.c_int32, [C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p,
@@ -503,6 +515,84 @@ def netkv_kv_read(h: int, kv: netkv_kv_t, seqs: Sequences, k: torch.Tensor, v: t
                                            _stream(device)))
 
 
+class Rope:
+    """A rotation by positions (netkv_rope_t) on the device of `sel`'s handle:
+    table f32[n_pos][rot_dim], rot_dim / 2 cosines and as many sines of every
+    position; axis: each pair's (a sequence of rot_dim / 2 numbers below 4), all
+    of one axis if None; interleaved: pairs of neighbours, else of halves.  A
+    program keeps it for all layers and steps."""
+
+    def __init__(self, sel: "Selector", table: torch.Tensor, axis: Optional[Iterable[int]] = None,
+                 interleaved: bool = False):
+        c = netkv_rope_t()
+        c.table = _dptr(table, torch.float32, None, "table")
+        _on_all(sel.device, table=table)
+        if table.dim() != 2:
+            raise ValueError(f"table must be [n_pos][rot_dim], not {list(table.shape)}")
+        c.n_pos, c.rot_dim, c.n_axes, c.interleaved = int(table.shape[0]), int(table.shape[1]), 1, int(bool(interleaved))
+        axes = None
+        if axis is not None:
+            which = [int(x) for x in axis]
+            if len(which) != c.rot_dim // 2 or any(x < 0 or x > 3 for x in which):
+                raise ValueError(f"axis must be {c.rot_dim // 2} numbers from 0 to 3")
+            axes = (C.c_uint8 * len(which))(*which)
+            c.axis, c.n_axes = C.addressof(axes), 1 + max(which, default=0)
+        self.sel, self.c, self.device = sel, c, sel.device
+        self._held = (table, axes)
+
+    def rotate(self, x: torch.Tensor, pos: torch.Tensor, out: Optional[torch.Tensor] = None,
+               transpose: bool = False) -> torch.Tensor:
+        """The heads of rows x [n][heads][dim] turned by their positions pos
+        u32[n_axes][n] (or [n]), or the other way (the gradient for x from that
+        for out).  out may be x itself."""
+        if out is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        netkv_rope_rotate(self.sel.h, self.c, x, pos, out, transpose, self.device)
+        return out
+
+
+def _positions(pos: Optional[torch.Tensor], rope: netkv_rope_t, rows: int, device):
+    """Address and axis stride of positions [n_axes][rows]."""
+    if pos is None:
+        return None, 0
+    p = _dptr(pos, torch.uint32, None, "pos")
+    _on(pos, device, "pos")
+    shape = tuple(pos.shape) if pos.dim() == 2 else (1, pos.numel())
+    if pos.dim() not in (1, 2) or shape[0] < rope.n_axes or shape[1] < rows:
+        raise ValueError(f"pos must be [{rope.n_axes}][{rows}], not {list(pos.shape)}")
+    return p, int(shape[1])
+
+
+def netkv_rope_rotate(h: int, rope: netkv_rope_t, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor, transpose: bool,
+                      device) -> None:
+    n, heads, dim = (int(v) for v in x.shape) if x.dim() == 3 else (0, 0, 0)
+    xp, xs = _rows(x, n, heads, dim, device, "x")
+    op, os_ = _rows(out, n, heads, dim, device, "out")
+    if x.dtype != out.dtype:
+        raise TypeError("x and out must have one dtype")
+    pp, ps = _positions(pos, rope, n, device)
+    _check(h, load_library().netkv_rope_rotate(h, C.byref(rope), n, pp, ps, xp, xs, op, os_, heads, dim, _DTYPE[x.dtype],
+                                               int(bool(transpose)), _stream(device)))
+
+
+def netkv_kv_append(h: int, kv: netkv_kv_t, seqs: Sequences, rope: netkv_rope_t, pos: Optional[torch.Tensor],
+                    q: Optional[torch.Tensor], q_out: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                    device) -> None:
+    _on(seqs, device, "the sequences")
+    kp, ks = _rows(k, seqs.n_tok, kv.n_kv_heads, kv.head_dim, device, "k")
+    vp, vs = _rows(v, seqs.n_tok, kv.n_kv_heads, kv.head_dim, device, "v")
+    heads, qp, qs, op, os_ = 0, None, 0, None, 0
+    if q is not None:
+        heads = int(q.shape[1]) if q.dim() == 3 else 0
+        qp, qs = _rows(q, seqs.n_tok, heads, kv.head_dim, device, "q")
+        op, os_ = _rows(q_out, seqs.n_tok, heads, kv.head_dim, device, "q_out")
+    if len({t.dtype for t in (q, q_out, k, v) if t is not None}) > 1:
+        raise TypeError("q, q_out, k and v must have one dtype")
+    pp, ps = _positions(pos, rope, seqs.n_tok, device)
+    _check(h, load_library().netkv_kv_append(h, C.byref(kv), C.byref(seqs.c), C.byref(rope), pp, ps, qp, heads, qs, op, os_,
+                                             kp, ks, vp, vs, _DTYPE[k.dtype], _stream(device)))
+
+
 def netkv_kv_attend_workspace(h: int, kv: netkv_kv_t, seqs: Sequences, n_heads: int, weights: bool) -> int:
     n = C.c_uint64()
     _check(h, load_library().netkv_kv_attend_workspace(h, C.byref(kv), C.byref(seqs.c), int(n_heads), int(bool(weights)),
@@ -791,6 +881,18 @@ class BlockCache:
         """Quantise the sequences' new tokens [n_tok][n_kv_heads][head_dim]
         into their blocks."""
         netkv_kv_store(self.sel.h, self.c, seqs, k, v, self.device)
+
+    def append(self, seqs: Sequences, rope: Rope, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+               pos: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """Rotate the sequences' new queries q [n_tok][n_heads][head_dim] and keys
+        by their positions and quantise keys and values into their blocks, in one
+        call; returns the rotated queries (out, which may be q itself).  pos
+        u32[n_axes][n_tok]; None: each token's place in its sequence."""
+        if q is not None and out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        _on(rope, self.device, "the rotation")
+        netkv_kv_append(self.sel.h, self.c, seqs, rope.c, pos, q, out if q is not None else None, k, v, self.device)
+        return out if q is not None else None
 
     def read(self, seqs: Sequences, dtype: torch.dtype = torch.bfloat16):
         """(k, v) [n_tok][n_kv_heads][head_dim] of the sequences' last tokens."""
