@@ -641,6 +641,36 @@ netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, const netkv_k
 netkv_status netkv_kv_attend_workspace(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
                                        uint32_t n_heads, int weights, uint64_t *bytes);
 
+/* Differential attention of the sequences' last rows over their cached tokens:
+ * the difference of two softmax maps.  KV heads 2 p and 2 p + 1 are a pair: each
+ * has its own keys, and their values side by side are the pair's, v of 2 head_dim
+ * elements.  Query heads 2 j and 2 j + 1 are query pair j, which reads KV pair
+ * j / (n_heads / n_kv_heads):
+ *     o_j = softmax(scale q_2j k_2p) v - lambda_j softmax(scale q_2j+1 k_2p+1) v,
+ *     out_j = gain norm o_j / sqrt(mean(o_j^2) + eps)    (norm NULL: gain o_j),
+ * which rows see what as for netkv_kv_attend.  out [n_tok][n_heads / 2][2 head_dim]:
+ * a token has as many elements as in q.  n_kv_heads even, head_dim 64 or 128,
+ * n_heads a multiple of n_kv_heads (at most 64 times).  lambda: DEVICE
+ * f32[n_heads / 2]; norm: DEVICE f32[2 head_dim], 16-byte aligned, or NULL; eps > 0 with a
+ * norm.  q, out, scale, work, rows of invalid sequences, rows that see nothing
+ * and all else as for netkv_kv_attend, and its rounding: a pair's weights are multiplied
+ * by the larger of its two value scales of a page before they are rounded to 11
+ * bits, the values of the other head by the ratio of the scales, exactly where
+ * that is a power of two from 2^-15 on, else to 11 bits and 2^-25 of the larger scale.  The
+ * maps' difference and the norm are fp32, and out is rounded once.  No block
+ * weights, no gradient.  One form for the call, by max_tok * n_heads /
+ * n_kv_heads rows (more than 96 or 32 at head_dim 64 or 128: the form for
+ * prompts). */
+netkv_status netkv_kv_attend_diff(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *q,
+                                  int dtype, uint32_t n_heads, uint64_t q_stride, float scale, const float *lambda,
+                                  const float *norm, float eps, float gain, void *out, uint64_t out_stride,
+                                  void *work, uint64_t work_bytes, void *stream);
+
+/* Bytes of work for a netkv_kv_attend_diff of these shapes, from the host values
+ * only: at most 300 MB. */
+netkv_status netkv_kv_attend_diff_workspace(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
+                                            uint32_t n_heads, uint64_t *bytes);
+
 /* Add block weights (as netkv_kv_attend gives them) to the weights of their
  * pages, page_weight u64[n_pages] (DEVICE), in units of 2^-24 and rounded to
  * the nearest one: integer sums, so pages shared between sequences come out

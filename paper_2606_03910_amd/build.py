@@ -9,7 +9,8 @@ ROOT = os.path.dirname(HERE)
 SRC = os.path.join(HERE, "csrc", "netkv.hip")
 # the selection path and the handle; the flow-level transfer simulation; the
 # decode instance's block cache, rotary positions and the eviction
-SOURCES = [SRC] + [os.path.join(HERE, "csrc", f) for f in ("flowsim.hip", "blockcache.hip", "append.hip", "evict.hip")]
+SOURCES = [SRC] + [os.path.join(HERE, "csrc", f) for f in ("flowsim.hip", "blockcache.hip", "diffattend.hip", "append.hip",
+                                                           "evict.hip")]
 LIB = os.path.join(HERE, "libnetkv.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

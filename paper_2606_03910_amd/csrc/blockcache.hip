@@ -98,6 +98,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     fill_bad(a);
 }
 
+}  // namespace
+
+void blockdev::launch_plan(const PlanArgs &a, hipStream_t s) { plan_kernel<<<1, kPlanThreads, 0, s>>>(a); }
+
+namespace {
+
 // ------------------------------------------------------------------ attention
 
 struct AttendArgs : PlanArgs {
@@ -1522,7 +1528,7 @@ extern "C" netkv_status netkv_kv_attend(netkv_handle h, const netkv_kv_t *kv, co
         t.head = (PlanHead *)(ws + y.head);
         t.items = (Item *)(ws + y.items);
         t.joins = (Join *)(ws + y.joins);
-        plan_kernel<<<1, kPlanThreads, 0, s>>>(t);
+        launch_plan(t, s);
     }
     t.Hq = n_heads;
     t.q_stride = q_stride;

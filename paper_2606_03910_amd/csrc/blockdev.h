@@ -173,6 +173,9 @@ struct PlanArgs : Split {
 
 constexpr uint32_t kListed = 256;
 
+// Starts plan_kernel for a call of more sequences than kListed.
+void launch_plan(const PlanArgs &a, hipStream_t s);
+
 constexpr int kPlanThreads = 1024;
 
 // Exclusive scan of three counts over the workgroup; totals in tot.

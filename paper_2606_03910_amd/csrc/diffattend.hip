@@ -1,0 +1,1137 @@
+// Differential attention over the block cache on MI355X (gfx950): the
+// difference of two softmax maps over one head's values, of twice the keys'
+// dimension.
+//
+//   pair_kernel         -- up to 16 rows over a token range.
+//   pair_prompt_kernel  -- the same of up to 128 or 64 rows.
+//   pair_join_kernel    -- joins the ranges of the rows that were split.
+//
+// KV heads 2 p and 2 p + 1 of the cache are a pair: each has its own keys, and
+// their values side by side are the pair's values v of 2 D elements.  A row is
+// a token's query pair j (heads 2 j and 2 j + 1) on KV pair p = j / G:
+//     out = softmax(s q_2j k_2p) v - lambda_j softmax(s q_2j+1 k_2p+1) v,
+// normalised on demand by the root of its mean square.  Each map has a running
+// maximum and sum of its own, as attend_kernel keeps them; what they cannot
+// share is only known at the end, so each has its own sums over the values
+// too.  A product of 2 D with the difference of the maps would need every
+// score's sum first, and so all scores twice: 6 D operations a head and token
+// either way.
+//
+// The two value heads of a page have scales of their own.  The weights are
+// multiplied by the larger one S, as attend_kernel does with its one; the other
+// head's values are widened times r = its scale / S in fp16, exact for the
+// powers of two that the cache's own calls write down to 2^-15 (of smaller
+// ones what is below 2^-25 S is lost), and rounded to 11 bits for others.
+
+#include <hip/hip_runtime.h>
+
+#include "blockdev.h"
+
+namespace {
+
+using namespace blockdev;
+
+struct PairArgs : PlanArgs {
+    uint32_t pairs;                  // KV pairs
+    uint64_t q_stride;
+    const void *q;
+    void *out;
+    float c0;                        // |scale| * log2(e)
+    uint32_t q_sign;
+    const float *lambda;             // [query pair]
+    const float *norm;               // [2 D], or null
+    float root_eps, gain;
+    float *part;                     // [slot][pair][map][tile_rows][2 D]
+    f32x4 *part_ml;                  // [slot][pair][map][tile_rows] m, l, y
+};
+
+// 1 / sqrt(mean of o^2 + eps) of a row as a product of two factors: with its
+// largest element or sqrt(eps) brought near 1 the squares neither overflow nor
+// vanish.
+struct Rms {
+    float t, f;
+    __device__ explicit Rms(float most, float root_eps) {
+        const float s = fmaxf(most, root_eps);
+        const uint32_t e = min(max(__float_as_uint(s) >> 23, 1u), 253u);
+        t = __uint_as_float((254u - e) << 23);
+        f = 1.0f;
+    }
+    __device__ float square(float o) const { return o * t * (o * t); }
+    __device__ void close(float sum, float inv_n, float root_eps) {
+        const float e = root_eps * t;
+        f = 1.0f / sqrtf(fmaf(e, e, sum * inv_n));
+    }
+    __device__ float operator()(float o) const { return o * t * f; }
+};
+
+// Four elements of a row at column `col` to the output, by kCols lanes side by
+// side that hold it all: o1 and o2 are the two maps' products.
+template <int VD, typename T>
+__device__ inline void finish(const PairArgs &a, f32x4 o1, f32x4 o2, uint32_t j, T *out, uint32_t col) {
+    constexpr uint32_t kCols = VD / 4;
+    const float lam = a.lambda[j];
+    f32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(-lam, o2[i], o1[i]);
+    if (a.norm) {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(o[i]));
+        for (uint32_t d = kCols / 2; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+        Rms rms(most, a.root_eps);
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += rms.square(o[i]);
+        for (uint32_t d = kCols / 2; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+        rms.close(sum, 1.0f / VD, a.root_eps);
+        const f32x4 w = *(const f32x4 *)(a.norm + 4 * col);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = rms(o[i]) * w[i];
+    }
+    T z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = (T)(o[i] * a.gain);
+    *(u32x2 *)(out + 4 * col) = *(u32x2 *)z;
+}
+
+// What a step's values are multiplied by: S, and each half's r.
+struct ValScale {
+    float s, r[2];
+};
+__device__ inline ValScale val_scale(float x, float y) {
+    ValScale v;
+    v.s = fmaxf(x, y);
+    v.r[0] = v.s > 0.0f ? x / v.s : 1.0f;      // NaN stays NaN
+    v.r[1] = v.s > 0.0f ? y / v.s : 1.0f;
+    if (!(x == x && y == y)) v.s = NAN;
+    return v;
+}
+
+__device__ inline f16x8 times(f16x8 x, float r) {
+    const _Float16 h = (_Float16)r;
+    return x * f16x8{h, h, h, h, h, h, h, h};
+}
+
+// As attend_kernel, with the two maps in the place of two row tiles: each has
+// its own keys, and both take one step's values, which are loaded and widened
+// once.  The four wavefronts take every fourth step each, joined through LDS.
+template <int D, bool HALF, bool SMALL>
+__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairArgs a) {
+    typedef typename Elem<HALF>::T T;
+    typedef typename Elem<HALF>::T8 T8;
+    constexpr int VD = 2 * D, kDT = VD / 16, kHalf = D / 16;
+    constexpr int kPitch = VD + 4;
+    __shared__ float lds[kWaves * 16 * kPitch];
+    __shared__ float lds_ml[2][kWaves][16][3];
+
+    const uint32_t hk = a.kv.hk;
+    const uint32_t p = blockIdx.x % a.pairs, item = blockIdx.x / a.pairs;
+    Item it;
+    Head hd;
+    if (!find_item(a, item, it, hd)) return;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
+    const uint32_t c = lane & 15, g = lane >> 4;
+    const uint32_t n_rows = hd.n * a.G;
+    const uint32_t row0 = it.tile * a.tile_rows;
+    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep);
+    const uint64_t hb = head_bytes(a.kv, D);
+    const uint32_t *pages = a.kv.pages + (uint64_t)it.seq * a.kv.max_pages;
+    const uint32_t last_block = hd.ctx ? (hd.ctx - 1) >> a.kv.btl : 0u;
+
+    T8 qf[2][D / 32];
+    uint32_t lim;
+    {
+        const uint32_t r = row0 + c;
+        const bool valid = r < n_rows;
+        const uint32_t t = valid ? r / a.G : 0u, j = p * a.G + (valid ? r % a.G : 0u);
+        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
+        lim = !valid ? hd.ctx : seen > 0 ? (uint32_t)seen : 0u;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)(2 * j + m) * D + 16 * g;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                u32x4 x = {0, 0, 0, 0};
+                if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
+                qf[m][i] = __builtin_bit_cast(T8, x ^ a.q_sign);
+            }
+        }
+    }
+    // tokens that every row sees, and steps that any row sees
+    const uint32_t row_last = min(row0 + a.tile_rows, n_rows) - 1;
+    const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
+    const int64_t see_any = (int64_t)hd.ctx - hd.n + row_last / a.G + 1;
+    const uint32_t all_lim = see_all > 0 ? (uint32_t)min(see_all, (int64_t)hd.ctx) : 0u;
+    const uint32_t end = min(it.k1, see_any > 0 ? (uint32_t)((see_any + kStep - 1) / kStep) : 0u);
+
+    f32x4 acc[2][kDT];
+    float m[2], l[2], y[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        m[n] = y[n] = -INFINITY;
+        l[n] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) acc[n][d] = f32x4{0, 0, 0, 0};
+    }
+
+    // pages, scales and addresses are scalar where a step lies in one block
+    auto page_at = [&](uint32_t kt, uint32_t group) {
+        const uint32_t b = min((kt * kStep + (SMALL ? 16 * group : 0u)) >> a.kv.btl, last_block);
+        return SMALL ? pages[b] : scalar(pages)[b];
+    };
+    const uint64_t page_bytes = hk * hb;
+    const uint32_t key_in_page = (((SMALL ? (16 * (c >> 2)) & (tile - 1) : 16 * (c >> 2)) + (c & 3)) * D + 16 * g);
+    const uint32_t val_in_page = SMALL ? c * tile + ((16 * g) & (tile - 1)) : c * kStep + 16 * g;
+    const uint32_t val_piece = SMALL ? 16 * tile : 16 * kStep;
+    auto in_cache = [&](const uint8_t *x, uint32_t kt, uint32_t page) {
+        return x + 2 * p * hb + (page < a.kv.n_pages ? page : 0u) * page_bytes + (uint64_t)((kt * kStep) & (bt - 1)) * D;
+    };
+
+    // The next step's keys are asked for as soon as this one's have been
+    // multiplied, its values likewise; pages a step earlier.
+    KeyRegs<D> kf[2];
+    ValRegs<VD> vf;
+    f32x4 st[2][4];
+    f16x8 pf[2][2];
+    float sc_next[2] = {0.0f, 0.0f}, sc[2];
+    float va_next = 0.0f, vb_next = 0.0f;
+    ValScale vs;
+    uint64_t nan_sums = 0;                             // sums of this lane that a NaN value belongs to, in both maps
+    static_assert(4 * kDT <= 64, "a bit a sum");
+    uint32_t pk = 0, pv = 0;
+    auto load_keys = [&](uint32_t kt, uint32_t page) {
+        const uint8_t *x = in_cache(a.kv.k, kt, page);
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) kf[n].f[t][i] = *(const u32x4 *)(x + n * hb + key_in_page + 4 * t * D + 64 * i);
+    };
+    auto load_vals = [&](uint32_t kt, uint32_t page) {
+        const uint8_t *x = in_cache(a.kv.v, kt, page);
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) vf.f[d] = *(const u32x4 *)(x + (d / kHalf) * hb + val_in_page + (d % kHalf) * val_piece);
+    };
+    auto load_scales = [&]() {
+        const bool bad = pv >= a.kv.n_pages;
+        if (bad) report(a.kv);
+        const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk + 2 * p;
+        sc_next[0] = SMALL ? a.kv.ks[si] : scalar(a.kv.ks)[si];
+        sc_next[1] = SMALL ? a.kv.ks[si + 1] : scalar(a.kv.ks)[si + 1];
+        va_next = SMALL ? a.kv.vs[si] : scalar(a.kv.vs)[si];
+        vb_next = SMALL ? a.kv.vs[si + 1] : scalar(a.kv.vs)[si + 1];
+        if (bad) sc_next[0] = sc_next[1] = va_next = vb_next = NAN;
+    };
+    auto find_pages = [&](uint32_t kt) {
+        pk = page_at(kt, c >> 2);
+        pv = SMALL ? page_at(kt, g) : pk;
+    };
+    auto scores = [&](uint32_t kt) {
+        vs = val_scale(va_next, vb_next);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const float x = sc_next[n] * a.c0;
+            sc[n] = x == 0.0f ? 1.0e-30f : x;          // not 0, which would turn a masked score's -inf into NaN
+#pragma unroll
+            for (int t = 0; t < 4; ++t) st[n][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    const u32x4 k = kf[n].f[t][i];
+                    st[n][t] = product(widen<HALF>(k[0], k[1]), qf[n][2 * i], st[n][t]);
+                    st[n][t] = product(widen<HALF>(k[2], k[3]), qf[n][2 * i + 1], st[n][t]);
+                }
+        }
+        if (kt + kWaves < end) {
+            load_keys(kt + kWaves, pk);
+            load_scales();
+        }
+    };
+    auto values = [&](uint32_t kt) {
+        auto go = [&](auto scaled) {
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) {
+                f16x8 lo = widen_f16(vf.f[d][0], vf.f[d][1]), hi = widen_f16(vf.f[d][2], vf.f[d][3]);
+                if constexpr (decltype(scaled)::value) {
+                    lo = times(lo, vs.r[d / kHalf]);
+                    hi = times(hi, vs.r[d / kHalf]);
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    acc[n][d] = product(lo, pf[n][0], acc[n][d]);
+                    acc[n][d] = product(hi, pf[n][1], acc[n][d]);
+                }
+            }
+        };
+        if (__all(vs.r[0] == 1.0f && vs.r[1] == 1.0f)) go(std::false_type());
+        else go(std::true_type());
+        if (kt + kWaves < end) {
+            load_vals(kt + kWaves, pv);
+            find_pages(kt + 2 * kWaves);
+        }
+    };
+    // as attend_kernel's
+    auto softmax = [&]() {
+        const float vlog = log2_of(vs.s);
+        float up[2], sum[2];
+        bool fits = true;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const float by = vlog - y[n];
+            up[n] = -by - m[n];
+            sum[n] = weights_of(st[n], sc[n], by, pf[n]);
+            fits &= sum[n] <= kMaxSum && fabsf(up[n]) < 64.0f;
+        }
+        if (!__all(fits)) return false;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) l[n] += sum[n] * exp2_of(up[n]);
+        return true;
+    };
+    auto softmax_any = [&](uint32_t kt) {
+        const float vlog = log2_of(vs.s);
+        const uint32_t tok0 = kt * kStep + 16 * g;
+        const int left = (int)lim - (int)tok0;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    st[n][t][i] = left > 4 * t + i ? st[n][t][i] : -INFINITY;
+                    mx = fmaxf(mx, st[n][t][i]);
+                }
+            mx = mx == -INFINITY ? -INFINITY : mx * sc[n];
+            const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog) - kLift);
+            l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
+            const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
+            m[n] = mn;
+            y[n] = yn;
+#pragma unroll
+            for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
+            l[n] += weights_of(st[n], sc[n], mn == -INFINITY ? 0.0f : -mn, pf[n]);
+            weights_of(st[n], sc[n], yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
+        }
+        if (kt * kStep + kStep <= all_lim) return;
+        // Tokens that not every row sees: bytes of slots that hold none may be
+        // anything, and a NaN that some rows see and others do not is left out of
+        // the product and found by one of the masks (see attend_kernel).
+        const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
+        u32x4 keep;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = have - 4 * i;
+            keep[i] = b >= 4 ? 0xFFFFFFFFu : b <= 0 ? 0u : (1u << (8 * b)) - 1u;
+        }
+        bool nan = false;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) {
+            vf.f[d] &= keep;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) nan |= nan_bytes(vf.f[d][i]) != 0;
+        }
+        if (!__any(nan)) return;
+        uint64_t found = 0;                            // four bits at a time, from the top
+        f16x8 see[2];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) see[j >> 3][j & 7] = left > j ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) {
+            u32x4 z;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = nan_bytes(vf.f[d][i]);
+            const u32x4 one = z * 0x38u;               // 1.0 per NaN
+            vf.f[d] &= ~(z * 0xFFu);
+            f32x4 hit = {0, 0, 0, 0};
+            hit = product(widen_f16(one[0], one[1]), see[0], hit);
+            hit = product(widen_f16(one[2], one[3]), see[1], hit);
+            uint32_t bits = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits |= hit[i] > 0.0f ? 1u << i : 0u;
+            found = found >> 4 | (uint64_t)bits << 60;
+        }
+        nan_sums |= found >> (64 - 4 * kDT);
+    };
+    if (it.k0 + w < end) {
+        find_pages(it.k0 + w);
+        load_keys(it.k0 + w, pk);
+        load_scales();
+        load_vals(it.k0 + w, pv);
+        find_pages(it.k0 + w + kWaves);
+    }
+    // the ordinary steps have a loop of their own (see prompt_kernel)
+    for (uint32_t kt = it.k0 + w; kt < end; kt += kWaves) {
+        bool done;
+        do {
+            scores(kt);
+            done = kt * kStep + kStep <= all_lim;
+            if (done) done = softmax();
+            if (!done) break;
+            values(kt);
+            kt += kWaves;
+        } while (kt < end);
+        if (done) break;
+        softmax_any(kt);
+        values(kt);
+    }
+    if (nan_sums)
+#pragma unroll
+        for (int d = 0; d < kDT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (nan_sums >> (4 * d + i) & 1) acc[0][d][i] = acc[1][d][i] = NAN;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        l[n] = row_sum(l[n]);
+        if (g == 0) {
+            lds_ml[n][w][c][0] = m[n];
+            lds_ml[n][w][c][1] = l[n];
+            lds_ml[n][w][c][2] = y[n];
+        }
+    }
+    constexpr int kEach = 16 * VD / 4 / kThreads;      // pieces of four columns a thread joins
+    f32x4 o[2][kEach];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) *(f32x4 *)&lds[(w * 16 + c) * kPitch + d * 16 + 4 * g] = acc[n][d];
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const uint32_t i = threadIdx.x + e * kThreads, row = i / (VD / 4), d4 = i % (VD / 4) * 4, r = row0 + row;
+            float M = -INFINITY, Y = -INFINITY;
+            for (int v = 0; v < kWaves; ++v) {
+                M = fmaxf(M, lds_ml[n][v][row][0]);
+                Y = fmaxf(Y, lds_ml[n][v][row][2]);
+            }
+            float L = 0.0f;
+            f32x4 x = {0, 0, 0, 0};
+            for (int v = 0; v < kWaves; ++v) {
+                const float *ml = lds_ml[n][v][row];
+                L += joined(ml[0], M) * ml[1];
+                const float f = joined(ml[2], Y);
+                const f32x4 z = *(const f32x4 *)&lds[(v * 16 + row) * kPitch + d4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] += z[k] * f;
+            }
+            if (it.slot != kNoSlot) {
+                if (r >= n_rows) continue;
+                const uint64_t at = (((uint64_t)it.slot * a.pairs + p) * 2 + n) * a.tile_rows + row;
+                if (d4 == 0) a.part_ml[at] = f32x4{M, L, Y, 0.0f};
+                *(f32x4 *)(a.part + at * VD + d4) = x;
+            } else {
+                const Over over(Y, M, L, hd.ctx + r / a.G >= hd.n);   // both below 2^31
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[n][e][k] = over(x[k]);
+            }
+        }
+    }
+    if (it.slot != kNoSlot) return;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const uint32_t i = threadIdx.x + e * kThreads, row = i / (VD / 4), r = row0 + row;
+        if (r >= n_rows) continue;                     // a row's lanes go together
+        const uint32_t j = p * a.G + r % a.G;
+        finish<VD>(a, o[0][e], o[1][e], j, (T *)a.out + (hd.row0 + r / a.G) * a.out_stride + (uint64_t)j * VD, i % (VD / 4));
+    }
+}
+
+// The same for prompts, as prompt_kernel: every step's keys and values are
+// widened into LDS once, and two groups of four wavefronts go through the
+// tokens half a step apart.  The first group has the first map, the second one
+// the other, of the same 64 NT rows, so each reads its own keys and both the
+// pair's values.  Slot 2 k is the first group's products of step k (O of the
+// step before, S of this one) and the second one's softmax of step k - 1, slot
+// 2 k + 1 the reverse.  The first group widens both maps' keys k + 1 with its
+// softmax k (slot 2 k + 1: its own keys k - 1, in the same buffer, were last
+// read in slot 2 k - 2, the second group's in slot 2 k - 1), the second one
+// values k + 1 with its own (slot 2 k + 2: values k - 1 were last read in slot
+// 2 k + 1, values k + 1 are first read in slot 2 k + 4).  At the end the second
+// map's rows go to the first group through LDS.
+template <int D, int NT, bool HALF, bool SMALL>
+__global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs a) {
+    typedef typename Elem<HALF>::T T;
+    typedef typename Elem<HALF>::T8 T8;
+    constexpr int VD = 2 * D, kDT = VD / 16;
+    constexpr int kAhead = 6;                         // fragments read ahead of their products
+    constexpr int kShare = D / 32;                    // 16-byte pieces of keys or values a lane stages
+    constexpr int kKeys = D / 8, kVals = D / 4;       // fragments of one map's keys, of the values
+    __shared__ u32x4 lds[2 * (2 * kKeys + kVals)][64];
+    __shared__ uint8_t lds_bits[2][kVals][64];        // which of a fragment lane's 8 values were NaN
+    __shared__ uint32_t lds_nan[2];
+    static_assert(4 * NT * kDT <= 2 * (2 * kKeys + kVals), "a map's rows fit");
+
+    const uint32_t hk = a.kv.hk;
+    const uint32_t p = blockIdx.x % a.pairs, item = blockIdx.x / a.pairs;
+    Item it;
+    Head hd;
+    if (!find_item(a, item, it, hd)) return;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
+    const bool second = w >= 4;
+    const uint32_t map = second;
+    auto lds_k = [&](int b, uint32_t q, int f) -> u32x4 * { return lds[(2 * b + q) * kKeys + f]; };
+    auto lds_v = [&](int b, int f) -> u32x4 * { return lds[4 * kKeys + b * kVals + f]; };
+    const uint32_t c = lane & 15, g = lane >> 4;
+    const uint32_t n_rows = hd.n * a.G;
+    const uint32_t row0 = it.tile * a.tile_rows + (w & 3) * 16 * NT;
+    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep);
+    const uint64_t hb = head_bytes(a.kv, D);
+    const uint32_t *pages = a.kv.pages + (uint64_t)it.seq * a.kv.max_pages;
+    const uint32_t last_block = hd.ctx ? (hd.ctx - 1) >> a.kv.btl : 0u;
+
+    T8 qf[NT][D / 32];
+    uint32_t lim[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t r = row0 + n * 16 + c;
+        const bool valid = r < n_rows;
+        const uint32_t t = valid ? r / a.G : 0u, j = p * a.G + (valid ? r % a.G : 0u);
+        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
+        lim[n] = !valid ? hd.ctx : seen > 0 ? (uint32_t)seen : 0u;
+        const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)(2 * j + map) * D + 16 * g;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            u32x4 x = {0, 0, 0, 0};
+            if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
+            qf[n][i] = __builtin_bit_cast(T8, x ^ a.q_sign);
+        }
+    }
+    // tokens that every row of this wavefront sees, and of the tile (see prompt_kernel)
+    const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
+    const uint32_t all_lim = see_all > 0 ? (uint32_t)min(see_all, (int64_t)hd.ctx) : 0u;
+    const int64_t see_tile = (int64_t)hd.ctx - hd.n + it.tile * a.tile_rows / a.G + 1;
+    const uint32_t tile_lim = see_tile > 0 ? (uint32_t)min(see_tile, (int64_t)hd.ctx) : 0u;
+
+    f32x4 acc[NT][kDT], st[NT][4];
+    f16x8 pf[NT][2];
+    float m[NT], l[NT], y[NT];
+    uint64_t nan_sums = 0;                            // sums of this lane that a NaN value belongs to
+    static_assert(4 * NT * kDT <= 64, "a bit a sum");
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = y[n] = -INFINITY;
+        l[n] = 0.0f;
+        pf[n][0] = pf[n][1] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) acc[n][d] = f32x4{0, 0, 0, 0};
+    }
+
+    // this lane's pieces: 64 dimensions of key row c of a product, of each
+    // map, or 16 tokens of dimension 16 d + c
+    u32x4 px[kShare];
+    float sc_at[2], vs_at[2], rv_at[2];                // scales of this step and the next; r of the half that this wavefront widens
+    const uint32_t half = second ? (w - 4) >> 1 : 0u;
+    const uint32_t own_group = SMALL ? second ? g : c >> 2 : 0u;   // whose page this lane's pieces are in
+    auto page_at = [&](uint32_t kt, uint32_t group) {
+        const uint32_t block = min((kt * kStep + (SMALL ? 16 * group : 0u)) >> a.kv.btl, last_block);
+        return SMALL ? pages[block] : scalar(pages)[block];
+    };
+    const uint8_t *own = (second ? a.kv.v : a.kv.k) + (2 * p + half) * hb;
+    const uint64_t page_bytes = hk * hb;
+    const uint32_t in_page = second ? c * tile + ((16 * g) & (tile - 1)) + (w & 1) * kShare * 16 * tile
+                                    : ((16 * (c >> 2)) & (tile - 1)) * D + ((c & 3) + 4 * w) * D + 16 * g;
+    const uint64_t piece = second ? 16 * tile : 64, map_step = second ? (uint64_t)kShare / 2 * 16 * tile : hb;
+    const float *ks = a.kv.ks + 2 * p + map, *vs = a.kv.vs + 2 * p;
+    auto scales_of = [&](uint32_t pv, float &sc, float &vsc, float &rv) {
+        const bool bad = pv >= a.kv.n_pages;
+        if (bad) report(a.kv);
+        const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk;
+        sc = SMALL ? ks[si] : scalar(ks)[si];
+        const float va = SMALL ? vs[si] : scalar(vs)[si], vb = SMALL ? vs[si + 1] : scalar(vs)[si + 1];
+        const ValScale v = val_scale(va, vb);
+        vsc = v.s;
+        rv = half ? v.r[1] : v.r[0];
+        if (bad) sc = vsc = NAN;
+    };
+    // pieces i: keys, D / 64 of the first map, then of the second; values, tiles in a row
+    auto fetch = [&](uint32_t kt, uint32_t po) {
+        const uint8_t *x = own + (po < a.kv.n_pages ? po : 0u) * page_bytes + (uint64_t)((kt * kStep) & (bt - 1)) * D;
+#pragma unroll
+        for (int i = 0; i < kShare; ++i) px[i] = *(const u32x4 *)(x + in_page + (i / (kShare / 2)) * map_step + (i % (kShare / 2)) * piece);
+    };
+    auto stage = [&](uint32_t kt, float rv) {
+        const int b = kt & 1;
+        if (!second) {
+#pragma unroll
+            for (int i = 0; i < kShare; ++i) {
+                const int f = w * (D / 32) + 2 * (i % (kShare / 2));
+                lds_k(b, i / (kShare / 2), f)[lane] = __builtin_bit_cast(u32x4, widen<HALF>(px[i][0], px[i][1]));
+                lds_k(b, i / (kShare / 2), f + 1)[lane] = __builtin_bit_cast(u32x4, widen<HALF>(px[i][2], px[i][3]));
+            }
+            return;
+        }
+        if (kt * kStep + kStep > tile_lim) {
+            // bytes of slots that hold no token are cleared, a NaN is taken out
+            // and noted
+            const uint32_t tok0 = kt * kStep + 16 * g;
+            const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
+            bool nan = false;
+#pragma unroll
+            for (int i = 0; i < kShare; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int n = have - 4 * j;
+                    px[i][j] &= n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+                    nan |= nan_bytes(px[i][j]) != 0;
+                }
+            if (__any(nan)) {
+#pragma unroll
+                for (int i = 0; i < kShare; ++i) {
+                    const uint32_t j = (w - 4) * kShare + i;
+                    uint32_t bits = 0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t z = nan_bytes(px[i][q]);
+                        px[i][q] &= ~(z * 0xFFu);
+                        bits |= ((z | z >> 7 | z >> 14 | z >> 21) & 15u) << (4 * q);
+                    }
+                    lds_bits[b][2 * j][lane] = (uint8_t)bits;
+                    lds_bits[b][2 * j + 1][lane] = (uint8_t)(bits >> 8);
+                }
+                if (lane == 0) atomicOr(&lds_nan[b], 1u << (w - 4));
+            } else if (lane == 0) {
+                atomicAnd(&lds_nan[b], ~(1u << (w - 4)));
+            }
+        }
+        const bool scaled = !__all(rv == 1.0f);
+#pragma unroll
+        for (int i = 0; i < kShare; ++i) {
+            const uint32_t j = (w - 4) * kShare + i;
+            f16x8 lo = widen_f16(px[i][0], px[i][1]), hi = widen_f16(px[i][2], px[i][3]);
+            if (scaled) {
+                lo = times(lo, rv);
+                hi = times(hi, rv);
+            }
+            lds_v(b, 2 * j)[lane] = __builtin_bit_cast(u32x4, lo);
+            lds_v(b, 2 * j + 1)[lane] = __builtin_bit_cast(u32x4, hi);
+        }
+    };
+    // LDS alone is handed over: loads from memory stay in flight
+    auto meet = [&]() {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    };
+    // a product's sums are four fragments apart: each waits for none
+    auto scores = [&](uint32_t kt) {
+        const int b = kt & 1;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) st[n][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < 4; t += 2)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const T8 kf = __builtin_bit_cast(T8, lds_k(b, map, (t + q) * (D / 32) + i)[lane]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) st[n][t + q] = product(kf, qf[n][i], st[n][t + q]);
+                }
+    };
+    auto values = [&](uint32_t kt) {
+        const int b = kt & 1;
+#pragma unroll
+        for (int d = 0; d < kDT; d += 2)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const f16x8 vf = __builtin_bit_cast(f16x8, lds_v(b, 2 * (d + q) + u)[lane]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[n][d + q] = product(vf, pf[n][u], acc[n][d + q]);
+                }
+    };
+    // `reads` fragments in all, each for NT products: kAhead on their way
+    auto interleave = [&](auto reads) {
+        constexpr int kReads = decltype(reads)::value;
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < kReads - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, NT, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead * NT, 0);
+    };
+    // not 0, which would turn a masked score's -inf into NaN
+    auto scale_of = [&]() {
+        const float x = sc_at[0] * a.c0;
+        return x == 0.0f ? 1.0e-30f : x;
+    };
+    // as prompt_kernel's
+    auto softmax = [&]() {
+        const float sc = scale_of(), vlog = log2_of(vs_at[0]);
+        float up[NT], sum[NT];                         // up: log2 of a weight over its P
+        bool fits = true;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float by = vlog - y[n];
+            up[n] = -by - m[n];
+            sum[n] = weights_of(st[n], sc, by, pf[n]);
+            fits &= sum[n] <= kMaxSum && fabsf(up[n]) < 64.0f;
+        }
+        if (!__all(fits)) return false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) l[n] += sum[n] * exp2_of(up[n]);
+        return true;
+    };
+    auto softmax_any = [&](uint32_t kt) {
+        const float sc = scale_of(), vlog = log2_of(vs_at[0]);
+        const uint32_t tok0 = kt * kStep + 16 * g;
+        if (kt * kStep + kStep > tile_lim) {
+            const uint32_t noted = lds_nan[kt & 1];
+            if (noted)
+#pragma unroll 1
+                for (int d = 0; d < kDT; ++d) {
+                    if (!(noted >> (d / kShare) & 1)) continue;
+                    f32x4 hit[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) hit[n] = f32x4{0, 0, 0, 0};
+#pragma unroll 1
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t bits = lds_bits[kt & 1][2 * d + u][lane];
+                        f16x8 one;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) one[j] = bits >> j & 1 ? (_Float16)1.0f : (_Float16)0.0f;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const int left = (int)lim[n] - (int)tok0 - 8 * u;
+                            f16x8 see;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) see[j] = left > j ? (_Float16)1.0f : (_Float16)0.0f;
+                            hit[n] = product(one, see, hit[n]);
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) nan_sums |= (uint64_t)(hit[n][i] > 0.0f) << (4 * (n * kDT + d) + i);
+                }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int left = (int)lim[n] - (int)tok0;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    st[n][t][i] = left > 4 * t + i ? st[n][t][i] : -INFINITY;
+                    mx = fmaxf(mx, st[n][t][i]);
+                }
+            mx = mx == -INFINITY ? -INFINITY : mx * sc;
+            const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog) - kLift);
+            l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
+            const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
+            m[n] = mn;
+            y[n] = yn;
+#pragma unroll
+            for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
+            l[n] += weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
+            weights_of(st[n], sc, yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
+        }
+    };
+
+    // pages of the step after next and the one after it
+    uint32_t po = 0, pv = 0, po_on = 0, pv_on = 0;
+    float sc_on = 0.0f, vs_on = 0.0f, rv_on = 1.0f;   // scales of the step after next
+    if (threadIdx.x < 2) lds_nan[threadIdx.x] = 0;
+    // the first step's products with "the step before" are of zeros
+    for (uint32_t i = threadIdx.x; i < kVals * 64; i += kPromptThreads) lds_v(~it.k0 & 1, 0)[i] = u32x4{0, 0, 0, 0};
+    meet();
+    sc_at[0] = vs_at[0] = sc_at[1] = vs_at[1] = 0.0f;
+    rv_at[0] = rv_at[1] = 1.0f;
+    if (it.k0 < it.k1) {
+        fetch(it.k0, page_at(it.k0, own_group));
+        scales_of(page_at(it.k0, g), sc_at[0], vs_at[0], rv_at[0]);
+        stage(it.k0, rv_at[0]);
+        fetch(it.k0 + 1, page_at(it.k0 + 1, own_group));
+        scales_of(page_at(it.k0 + 1, g), sc_at[1], vs_at[1], rv_at[1]);
+        po = page_at(it.k0 + 2, own_group);
+        pv = SMALL ? page_at(it.k0 + 2, g) : po;
+    }
+    meet();
+    if (second) meet();
+    // Small loads for later steps go out before the softmax, which hides them
+    // (page_at stays within the sequence's blocks past its end).
+    auto look_ahead = [&](uint32_t kt) {
+        scales_of(pv, sc_on, vs_on, rv_on);
+        po_on = page_at(kt + 3, own_group);
+        pv_on = SMALL ? page_at(kt + 3, g) : po_on;
+    };
+    auto pass_on = [&](uint32_t kt) {
+        if (kt + 1 < it.k1) {
+            stage(kt + 1, rv_at[1]);
+            fetch(kt + 2, po);
+        }
+        sc_at[0] = sc_at[1];
+        vs_at[0] = vs_at[1];
+        sc_at[1] = sc_on;
+        vs_at[1] = vs_on;
+        rv_at[1] = rv_on;
+        po = po_on;
+        pv = pv_on;
+        meet();
+    };
+    // the ordinary steps have a loop of their own (see prompt_kernel)
+    for (uint32_t kt = it.k0; kt < it.k1; ++kt) {
+        bool done;
+        do {
+            values(kt - 1);
+            scores(kt);
+            interleave(std::integral_constant<int, 3 * D / 8>());
+            meet();
+            done = kt * kStep + kStep <= all_lim && kt > it.k0;   // the first step sets the maxima
+            if (kt * kStep + kStep > tile_lim) done = done && __builtin_amdgcn_readfirstlane(lds_nan[kt & 1]) == 0;
+            look_ahead(kt);
+            if (done) done = softmax();
+            if (!done) break;
+            pass_on(kt);
+            ++kt;
+        } while (kt < it.k1);
+        if (done) break;
+        softmax_any(kt);
+        pass_on(kt);
+    }
+    if (!second) meet();
+    if (it.k0 < it.k1) values(it.k1 - 1);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        l[n] = row_sum(l[n]);
+        if (nan_sums)
+#pragma unroll
+            for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (nan_sums >> (4 * (n * kDT + d) + i) & 1) acc[n][d][i] = NAN;
+    }
+    if (it.slot != kNoSlot) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t tr = (w & 3) * 16 * NT + n * 16 + c;
+            if (row0 + n * 16 + c >= n_rows) continue;
+            const uint64_t at = (((uint64_t)it.slot * a.pairs + p) * 2 + map) * a.tile_rows + tr;
+            if (g == 0) a.part_ml[at] = f32x4{m[n], l[n], y[n], 0.0f};
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) *(f32x4 *)(a.part + at * VD + d * 16 + 4 * g) = acc[n][d];
+        }
+        return;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const Over over(y[n], m[n], l[n], lim[n] > 0);
+#pragma unroll
+        for (int d = 0; d < kDT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[n][d][i] = over(acc[n][d][i]);
+    }
+    __syncthreads();                                  // the last values have been read
+    f32x4(*other)[64] = (f32x4(*)[64]) & lds[(w & 3) * NT * kDT];
+    if (second)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) other[n * kDT + d][lane] = acc[n][d];
+    __syncthreads();
+    if (second) return;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t r = row0 + n * 16 + c;
+        const bool valid = r < n_rows;
+        const uint32_t j = p * a.G + (valid ? r % a.G : 0u);
+        const float lam = a.lambda[j];
+        float most = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) {
+            const f32x4 x = other[n * kDT + d][lane];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                acc[n][d][i] = fmaf(-lam, x[i], acc[n][d][i]);
+                most = fmaxf(most, fabsf(acc[n][d][i]));
+            }
+        }
+        if (a.norm) {
+            Rms rms(row_max(most), a.root_eps);
+            float sum = 0.0f;
+#pragma unroll
+            for (int d = 0; d < kDT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum += rms.square(acc[n][d][i]);
+            rms.close(row_sum(sum), 1.0f / VD, a.root_eps);
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) {
+                const f32x4 wn = *(const f32x4 *)(a.norm + d * 16 + 4 * g);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[n][d][i] = rms(acc[n][d][i]) * wn[i];
+            }
+        }
+        if (!valid) continue;
+        T *out = (T *)a.out + (hd.row0 + r / a.G) * a.out_stride + (uint64_t)j * VD + 4 * g;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) {
+            T o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = (T)(acc[n][d][i] * a.gain);
+            *(u32x2 *)(out + d * 16) = *(u32x2 *)o;
+        }
+    }
+}
+
+// Joins the ranges of one row, each map as join_row does, by WAVES wavefronts.
+template <int VD, bool HALF, int WAVES>
+__device__ inline void join_pair(const PairArgs &a, const Join &j, uint32_t p, uint32_t tr, f32x4 *lo, float *factor, float (*red)[kWaves]) {
+    typedef typename Elem<HALF>::T T;
+    constexpr uint32_t kLanes = 64 * WAVES, kCols = VD / 4, kGroups = kLanes / kCols;
+    auto meet = [&]() {
+        if constexpr (WAVES > 1) __syncthreads();
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    const uint32_t rows = a.tile_rows;
+    const uint32_t me = threadIdx.x % kLanes, lane = threadIdx.x & 63, w = me >> 6;
+    const uint32_t col = me % kCols, grp = me / kCols;
+    const Head hd = seq_head(a.kv, j.seq);
+    const uint32_t r = j.tile * rows + tr;
+    if (r >= hd.n * a.G) return;
+    const uint64_t by = (uint64_t)a.pairs * 2 * rows;
+    f32x4 both[2];
+#pragma unroll
+    for (int map = 0; map < 2; ++map) {
+        const uint64_t at = (((uint64_t)j.slot * a.pairs + p) * 2 + map) * rows + tr;
+        float M = -INFINITY, Y = -INFINITY;
+        for (uint32_t i = me; i < j.n; i += kLanes) {
+            const f32x4 ml = a.part_ml[at + i * by];
+            M = fmaxf(M, ml[0]);
+            Y = fmaxf(Y, ml[2]);
+        }
+        for (int d = 32; d; d >>= 1) {
+            M = fmaxf(M, __shfl_xor(M, d, 64));
+            Y = fmaxf(Y, __shfl_xor(Y, d, 64));
+        }
+        if constexpr (WAVES > 1) {
+            if (lane == 0) {
+                red[0][w] = M;
+                red[1][w] = Y;
+            }
+            __syncthreads();
+            for (int v = 0; v < WAVES; ++v) {
+                M = fmaxf(M, red[0][v]);
+                Y = fmaxf(Y, red[1][v]);
+            }
+        }
+        float L = 0.0f;
+        f32x4 o = {0, 0, 0, 0};
+        for (uint32_t i0 = 0; i0 < j.n; i0 += kLanes) {
+            const uint32_t i = i0 + me;
+            if (i < j.n) {
+                const f32x4 ml = a.part_ml[at + i * by];
+                factor[me] = joined(ml[2], Y);
+                L += joined(ml[0], M) * ml[1];
+            }
+            meet();
+            const uint32_t n = min(j.n - i0, kLanes);
+            const float *x0 = a.part + (at + i0 * by) * VD + col * 4;
+#pragma unroll 4
+            for (uint32_t q = grp; q < n; q += kGroups) {
+                const f32x4 x = *(const f32x4 *)(x0 + q * by * VD);
+                const float f = factor[q];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] += f * x[e];
+            }
+            meet();
+        }
+        for (int d = 32; d; d >>= 1) L += __shfl_xor(L, d, 64);
+        if (WAVES > 1 && lane == 0) red[2][w] = L;
+        lo[grp * kCols + col] = o;
+        meet();
+        if constexpr (WAVES > 1) {
+            L = 0.0f;
+            for (int v = 0; v < WAVES; ++v) L += red[2][v];
+        }
+        o = f32x4{0, 0, 0, 0};
+        for (uint32_t i = 0; i < kGroups; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += lo[i * kCols + col][e];
+        const Over over(Y, M, L, hd.ctx + r / a.G >= hd.n);   // both below 2^31
+#pragma unroll
+        for (int e = 0; e < 4; ++e) both[map][e] = over(o[e]);
+        meet();
+    }
+    if (grp) return;
+    const uint32_t jq = p * a.G + r % a.G;
+    finish<VD>(a, both[0], both[1], jq, (T *)a.out + (hd.row0 + r / a.G) * a.out_stride + (uint64_t)jq * VD, col);
+}
+
+// As join_kernel: a workgroup a row as long as there are no more rows than
+// workgroups, else a wavefront a row.
+template <int VD, bool HALF>
+__global__ __launch_bounds__(kThreads) void pair_join_kernel(PairArgs a, uint32_t rows) {
+    __shared__ f32x4 lo[kThreads];
+    __shared__ float factor[kThreads], red[3][kWaves];
+    const uint32_t w = threadIdx.x >> 6;
+    auto all = [&](uint32_t n_joins, auto join) {
+        const uint32_t n = n_joins * a.pairs * rows;   // at most 2,048 joins and pairs, 128 rows
+        auto row = [&](uint32_t task, auto waves, uint32_t at) {
+            const uint32_t jp = task / rows;
+            join_pair<VD, HALF, decltype(waves)::value>(a, join(jp / a.pairs), jp % a.pairs, task % rows, lo + at, factor + at, red);
+        };
+        if (n <= gridDim.x) {
+            if (blockIdx.x < n) row(blockIdx.x, std::integral_constant<int, kWaves>(), 0);
+        } else {
+            for (uint32_t task = blockIdx.x * kWaves + w; task < n; task += gridDim.x * kWaves) row(task, std::integral_constant<int, 1>(), 64 * w);
+        }
+    };
+    if (a.joins) {
+        all(a.head->n_joins, [&](uint32_t i) { return a.joins[i]; });
+    } else {
+        const Shares sh(a);
+        all(sh.n_joins(), [&](uint32_t i) { return sh.join(i); });
+    }
+}
+
+// ------------------------------------------------------------------ host
+
+struct PairLayout : Split {
+    uint32_t pairs;
+    bool rows;             // pair_prompt_kernel
+    uint32_t item_cap, slot_cap, join_cap, tile_most;
+    uint64_t head, items, joins, ml, part, total;
+};
+
+netkv_status make_pair_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t heads, PairLayout &y) {
+    if (D != 64 && D != 128) return invalid(h, "head_dim must be 64 or 128");
+    if (a.hk % 2) return invalid(h, "n_kv_heads must be even");
+    if (heads < 1 || heads % a.hk) return invalid(h, "n_heads must be a multiple of n_kv_heads");
+    y.pairs = a.hk / 2;
+    y.G = heads / a.hk;
+    if (y.G > 64) return invalid(h, "n_heads / n_kv_heads must be <= 64");
+    const uint64_t most = (uint64_t)a.max_tok * y.G;   // rows of the longest sequence's pair
+    if (most > 0xFFFFFFFFull - 1024) return invalid(h, "max_tok * n_heads / n_kv_heads must be < 2^32 - 1024");
+    y.rows = most > (D == 64 ? 96u : 32u);
+    y.tile_rows = !y.rows ? 16u : D == 64 ? 128u : 64u;
+    y.tile_most = (uint32_t)(most < y.tile_rows ? most : y.tile_rows);
+    y.target = (512u + y.pairs - 1) / y.pairs;
+    y.fine = y.rows || D == 128 ? y.target : (1024u + y.pairs - 1) / y.pairs;
+    const uint32_t bt = 1u << a.btl;
+    y.least = y.rows ? 8 : kWaves;
+    y.round = !y.rows ? kWaves : bt > kStep ? bt / kStep : 1;
+    const Caps caps = caps_of(a, y);
+    if (!grid_fits(caps.items * y.pairs, y.rows ? kPromptThreads : kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
+    y.item_cap = (uint32_t)caps.items;
+    y.slot_cap = (uint32_t)caps.slots;
+    y.join_cap = (uint32_t)caps.joins;
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        const uint64_t p = at;
+        at += align256(bytes);
+        return p;
+    };
+    y.head = take(sizeof(PlanHead));
+    y.items = take(sizeof(Item) * y.item_cap);
+    y.joins = take(sizeof(Join) * y.join_cap);
+    const uint64_t parts = 2ull * y.slot_cap * y.pairs * y.tile_rows;
+    y.ml = take(16 * parts);
+    y.part = take(4 * parts * 2 * D);
+    y.total = at;
+    return NETKV_OK;
+}
+
+template <int D, bool HALF>
+void launch_pairs(const PairLayout &y, const PairArgs &a, hipStream_t s) {
+    const dim3 grid(y.item_cap * y.pairs);
+    const bool small = a.kv.btl < 6;
+    if (y.rows)
+        small ? pair_prompt_kernel<D, D == 64 ? 2 : 1, HALF, true><<<grid, kPromptThreads, 0, s>>>(a)
+              : pair_prompt_kernel<D, D == 64 ? 2 : 1, HALF, false><<<grid, kPromptThreads, 0, s>>>(a);
+    else
+        small ? pair_kernel<D, HALF, true><<<grid, kThreads, 0, s>>>(a) : pair_kernel<D, HALF, false><<<grid, kThreads, 0, s>>>(a);
+    // nothing is split where no sequence can be longer than the shortest range
+    const uint64_t steps_most = (((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep;
+    const uint64_t joins_most = (uint64_t)y.join_cap * y.pairs * y.tile_most, quarter = (joins_most + 3) / 4;
+    // as launch_attend's
+    const uint64_t groups = joins_most < 512 ? joins_most : quarter < 512 ? 512 : quarter < 1024 ? quarter : 1024;
+    if (steps_most > a.least && groups) pair_join_kernel<2 * D, HALF><<<(uint32_t)groups, kThreads, 0, s>>>(a, y.tile_most);
+}
+
+}  // namespace
+
+extern "C" netkv_status netkv_kv_attend_diff_workspace(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
+                                                       uint32_t n_heads, uint64_t *bytes) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    if (!bytes) return invalid(h, "bytes must not be NULL");
+    Kv a{};
+    netkv_status st = make_kv(h, kv, seqs, a);
+    if (st != NETKV_OK) return st;
+    PairLayout y{};
+    if ((st = make_pair_layout(h, a, kv->head_dim, n_heads, y)) != NETKV_OK) return st;
+    *bytes = y.total;
+    return NETKV_OK;
+}
+
+extern "C" netkv_status netkv_kv_attend_diff(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *q,
+                                             int dtype, uint32_t n_heads, uint64_t q_stride, float scale, const float *lambda,
+                                             const float *norm, float eps, float gain, void *out, uint64_t out_stride,
+                                             void *work, uint64_t work_bytes, void *stream) {
+    if (!h) return NETKV_EINVAL;
+    netkv_internal_clear(h);
+    Kv a{};
+    netkv_status st = make_kv(h, kv, seqs, a);
+    if (st != NETKV_OK) return st;
+    if (dtype != NETKV_BF16 && dtype != NETKV_FP16) return invalid(h, "dtype must be NETKV_BF16 or NETKV_FP16");
+    PairLayout y{};
+    if ((st = make_pair_layout(h, a, kv->head_dim, n_heads, y)) != NETKV_OK) return st;
+    if (!std::isfinite(scale) || !std::isfinite(gain)) return invalid(h, "scale and gain must be finite");
+    if (!lambda || (uintptr_t)lambda & 3) return invalid(h, "lambda must not be NULL");
+    if (norm && !aligned16(norm)) return invalid(h, "norm must be 16-byte aligned");
+    if (norm && !(std::isfinite(eps) && eps > 0.0f)) return invalid(h, "eps must be finite and > 0");
+    const uint64_t width = (uint64_t)n_heads * kv->head_dim;
+    if ((st = check_rows(h, q, q_stride, width, a.n_tok, "q must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    if ((st = check_rows(h, out, out_stride, width, a.n_tok, "out must be 16-byte aligned, its stride a multiple of 8 and at least a token's elements")) != NETKV_OK) return st;
+    // a row is read by the one workgroup that writes it, or before a join does
+    if (rows_overlap(q, q_stride, out, out_stride, width, a.n_tok) && (q != out || q_stride != out_stride))
+        return invalid(h, "out must not overlap q (it may be q itself)");
+    if (a.n_seq == 0) return NETKV_OK;
+    if (!work || ((uintptr_t)work & 255) || work_bytes < y.total) return invalid(h, "work must be 256-byte aligned and of at least netkv_kv_attend_diff_workspace's bytes");
+    DeviceScope scope(netkv_internal_device(h));
+    hipStream_t s = (hipStream_t)stream;
+    uint8_t *ws = (uint8_t *)work;
+    const bool half = dtype == NETKV_FP16;
+    PairArgs t{};
+    t.kv = a;
+    (Split &)t = y;
+    t.bad_out = (uint16_t *)out;
+    t.out_stride = out_stride;
+    t.row_elems = (uint32_t)width;
+    t.nan16 = half ? 0x7E00u : 0x7FC0u;
+    if (a.n_seq > kListed) {
+        t.head = (PlanHead *)(ws + y.head);
+        t.items = (Item *)(ws + y.items);
+        t.joins = (Join *)(ws + y.joins);
+        launch_plan(t, s);
+    }
+    t.pairs = y.pairs;
+    t.q_stride = q_stride;
+    t.q = q;
+    t.out = out;
+    t.c0 = std::fabs(scale) * kLog2e;
+    t.q_sign = scale < 0.0f ? 0x80008000u : 0u;
+    t.lambda = lambda;
+    t.norm = norm;
+    t.root_eps = norm ? std::sqrt(eps) : 0.0f;
+    t.gain = gain;
+    t.part = (float *)(ws + y.part);
+    t.part_ml = (f32x4 *)(ws + y.ml);
+    if (kv->head_dim == 64)
+        half ? launch_pairs<64, true>(y, t, s) : launch_pairs<64, false>(y, t, s);
+    else
+        half ? launch_pairs<128, true>(y, t, s) : launch_pairs<128, false>(y, t, s);
+    return launched(h, "differential attention launch failed");
+}

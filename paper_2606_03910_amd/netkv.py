@@ -131,6 +131,11 @@ _SIGS = {
                                     C.POINTER(netkv_rope_t), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint32, C.c_uint64,
                                     C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_int,
                                     C.c_void_p]),
+    "netkv_kv_attend_diff": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_t), C.POINTER(netkv_kv_seqs_t), C.c_void_p,
+                                         C.c_int, C.c_uint32, C.c_uint64, C.c_float, C.c_void_p, C.c_void_p, C.c_float,
+                                         C.c_float, C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]),
+    "netkv_kv_attend_diff_workspace": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_t), C.POINTER(netkv_kv_seqs_t),
+                                                   C.c_uint32, C.POINTER(C.c_uint64)]),
     "netkv_kv_weigh": (C.c_int32, [C.c_void_p, C.POINTER(netkv_kv_seqs_t), C.c_uint32, C.c_void_p, C.c_uint32,
                                    C.c_void_p, C.c_void_p]),
     "netkv_cache_evict": (C.c_int32, [C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p, C.c_void_p,
@@ -615,6 +620,31 @@ def netkv_kv_attend(h: int, kv: netkv_kv_t, seqs: Sequences, q: torch.Tensor, sc
         _dptr(work, torch.uint8, name="work"), int(work.numel()), _stream(device)))
 
 
+def netkv_kv_attend_diff_workspace(h: int, kv: netkv_kv_t, seqs: Sequences, n_heads: int) -> int:
+    n = C.c_uint64()
+    _check(h, load_library().netkv_kv_attend_diff_workspace(h, C.byref(kv), C.byref(seqs.c), int(n_heads), C.byref(n)))
+    return int(n.value)
+
+
+def netkv_kv_attend_diff(h: int, kv: netkv_kv_t, seqs: Sequences, q: torch.Tensor, scale: float, lam: torch.Tensor,
+                         norm: Optional[torch.Tensor], eps: float, gain: float, out: torch.Tensor, work: torch.Tensor,
+                         device) -> None:
+    _on(seqs, device, "the sequences")
+    heads = int(q.shape[1]) if q.dim() == 3 else 0
+    qp, qs = _rows(q, seqs.n_tok, heads, kv.head_dim, device, "q")
+    op, os_ = _rows(out, seqs.n_tok, heads // 2, 2 * kv.head_dim, device, "out")
+    if q.dtype != out.dtype:
+        raise TypeError("q and out must have one dtype")
+    for name, t in (("lam", lam), ("norm", norm)):
+        if t is not None:
+            _no_gradient(t, name)
+    _on_all(device, lam=lam, norm=norm, work=work)
+    _check(h, load_library().netkv_kv_attend_diff(
+        h, C.byref(kv), C.byref(seqs.c), qp, _DTYPE[q.dtype], heads, qs, float(scale),
+        _dptr(lam, torch.float32, heads // 2, "lam"), _dptr(norm, torch.float32, 2 * kv.head_dim, "norm"), float(eps),
+        float(gain), op, os_, _dptr(work, torch.uint8, name="work"), int(work.numel()), _stream(device)))
+
+
 def netkv_kv_weigh(h: int, seqs: Sequences, block_tokens: int, block_weight: torch.Tensor, page_weight: torch.Tensor,
                    device) -> None:
     _on(seqs, device, "the sequences")
@@ -918,6 +948,25 @@ class BlockCache:
         w = torch.empty((seqs.n_seq, seqs.max_pages), dtype=torch.float32, device=self.device) if weights else None
         netkv_kv_attend(self.sel.h, self.c, seqs, q, scale, out, w, work, self.device)
         return (out, w) if weights else out
+
+    def attend_diff(self, seqs: Sequences, q: torch.Tensor, lam: torch.Tensor, scale: Optional[float] = None,
+                    norm: Optional[torch.Tensor] = None, eps: float = 1e-5, gain: float = 1.0,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Differential attention of the sequences' last tokens q [n_tok][n_heads][head_dim]
+        over their blocks: [n_tok][n_heads / 2][2 head_dim], query pair j (heads 2 j,
+        2 j + 1) over the two maps of its pair of KV heads, the second one times
+        lam f32[n_heads / 2]; with norm f32[2 head_dim] each pair's row over the root of
+        its mean square (and eps), times norm; times gain.  out may be
+        q.view(n_tok, n_heads / 2, 2 head_dim).  No gradient."""
+        if scale is None:
+            scale = self.c.head_dim ** -0.5
+        heads = int(q.shape[1]) if q.dim() == 3 else 0
+        if out is None:
+            out = torch.empty((q.shape[0], heads // 2, 2 * self.c.head_dim), dtype=q.dtype, device=q.device)
+        work = torch.empty(netkv_kv_attend_diff_workspace(self.sel.h, self.c, seqs, heads), dtype=torch.uint8,
+                           device=self.device)
+        netkv_kv_attend_diff(self.sel.h, self.c, seqs, q, scale, lam, norm, eps, gain, out, work, self.device)
+        return out
 
     def weigh(self, seqs: Sequences, block_weight: torch.Tensor, page_weight: torch.Tensor) -> None:
         """Add attend's block weights to page_weight u64[n_pages]."""

@@ -187,3 +187,31 @@ def test_binding_refuses_without_a_gpu():
     assert nk._positions(None, nk.netkv_rope_t(n_axes=1), 3, sel.device) == (None, 0)
     with pytest.raises(TypeError, match="pos"):
         nk._positions(torch.zeros(3, dtype=torch.int32), nk.netkv_rope_t(n_axes=1), 3, sel.device)
+
+
+def test_differential_attention_by_hand():
+    """Against a loop over tokens, with the norm."""
+    from tests import blockcache_ref as R
+    from tests import diff_ref as F
+    rng = np.random.default_rng(3)
+    c = R.Cache(3, 2, 64, 16, rng)
+    c.put(2, 16)
+    c.put(0, 2)
+    q, lam, norm = rng.standard_normal((2, 4, 64)), np.array([0.4, -0.2]), rng.standard_normal(128)
+    for nm in (None, norm):
+        o, tol = F.attend(c, np.array([[2, 0]]), [18], [2], q, 0.125, lam, nm, 1e-3, 0.7)
+        for t, seen in ((0, 17), (1, 18)):
+            for j in range(2):
+                d = np.zeros(128)
+                for m, f in ((0, 1.0), (1, -lam[j])):
+                    e, acc = [], np.zeros(128)
+                    for i in range(seen):
+                        pg, sl = ((2, i) if i < 16 else (0, i - 16))
+                        k = R.values(c.k[pg, m, sl]) * c.ks[pg, m]
+                        v = np.concatenate([R.values(c.v[pg, h, sl]) * c.vs[pg, h] for h in range(2)])
+                        e.append(np.exp(0.125 * (q[t, 2 * j + m] @ k)))
+                        acc += e[-1] * v
+                    d += f * acc / sum(e)
+                if nm is not None:
+                    d = d / np.sqrt((d * d).mean() + 1e-3) * nm
+                assert np.allclose(o[t, j], 0.7 * d, rtol=1e-11, atol=1e-13) and (tol[t, j] > 0).all()
