@@ -26,13 +26,16 @@
 #include <hip/hip_runtime.h>
 
 #include "blockdev.h"
+#include "pairplan.h"
 
 namespace {
 
 using namespace blockdev;
+using namespace pairplan;
 
 struct PairArgs : PlanArgs {
     uint32_t pairs;                  // KV pairs
+    uint32_t tile_log;               // log2 of tile_rows
     uint64_t q_stride;
     const void *q;
     void *out;
@@ -112,24 +115,174 @@ __device__ inline f16x8 times(f16x8 x, float r) {
     return x * f16x8{h, h, h, h, h, h, h, h};
 }
 
-// As attend_kernel, with the two maps in the place of two row tiles: each has
-// its own keys, and both take one step's values, which are loaded and widened
-// once.  The four wavefronts take every fourth step each, joined through LDS.
-template <int D, bool HALF, bool SMALL>
-__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairArgs a) {
+// Inclusive sums over the wavefront.
+__device__ inline uint32_t wave_sums(uint32_t x) {
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);   // from 1, 2, 4, 8 lanes before, within 16
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);   // lane 15 to 16 .. 31, 47 to 48 .. 63
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);   // lane 31 to 32 .. 63
+    return x;
+}
+
+// pair_kernel's work list as a wavefront has it in its registers, as Shares:
+// each lane takes up to four sequences in a row (n_seq <= kListed), and a row
+// tile's ranges are of one length.  By sums across lanes in place of LDS
+// shuffles and by 32-bit divisions: one sequence's workgroup has its item after 1.4
+// us, by Shares after 2.9.
+struct PairShares {
+    uint32_t rt[4], len[4], parts[4], per;
+    uint32_t items, slots, joins, own_items, own_slots, own_joins;   // sums up to this lane, and its own
+    bool bad;
+
+    __device__ explicit PairShares(const PairArgs &a) {
+        const uint32_t lane = threadIdx.x & 63;
+        per = (a.kv.n_seq + 63) / 64;
+        bool rows_ok = true;
+        uint32_t kt[4];
+        bad = false;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            rt[j] = kt[j] = 0;
+            const uint32_t s = lane * per + j;
+            if (j >= per || s >= a.kv.n_seq) continue;
+            const Head h = seq_head(a.kv, s);
+            rt[j] = (h.n * a.G + a.tile_rows - 1) >> a.tile_log;   // below 2^32 (make_pair_layout)
+            kt[j] = steps_of(h);
+            bad |= !h.ok;
+            rows_ok &= h.rows_ok;
+        }
+        if (__builtin_expect(__any(!rows_ok), 0)) {
+            // without those that begin among rows of an earlier one
+            const Shares sh(a);
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                rt[j] = sh.rt[j];
+                kt[j] = sh.kt[j];
+            }
+        }
+        // the call's steps; their sum by halves of 32 bits
+        uint64_t work = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) work += (uint64_t)rt[j] * kt[j];
+        const bool wide = __any(work >> 26);               // 64 lanes of less fit 32 bits
+        uint32_t C;
+        if (!wide) {
+            const uint32_t w = (uint32_t)__builtin_amdgcn_readlane((int)wave_sums((uint32_t)work), 63);
+            uint32_t n = (w + a.target - 1) / a.target;
+            if (n > kEnough) n = max((w + a.fine - 1) / a.fine, kEnough);
+            n = max(n, a.least);
+            C = n + (n & 1);
+        } else {
+            for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d, 64);
+            C = range_steps(a, work);
+        }
+        own_items = own_slots = own_joins = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            len[j] = parts[j] = 1;
+            if (j >= per) continue;
+            len[j] = even_steps(kt[j], C);
+            parts[j] = even_parts(kt[j], C);
+            own_items += rt[j] * parts[j];
+            own_slots += parts[j] > 1 ? rt[j] * parts[j] : 0u;
+            own_joins += parts[j] > 1 ? rt[j] : 0u;
+        }
+        items = wave_sums(own_items);
+        slots = wave_sums(own_slots);
+        joins = wave_sums(own_joins);
+    }
+
+    // Item or join i; false if there are not so many.
+    __device__ bool item(const PairArgs &a, uint32_t i, Item &it) const {
+        const uint64_t past = __ballot(items > i);
+        if (!past) return false;
+        const int l = __ffsll((unsigned long long)past) - 1;
+        uint32_t at = items - own_items, slot = slots - own_slots, seq = 0, p = 1, n = 1, rest = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t x = rt[j] * parts[j];
+            if (i >= at && i < at + x) {
+                seq = (threadIdx.x & 63) * per + j;
+                p = parts[j];
+                n = len[j];
+                rest = i - at;
+                break;
+            }
+            at += x;
+            slot += parts[j] > 1 ? x : 0u;
+        }
+        auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
+        p = of(p);
+        n = of(n);
+        rest = of(rest);
+        it.seq = of(seq);
+        it.tile = rest / p;
+        it.k0 = rest % p * n;
+        const Head h = seq_head(a.kv, it.seq);
+        const uint32_t end = tile_end(h, a.G, it.tile, a.tile_rows);
+        it.k1 = p > 1 ? min(end, it.k0 + n) : end;
+        it.slot = p > 1 ? of(slot) + rest : kNoSlot;
+        return true;
+    }
+    __device__ uint32_t n_joins() const { return (uint32_t)__builtin_amdgcn_readlane((int)joins, 63); }
+    __device__ Join join(uint32_t i) const {
+        const int l = __ffsll((unsigned long long)__ballot(joins > i)) - 1;
+        uint32_t at = joins - own_joins, slot = slots - own_slots, seq = 0, tile = 0, p = 1;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t q = parts[j], x = q > 1 ? rt[j] : 0u;
+            if (i >= at && i < at + x) {
+                seq = (threadIdx.x & 63) * per + j;
+                tile = i - at;
+                p = q;
+                slot += tile * q;
+                break;
+            }
+            at += x;
+            slot += x * q;
+        }
+        auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
+        return Join{of(seq), of(tile), of(slot), of(p)};
+    }
+};
+
+// find_item by it.
+__device__ inline bool find_range(const PairArgs &a, uint32_t i, Item &it, Head &hd) {
+    if (a.items) return find_item(a, i, it, hd);
+    const PairShares sh(a);
+    if (blockIdx.x == 0 && __builtin_expect(__any(sh.bad), 0)) fill_bad(a);
+    if (!sh.item(a, i, it)) return false;
+    auto one = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+    it = Item{one(it.seq), one(it.tile), one(it.k0), one(it.k1), one(it.slot), {0, 0, 0}};
+    hd = seq_head(a.kv, it.seq);
+    hd.row0 = (uint64_t)one((uint32_t)(hd.row0 >> 32)) << 32 | one((uint32_t)hd.row0);
+    hd.n = one(hd.n);
+    hd.ctx = one(hd.ctx);
+    return true;
+}
+
+// As attend_kernel, each wavefront for one map: the first and third take the
+// first map, the others the second, two steps of the range at a time.  The two
+// that work on one step read its values once from memory and once from the
+// caches.  Joined through LDS.
+template <int D, int NT, bool HALF, bool SMALL>
+__global__ __launch_bounds__(kThreads, 2) void pair_kernel(PairArgs a) {
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
     constexpr int VD = 2 * D, kDT = VD / 16, kHalf = D / 16;
     constexpr int kPitch = VD + 4;
     __shared__ float lds[kWaves * 16 * kPitch];
-    __shared__ float lds_ml[2][kWaves][16][3];
+    __shared__ float lds_ml[kWaves][16 * NT][3];
 
     const uint32_t hk = a.kv.hk;
     const uint32_t p = blockIdx.x % a.pairs, item = blockIdx.x / a.pairs;
     Item it;
     Head hd;
-    if (!find_item(a, item, it, hd)) return;
+    if (!find_range(a, item, it, hd)) return;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
+    const uint32_t map = w & 1, first = it.k0 + (w >> 1);
     const uint32_t c = lane & 15, g = lane >> 4;
     const uint32_t n_rows = hd.n * a.G;
     const uint32_t row0 = it.tile * a.tile_rows;
@@ -138,25 +291,8 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
     const uint32_t *pages = a.kv.pages + (uint64_t)it.seq * a.kv.max_pages;
     const uint32_t last_block = hd.ctx ? (hd.ctx - 1) >> a.kv.btl : 0u;
 
-    T8 qf[2][D / 32];
-    uint32_t lim;
-    {
-        const uint32_t r = row0 + c;
-        const bool valid = r < n_rows;
-        const uint32_t t = valid ? r / a.G : 0u, j = p * a.G + (valid ? r % a.G : 0u);
-        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
-        lim = !valid ? hd.ctx : seen > 0 ? (uint32_t)seen : 0u;
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)(2 * j + m) * D + 16 * g;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                u32x4 x = {0, 0, 0, 0};
-                if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
-                qf[m][i] = __builtin_bit_cast(T8, x ^ a.q_sign);
-            }
-        }
-    }
+    T8 qf[NT][D / 32];
+    uint32_t lim[NT];
     // tokens that every row sees, and steps that any row sees
     const uint32_t row_last = min(row0 + a.tile_rows, n_rows) - 1;
     const int64_t see_all = (int64_t)hd.ctx - hd.n + row0 / a.G + 1;
@@ -164,10 +300,10 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
     const uint32_t all_lim = see_all > 0 ? (uint32_t)min(see_all, (int64_t)hd.ctx) : 0u;
     const uint32_t end = min(it.k1, see_any > 0 ? (uint32_t)((see_any + kStep - 1) / kStep) : 0u);
 
-    f32x4 acc[2][kDT];
-    float m[2], l[2], y[2];
+    f32x4 acc[NT][kDT];
+    float m[NT], l[NT], y[NT];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < NT; ++n) {
         m[n] = y[n] = -INFINITY;
         l[n] = 0.0f;
 #pragma unroll
@@ -183,33 +319,32 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
     const uint32_t key_in_page = (((SMALL ? (16 * (c >> 2)) & (tile - 1) : 16 * (c >> 2)) + (c & 3)) * D + 16 * g);
     const uint32_t val_in_page = SMALL ? c * tile + ((16 * g) & (tile - 1)) : c * kStep + 16 * g;
     const uint32_t val_piece = SMALL ? 16 * tile : 16 * kStep;
+    const uint8_t *keys = a.kv.k + (2 * p + map) * hb, *vals = a.kv.v + 2 * p * hb;
     auto in_cache = [&](const uint8_t *x, uint32_t kt, uint32_t page) {
-        return x + 2 * p * hb + (page < a.kv.n_pages ? page : 0u) * page_bytes + (uint64_t)((kt * kStep) & (bt - 1)) * D;
+        return x + (page < a.kv.n_pages ? page : 0u) * page_bytes + (uint64_t)((kt * kStep) & (bt - 1)) * D;
     };
 
     // The next step's keys are asked for as soon as this one's have been
     // multiplied, its values likewise; pages a step earlier.
-    KeyRegs<D> kf[2];
+    constexpr uint32_t kOn = kWaves / 2;
+    KeyRegs<D> kf;
     ValRegs<VD> vf;
-    f32x4 st[2][4];
-    f16x8 pf[2][2];
-    float sc_next[2] = {0.0f, 0.0f}, sc[2];
-    float va_next = 0.0f, vb_next = 0.0f;
+    f32x4 st[NT][4];
+    f16x8 pf[NT][2];
+    float sc_next = 0.0f, va_next = 0.0f, vb_next = 0.0f, sc = 0.0f;
     ValScale vs;
-    uint64_t nan_sums = 0;                             // sums of this lane that a NaN value belongs to, in both maps
-    static_assert(4 * kDT <= 64, "a bit a sum");
+    uint64_t nan_sums = 0;                             // sums of this lane that a NaN value belongs to
+    static_assert(4 * NT * kDT <= 64, "a bit a sum");
     uint32_t pk = 0, pv = 0;
     auto load_keys = [&](uint32_t kt, uint32_t page) {
-        const uint8_t *x = in_cache(a.kv.k, kt, page);
+        const uint8_t *x = in_cache(keys, kt, page);
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) kf[n].f[t][i] = *(const u32x4 *)(x + n * hb + key_in_page + 4 * t * D + 64 * i);
+            for (int i = 0; i < D / 64; ++i) kf.f[t][i] = *(const u32x4 *)(x + key_in_page + 4 * t * D + 64 * i);
     };
     auto load_vals = [&](uint32_t kt, uint32_t page) {
-        const uint8_t *x = in_cache(a.kv.v, kt, page);
+        const uint8_t *x = in_cache(vals, kt, page);
 #pragma unroll
         for (int d = 0; d < kDT; ++d) vf.f[d] = *(const u32x4 *)(x + (d / kHalf) * hb + val_in_page + (d % kHalf) * val_piece);
     };
@@ -217,11 +352,10 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
         const bool bad = pv >= a.kv.n_pages;
         if (bad) report(a.kv);
         const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk + 2 * p;
-        sc_next[0] = SMALL ? a.kv.ks[si] : scalar(a.kv.ks)[si];
-        sc_next[1] = SMALL ? a.kv.ks[si + 1] : scalar(a.kv.ks)[si + 1];
+        sc_next = SMALL ? a.kv.ks[si + map] : scalar(a.kv.ks)[si + map];
         va_next = SMALL ? a.kv.vs[si] : scalar(a.kv.vs)[si];
         vb_next = SMALL ? a.kv.vs[si + 1] : scalar(a.kv.vs)[si + 1];
-        if (bad) sc_next[0] = sc_next[1] = va_next = vb_next = NAN;
+        if (bad) sc_next = va_next = vb_next = NAN;
     };
     auto find_pages = [&](uint32_t kt) {
         pk = page_at(kt, c >> 2);
@@ -229,72 +363,68 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
     };
     auto scores = [&](uint32_t kt) {
         vs = val_scale(va_next, vb_next);
+        const float x = sc_next * a.c0;
+        sc = x == 0.0f ? 1.0e-30f : x;                 // not 0, which would turn a masked score's -inf into NaN
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const float x = sc_next[n] * a.c0;
-            sc[n] = x == 0.0f ? 1.0e-30f : x;          // not 0, which would turn a masked score's -inf into NaN
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int t = 0; t < 4; ++t) st[n][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    const u32x4 k = kf[n].f[t][i];
-                    st[n][t] = product(widen<HALF>(k[0], k[1]), qf[n][2 * i], st[n][t]);
-                    st[n][t] = product(widen<HALF>(k[2], k[3]), qf[n][2 * i + 1], st[n][t]);
+            for (int i = 0; i < D / 64; ++i) {
+                const T8 lo = widen<HALF>(kf.f[t][i][0], kf.f[t][i][1]);
+                const T8 hi = widen<HALF>(kf.f[t][i][2], kf.f[t][i][3]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    st[n][t] = product(lo, qf[n][2 * i], st[n][t]);
+                    st[n][t] = product(hi, qf[n][2 * i + 1], st[n][t]);
                 }
-        }
-        if (kt + kWaves < end) {
-            load_keys(kt + kWaves, pk);
+            }
+        if (kt + kOn < end) {
+            load_keys(kt + kOn, pk);
             load_scales();
         }
     };
     auto values = [&](uint32_t kt) {
-        auto go = [&](auto scaled) {
 #pragma unroll
-            for (int d = 0; d < kDT; ++d) {
-                f16x8 lo = widen_f16(vf.f[d][0], vf.f[d][1]), hi = widen_f16(vf.f[d][2], vf.f[d][3]);
-                if constexpr (decltype(scaled)::value) {
-                    lo = times(lo, vs.r[d / kHalf]);
-                    hi = times(hi, vs.r[d / kHalf]);
-                }
+        for (int d = 0; d < kDT; ++d) {
+            const f16x8 lo = times(widen_f16(vf.f[d][0], vf.f[d][1]), vs.r[d / kHalf]);
+            const f16x8 hi = times(widen_f16(vf.f[d][2], vf.f[d][3]), vs.r[d / kHalf]);
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    acc[n][d] = product(lo, pf[n][0], acc[n][d]);
-                    acc[n][d] = product(hi, pf[n][1], acc[n][d]);
-                }
+            for (int n = 0; n < NT; ++n) {
+                acc[n][d] = product(lo, pf[n][0], acc[n][d]);
+                acc[n][d] = product(hi, pf[n][1], acc[n][d]);
             }
-        };
-        if (__all(vs.r[0] == 1.0f && vs.r[1] == 1.0f)) go(std::false_type());
-        else go(std::true_type());
-        if (kt + kWaves < end) {
-            load_vals(kt + kWaves, pv);
-            find_pages(kt + 2 * kWaves);
+        }
+        if (kt + kOn < end) {
+            load_vals(kt + kOn, pv);
+            find_pages(kt + 2 * kOn);
         }
     };
     // as attend_kernel's
     auto softmax = [&]() {
         const float vlog = log2_of(vs.s);
-        float up[2], sum[2];
+        float up[NT], sum[NT];
         bool fits = true;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < NT; ++n) {
             const float by = vlog - y[n];
             up[n] = -by - m[n];
-            sum[n] = weights_of(st[n], sc[n], by, pf[n]);
+            sum[n] = weights_of(st[n], sc, by, pf[n]);
             fits &= sum[n] <= kMaxSum && fabsf(up[n]) < 64.0f;
         }
         if (!__all(fits)) return false;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) l[n] += sum[n] * exp2_of(up[n]);
+        for (int n = 0; n < NT; ++n) l[n] += sum[n] * exp2_of(up[n]);
         return true;
     };
     auto softmax_any = [&](uint32_t kt) {
         const float vlog = log2_of(vs.s);
         const uint32_t tok0 = kt * kStep + 16 * g;
-        const int left = (int)lim - (int)tok0;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < NT; ++n) {
+            const int left = (int)lim[n] - (int)tok0;
             float mx = -INFINITY;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -303,7 +433,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
                     st[n][t][i] = left > 4 * t + i ? st[n][t][i] : -INFINITY;
                     mx = fmaxf(mx, st[n][t][i]);
                 }
-            mx = mx == -INFINITY ? -INFINITY : mx * sc[n];
+            mx = mx == -INFINITY ? -INFINITY : mx * sc;
             const float mn = fmaxf(m[n], row_max(mx)), yn = fmaxf(y[n], row_max(mx + vlog) - kLift);
             l[n] *= m[n] == -INFINITY ? 1.0f : exp2_of(m[n] - mn);   // nothing so far: 0, or NaN
             const float al = y[n] == -INFINITY ? 1.0f : exp2_of(y[n] - yn);
@@ -313,8 +443,8 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
             for (int d = 0; d < kDT; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
-            l[n] += weights_of(st[n], sc[n], mn == -INFINITY ? 0.0f : -mn, pf[n]);
-            weights_of(st[n], sc[n], yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
+            l[n] += weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
+            weights_of(st[n], sc, yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
         }
         if (kt * kStep + kStep <= all_lim) return;
         // Tokens that not every row sees: bytes of slots that hold none may be
@@ -336,9 +466,6 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
         }
         if (!__any(nan)) return;
         uint64_t found = 0;                            // four bits at a time, from the top
-        f16x8 see[2];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) see[j >> 3][j & 7] = left > j ? (_Float16)1.0f : (_Float16)0.0f;
 #pragma unroll
         for (int d = 0; d < kDT; ++d) {
             u32x4 z;
@@ -346,25 +473,48 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
             for (int i = 0; i < 4; ++i) z[i] = nan_bytes(vf.f[d][i]);
             const u32x4 one = z * 0x38u;               // 1.0 per NaN
             vf.f[d] &= ~(z * 0xFFu);
-            f32x4 hit = {0, 0, 0, 0};
-            hit = product(widen_f16(one[0], one[1]), see[0], hit);
-            hit = product(widen_f16(one[2], one[3]), see[1], hit);
-            uint32_t bits = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) bits |= hit[i] > 0.0f ? 1u << i : 0u;
-            found = found >> 4 | (uint64_t)bits << 60;
+            for (int n = 0; n < NT; ++n) {
+                const int left = (int)lim[n] - (int)tok0;
+                f16x8 see[2];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) see[j >> 3][j & 7] = left > j ? (_Float16)1.0f : (_Float16)0.0f;
+                f32x4 hit = {0, 0, 0, 0};
+                hit = product(widen_f16(one[0], one[1]), see[0], hit);
+                hit = product(widen_f16(one[2], one[3]), see[1], hit);
+                uint32_t bits = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bits |= hit[i] > 0.0f ? 1u << i : 0u;
+                found = found >> 4 | (uint64_t)bits << 60;
+            }
         }
-        nan_sums |= found >> (64 - 4 * kDT);
+        nan_sums |= found;
     };
-    if (it.k0 + w < end) {
-        find_pages(it.k0 + w);
-        load_keys(it.k0 + w, pk);
+    if (first < end) {
+        find_pages(first);
+        load_keys(first, pk);
         load_scales();
-        load_vals(it.k0 + w, pv);
-        find_pages(it.k0 + w + kWaves);
+        load_vals(first, pv);
+        find_pages(first + kOn);
+    }
+    // the queries, behind the first step's loads
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t r = row0 + n * 16 + c;
+        const bool valid = r < n_rows;
+        const uint32_t t = valid ? r / a.G : 0u, j = p * a.G + (valid ? r % a.G : 0u);
+        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
+        lim[n] = !valid ? hd.ctx : seen > 0 ? (uint32_t)seen : 0u;
+        const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)(2 * j + map) * D + 16 * g;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            u32x4 x = {0, 0, 0, 0};
+            if (valid) x = *(const u32x4 *)(q + (i / 2) * 64 + (i % 2) * 8);
+            qf[n][i] = __builtin_bit_cast(T8, x ^ a.q_sign);
+        }
     }
     // the ordinary steps have a loop of their own (see prompt_kernel)
-    for (uint32_t kt = it.k0 + w; kt < end; kt += kWaves) {
+    for (uint32_t kt = first; kt < end; kt += kOn) {
         bool done;
         do {
             scores(kt);
@@ -372,7 +522,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
             if (done) done = softmax();
             if (!done) break;
             values(kt);
-            kt += kWaves;
+            kt += kOn;
         } while (kt < end);
         if (done) break;
         softmax_any(kt);
@@ -380,64 +530,54 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void pair_kernel(PairAr
     }
     if (nan_sums)
 #pragma unroll
-        for (int d = 0; d < kDT; ++d)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (nan_sums >> (4 * d + i) & 1) acc[0][d][i] = acc[1][d][i] = NAN;
+            for (int d = 0; d < kDT; ++d)
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+                for (int i = 0; i < 4; ++i)
+                    if (nan_sums >> (64 - 4 * NT * kDT + 4 * (d * NT + n) + i) & 1) acc[n][d][i] = NAN;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
         l[n] = row_sum(l[n]);
         if (g == 0) {
-            lds_ml[n][w][c][0] = m[n];
-            lds_ml[n][w][c][1] = l[n];
-            lds_ml[n][w][c][2] = y[n];
+            lds_ml[w][n * 16 + c][0] = m[n];
+            lds_ml[w][n * 16 + c][1] = l[n];
+            lds_ml[w][n * 16 + c][2] = y[n];
         }
     }
-    constexpr int kEach = 16 * VD / 4 / kThreads;      // pieces of four columns a thread joins
-    f32x4 o[2][kEach];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < NT; ++n) {
         __syncthreads();
 #pragma unroll
         for (int d = 0; d < kDT; ++d) *(f32x4 *)&lds[(w * 16 + c) * kPitch + d * 16 + 4 * g] = acc[n][d];
         __syncthreads();
+        for (uint32_t e = threadIdx.x; e < 16 * VD / 4; e += kThreads) {
+            const uint32_t row = e / (VD / 4), d4 = e % (VD / 4) * 4, r = row0 + n * 16 + row;
+            if (r >= n_rows) continue;                 // a row's lanes go together
+            f32x4 o[2];
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const uint32_t i = threadIdx.x + e * kThreads, row = i / (VD / 4), d4 = i % (VD / 4) * 4, r = row0 + row;
-            float M = -INFINITY, Y = -INFINITY;
-            for (int v = 0; v < kWaves; ++v) {
-                M = fmaxf(M, lds_ml[n][v][row][0]);
-                Y = fmaxf(Y, lds_ml[n][v][row][2]);
-            }
-            float L = 0.0f;
-            f32x4 x = {0, 0, 0, 0};
-            for (int v = 0; v < kWaves; ++v) {
-                const float *ml = lds_ml[n][v][row];
-                L += joined(ml[0], M) * ml[1];
-                const float f = joined(ml[2], Y);
-                const f32x4 z = *(const f32x4 *)&lds[(v * 16 + row) * kPitch + d4];
+            for (int q = 0; q < 2; ++q) {
+                const float *a0 = lds_ml[q][n * 16 + row], *a1 = lds_ml[q + 2][n * 16 + row];
+                const float M = fmaxf(a0[0], a1[0]), Y = fmaxf(a0[2], a1[2]);
+                const float L = joined(a0[0], M) * a0[1] + joined(a1[0], M) * a1[1];
+                const float f0 = joined(a0[2], Y), f1 = joined(a1[2], Y);
+                const f32x4 x0 = *(const f32x4 *)&lds[(q * 16 + row) * kPitch + d4], x1 = *(const f32x4 *)&lds[((q + 2) * 16 + row) * kPitch + d4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] += z[k] * f;
-            }
-            if (it.slot != kNoSlot) {
-                if (r >= n_rows) continue;
-                const uint64_t at = (((uint64_t)it.slot * a.pairs + p) * 2 + n) * a.tile_rows + row;
-                if (d4 == 0) a.part_ml[at] = f32x4{M, L, Y, 0.0f};
-                *(f32x4 *)(a.part + at * VD + d4) = x;
-            } else {
-                const Over over(Y, M, L, hd.ctx + r / a.G >= hd.n);   // both below 2^31
+                for (int i = 0; i < 4; ++i) o[q][i] = x0[i] * f0 + x1[i] * f1;
+                if (it.slot != kNoSlot) {
+                    const uint64_t at = (((uint64_t)it.slot * a.pairs + p) * 2 + q) * a.tile_rows + n * 16 + row;
+                    if (d4 == 0) a.part_ml[at] = f32x4{M, L, Y, 0.0f};
+                    *(f32x4 *)(a.part + at * VD + d4) = o[q];
+                } else {
+                    const Over over(Y, M, L, hd.ctx + r / a.G >= hd.n);   // both below 2^31
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[n][e][k] = over(x[k]);
+                    for (int i = 0; i < 4; ++i) o[q][i] = over(o[q][i]);
+                }
             }
+            if (it.slot != kNoSlot) continue;
+            const uint32_t j = p * a.G + r % a.G;
+            finish<VD>(a, o[0], o[1], j, (T *)a.out + (hd.row0 + r / a.G) * a.out_stride + (uint64_t)j * VD, d4 / 4);
         }
-    }
-    if (it.slot != kNoSlot) return;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-        const uint32_t i = threadIdx.x + e * kThreads, row = i / (VD / 4), r = row0 + row;
-        if (r >= n_rows) continue;                     // a row's lanes go together
-        const uint32_t j = p * a.G + r % a.G;
-        finish<VD>(a, o[0][e], o[1][e], j, (T *)a.out + (hd.row0 + r / a.G) * a.out_stride + (uint64_t)j * VD, i % (VD / 4));
     }
 }
 
@@ -900,70 +1040,84 @@ __device__ inline void join_pair(const PairArgs &a, const Join &j, uint32_t p, u
     const Head hd = seq_head(a.kv, j.seq);
     const uint32_t r = j.tile * rows + tr;
     if (r >= hd.n * a.G) return;
-    const uint64_t by = (uint64_t)a.pairs * 2 * rows;
-    f32x4 both[2];
+    const uint64_t by = (uint64_t)a.pairs * 2 * rows, at = ((uint64_t)j.slot * a.pairs + p) * 2 * rows + tr;
+    float M[2] = {-INFINITY, -INFINITY}, Y[2] = {-INFINITY, -INFINITY};
+    for (uint32_t i = me; i < j.n; i += kLanes)
 #pragma unroll
-    for (int map = 0; map < 2; ++map) {
-        const uint64_t at = (((uint64_t)j.slot * a.pairs + p) * 2 + map) * rows + tr;
-        float M = -INFINITY, Y = -INFINITY;
-        for (uint32_t i = me; i < j.n; i += kLanes) {
-            const f32x4 ml = a.part_ml[at + i * by];
-            M = fmaxf(M, ml[0]);
-            Y = fmaxf(Y, ml[2]);
+        for (int q = 0; q < 2; ++q) {
+            const f32x4 ml = a.part_ml[at + i * by + q * rows];
+            M[q] = fmaxf(M[q], ml[0]);
+            Y[q] = fmaxf(Y[q], ml[2]);
         }
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
         for (int d = 32; d; d >>= 1) {
-            M = fmaxf(M, __shfl_xor(M, d, 64));
-            Y = fmaxf(Y, __shfl_xor(Y, d, 64));
+            M[q] = fmaxf(M[q], __shfl_xor(M[q], d, 64));
+            Y[q] = fmaxf(Y[q], __shfl_xor(Y[q], d, 64));
         }
-        if constexpr (WAVES > 1) {
-            if (lane == 0) {
-                red[0][w] = M;
-                red[1][w] = Y;
+    if constexpr (WAVES > 1) {
+        if (lane == 0)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                red[q][w] = M[q];
+                red[2 + q][w] = Y[q];
             }
-            __syncthreads();
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
             for (int v = 0; v < WAVES; ++v) {
-                M = fmaxf(M, red[0][v]);
-                Y = fmaxf(Y, red[1][v]);
+                M[q] = fmaxf(M[q], red[q][v]);
+                Y[q] = fmaxf(Y[q], red[2 + q][v]);
             }
-        }
-        float L = 0.0f;
-        f32x4 o = {0, 0, 0, 0};
-        for (uint32_t i0 = 0; i0 < j.n; i0 += kLanes) {
-            const uint32_t i = i0 + me;
-            if (i < j.n) {
-                const f32x4 ml = a.part_ml[at + i * by];
-                factor[me] = joined(ml[2], Y);
-                L += joined(ml[0], M) * ml[1];
-            }
-            meet();
-            const uint32_t n = min(j.n - i0, kLanes);
-            const float *x0 = a.part + (at + i0 * by) * VD + col * 4;
-#pragma unroll 4
-            for (uint32_t q = grp; q < n; q += kGroups) {
-                const f32x4 x = *(const f32x4 *)(x0 + q * by * VD);
-                const float f = factor[q];
+    }
+    float L[2] = {0.0f, 0.0f};
+    f32x4 o[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    for (uint32_t i0 = 0; i0 < j.n; i0 += kLanes) {
+        const uint32_t i = i0 + me;
+        if (i < j.n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += f * x[e];
+            for (int q = 0; q < 2; ++q) {
+                const f32x4 ml = a.part_ml[at + i * by + q * rows];
+                factor[q * kThreads + me] = joined(ml[2], Y[q]);
+                L[q] += joined(ml[0], M[q]) * ml[1];
             }
-            meet();
-        }
-        for (int d = 32; d; d >>= 1) L += __shfl_xor(L, d, 64);
-        if (WAVES > 1 && lane == 0) red[2][w] = L;
-        lo[grp * kCols + col] = o;
         meet();
-        if constexpr (WAVES > 1) {
-            L = 0.0f;
-            for (int v = 0; v < WAVES; ++v) L += red[2][v];
-        }
-        o = f32x4{0, 0, 0, 0};
-        for (uint32_t i = 0; i < kGroups; ++i)
+        const uint32_t n = min(j.n - i0, kLanes);
+        const float *x0 = a.part + (at + i0 * by) * VD + col * 4;
+#pragma unroll 4
+        for (uint32_t g = grp; g < n; g += kGroups)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += lo[i * kCols + col][e];
-        const Over over(Y, M, L, hd.ctx + r / a.G >= hd.n);   // both below 2^31
+            for (int q = 0; q < 2; ++q) {
+                const f32x4 x = *(const f32x4 *)(x0 + (g * by + q * rows) * VD);
+                const float f = factor[q * kThreads + g];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) both[map][e] = over(o[e]);
+                for (int e = 0; e < 4; ++e) o[q][e] += f * x[e];
+            }
         meet();
     }
+    f32x4 both[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        for (int d = 32; d; d >>= 1) L[q] += __shfl_xor(L[q], d, 64);
+        if (WAVES > 1 && lane == 0) red[4 + q][w] = L[q];
+        lo[q * kThreads + grp * kCols + col] = o[q];
+    }
+    meet();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        if constexpr (WAVES > 1) {
+            L[q] = 0.0f;
+            for (int v = 0; v < WAVES; ++v) L[q] += red[4 + q][v];
+        }
+        o[q] = f32x4{0, 0, 0, 0};
+        for (uint32_t i = 0; i < kGroups; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[q][e] += lo[q * kThreads + i * kCols + col][e];
+        const Over over(Y[q], M[q], L[q], hd.ctx + r / a.G >= hd.n);   // both below 2^31
+#pragma unroll
+        for (int e = 0; e < 4; ++e) both[q][e] = over(o[q][e]);
+    }
+    meet();
     if (grp) return;
     const uint32_t jq = p * a.G + r % a.G;
     finish<VD>(a, both[0], both[1], jq, (T *)a.out + (hd.row0 + r / a.G) * a.out_stride + (uint64_t)jq * VD, col);
@@ -973,8 +1127,8 @@ __device__ inline void join_pair(const PairArgs &a, const Join &j, uint32_t p, u
 // workgroups, else a wavefront a row.
 template <int VD, bool HALF>
 __global__ __launch_bounds__(kThreads) void pair_join_kernel(PairArgs a, uint32_t rows) {
-    __shared__ f32x4 lo[kThreads];
-    __shared__ float factor[kThreads], red[3][kWaves];
+    __shared__ f32x4 lo[2 * kThreads];
+    __shared__ float factor[2 * kThreads], red[6][kWaves];
     const uint32_t w = threadIdx.x >> 6;
     auto all = [&](uint32_t n_joins, auto join) {
         const uint32_t n = n_joins * a.pairs * rows;   // at most 2,048 joins and pairs, 128 rows
@@ -990,6 +1144,9 @@ __global__ __launch_bounds__(kThreads) void pair_join_kernel(PairArgs a, uint32_
     };
     if (a.joins) {
         all(a.head->n_joins, [&](uint32_t i) { return a.joins[i]; });
+    } else if (a.tile_log) {
+        const PairShares sh(a);
+        all(sh.n_joins(), [&](uint32_t i) { return sh.join(i); });
     } else {
         const Shares sh(a);
         all(sh.n_joins(), [&](uint32_t i) { return sh.join(i); });
@@ -1001,6 +1158,7 @@ __global__ __launch_bounds__(kThreads) void pair_join_kernel(PairArgs a, uint32_
 struct PairLayout : Split {
     uint32_t pairs;
     bool rows;             // pair_prompt_kernel
+    int NT;                // row tiles of pair_kernel
     uint32_t item_cap, slot_cap, join_cap, tile_most;
     uint64_t head, items, joins, ml, part, total;
 };
@@ -1015,13 +1173,27 @@ netkv_status make_pair_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t 
     const uint64_t most = (uint64_t)a.max_tok * y.G;   // rows of the longest sequence's pair
     if (most > 0xFFFFFFFFull - 1024) return invalid(h, "max_tok * n_heads / n_kv_heads must be < 2^32 - 1024");
     y.rows = most > (D == 64 ? 96u : 32u);
-    y.tile_rows = !y.rows ? 16u : D == 64 ? 128u : 64u;
+    y.NT = D == 128 || most <= 16 ? 1 : 2;
+    y.tile_rows = !y.rows ? 16u * y.NT : D == 64 ? 128u : 64u;
     y.tile_most = (uint32_t)(most < y.tile_rows ? most : y.tile_rows);
-    y.target = (512u + y.pairs - 1) / y.pairs;
-    y.fine = y.rows || D == 128 ? y.target : (1024u + y.pairs - 1) / y.pairs;
+    // Ranges a pair, of the card's 512 workgroup slots.  Prompts: as make_layout's.
+    // Few rows, 128 dimensions: one workgroup a CU streams as fast as two, whose
+    // second reads of the values miss the caches more often, so few tiles (long
+    // sequences) get 256 ranges in all; where unequal tiles leave some short 320,
+    // us, 256, 320, 512: 8 sequences of 131,071 tokens and 4 pairs 368, 510, 411, one
+    // of 131,072 54, 73, 59, 64 of up to 16,384 195, 169, 190, 16 of up to 30,000
+    // and 16 pairs 400, 321, 360, 37 of up to 3,000 33, 33, 42, 200 of up to 1,000
+    // 48, 54, 56.  64 dimensions: 384, or with more than kEnough steps each 1,024;
+    // us, 256, 384, 512 and 1,024: 64 of up to 16,384 and 8 pairs 197, 170, 159, 37 of
+    // up to 5,003 and 3 pairs 30, 27, 31.
+    const uint64_t slots = (512u + y.pairs - 1) / y.pairs, tiles = (uint64_t)a.n_seq * ((most + y.tile_rows - 1) / y.tile_rows);
+    uint64_t ranges = slots;
+    if (!y.rows) ranges = D == 64 ? 3 * slots / 4 : tiles <= slots / 8 || tiles > slots ? slots / 2 : 5 * slots / 8;
+    y.target = (uint32_t)(ranges ? ranges : 1);
+    y.fine = y.rows || D == 128 ? y.target : (uint32_t)(2 * slots);
     const uint32_t bt = 1u << a.btl;
-    y.least = y.rows ? 8 : kWaves;
-    y.round = !y.rows ? kWaves : bt > kStep ? bt / kStep : 1;
+    y.least = y.rows ? 8 : 4;
+    y.round = !y.rows ? 2 : bt > kStep ? bt / kStep : 1;
     const Caps caps = caps_of(a, y);
     if (!grid_fits(caps.items * y.pairs, y.rows ? kPromptThreads : kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
     y.item_cap = (uint32_t)caps.items;
@@ -1050,8 +1222,10 @@ void launch_pairs(const PairLayout &y, const PairArgs &a, hipStream_t s) {
     if (y.rows)
         small ? pair_prompt_kernel<D, D == 64 ? 2 : 1, HALF, true><<<grid, kPromptThreads, 0, s>>>(a)
               : pair_prompt_kernel<D, D == 64 ? 2 : 1, HALF, false><<<grid, kPromptThreads, 0, s>>>(a);
-    else
-        small ? pair_kernel<D, HALF, true><<<grid, kThreads, 0, s>>>(a) : pair_kernel<D, HALF, false><<<grid, kThreads, 0, s>>>(a);
+    else if (D == 128 || y.NT == 1)
+        small ? pair_kernel<D, 1, HALF, true><<<grid, kThreads, 0, s>>>(a) : pair_kernel<D, 1, HALF, false><<<grid, kThreads, 0, s>>>(a);
+    else if constexpr (D == 64)
+        small ? pair_kernel<D, 2, HALF, true><<<grid, kThreads, 0, s>>>(a) : pair_kernel<D, 2, HALF, false><<<grid, kThreads, 0, s>>>(a);
     // nothing is split where no sequence can be longer than the shortest range
     const uint64_t steps_most = (((uint64_t)a.kv.max_pages << a.kv.btl) + kStep - 1) / kStep;
     const uint64_t joins_most = (uint64_t)y.join_cap * y.pairs * y.tile_most, quarter = (joins_most + 3) / 4;
@@ -1118,6 +1292,7 @@ extern "C" netkv_status netkv_kv_attend_diff(netkv_handle h, const netkv_kv_t *k
         launch_plan(t, s);
     }
     t.pairs = y.pairs;
+    t.tile_log = y.rows ? 0 : y.NT == 2 ? 5 : 4;
     t.q_stride = q_stride;
     t.q = q;
     t.out = out;

@@ -38,6 +38,8 @@ def weights(seed, heads, dim):
 
 
 def run(cache, seqs, qd, lam, norm=None, **kw):
+    if "out" not in kw:                                    # a row left out must not hold an earlier call's answer
+        kw["out"] = torch.full((qd.shape[0], qd.shape[1] // 2, 2 * qd.shape[2]), -77.0, dtype=qd.dtype, device="cuda")
     return cache.attend_diff(seqs, qd, dev(lam, np.float32), norm=None if norm is None else dev(norm, np.float32), **kw)
 
 
@@ -347,7 +349,10 @@ def test_invalid_sequences(nk, sel, dim, n_new):
         with pytest.raises(nk.NetKVError, match="block cache"):
             sel.sync_errors()
         sel.sync_errors()
-        assert torch.isnan(o[lo:hi]).all() and torch.equal(o[:lo], good[:lo]) and torch.equal(o[hi:], good[hi:])
+        assert torch.isnan(o[lo:hi]).all()
+        # how a sequence is split may depend on the others: within what its sums may be off
+        check(c, table[:1], ctx[:1], new[:1], q[:lo], o[:lo], lam, norm)
+        check(c, table[2:], ctx[2:], new[2:], q[hi:], o[hi:], lam, norm)
     out = torch.full((3 * n_new, 2, 2 * dim), 5.0, dtype=torch.bfloat16, device="cuda")
     go(sequences(nk, new, ctx, table, off=[0, 2 * n_new, n_new, 3 * n_new + 1], max_tok=2 * n_new + 1), out=out)
     with pytest.raises(nk.NetKVError, match="block cache"):
