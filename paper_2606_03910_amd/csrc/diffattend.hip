@@ -32,6 +32,7 @@ namespace {
 
 using namespace blockdev;
 using namespace pairplan;
+using blockdev::weights_of;
 
 struct PairArgs : PlanArgs {
     uint32_t pairs;                  // KV pairs
@@ -261,6 +262,27 @@ __device__ inline bool find_range(const PairArgs &a, uint32_t i, Item &it, Head 
     hd.n = one(hd.n);
     hd.ctx = one(hd.ctx);
     return true;
+}
+
+// weights_of (blockdev.h) of 8 scores.
+__device__ __forceinline__ float weights_of(const f32x4 (&st)[2], float sc, float by, f16x8 (&pf)[1]) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = exp2_of(fmaf(st[t][i], sc, by));
+            sum += p[i];
+        }
+        const f16x2 u = __builtin_convertvector((f32x2{p[0], p[1]}), f16x2), v = __builtin_convertvector((f32x2{p[2], p[3]}), f16x2);
+        pf[0][4 * t] = u[0];
+        pf[0][4 * t + 1] = u[1];
+        pf[0][4 * t + 2] = v[0];
+        pf[0][4 * t + 3] = v[1];
+    }
+    asm volatile("" : "+v"(pf[0]), "+v"(sum));
+    return sum;
 }
 
 // As attend_kernel, each wavefront for one map: the first and third take the
@@ -593,18 +615,20 @@ __global__ __launch_bounds__(kThreads, 2) void pair_kernel(PairArgs a) {
 // values k + 1 with its own (slot 2 k + 2: values k - 1 were last read in slot
 // 2 k + 1, values k + 1 are first read in slot 2 k + 4).  At the end the second
 // map's rows go to the first group through LDS.
-template <int D, int NT, bool HALF, bool SMALL>
+template <int D, int NT, int STEP, bool HALF, bool SMALL>
 __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs a) {
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
     constexpr int VD = 2 * D, kDT = VD / 16;
     constexpr int kAhead = 6;                         // fragments read ahead of their products
-    constexpr int kShare = D / 32;                    // 16-byte pieces of keys or values a lane stages
-    constexpr int kKeys = D / 8, kVals = D / 4;       // fragments of one map's keys, of the values
+    constexpr int kT = STEP / 16, kU = STEP / 32;     // products with the keys, fragments of a tile of values a step
+    constexpr uint32_t kGroup = STEP / 4;             // tokens of a lane
+    constexpr int kShare = kT * D / 128;              // 16-byte pieces of keys or values a lane stages
+    constexpr int kKeys = kT * D / 32, kVals = kU * kDT;   // fragments of one map's keys, of the values
     __shared__ u32x4 lds[2 * (2 * kKeys + kVals)][64];
     __shared__ uint8_t lds_bits[2][kVals][64];        // which of a fragment lane's 8 values were NaN
     __shared__ uint32_t lds_nan[2];
-    static_assert(4 * NT * kDT <= 2 * (2 * kKeys + kVals), "a map's rows fit");
+    static_assert(4 * kDT <= 2 * (2 * kKeys + kVals), "a map's 64 rows fit");
 
     const uint32_t hk = a.kv.hk;
     const uint32_t p = blockIdx.x % a.pairs, item = blockIdx.x / a.pairs;
@@ -619,7 +643,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     const uint32_t c = lane & 15, g = lane >> 4;
     const uint32_t n_rows = hd.n * a.G;
     const uint32_t row0 = it.tile * a.tile_rows + (w & 3) * 16 * NT;
-    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep);
+    const uint32_t bt = 1u << a.kv.btl, tile = min(bt, kStep), in_step = min(bt, (uint32_t)STEP);
     const uint64_t hb = head_bytes(a.kv, D);
     const uint32_t *pages = a.kv.pages + (uint64_t)it.seq * a.kv.max_pages;
     const uint32_t last_block = hd.ctx ? (hd.ctx - 1) >> a.kv.btl : 0u;
@@ -647,37 +671,53 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     const int64_t see_tile = (int64_t)hd.ctx - hd.n + it.tile * a.tile_rows / a.G + 1;
     const uint32_t tile_lim = see_tile > 0 ? (uint32_t)min(see_tile, (int64_t)hd.ctx) : 0u;
 
-    f32x4 acc[NT][kDT], st[NT][4];
-    f16x8 pf[NT][2];
+    // the range's steps, those that no row sees left out
+    const int64_t see_any = (int64_t)hd.ctx - hd.n + (min((it.tile + 1) * a.tile_rows, n_rows) - 1) / a.G + 1;
+    const uint32_t k0 = it.k0 * (kStep / STEP), k1 = min(it.k1 * (kStep / STEP), see_any > 0 ? (uint32_t)((see_any + STEP - 1) / STEP) : 0u);
+
+    f32x4 acc[NT][kDT], st[NT][kT];
+    f16x8 pf[NT][kU];
     float m[NT], l[NT], y[NT];
-    uint64_t nan_sums = 0;                            // sums of this lane that a NaN value belongs to
-    static_assert(4 * NT * kDT <= 64, "a bit a sum");
+    uint64_t nan_sums[NT];                            // sums of this lane that a NaN value belongs to
+    static_assert(4 * kDT <= 64, "a bit a sum");
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         m[n] = y[n] = -INFINITY;
         l[n] = 0.0f;
-        pf[n][0] = pf[n][1] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        nan_sums[n] = 0;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) pf[n][u] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
         for (int d = 0; d < kDT; ++d) acc[n][d] = f32x4{0, 0, 0, 0};
     }
 
-    // this lane's pieces: 64 dimensions of key row c of a product, of each
-    // map, or 16 tokens of dimension 16 d + c
+    // this lane's pieces: 16 dimensions of key row c of a product, and values: 16
+    // tokens of a dimension, the lane's own 16, or of 32-token steps those of two
+    // groups of lanes
     u32x4 px[kShare];
     float sc_at[2], vs_at[2], rv_at[2];                // scales of this step and the next; r of the half that this wavefront widens
     const uint32_t half = second ? (w - 4) >> 1 : 0u;
-    const uint32_t own_group = SMALL ? second ? g : c >> 2 : 0u;   // whose page this lane's pieces are in
+    const uint32_t v_dim = STEP == 64 ? c : lane >> 1, v_group = STEP == 64 ? g : lane & 1;
+    const uint32_t own_group = SMALL ? second ? v_group : kGroup * (c >> 2) / 16 : 0u;   // whose page this lane's pieces are in
+    const uint32_t group = kGroup * g / 16;            // and its scores' tokens
     auto page_at = [&](uint32_t kt, uint32_t group) {
-        const uint32_t block = min((kt * kStep + (SMALL ? 16 * group : 0u)) >> a.kv.btl, last_block);
+        const uint32_t block = min((kt * STEP + (SMALL ? 16 * group : 0u)) >> a.kv.btl, last_block);
         return SMALL ? pages[block] : scalar(pages)[block];
     };
     const uint8_t *own = (second ? a.kv.v : a.kv.k) + (2 * p + half) * hb;
     const uint64_t page_bytes = hk * hb;
-    const uint32_t in_page = second ? c * tile + ((16 * g) & (tile - 1)) + (w & 1) * kShare * 16 * tile
-                                    : ((16 * (c >> 2)) & (tile - 1)) * D + ((c & 3) + 4 * w) * D + 16 * g;
-    const uint64_t piece = second ? 16 * tile : 64, map_step = second ? (uint64_t)kShare / 2 * 16 * tile : hb;
+    constexpr int kTiles = STEP == 64 ? 1 : 2;         // value tiles a piece
+    // pieces i: keys, of product t D / 64 of one map, then of the other (64-token
+    // steps), or of one map (32); values, kTiles tiles in a row
+    const uint32_t t_own = STEP == 64 ? w & 3 : w & 1, q_own = STEP == 64 ? 0u : (w & 3) >> 1;
+    const uint32_t in_page = second ? v_dim * tile + ((16 * v_group) & (in_step - 1)) + (w & 1) * kShare * kTiles * 16 * tile
+                                    : (((kGroup * (c >> 2)) & (in_step - 1)) + (c & 3) + 4 * t_own) * D + 16 * g;
+    const uint64_t piece = second ? kTiles * 16 * tile : 64;
+    const uint64_t jump = second ? (uint64_t)(D / 64) * piece : hb;   // from piece D / 64 on
+    if (!second) own += q_own * hb;
     const float *ks = a.kv.ks + 2 * p + map, *vs = a.kv.vs + 2 * p;
-    auto scales_of = [&](uint32_t pv, float &sc, float &vsc, float &rv) {
+    // of the scores' page pv, r of the pieces' page po
+    auto scales_of = [&](uint32_t pv, uint32_t po, float &sc, float &vsc, float &rv) {
         const bool bad = pv >= a.kv.n_pages;
         if (bad) report(a.kv);
         const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk;
@@ -686,29 +726,40 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
         const ValScale v = val_scale(va, vb);
         vsc = v.s;
         rv = half ? v.r[1] : v.r[0];
+        if (SMALL && STEP == 32 && second) {
+            const uint64_t so = (uint64_t)(po < a.kv.n_pages ? po : 0u) * hk;
+            const ValScale o = val_scale(vs[so], vs[so + 1]);
+            rv = half ? o.r[1] : o.r[0];
+        }
         if (bad) sc = vsc = NAN;
     };
-    // pieces i: keys, D / 64 of the first map, then of the second; values, tiles in a row
     auto fetch = [&](uint32_t kt, uint32_t po) {
-        const uint8_t *x = own + (po < a.kv.n_pages ? po : 0u) * page_bytes + (uint64_t)((kt * kStep) & (bt - 1)) * D;
+        const uint32_t t0 = (kt * STEP) & (bt - 1);
+        const uint8_t *x = own + (po < a.kv.n_pages ? po : 0u) * page_bytes + (second ? (uint64_t)(t0 & ~(tile - 1)) * D + (t0 & (tile - 1)) : (uint64_t)t0 * D);
 #pragma unroll
-        for (int i = 0; i < kShare; ++i) px[i] = *(const u32x4 *)(x + in_page + (i / (kShare / 2)) * map_step + (i % (kShare / 2)) * piece);
+        for (int i = 0; i < kShare; ++i) px[i] = *(const u32x4 *)(x + in_page + (i / (D / 64)) * jump + (i % (D / 64)) * piece);
     };
     auto stage = [&](uint32_t kt, float rv) {
         const int b = kt & 1;
         if (!second) {
 #pragma unroll
             for (int i = 0; i < kShare; ++i) {
-                const int f = w * (D / 32) + 2 * (i % (kShare / 2));
-                lds_k(b, i / (kShare / 2), f)[lane] = __builtin_bit_cast(u32x4, widen<HALF>(px[i][0], px[i][1]));
-                lds_k(b, i / (kShare / 2), f + 1)[lane] = __builtin_bit_cast(u32x4, widen<HALF>(px[i][2], px[i][3]));
+                const int f = t_own * (D / 32) + 2 * (i % (D / 64));
+                lds_k(b, q_own + i / (D / 64), f)[lane] = __builtin_bit_cast(u32x4, widen<HALF>(px[i][0], px[i][1]));
+                lds_k(b, q_own + i / (D / 64), f + 1)[lane] = __builtin_bit_cast(u32x4, widen<HALF>(px[i][2], px[i][3]));
             }
             return;
         }
-        if (kt * kStep + kStep > tile_lim) {
+        // where a piece's 16 tokens go: two fragments of a tile at the lane's own
+        // place, or one at two lanes' places
+        auto place = [&](int i, int h) {
+            const uint32_t d = ((w - 4) * kShare + i) * kTiles + (STEP == 64 ? 0u : v_dim >> 4);
+            return STEP == 64 ? (2 * d + h) * 64 + lane : d * 64 + (2 * v_group + h) * 16 + (v_dim & 15);
+        };
+        if (kt * STEP + STEP > tile_lim) {
             // bytes of slots that hold no token are cleared, a NaN is taken out
             // and noted
-            const uint32_t tok0 = kt * kStep + 16 * g;
+            const uint32_t tok0 = kt * STEP + 16 * v_group;
             const int have = (int)min(16u, hd.ctx > tok0 ? hd.ctx - tok0 : 0u);
             bool nan = false;
 #pragma unroll
@@ -720,9 +771,9 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
                     nan |= nan_bytes(px[i][j]) != 0;
                 }
             if (__any(nan)) {
+                uint8_t *bits_at = &lds_bits[b][0][0];
 #pragma unroll
                 for (int i = 0; i < kShare; ++i) {
-                    const uint32_t j = (w - 4) * kShare + i;
                     uint32_t bits = 0;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
@@ -730,8 +781,8 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
                         px[i][q] &= ~(z * 0xFFu);
                         bits |= ((z | z >> 7 | z >> 14 | z >> 21) & 15u) << (4 * q);
                     }
-                    lds_bits[b][2 * j][lane] = (uint8_t)bits;
-                    lds_bits[b][2 * j + 1][lane] = (uint8_t)(bits >> 8);
+                    bits_at[place(i, 0)] = (uint8_t)bits;
+                    bits_at[place(i, 1)] = (uint8_t)(bits >> 8);
                 }
                 if (lane == 0) atomicOr(&lds_nan[b], 1u << (w - 4));
             } else if (lane == 0) {
@@ -739,16 +790,16 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
             }
         }
         const bool scaled = !__all(rv == 1.0f);
+        u32x4 *to = lds_v(b, 0);
 #pragma unroll
         for (int i = 0; i < kShare; ++i) {
-            const uint32_t j = (w - 4) * kShare + i;
             f16x8 lo = widen_f16(px[i][0], px[i][1]), hi = widen_f16(px[i][2], px[i][3]);
             if (scaled) {
                 lo = times(lo, rv);
                 hi = times(hi, rv);
             }
-            lds_v(b, 2 * j)[lane] = __builtin_bit_cast(u32x4, lo);
-            lds_v(b, 2 * j + 1)[lane] = __builtin_bit_cast(u32x4, hi);
+            to[place(i, 0)] = __builtin_bit_cast(u32x4, lo);
+            to[place(i, 1)] = __builtin_bit_cast(u32x4, hi);
         }
     };
     // LDS alone is handed over: loads from memory stay in flight
@@ -763,9 +814,9 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) st[n][t] = f32x4{0, 0, 0, 0};
+            for (int t = 0; t < kT; ++t) st[n][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 4; t += 2)
+        for (int t = 0; t < kT; t += 2)
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -780,10 +831,10 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
 #pragma unroll
         for (int d = 0; d < kDT; d += 2)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < kU; ++u)
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    const f16x8 vf = __builtin_bit_cast(f16x8, lds_v(b, 2 * (d + q) + u)[lane]);
+                    const f16x8 vf = __builtin_bit_cast(f16x8, lds_v(b, kU * (d + q) + u)[lane]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) acc[n][d + q] = product(vf, pf[n][u], acc[n][d + q]);
                 }
@@ -823,19 +874,19 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     };
     auto softmax_any = [&](uint32_t kt) {
         const float sc = scale_of(), vlog = log2_of(vs_at[0]);
-        const uint32_t tok0 = kt * kStep + 16 * g;
-        if (kt * kStep + kStep > tile_lim) {
+        const uint32_t tok0 = kt * STEP + kGroup * g;
+        if (kt * STEP + STEP > tile_lim) {
             const uint32_t noted = lds_nan[kt & 1];
             if (noted)
 #pragma unroll 1
                 for (int d = 0; d < kDT; ++d) {
-                    if (!(noted >> (d / kShare) & 1)) continue;
+                    if (!(noted >> (d / (kDT / 4)) & 1)) continue;
                     f32x4 hit[NT];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) hit[n] = f32x4{0, 0, 0, 0};
 #pragma unroll 1
-                    for (int u = 0; u < 2; ++u) {
-                        const uint32_t bits = lds_bits[kt & 1][2 * d + u][lane];
+                    for (int u = 0; u < kU; ++u) {
+                        const uint32_t bits = lds_bits[kt & 1][kU * d + u][lane];
                         f16x8 one;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) one[j] = bits >> j & 1 ? (_Float16)1.0f : (_Float16)0.0f;
@@ -851,7 +902,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) nan_sums |= (uint64_t)(hit[n][i] > 0.0f) << (4 * (n * kDT + d) + i);
+                        for (int i = 0; i < 4; ++i) nan_sums[n] |= (uint64_t)(hit[n][i] > 0.0f) << (4 * d + i);
                 }
         }
 #pragma unroll
@@ -859,7 +910,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
             const int left = (int)lim[n] - (int)tok0;
             float mx = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < kT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     st[n][t][i] = left > 4 * t + i ? st[n][t][i] : -INFINITY;
@@ -885,30 +936,30 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     float sc_on = 0.0f, vs_on = 0.0f, rv_on = 1.0f;   // scales of the step after next
     if (threadIdx.x < 2) lds_nan[threadIdx.x] = 0;
     // the first step's products with "the step before" are of zeros
-    for (uint32_t i = threadIdx.x; i < kVals * 64; i += kPromptThreads) lds_v(~it.k0 & 1, 0)[i] = u32x4{0, 0, 0, 0};
+    for (uint32_t i = threadIdx.x; i < kVals * 64; i += kPromptThreads) lds_v(~k0 & 1, 0)[i] = u32x4{0, 0, 0, 0};
     meet();
     sc_at[0] = vs_at[0] = sc_at[1] = vs_at[1] = 0.0f;
     rv_at[0] = rv_at[1] = 1.0f;
-    if (it.k0 < it.k1) {
-        fetch(it.k0, page_at(it.k0, own_group));
-        scales_of(page_at(it.k0, g), sc_at[0], vs_at[0], rv_at[0]);
-        stage(it.k0, rv_at[0]);
-        fetch(it.k0 + 1, page_at(it.k0 + 1, own_group));
-        scales_of(page_at(it.k0 + 1, g), sc_at[1], vs_at[1], rv_at[1]);
-        po = page_at(it.k0 + 2, own_group);
-        pv = SMALL ? page_at(it.k0 + 2, g) : po;
+    if (k0 < k1) {
+        fetch(k0, page_at(k0, own_group));
+        scales_of(page_at(k0, group), page_at(k0, own_group), sc_at[0], vs_at[0], rv_at[0]);
+        stage(k0, rv_at[0]);
+        fetch(k0 + 1, page_at(k0 + 1, own_group));
+        scales_of(page_at(k0 + 1, group), page_at(k0 + 1, own_group), sc_at[1], vs_at[1], rv_at[1]);
+        po = page_at(k0 + 2, own_group);
+        pv = SMALL ? page_at(k0 + 2, group) : po;
     }
     meet();
     if (second) meet();
     // Small loads for later steps go out before the softmax, which hides them
     // (page_at stays within the sequence's blocks past its end).
     auto look_ahead = [&](uint32_t kt) {
-        scales_of(pv, sc_on, vs_on, rv_on);
+        scales_of(pv, po, sc_on, vs_on, rv_on);
         po_on = page_at(kt + 3, own_group);
-        pv_on = SMALL ? page_at(kt + 3, g) : po_on;
+        pv_on = SMALL ? page_at(kt + 3, group) : po_on;
     };
     auto pass_on = [&](uint32_t kt) {
-        if (kt + 1 < it.k1) {
+        if (kt + 1 < k1) {
             stage(kt + 1, rv_at[1]);
             fetch(kt + 2, po);
         }
@@ -922,36 +973,36 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
         meet();
     };
     // the ordinary steps have a loop of their own (see prompt_kernel)
-    for (uint32_t kt = it.k0; kt < it.k1; ++kt) {
+    for (uint32_t kt = k0; kt < k1; ++kt) {
         bool done;
         do {
             values(kt - 1);
             scores(kt);
-            interleave(std::integral_constant<int, 3 * D / 8>());
+            interleave(std::integral_constant<int, kVals + kKeys>());
             meet();
-            done = kt * kStep + kStep <= all_lim && kt > it.k0;   // the first step sets the maxima
-            if (kt * kStep + kStep > tile_lim) done = done && __builtin_amdgcn_readfirstlane(lds_nan[kt & 1]) == 0;
+            done = kt * STEP + STEP <= all_lim && kt > k0;   // the first step sets the maxima
+            if (kt * STEP + STEP > tile_lim) done = done && __builtin_amdgcn_readfirstlane(lds_nan[kt & 1]) == 0;
             look_ahead(kt);
             if (done) done = softmax();
             if (!done) break;
             pass_on(kt);
             ++kt;
-        } while (kt < it.k1);
+        } while (kt < k1);
         if (done) break;
         softmax_any(kt);
         pass_on(kt);
     }
     if (!second) meet();
-    if (it.k0 < it.k1) values(it.k1 - 1);
+    if (k0 < k1) values(k1 - 1);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         l[n] = row_sum(l[n]);
-        if (nan_sums)
+        if (nan_sums[n])
 #pragma unroll
             for (int d = 0; d < kDT; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (nan_sums >> (4 * (n * kDT + d) + i) & 1) acc[n][d][i] = NAN;
+                    if (nan_sums[n] >> (4 * d + i) & 1) acc[n][d][i] = NAN;
     }
     if (it.slot != kNoSlot) {
 #pragma unroll
@@ -973,17 +1024,15 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[n][d][i] = over(acc[n][d][i]);
     }
-    __syncthreads();                                  // the last values have been read
-    f32x4(*other)[64] = (f32x4(*)[64]) & lds[(w & 3) * NT * kDT];
-    if (second)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int d = 0; d < kDT; ++d) other[n * kDT + d][lane] = acc[n][d];
-    __syncthreads();
-    if (second) return;
+    f32x4(*other)[64] = (f32x4(*)[64]) & lds[(w & 3) * kDT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+        __syncthreads();                              // the last values, or the rows before these, have been read
+        if (second)
+#pragma unroll
+            for (int d = 0; d < kDT; ++d) other[d][lane] = acc[n][d];
+        __syncthreads();
+        if (second) continue;
         const uint32_t r = row0 + n * 16 + c;
         const bool valid = r < n_rows;
         const uint32_t j = p * a.G + (valid ? r % a.G : 0u);
@@ -991,7 +1040,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
         float most = 0.0f;
 #pragma unroll
         for (int d = 0; d < kDT; ++d) {
-            const f32x4 x = other[n * kDT + d][lane];
+            const f32x4 x = other[d][lane];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 acc[n][d][i] = fmaf(-lam, x[i], acc[n][d][i]);
@@ -1174,7 +1223,7 @@ netkv_status make_pair_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t 
     if (most > 0xFFFFFFFFull - 1024) return invalid(h, "max_tok * n_heads / n_kv_heads must be < 2^32 - 1024");
     y.rows = most > (D == 64 ? 96u : 32u);
     y.NT = D == 128 || most <= 16 ? 1 : 2;
-    y.tile_rows = !y.rows ? 16u * y.NT : D == 64 ? 128u : 64u;
+    y.tile_rows = !y.rows ? 16u * y.NT : 128u;
     y.tile_most = (uint32_t)(most < y.tile_rows ? most : y.tile_rows);
     // Ranges a pair, of the card's 512 workgroup slots.  Prompts: as make_layout's.
     // Few rows, 128 dimensions: one workgroup a CU streams as fast as two, whose
@@ -1220,8 +1269,8 @@ void launch_pairs(const PairLayout &y, const PairArgs &a, hipStream_t s) {
     const dim3 grid(y.item_cap * y.pairs);
     const bool small = a.kv.btl < 6;
     if (y.rows)
-        small ? pair_prompt_kernel<D, D == 64 ? 2 : 1, HALF, true><<<grid, kPromptThreads, 0, s>>>(a)
-              : pair_prompt_kernel<D, D == 64 ? 2 : 1, HALF, false><<<grid, kPromptThreads, 0, s>>>(a);
+        small ? pair_prompt_kernel<D, 2, D == 64 ? 64 : 32, HALF, true><<<grid, kPromptThreads, 0, s>>>(a)
+              : pair_prompt_kernel<D, 2, D == 64 ? 64 : 32, HALF, false><<<grid, kPromptThreads, 0, s>>>(a);
     else if (D == 128 || y.NT == 1)
         small ? pair_kernel<D, 1, HALF, true><<<grid, kThreads, 0, s>>>(a) : pair_kernel<D, 1, HALF, false><<<grid, kThreads, 0, s>>>(a);
     else if constexpr (D == 64)
