@@ -659,7 +659,7 @@ netkv_status netkv_kv_attend_workspace(netkv_handle h, const netkv_kv_t *kv, con
  * that is a power of two from 2^-15 on, else to 11 bits and 2^-25 of the larger scale.  The
  * maps' difference and the norm are fp32, and out is rounded once.  No block
  * weights, no gradient.  One form for the call, by max_tok * n_heads /
- * n_kv_heads rows (more than 96 or 32 at head_dim 64 or 128: the form for
+ * n_kv_heads rows (more than 192 or 48 at head_dim 64 or 128: the form for
  * prompts). */
 netkv_status netkv_kv_attend_diff(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *q,
                                   int dtype, uint32_t n_heads, uint64_t q_stride, float scale, const float *lambda,

@@ -105,9 +105,12 @@ struct ValScale {
 __device__ inline ValScale val_scale(float x, float y) {
     ValScale v;
     v.s = fmaxf(x, y);
-    v.r[0] = v.s > 0.0f ? x / v.s : 1.0f;      // NaN stays NaN
-    v.r[1] = v.s > 0.0f ? y / v.s : 1.0f;
-    if (!(x == x && y == y)) v.s = NAN;
+    v.r[0] = v.r[1] = 1.0f;
+    if (x != y) {                              // NaN too, which s then stays
+        v.r[0] = v.s > 0.0f ? x / v.s : 1.0f;
+        v.r[1] = v.s > 0.0f ? y / v.s : 1.0f;
+        if (!(x == x && y == y)) v.s = NAN;
+    }
     return v;
 }
 
@@ -620,13 +623,14 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     typedef typename Elem<HALF>::T T;
     typedef typename Elem<HALF>::T8 T8;
     constexpr int VD = 2 * D, kDT = VD / 16;
-    constexpr int kAhead = 6;                         // fragments read ahead of their products
+    constexpr int kAhead = D == 128 ? 4 : 6;          // fragments read ahead of their products
     constexpr int kT = STEP / 16, kU = STEP / 32;     // products with the keys, fragments of a tile of values a step
     constexpr uint32_t kGroup = STEP / 4;             // tokens of a lane
     constexpr int kShare = kT * D / 128;              // 16-byte pieces of keys or values a lane stages
     constexpr int kKeys = kT * D / 32, kVals = kU * kDT;   // fragments of one map's keys, of the values
     __shared__ u32x4 lds[2 * (2 * kKeys + kVals)][64];
     __shared__ uint8_t lds_bits[2][kVals][64];        // which of a fragment lane's 8 values were NaN
+    __shared__ uint64_t lds_sums[NT][kPromptThreads];   // sums of a lane that a NaN value belongs to, a bit each
     __shared__ uint32_t lds_nan[2];
     static_assert(4 * kDT <= 2 * (2 * kKeys + kVals), "a map's 64 rows fit");
 
@@ -649,14 +653,17 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     const uint32_t last_block = hd.ctx ? (hd.ctx - 1) >> a.kv.btl : 0u;
 
     T8 qf[NT][D / 32];
-    uint32_t lim[NT];
+    // tokens that a row sees (all for one that is none); not kept, only some steps need it
+    auto lim_of = [&](int n) {
+        const uint32_t r = row0 + n * 16 + c;
+        const int64_t seen = (int64_t)hd.ctx - hd.n + r / a.G + 1;
+        return r >= n_rows ? hd.ctx : seen > 0 ? (uint32_t)seen : 0u;
+    };
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const uint32_t r = row0 + n * 16 + c;
         const bool valid = r < n_rows;
         const uint32_t t = valid ? r / a.G : 0u, j = p * a.G + (valid ? r % a.G : 0u);
-        const int64_t seen = (int64_t)hd.ctx - hd.n + t + 1;
-        lim[n] = !valid ? hd.ctx : seen > 0 ? (uint32_t)seen : 0u;
         const T *q = (const T *)a.q + (hd.row0 + t) * a.q_stride + (uint64_t)(2 * j + map) * D + 16 * g;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
@@ -678,13 +685,12 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     f32x4 acc[NT][kDT], st[NT][kT];
     f16x8 pf[NT][kU];
     float m[NT], l[NT], y[NT];
-    uint64_t nan_sums[NT];                            // sums of this lane that a NaN value belongs to
     static_assert(4 * kDT <= 64, "a bit a sum");
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         m[n] = y[n] = -INFINITY;
         l[n] = 0.0f;
-        nan_sums[n] = 0;
+        lds_sums[n][threadIdx.x] = 0;
 #pragma unroll
         for (int u = 0; u < kU; ++u) pf[n][u] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
@@ -716,22 +722,41 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     const uint64_t jump = second ? (uint64_t)(D / 64) * piece : hb;   // from piece D / 64 on
     if (!second) own += q_own * hb;
     const float *ks = a.kv.ks + 2 * p + map, *vs = a.kv.vs + 2 * p;
-    // of the scores' page pv, r of the pieces' page po
-    auto scales_of = [&](uint32_t pv, uint32_t po, float &sc, float &vsc, float &rv) {
-        const bool bad = pv >= a.kv.n_pages;
-        if (bad) report(a.kv);
-        const uint64_t si = (uint64_t)(bad ? 0u : pv) * hk;
-        sc = SMALL ? ks[si] : scalar(ks)[si];
-        const float va = SMALL ? vs[si] : scalar(vs)[si], vb = SMALL ? vs[si + 1] : scalar(vs)[si + 1];
-        const ValScale v = val_scale(va, vb);
+    // The scales of the scores' page pv, and for r those of the pieces' page pr:
+    // asked for first, looked at later.
+    struct Scales {
+        float k, va, vb, wa, wb;
+    };
+    auto ask = [&](uint32_t pv, uint32_t pr, Scales &x) {
+        const uint64_t si = (uint64_t)(pv < a.kv.n_pages ? pv : 0u) * hk;
+        x.k = SMALL ? ks[si] : scalar(ks)[si];
+        x.va = SMALL ? vs[si] : scalar(vs)[si];
+        x.vb = SMALL ? vs[si + 1] : scalar(vs)[si + 1];
+        if constexpr (SMALL && STEP == 32) {
+            const uint64_t so = (uint64_t)(pr < a.kv.n_pages ? pr : 0u) * hk;
+            x.wa = vs[so];
+            x.wb = vs[so + 1];
+        }
+    };
+    auto look = [&](uint32_t pv, const Scales &x, float &sc, float &vsc, float &rv) {
+        const ValScale v = val_scale(x.va, x.vb);
+        sc = x.k;
         vsc = v.s;
         rv = half ? v.r[1] : v.r[0];
-        if (SMALL && STEP == 32 && second) {
-            const uint64_t so = (uint64_t)(po < a.kv.n_pages ? po : 0u) * hk;
-            const ValScale o = val_scale(vs[so], vs[so + 1]);
+        if constexpr (SMALL && STEP == 32) {
+            const ValScale o = val_scale(x.wa, x.wb);
             rv = half ? o.r[1] : o.r[0];
         }
-        if (bad) sc = vsc = NAN;
+        if (pv >= a.kv.n_pages) {
+            report(a.kv);
+            sc = vsc = NAN;
+        }
+        if constexpr (!SMALL) {                        // the same for all lanes: in scalar registers
+            auto one = [](float &x) { x = __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x))); };
+            one(sc);
+            one(vsc);
+            one(rv);
+        }
     };
     auto fetch = [&](uint32_t kt, uint32_t po) {
         const uint32_t t0 = (kt * STEP) & (bt - 1);
@@ -892,7 +917,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
                         for (int j = 0; j < 8; ++j) one[j] = bits >> j & 1 ? (_Float16)1.0f : (_Float16)0.0f;
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            const int left = (int)lim[n] - (int)tok0 - 8 * u;
+                            const int left = (int)lim_of(n) - (int)tok0 - 8 * u;
                             f16x8 see;
 #pragma unroll
                             for (int j = 0; j < 8; ++j) see[j] = left > j ? (_Float16)1.0f : (_Float16)0.0f;
@@ -902,12 +927,12 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) nan_sums[n] |= (uint64_t)(hit[n][i] > 0.0f) << (4 * d + i);
+                        for (int i = 0; i < 4; ++i) lds_sums[n][threadIdx.x] |= (uint64_t)(hit[n][i] > 0.0f) << (4 * d + i);
                 }
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int left = (int)lim[n] - (int)tok0;
+            const int left = (int)lim_of(n) - (int)tok0;
             float mx = -INFINITY;
 #pragma unroll
             for (int t = 0; t < kT; ++t)
@@ -933,7 +958,8 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
 
     // pages of the step after next and the one after it
     uint32_t po = 0, pv = 0, po_on = 0, pv_on = 0;
-    float sc_on = 0.0f, vs_on = 0.0f, rv_on = 1.0f;   // scales of the step after next
+    Scales on;                                        // scales of the step after next
+    float sc_on = 0.0f, vs_on = 0.0f, rv_on = 1.0f;
     if (threadIdx.x < 2) lds_nan[threadIdx.x] = 0;
     // the first step's products with "the step before" are of zeros
     for (uint32_t i = threadIdx.x; i < kVals * 64; i += kPromptThreads) lds_v(~k0 & 1, 0)[i] = u32x4{0, 0, 0, 0};
@@ -942,10 +968,13 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     rv_at[0] = rv_at[1] = 1.0f;
     if (k0 < k1) {
         fetch(k0, page_at(k0, own_group));
-        scales_of(page_at(k0, group), page_at(k0, own_group), sc_at[0], vs_at[0], rv_at[0]);
+        Scales x;
+        ask(page_at(k0, group), page_at(k0, own_group), x);
+        look(page_at(k0, group), x, sc_at[0], vs_at[0], rv_at[0]);
         stage(k0, rv_at[0]);
         fetch(k0 + 1, page_at(k0 + 1, own_group));
-        scales_of(page_at(k0 + 1, group), page_at(k0 + 1, own_group), sc_at[1], vs_at[1], rv_at[1]);
+        ask(page_at(k0 + 1, group), page_at(k0 + 1, own_group), x);
+        look(page_at(k0 + 1, group), x, sc_at[1], vs_at[1], rv_at[1]);
         po = page_at(k0 + 2, own_group);
         pv = SMALL ? page_at(k0 + 2, group) : po;
     }
@@ -954,7 +983,8 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     // Small loads for later steps go out before the softmax, which hides them
     // (page_at stays within the sequence's blocks past its end).
     auto look_ahead = [&](uint32_t kt) {
-        scales_of(pv, po, sc_on, vs_on, rv_on);
+        ask(pv, po, on);
+        if constexpr (!SMALL) look(pv, on, sc_on, vs_on, rv_on);
         po_on = page_at(kt + 3, own_group);
         pv_on = SMALL ? page_at(kt + 3, group) : po_on;
     };
@@ -965,6 +995,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
         }
         sc_at[0] = sc_at[1];
         vs_at[0] = vs_at[1];
+        if constexpr (SMALL) look(pv, on, sc_on, vs_on, rv_on);
         sc_at[1] = sc_on;
         vs_at[1] = vs_on;
         rv_at[1] = rv_on;
@@ -997,12 +1028,13 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         l[n] = row_sum(l[n]);
-        if (nan_sums[n])
+        const uint64_t nan_sums = lds_sums[n][threadIdx.x];
+        if (nan_sums)
 #pragma unroll
             for (int d = 0; d < kDT; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (nan_sums[n] >> (4 * d + i) & 1) acc[n][d][i] = NAN;
+                    if (nan_sums >> (4 * d + i) & 1) acc[n][d][i] = NAN;
     }
     if (it.slot != kNoSlot) {
 #pragma unroll
@@ -1018,7 +1050,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const Over over(y[n], m[n], l[n], lim[n] > 0);
+        const Over over(y[n], m[n], l[n], lim_of(n) > 0);
 #pragma unroll
         for (int d = 0; d < kDT; ++d)
 #pragma unroll
@@ -1221,7 +1253,11 @@ netkv_status make_pair_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t 
     if (y.G > 64) return invalid(h, "n_heads / n_kv_heads must be <= 64");
     const uint64_t most = (uint64_t)a.max_tok * y.G;   // rows of the longest sequence's pair
     if (most > 0xFFFFFFFFull - 1024) return invalid(h, "max_tok * n_heads / n_kv_heads must be < 2^32 - 1024");
-    y.rows = most > (D == 64 ? 96u : 32u);
+    // Rows from which pair_prompt_kernel pays.  64 sequences of 8,192 tokens, 64 and
+    // 8 heads, pair_kernel against it, us: 64 dimensions, 96 rows 322, 360, 128 rows
+    // 376, 377, 192 rows 530, 597, 256 rows 671, 582; 128 dimensions, 32 rows 358, 464,
+    // 48 rows 415, 500, 64 rows 524, 496, 96 rows 733, 500.
+    y.rows = most > (D == 64 ? 192u : 48u);
     y.NT = D == 128 || most <= 16 ? 1 : 2;
     y.tile_rows = !y.rows ? 16u * y.NT : 128u;
     y.tile_most = (uint32_t)(most < y.tile_rows ? most : y.tile_rows);
