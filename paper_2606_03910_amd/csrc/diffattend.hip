@@ -468,8 +468,14 @@ __global__ __launch_bounds__(kThreads, 2) void pair_kernel(PairArgs a) {
             for (int d = 0; d < kDT; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
-            l[n] += weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
-            weights_of(st[n], sc, yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
+            // the weights and their sum from one pass where fp32 holds both
+            const float by = yn == -INFINITY ? -INFINITY : vlog - yn, up = -by - mn;
+            if (__all(fabsf(up) < 64.0f)) {
+                l[n] += weights_of(st[n], sc, by, pf[n]) * exp2_of(up);
+            } else {
+                l[n] += weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
+                weights_of(st[n], sc, by, pf[n]);
+            }
         }
         if (kt * kStep + kStep <= all_lim) return;
         // Tokens that not every row sees: bytes of slots that hold none may be
@@ -626,6 +632,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     constexpr int kAhead = D == 128 ? 4 : 6;          // fragments read ahead of their products
     constexpr int kT = STEP / 16, kU = STEP / 32;     // products with the keys, fragments of a tile of values a step
     constexpr uint32_t kGroup = STEP / 4;             // tokens of a lane
+    constexpr bool kApart = !SMALL;                   // the groups half a step apart
     constexpr int kShare = kT * D / 128;              // 16-byte pieces of keys or values a lane stages
     constexpr int kKeys = kT * D / 32, kVals = kU * kDT;   // fragments of one map's keys, of the values
     __shared__ u32x4 lds[2 * (2 * kKeys + kVals)][64];
@@ -951,8 +958,14 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
             for (int d = 0; d < kDT; ++d)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[n][d][i] *= al;
-            l[n] += weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
-            weights_of(st[n], sc, yn == -INFINITY ? -INFINITY : vlog - yn, pf[n]);
+            // the weights and their sum from one pass where fp32 holds both
+            const float by = yn == -INFINITY ? -INFINITY : vlog - yn, up = -by - mn;
+            if (__all(fabsf(up) < 64.0f)) {
+                l[n] += weights_of(st[n], sc, by, pf[n]) * exp2_of(up);
+            } else {
+                l[n] += weights_of(st[n], sc, mn == -INFINITY ? 0.0f : -mn, pf[n]);
+                weights_of(st[n], sc, by, pf[n]);
+            }
         }
     };
 
@@ -979,7 +992,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
         pv = SMALL ? page_at(k0 + 2, group) : po;
     }
     meet();
-    if (second) meet();
+    if (kApart && second) meet();
     // Small loads for later steps go out before the softmax, which hides them
     // (page_at stays within the sequence's blocks past its end).
     auto look_ahead = [&](uint32_t kt) {
@@ -1023,7 +1036,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
         softmax_any(kt);
         pass_on(kt);
     }
-    if (!second) meet();
+    if (kApart && !second) meet();
     if (k0 < k1) values(k1 - 1);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
