@@ -27,7 +27,7 @@ struct Turn {
     const float *table;               // [n_pos][2 pairs]: cosines, sines
     const uint32_t *pos;              // [axis][row]; null: a row's place in its sequence
     uint64_t pos_stride;
-    uint32_t n_pos, pairs;
+    uint32_t n_pos, pairs, n_axes;
     uint32_t interleaved;
     uint32_t sign;                    // flips the sines' signs: the transposed rotation
     uint32_t axes[kMaxPairs / 16];    // two bits a pair
@@ -42,11 +42,10 @@ struct Angles {
 // Positions past the table make their pairs NaN.
 __device__ inline void load_angles(const Turn &t, uint64_t row, uint32_t place, uint32_t u, Angles &a) {
     const uint32_t which = t.axes[u >> 1] >> (16 * (u & 1)) & 0xFFFFu;
-    auto position = [&](uint32_t axis) { return t.pos ? t.pos[axis * t.pos_stride + row] : place; };
     const uint32_t first = which & 3;
     bool bad = false;
     if (which == first * 0x5555u) {
-        const uint32_t p = position(first);
+        const uint32_t p = t.pos ? t.pos[first * t.pos_stride + row] : place;
         bad = p >= t.n_pos;
         const float *at = t.table + (uint64_t)(bad ? 0u : p) * 2 * t.pairs + 8 * u;
 #pragma unroll
@@ -59,13 +58,24 @@ __device__ inline void load_angles(const Turn &t, uint64_t row, uint32_t place, 
             }
         }
     } else {
+        // each axis's position and row once, then a look into them for each pair
+        uint32_t at[4], outside = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            uint32_t p = place;
+            if (t.pos) p = t.pos[min(i, t.n_axes - 1) * t.pos_stride + row];
+            const bool out = p >= t.n_pos;
+            outside |= out ? 1u << i : 0u;
+            at[i] = out ? 0u : p;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t p = position(which >> (2 * i) & 3);
-            const bool out = p >= t.n_pos;
-            const float *at = t.table + (uint64_t)(out ? 0u : p) * 2 * t.pairs + 8 * u + i;
-            a.c[i] = out ? NAN : at[0];
-            a.s[i] = out ? NAN : at[t.pairs];
+            const uint32_t k = which >> (2 * i) & 3, p = k & 2 ? (k & 1 ? at[3] : at[2]) : (k & 1 ? at[1] : at[0]);
+            const float *x = t.table + (uint64_t)p * 2 * t.pairs + 8 * u + i;
+            const bool out = outside >> k & 1;
+            a.c[i] = x[0];
+            a.s[i] = x[t.pairs];
+            if (out) a.c[i] = a.s[i] = NAN;
             bad |= out;
         }
     }
@@ -103,16 +113,23 @@ __device__ inline float cross(float a, float c, float b, float s) {
     return e == e ? t - e : t;        // w not finite
 }
 
-// A double to fp32, to odd where it is not exact: what is rounded from there to
-// 8 bits is as if rounded once.
-__device__ inline float to_odd(double x) {
-    const float f = (float)x;
-    uint32_t u = __float_as_uint(f);
-    if ((double)f != x) {
-        if (fabs((double)f) > fabs(x)) --u;
-        u |= 1;
+// A double to bfloat16's bits, to odd where it is not exact: what is rounded from
+// there to the 4 bits of e4m3 is as if rounded once, and what is compared with
+// 448 times a power of two comes out as the double would.
+__device__ inline uint32_t to_odd(double x) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+    const uint32_t hi = (uint32_t)(bits >> 32), rest = (hi & 0x1FFFu) | (uint32_t)bits;
+    uint32_t u = (hi >> 13 & 0x3FFFFu) - (896u << 7);         // exponent and seven bits, by bfloat16's exponents
+    if (u - (1u << 7) >= 254u << 7) {                         // 0, or outside its normal numbers
+        const float f = (float)x;
+        uint32_t v = __float_as_uint(f);
+        if ((double)f != x) {
+            if (fabs((double)f) > fabs(x)) --v;
+            v |= 1;
+        }
+        return v >> 16 | (uint32_t)((v & 0xFFFFu) != 0);
     }
-    return __uint_as_float(u);
+    return u | min(rest, 1u) | (hi >> 16 & 0x8000u);
 }
 
 // ------------------------------------------------------------------ rows
@@ -124,53 +141,57 @@ struct RowArgs {
     uint64_t x_stride, out_stride;
     uint32_t heads, dim;
     uint32_t units;                   // a head's: those that turn, and those copied
-    uint32_t part;                    // heads a thread takes, one after the other
     uint32_t half;
 };
+
+// A unit's two pieces turned, in their place.
+__device__ inline void turn_unit(const Turn &t, bool half, const Angles &g, u32x4 &lo, u32x4 &hi) {
+    Pairs e;
+    to_pairs(lo, hi, half, t.interleaved, e);
+    float y[8], z[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        y[j] = cross(e.a[j], g.c[j], e.b[j], g.s[j]);
+        z[j] = cross(e.b[j], g.c[j], e.a[j], -g.s[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (t.interleaved) {
+            lo[j] = pack16(y[j], z[j], half);
+            hi[j] = pack16(y[4 + j], z[4 + j], half);
+        } else {
+            lo[j] = pack16(y[2 * j], y[2 * j + 1], half);
+            hi[j] = pack16(z[2 * j], z[2 * j + 1], half);
+        }
+    }
+}
 
 // Rows [row, row + n) of the arrays; a row's position is `place` and on if the
 // turn has none of its own.
 __device__ inline void rotate_rows(const RowArgs &a, uint64_t row, uint32_t n, uint32_t place) {
-    const uint32_t parts = (a.heads + a.part - 1) / a.part;
-    const uint32_t each = parts * a.units;
+    const uint32_t each = (a.heads + kHeadsEach - 1) / kHeadsEach * a.units;
     for (uint32_t i = threadIdx.x; i < n * each; i += blockDim.x) {
-        const uint32_t t = i / each, u = i % each % a.units, h0 = i % each / a.units * a.part;
-        const uint32_t heads = min(a.part, a.heads - h0);
+        const uint32_t t = i / each, u = i % each % a.units, h0 = i % each / a.units * kHeadsEach;
+        const uint32_t last = min(kHeadsEach, a.heads - h0) - 1;
         const Unit p = unit_of(u, a.turn.pairs, a.turn.interleaved, a.dim);
         const uint16_t *x = a.x + (row + t) * a.x_stride + (uint64_t)h0 * a.dim;
         uint16_t *out = a.out + (row + t) * a.out_stride + (uint64_t)h0 * a.dim;
-        if (!p.turns) {
-            for (uint32_t h = 0; h < heads; ++h) {
-                *(u32x4 *)(out + h * a.dim + p.lo) = *(const u32x4 *)(x + h * a.dim + p.lo);
-                if (p.both) *(u32x4 *)(out + h * a.dim + p.hi) = *(const u32x4 *)(x + h * a.dim + p.hi);
-            }
-            continue;
+        u32x4 xl[kHeadsEach], xh[kHeadsEach];
+#pragma unroll
+        for (uint32_t j = 0; j < kHeadsEach; ++j) {
+            const uint16_t *from = x + min(j, last) * a.dim;
+            xl[j] = *(const u32x4 *)(from + p.lo);
+            xh[j] = *(const u32x4 *)(from + (p.both ? p.hi : p.lo));
         }
         Angles g;
-        load_angles(a.turn, row + t, place + t, u, g);
-        for (uint32_t h = 0; h < heads; ++h) {
-            const u32x4 xl = *(const u32x4 *)(x + h * a.dim + p.lo), xh = *(const u32x4 *)(x + h * a.dim + p.hi);
-            Pairs e;
-            to_pairs(xl, xh, a.half, a.turn.interleaved, e);
-            float y[8], z[8];
+        if (p.turns) load_angles(a.turn, row + t, place + t, u, g);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                y[j] = cross(e.a[j], g.c[j], e.b[j], g.s[j]);
-                z[j] = cross(e.b[j], g.c[j], e.a[j], -g.s[j]);
-            }
-            u32x4 yl, yh;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (a.turn.interleaved) {
-                    yl[j] = pack16(y[j], z[j], a.half);
-                    yh[j] = pack16(y[4 + j], z[4 + j], a.half);
-                } else {
-                    yl[j] = pack16(y[2 * j], y[2 * j + 1], a.half);
-                    yh[j] = pack16(z[2 * j], z[2 * j + 1], a.half);
-                }
-            }
-            *(u32x4 *)(out + h * a.dim + p.lo) = yl;
-            *(u32x4 *)(out + h * a.dim + p.hi) = yh;
+        for (uint32_t j = 0; j < kHeadsEach; ++j) {
+            if (j > last) continue;
+            uint16_t *to = out + j * a.dim;
+            if (p.turns) turn_unit(a.turn, a.half, g, xl[j], xh[j]);
+            *(u32x4 *)(to + p.lo) = xl[j];
+            if (p.both) *(u32x4 *)(to + p.hi) = xh[j];
         }
     }
 }
@@ -193,12 +214,12 @@ struct AppendArgs {
 // and quantises them, as store_block does values.  A rotated key is computed in
 // 64 bits, where the products of 16-bit elements and 32-bit cosines are exact,
 // and rounded once, to 8 bits: in fp32 one in some hundred thousand would
-// come out a step off, and a block's scale by a factor of two.
-template <int D, int THREADS>
+// come out a step off, and a block's scale by a factor of two.  Between the
+// largest value and the rounding it is held in 16 bits, to odd (to_odd).
+template <int D, int THREADS, int kEach>
 __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, uint32_t h) {
-    constexpr int kEach = 4;                                  // units a thread keeps
-    constexpr uint32_t kUnits = D / 16;                       // of a token
-    __shared__ uint32_t red[THREADS / 64];
+    constexpr uint32_t kUnits = D / 16;                       // of a token; a thread keeps kEach
+    __shared__ uint32_t red[2][THREADS / 64];
     const Kv &kv = g.move.kv;
     const Turn &turn = g.rows.turn;
     Place pl;
@@ -206,70 +227,83 @@ __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, 
     const uint64_t at = (uint64_t)pl.page * kv.hk + h;
     uint8_t *dst = kv.k + at * head_bytes(kv, D);
     const uint16_t *src = (const uint16_t *)g.move.k + (uint64_t)h * D;
-    const uint32_t units = (pl.p1 - pl.p0) * kUnits, turning = turn.pairs / 8, half = g.rows.half;
+    const uint32_t units = (pl.p1 - pl.p0) * kUnits, half = g.rows.half;
 
-    float x[kEach][16];
+    u32x4 x[kEach][2];
     auto unit = [&](uint32_t e) { return unit_of(e % kUnits, turn.pairs, turn.interleaved, D); };
     auto load = [&](uint32_t base) {
-        u32x4 lo[kEach], hi[kEach];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t e = base + i * THREADS + threadIdx.x;
-            lo[i] = hi[i] = u32x4{0, 0, 0, 0};
+            x[i][0] = x[i][1] = u32x4{0, 0, 0, 0};
             if (e >= units) continue;
             const uint16_t *p = src + (pl.row0 + e / kUnits) * g.move.k_stride;
             const Unit w = unit(e);
-            lo[i] = *(const u32x4 *)(p + w.lo);
-            hi[i] = *(const u32x4 *)(p + w.hi);
+            x[i][0] = *(const u32x4 *)(p + w.lo);
+            x[i][1] = *(const u32x4 *)(p + w.hi);
         }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t e = base + i * THREADS + threadIdx.x, t = e / kUnits, u = e % kUnits;
-            if (e >= units || u >= turning) {
+            if (e >= units) continue;
+            if (u < turn.pairs / 8) {
+                Angles a;
+                Pairs p;
+                load_angles(turn, pl.row0 + t, pl.token + t, u, a);
+                to_pairs(x[i][0], x[i][1], half, turn.interleaved, p);
+                uint32_t y[8], z[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    x[i][j] = to_f32(half_of(lo[i], j), half);
-                    x[i][8 + j] = to_f32(half_of(hi[i], j), half);
+                    const double c = a.c[j], s = a.s[j], pa = p.a[j], pb = p.b[j];
+                    y[j] = to_odd(fma(pa, c, -(pb * s)));
+                    z[j] = to_odd(fma(pb, c, pa * s));
                 }
-                continue;
-            }
-            Angles a;
-            Pairs p;
-            load_angles(turn, pl.row0 + t, pl.token + t, u, a);
-            to_pairs(lo[i], hi[i], half, turn.interleaved, p);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const double c = a.c[j], s = a.s[j], pa = p.a[j], pb = p.b[j];
-                const float y = to_odd(fma(pa, c, -(pb * s))), z = to_odd(fma(pb, c, pa * s));
-                if (turn.interleaved) {
-                    x[i][2 * j] = y;
-                    x[i][2 * j + 1] = z;
-                } else {
-                    x[i][j] = y;
-                    x[i][8 + j] = z;
+                for (int j = 0; j < 4; ++j) {
+                    x[i][0][j] = turn.interleaved ? y[j] | z[j] << 16 : y[2 * j] | y[2 * j + 1] << 16;
+                    x[i][1][j] = turn.interleaved ? y[4 + j] | z[4 + j] << 16 : z[2 * j] | z[2 * j + 1] << 16;
                 }
+            } else if (half) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[i][q][j] = to_odd(to_f32(x[i][q][j] & 0xFFFFu, true)) | to_odd(to_f32(x[i][q][j] >> 16, true)) << 16;
             }
         }
     };
-    // the largest finite value, by its bits
-    uint32_t top = 0;
+    // the largest of the values' bits without their signs, and of the finite ones'
+    constexpr uint32_t kNotFinite = 0x7F80u;
+    u16x2 all = {0, 0}, some = {0, 0};
     for (uint32_t base = 0; base < units; base += THREADS * kEach) {
         load(base);
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const uint32_t z = __float_as_uint(x[i][j]) & 0x7FFFFFFFu;
-                top = max(top, z < 0x7F800000u ? z : 0u);
-            }
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u16x2 z = __builtin_bit_cast(u16x2, x[i][q][j] & 0x7FFF7FFFu);
+                    all = __builtin_elementwise_max(all, z);
+                    some = __builtin_elementwise_max(some, u16x2{z[0] < kNotFinite ? z[0] : (uint16_t)0, z[1] < kNotFinite ? z[1] : (uint16_t)0});
+                }
     }
-    for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor(top, d, 64));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
+    uint32_t top = max(some[0], some[1]), any = max(all[0], all[1]);
+    for (int d = 32; d; d >>= 1) {
+        top = max(top, (uint32_t)__shfl_xor(top, d, 64));
+        any = max(any, (uint32_t)__shfl_xor(any, d, 64));
+    }
+    if ((threadIdx.x & 63) == 0) {
+        red[0][threadIdx.x >> 6] = top;
+        red[1][threadIdx.x >> 6] = any;
+    }
     __syncthreads();
-    for (int i = 0; i < THREADS / 64; ++i) top = max(top, red[i]);
+    for (int i = 0; i < THREADS / 64; ++i) {
+        top = max(top, red[0][i]);
+        any = max(any, red[1][i]);
+    }
 
     float *scale = kv.ks + at;
-    float sc = scale_for(__uint_as_float(top));
+    float sc = scale_for(__uint_as_float(top << 16));
     if (pl.p0) {
         const float was = *scale;
         sc = was > sc ? was : sc;
@@ -281,16 +315,30 @@ __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, 
     __syncthreads();   // every thread has read the old scale
     if (threadIdx.x == 0) *scale = sc;
     const float inv = 1.0f / sc;
+    // the narrowing instruction takes a power of two
+    const bool plain = any < kNotFinite && (__float_as_uint(sc) & 0x7FFFFFu) == 0;
     for (uint32_t base = 0; base < units; base += THREADS * kEach) {
         if (units > THREADS * kEach) load(base);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t e = base + i * THREADS + threadIdx.x;
             if (e >= units) continue;
-            uint8_t *p = dst + (uint64_t)(pl.p0 + e / kUnits) * D;
             const Unit w = unit(e);
-            *(u32x2 *)(p + w.lo) = u32x2{narrow4(x[i], inv), narrow4(x[i] + 4, inv)};
-            *(u32x2 *)(p + w.hi) = u32x2{narrow4(x[i] + 8, inv), narrow4(x[i] + 12, inv)};
+            uint8_t *p = dst + (uint64_t)(pl.p0 + e / kUnits) * D;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const u32x4 v = x[i][q];
+                u32x2 y;
+                if (plain) {
+                    y = u32x2{narrow4_finite(v[0], v[1], sc, false), narrow4_finite(v[2], v[3], sc, false)};
+                } else {
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = to_f32(half_of(v, j), false);
+                    y = u32x2{narrow4(f, inv), narrow4(f + 4, inv)};
+                }
+                *(u32x2 *)(p + (q ? w.hi : w.lo)) = y;
+            }
         }
     }
 }
@@ -306,8 +354,9 @@ __device__ inline void append_queries(const AppendArgs &a, uint32_t task) {
     rotate_rows(a.rows, h.row0 + t, min(a.chunk, h.n - t), h.ctx - h.n + t);
 }
 
-template <int D, int THREADS>
-__global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a) {
+// All of a small call: latency.
+template <int D>
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     if (blockIdx.x < a.row_tasks) {
         append_queries(a, blockIdx.x);
         return;
@@ -316,9 +365,24 @@ __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a) {
     const bool vals = r >= a.move.kv.hk;
     if (r == 0) report_bad(a.move.kv, task, a.store_tasks);
     if (vals)
-        store_block<D, THREADS>(a.move, a.rows.half, task, h, true);
+        store_block<D, kThreads>(a.move, a.rows.half, task, h, true);
     else
-        append_keys<D, THREADS>(a, task, h);
+        append_keys<D, kThreads, 4>(a, task, h);
+}
+
+// The three shares of a large one by themselves, each with the registers and
+// the workgroups that it wants.
+__global__ __launch_bounds__(kThreads) void append_rows_kernel(AppendArgs a) { append_queries(a, blockIdx.x); }
+
+template <int D>
+__global__ __launch_bounds__(512, 4) void append_keys_kernel(AppendArgs a) {
+    if (blockIdx.y == 0) report_bad(a.move.kv, blockIdx.x, gridDim.x);
+    append_keys<D, 512, 8>(a, blockIdx.x, blockIdx.y);
+}
+
+template <int D>
+__global__ __launch_bounds__(1024, 8) void append_values_kernel(AppendArgs a) {
+    store_block<D, 1024>(a.move, a.rows.half, blockIdx.x, blockIdx.y, true);
 }
 
 // ------------------------------------------------------------------ host
@@ -331,10 +395,24 @@ netkv_status make_turn(netkv_handle h, const netkv_rope_t *rope, uint32_t head_d
     t.pos_stride = pos_stride;
     t.n_pos = rope->n_pos;
     t.pairs = rope->rot_dim / 2;
+    t.n_axes = rope->n_axes;
     t.interleaved = rope->interleaved;
     for (uint32_t i = 0; rope->axis && i < t.pairs; ++i) t.axes[i / 16] |= (uint32_t)rope->axis[i] << (2 * (i % 16));
     t.err = netkv_internal_errword(h);
     return NETKV_OK;
+}
+
+template <int D>
+void launch_append(const AppendArgs &a, uint32_t block_rows, hipStream_t s) {
+    // blocks that a workgroup of 256 takes in one pass (append_keys' and store_block's kEach)
+    if (block_rows * D <= 256 * 64) {
+        append_kernel<D><<<a.row_tasks + a.store_tasks * a.move.kv.hk * 2, kThreads, 0, s>>>(a);
+        return;
+    }
+    const dim3 grid(a.store_tasks, a.move.kv.hk);
+    if (a.row_tasks) append_rows_kernel<<<a.row_tasks, kThreads, 0, s>>>(a);
+    append_keys_kernel<D><<<grid, 512, 0, s>>>(a);
+    append_values_kernel<D><<<grid, 1024, 0, s>>>(a);
 }
 
 }  // namespace
@@ -366,8 +444,7 @@ extern "C" netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *ro
     a.dim = head_dim;
     a.half = dtype == NETKV_FP16;
     a.units = units_of(a.turn.pairs, head_dim, in_place);
-    a.part = part_of(n_rows, n_heads, a.units);
-    const uint64_t each = (uint64_t)((n_heads + a.part - 1) / a.part) * a.units;
+    const uint64_t each = (uint64_t)((n_heads + kHeadsEach - 1) / kHeadsEach) * a.units;
     const uint32_t chunk = (uint32_t)(each >= kThreads ? 1 : kThreads / each);
     const uint64_t groups = (n_rows + chunk - 1) / chunk;
     if (!grid_fits(groups, kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many rows for one call");
@@ -417,20 +494,21 @@ extern "C" netkv_status netkv_kv_append(netkv_handle h, const netkv_kv_t *kv, co
         r.heads = n_heads;
         r.dim = kv->head_dim;
         r.units = units_of(r.turn.pairs, kv->head_dim, in_place);
-        r.part = part_of(kv_.n_tok, n_heads, r.units);
         a.chunk = kv_.max_tok < 16 ? 1 : 16;
         row_tasks = row_groups(kv_, a.chunk);
     }
     const uint64_t tasks = store_groups(kv_), groups = row_tasks + tasks * kv_.hk * 2;
-    if (!grid_fits(groups, kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many rows for one call");
+    // in workgroups of 256, or of 1,024 for each head
+    if (!grid_fits(groups, kThreads) || !grid_fits(tasks, 1024)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many rows for one call");
     a.row_tasks = (uint32_t)row_tasks;
     a.store_tasks = (uint32_t)tasks;
+    const uint32_t block_rows = kv_.max_tok < kv->block_tokens ? kv_.max_tok : kv->block_tokens;
     DeviceScope scope(netkv_internal_device(h));
     hipStream_t s = (hipStream_t)stream;
     switch (kv->head_dim) {
-        case 64: append_kernel<64, kThreads><<<(uint32_t)groups, kThreads, 0, s>>>(a); break;
-        case 128: append_kernel<128, kThreads><<<(uint32_t)groups, kThreads, 0, s>>>(a); break;
-        default: append_kernel<256, kThreads><<<(uint32_t)groups, kThreads, 0, s>>>(a); break;
+        case 64: launch_append<64>(a, block_rows, s); break;
+        case 128: launch_append<128>(a, block_rows, s); break;
+        default: launch_append<256>(a, block_rows, s); break;
     }
     return launched(h, "append launch failed");
 }

@@ -46,13 +46,10 @@ NETKV_BOTH inline Unit unit_of(uint32_t u, uint32_t pairs, bool interleaved, uin
 }
 inline uint32_t units_of(uint32_t pairs, uint32_t dim, bool in_place) { return pairs / 8 + (in_place ? 0 : (dim - 2 * pairs + 15) / 16); }
 
-// Heads that a thread takes one after the other with one look at its angles:
-// as many as leave the card (of 256 CUs) a thousand threads a CU.
-inline uint32_t part_of(uint64_t rows, uint32_t heads, uint32_t units) {
-    uint32_t part = 8;
-    while (part > 1 && rows * ((heads + part - 1) / part) * units < 256 * 1024) part /= 2;
-    return part;
-}
+// Heads that a thread takes with one look at its angles, their loads at once.  1,
+// 2, 4, 8, us: 16,384 rows of 32 heads of 128 elements 62, 48, 48, 52, 10,007 of 16
+// heads of 80 20, 16, 15, 18, 64 rows of 64 heads 10, 10, 10, 13.
+constexpr uint32_t kHeadsEach = 4;
 
 // Workgroups for a call's query rows, `chunk` at most each, all of one sequence.
 NETKV_BOTH inline uint32_t row_chunks(const blockplan::Head &h, uint32_t chunk) { return h.n <= h.ctx ? (h.n + chunk - 1) / chunk : 0u; }

@@ -21,7 +21,6 @@ extern "C" void unit(uint32_t u, uint32_t pairs, int interleaved, uint32_t dim, 
     out[0] = x.lo; out[1] = x.hi; out[2] = x.turns; out[3] = x.both;
 }
 extern "C" uint32_t units(uint32_t pairs, uint32_t dim, int in_place) { return units_of(pairs, dim, in_place); }
-extern "C" uint32_t part(uint64_t rows, uint32_t heads, uint32_t units) { return part_of(rows, heads, units); }
 extern "C" const char *error(const netkv_rope_t *r, uint32_t dim, const uint32_t *pos, uint64_t stride, uint64_t rows, int need) {
     return rope_error(r, dim, pos, stride, rows, need);
 }
@@ -107,15 +106,6 @@ def test_units_cover_a_head_once(lib, in_place):
                         assert p % 8 == 0 and p + 8 <= dim
                         seen[p:p + 8] += 1
                 assert (seen[:rot] == 1).all() and (seen[rot:] == (0 if in_place else 1)).all()
-
-
-def test_parts(lib):
-    for rows in (1, 7, 64, 1000, 1 << 31):
-        for heads in (1, 5, 64, 65535):
-            for units in (1, 8, 64):
-                p = lib.part(ctypes.c_uint64(rows), ctypes.c_uint32(heads), ctypes.c_uint32(units))
-                assert p in (1, 2, 4, 8)
-                assert p == 1 or rows * -(-heads // p) * units >= 256 * 1024
 
 
 @pytest.mark.parametrize("seed", range(10))
