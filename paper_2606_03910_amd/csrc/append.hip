@@ -113,6 +113,17 @@ __device__ inline float cross(float a, float c, float b, float s) {
     return e == e ? t - e : t;        // w not finite
 }
 
+// A double to fp32, to odd where it is not exact.
+__device__ inline float odd_f32(double x) {
+    const float f = (float)x;
+    uint32_t u = __float_as_uint(f);
+    if ((double)f != x) {
+        if (fabs((double)f) > fabs(x)) --u;
+        u |= 1;
+    }
+    return __uint_as_float(u);
+}
+
 // A double to bfloat16's bits, to odd where it is not exact: what is rounded from
 // there to the 4 bits of e4m3 is as if rounded once, and what is compared with
 // 448 times a power of two comes out as the double would.
@@ -121,12 +132,7 @@ __device__ inline uint32_t to_odd(double x) {
     const uint32_t hi = (uint32_t)(bits >> 32), rest = (hi & 0x1FFFu) | (uint32_t)bits;
     uint32_t u = (hi >> 13 & 0x3FFFFu) - (896u << 7);         // exponent and seven bits, by bfloat16's exponents
     if (u - (1u << 7) >= 254u << 7) {                         // 0, or outside its normal numbers
-        const float f = (float)x;
-        uint32_t v = __float_as_uint(f);
-        if ((double)f != x) {
-            if (fabs((double)f) > fabs(x)) --v;
-            v |= 1;
-        }
+        const uint32_t v = __float_as_uint(odd_f32(x));
         return v >> 16 | (uint32_t)((v & 0xFFFFu) != 0);
     }
     return u | min(rest, 1u) | (hi >> 16 & 0x8000u);
@@ -231,6 +237,19 @@ __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, 
 
     u32x4 x[kEach][2];
     auto unit = [&](uint32_t e) { return unit_of(e % kUnits, turn.pairs, turn.interleaved, D); };
+    // a unit's eight pairs, turned
+    auto turned = [&](uint32_t e, const u32x4 (&x)[2], auto take) {
+        const uint32_t t = e / kUnits, u = e % kUnits;
+        Angles a;
+        Pairs p;
+        load_angles(turn, pl.row0 + t, pl.token + t, u, a);
+        to_pairs(x[0], x[1], half, turn.interleaved, p);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const double c = a.c[j], s = a.s[j], pa = p.a[j], pb = p.b[j];
+            take(j, fma(pa, c, -(pb * s)), fma(pb, c, pa * s));
+        }
+    };
     auto load = [&](uint32_t base) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
@@ -244,20 +263,14 @@ __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, 
         }
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const uint32_t e = base + i * THREADS + threadIdx.x, t = e / kUnits, u = e % kUnits;
+            const uint32_t e = base + i * THREADS + threadIdx.x;
             if (e >= units) continue;
-            if (u < turn.pairs / 8) {
-                Angles a;
-                Pairs p;
-                load_angles(turn, pl.row0 + t, pl.token + t, u, a);
-                to_pairs(x[i][0], x[i][1], half, turn.interleaved, p);
+            if (e % kUnits < turn.pairs / 8) {
                 uint32_t y[8], z[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const double c = a.c[j], s = a.s[j], pa = p.a[j], pb = p.b[j];
-                    y[j] = to_odd(fma(pa, c, -(pb * s)));
-                    z[j] = to_odd(fma(pb, c, pa * s));
-                }
+                turned(e, x[i], [&](int j, double p, double q) {
+                    y[j] = to_odd(p);
+                    z[j] = to_odd(q);
+                });
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     x[i][0][j] = turn.interleaved ? y[j] | z[j] << 16 : y[2 * j] | y[2 * j + 1] << 16;
@@ -314,9 +327,33 @@ __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, 
     }
     __syncthreads();   // every thread has read the old scale
     if (threadIdx.x == 0) *scale = sc;
+    if (__builtin_expect((__float_as_uint(sc) & 0x7FFFFFu) != 0, 0)) {
+        // a scale that is no power of two, from another program: over it what was
+        // rounded to 16 bits would be rounded twice, so all once more from 64
+#pragma unroll 1
+        for (uint32_t e = threadIdx.x; e < units; e += THREADS) {
+            const uint16_t *from = src + (pl.row0 + e / kUnits) * g.move.k_stride;
+            const Unit w = unit(e);
+            const u32x4 v[2] = {*(const u32x4 *)(from + w.lo), *(const u32x4 *)(from + w.hi)};
+            float y[16];
+            auto over = [&](double x) { return odd_f32(x / (double)sc); };
+            if (w.turns) {
+                turned(e, v, [&](int j, double p, double q) {
+                    y[turn.interleaved ? 2 * j : j] = over(p);
+                    y[turn.interleaved ? 2 * j + 1 : 8 + j] = over(q);
+                });
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) y[j] = over(to_f32(half_of(v[j / 8], j % 8), half));
+            }
+            uint8_t *p = dst + (uint64_t)(pl.p0 + e / kUnits) * D;
+            *(u32x2 *)(p + w.lo) = u32x2{narrow4(y, 1.0f), narrow4(y + 4, 1.0f)};
+            *(u32x2 *)(p + w.hi) = u32x2{narrow4(y + 8, 1.0f), narrow4(y + 12, 1.0f)};
+        }
+        return;
+    }
     const float inv = 1.0f / sc;
-    // the narrowing instruction takes a power of two
-    const bool plain = any < kNotFinite && (__float_as_uint(sc) & 0x7FFFFFu) == 0;
+    const bool plain = any < kNotFinite;
     for (uint32_t base = 0; base < units; base += THREADS * kEach) {
         if (units > THREADS * kEach) load(base);
 #pragma unroll

@@ -268,6 +268,8 @@ __device__ __forceinline__ void store_block(const MoveArgs &a, bool half, uint32
     __syncthreads();   // every thread has read the old scale
     if (threadIdx.x == 0) *scale = sc;
     const float inv = 1.0f / sc;
+    // the narrowing instruction takes a scale's power of two alone
+    const bool plain = finite && (__float_as_uint(sc) & 0x7FFFFFu) == 0;
     const uint32_t tile = min(bt, kStep);
     if (pieces > THREADS * kEach) load(0);
     for (uint32_t base = 0;;) {
@@ -276,7 +278,7 @@ __device__ __forceinline__ void store_block(const MoveArgs &a, bool half, uint32
             const uint32_t e = base + i * THREADS + threadIdx.x;
             u32x2 y = {0, 0};
             if (e < pieces) {
-                if (finite) {
+                if (plain) {
                     y = u32x2{narrow4_finite(x[i][0], x[i][1], sc, half), narrow4_finite(x[i][2], x[i][3], sc, half)};
                 } else {
                     float z[8];

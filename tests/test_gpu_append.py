@@ -553,3 +553,42 @@ def test_append_offsets_past_32_bits(nk, sel):
     want = T.rotate(x[:, hk:2 * hk].double().numpy(), last, pos, [0] * 64, False)
     s = np.array([R.scale_for(np.abs(want[:, h]).max()) for h in range(hk)])
     assert np.array_equal(k.double().cpu().numpy(), R.values(R.nearest(want / s[:, None])) * s[:, None])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("n_new", [1, 30, 500])
+def test_pages_begun_with_any_scale(nk, sel, n_new, dtype):
+    """A page that another program began with a larger scale which is no power of
+    two keeps it: new keys and values are over that scale, by store and append."""
+    rng = np.random.default_rng(83)
+    ctx, block = [700], 512
+    table, pages = R.tables(rng, ctx, block)
+    for how in ("store", "append"):
+        c = R.Cache(pages, 2, 64, block, rng)
+        for i in range(2):
+            c.put(table[0, i], max(0, min(block, ctx[0] - n_new - i * block)))
+        c.ks, c.vs = ((x * 1.37).astype(np.float32).astype(np.float64) for x in (c.ks, c.vs))
+        x = torch.from_numpy(rng.standard_normal((n_new, 4, 64)) * 0.2).to(HALF[dtype])
+        cache, seqs, xd = upload(nk, sel, c), sequences(nk, [n_new], ctx, table), x.cuda()
+        f = x.double().numpy()
+        k = f[:, :2]
+        if how == "append":
+            tab = T.table(700, 64, rng)
+            cache.append(seqs, nk.Rope(sel, dev(tab, np.float32)), xd[:, :2], xd[:, 2:])
+            k = T.rotate(k, tab, own_places(ctx, [n_new]), [0] * 32, False)
+        else:
+            cache.store(seqs, xd[:, :2], xd[:, 2:])
+        sel.sync_errors()
+        ref_store(c, table, ctx, [n_new], k, f[:, 2:])
+        got = R.Cache(pages, 2, 64, block, rng)
+        got.from_device(cache.k.cpu().numpy(), cache.v.cpu().numpy())
+        assert np.array_equal(cache.k_scale.cpu().numpy().reshape(pages, 2), c.ks.astype(np.float32))
+        assert np.array_equal(cache.v_scale.cpu().numpy().reshape(pages, 2), c.vs.astype(np.float32))
+        for a, b, s in ((got.k, c.k, c.ks), (got.v, c.v, c.vs)):
+            for i in range(2):
+                n = min(block, ctx[0] - i * block)
+                pg = table[0, i]
+                va, vb = R.values(a[pg, :, :n]), R.values(b[pg, :, :n])
+                # x / s is computed as x (1 / s), 2^-23 off: next to the middle of two steps either is right
+                step = np.maximum(np.abs(vb), 2.0 ** -6) * 2.0 ** -3
+                assert (np.abs(va - vb) <= step).all() and (va != vb).mean() < 1e-3
