@@ -170,14 +170,9 @@ struct PairShares {
         uint64_t work = 0;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) work += (uint64_t)rt[j] * kt[j];
-        const bool wide = __any(work >> 26);               // 64 lanes of less fit 32 bits
         uint32_t C;
-        if (!wide) {
-            const uint32_t w = (uint32_t)__builtin_amdgcn_readlane((int)wave_sums((uint32_t)work), 63);
-            uint32_t n = (w + a.target - 1) / a.target;
-            if (n > kEnough) n = max((w + a.fine - 1) / a.fine, kEnough);
-            n = max(n, a.least);
-            C = n + (n & 1);
+        if (!__any(work >> kNarrow)) {
+            C = narrow_steps(a, (uint32_t)__builtin_amdgcn_readlane((int)wave_sums((uint32_t)work), 63));
         } else {
             for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d, 64);
             C = range_steps(a, work);

@@ -17,4 +17,17 @@ NETKV_BOTH inline uint32_t even_parts(uint32_t steps, uint32_t C) {
     return steps > C ? (steps + even_steps(steps, C) - 1) / even_steps(steps, C) : 1u;
 }
 
+// range_steps, to a multiple of two, in 32 bits: for the sum of 64 numbers below
+// 2^kNarrow each.
+constexpr uint32_t kNarrow = 25;
+NETKV_BOTH inline uint32_t narrow_steps(const blockplan::Split &a, uint32_t work) {
+    uint32_t len = (work + a.target - 1) / a.target;
+    if (len > blockplan::kEnough) {
+        len = (work + a.fine - 1) / a.fine;
+        len = len > blockplan::kEnough ? len : blockplan::kEnough;
+    }
+    len = len > a.least ? len : a.least;
+    return len + (len & 1);
+}
+
 }  // namespace pairplan

@@ -74,6 +74,8 @@ ROTATES = [
     (5, 2, 1024, 256, 1, False, False, False),
     (65, 1, 24, 16, 1, False, False, False),
     (65, 2, 16, 16, 4, True, True, False),
+    (3, 4099, 16, 16, 1, False, False, False),
+    (257, 6, 136, 112, 2, False, True, False),
 ]
 
 
@@ -223,6 +225,10 @@ APPENDS = [
     ([300, 1030], [299, 517], 2, 1, 256, 128, 256, 1, False, False),
     ([1030, 2050], [1030, 1027], 1, 1, 256, 1024, 96, 4, True, False),
     ([90, 5, 0, 33], [9, 0, 0, 2], 0, 2, 64, 64, 16, 1, False, False),
+    ([1100, 700], [1095, 513], 9, 2, 64, 1024, 32, 2, True, True),
+    ([600, 90], [590, 90], 0, 3, 256, 64, 240, 1, False, True),
+    ([300] * 3, [290, 0, 17], 70, 1, 128, 256, 128, 3, False, False),
+    ([9, 1], [2, 1], 512, 256, 64, 16, 64, 1, False, False),
 ]
 
 
@@ -592,3 +598,75 @@ def test_pages_begun_with_any_scale(nk, sel, n_new, dtype):
                 # x / s is computed as x (1 / s), 2^-23 off: next to the middle of two steps either is right
                 step = np.maximum(np.abs(vb), 2.0 ** -6) * 2.0 ** -3
                 assert (np.abs(va - vb) <= step).all() and (va != vb).mean() < 1e-3
+
+
+def test_positions_wider_than_the_call(nk, sel):
+    """Positions of more rows and axes than a call has, and an axis named where
+    there is one, are the same positions."""
+    rng = np.random.default_rng(93)
+    shape = ([60, 9], [41, 9], 4, 2, 64, 32, 64, 2, False, False)
+    rng, c, table, x = filled(shape)
+    x = torch.from_numpy(x).to(torch.bfloat16).cuda()
+    tab = dev(T.table(100, 64, rng), np.float32)
+    pos = places(rng, 2, 50, 100)
+    wide = np.full((3, 77), 1 << 20)
+    wide[:2, :50] = pos
+    two = nk.Rope(sel, tab, T.axes(64, 2, False))
+    a = two.rotate(x[:, :4], u32(pos.astype(np.uint32)))
+    assert torch.equal(a, two.rotate(x[:, :4], u32(wide.astype(np.uint32))))
+    seqs, caches = sequences(nk, shape[1], shape[0], table), [upload(nk, sel, c) for _ in range(2)]
+    for cache, p in zip(caches, (pos, wide)):
+        assert torch.equal(cache.append(seqs, two, x[:, 4:6], x[:, 6:], x[:, :4], u32(p.astype(np.uint32))), a)
+    assert torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].k_scale, caches[1].k_scale)
+    named, one = nk.Rope(sel, tab, [0] * 32), nk.Rope(sel, tab)
+    assert torch.equal(named.rotate(x, u32(pos[0].astype(np.uint32))), one.rotate(x, u32(wide[:1].astype(np.uint32))))
+    sel.sync_errors()
+
+
+@pytest.mark.parametrize("n_seq", [7, 701])
+def test_append_rows_of_two_sequences(nk, sel, n_seq):
+    """Rows that an earlier sequence names are that one's: of all sequences that
+    begin among them nothing is stored."""
+    off = ([0, 20] * n_seq)[:n_seq - 1] + [20, 21]
+    rng, c, table, x = filled(([20] * n_seq, [0] * n_seq, 4, 2, 64, 32, 64, 1, False, False))
+    x = torch.from_numpy(rng.standard_normal((21, 8, 64))).to(torch.bfloat16)
+    tab = T.table(20, 64, rng)
+    cache, xd = upload(nk, sel, c), x.cuda()
+    before = [t.clone() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    out = torch.full((21, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    cache.append(sequences(nk, None, [20] * n_seq, table, n_tok=21, max_tok=20, off=off), nk.Rope(sel, dev(tab, np.float32)), xd[:, 4:6],
+                 xd[:, 6:], xd[:, :4], out=out)
+    with pytest.raises(nk.NetKVError, match="block cache"):
+        sel.sync_errors()
+    pos = np.concatenate([np.arange(20), [19]])[None]
+    check_rotated(out, x[:, :4], tab, pos, [0] * 32, False)
+    f = x.double().numpy()
+    keys = T.rotate(f[:, 4:6], tab, pos, [0] * 32, False)
+    two = table[[0, n_seq - 1]]
+    ref_store(c, two, [20, 20], [20, 1], keys, f[:, 6:])
+    same_cache(cache, c, two, [20, 20])
+    rest = np.setdiff1d(np.arange(c.shape[0]), two[:, 0])
+    for t, b in zip((cache.k, cache.v, cache.k_scale, cache.v_scale), before):
+        assert torch.equal(t.view(c.shape[0], -1)[rest], b.view(c.shape[0], -1)[rest])
+
+
+def test_two_appends_at_once(nk, sel):
+    """Two streams append to sequences of one cache, as one call does."""
+    shape = ([700, 40, 900, 64], [690, 1, 900, 1], 8, 2, 128, 512, 128, 1, False, False)
+    rng, c, table, x = filled(shape)
+    ctx, n_new = shape[:2]
+    x = torch.from_numpy(x).to(torch.bfloat16).cuda()
+    rope = nk.Rope(sel, dev(T.table(1000, 128, rng), np.float32))
+    a, b = upload(nk, sel, c), upload(nk, sel, c)
+    want = a.append(sequences(nk, n_new, ctx, table), rope, x[:, 8:10], x[:, 10:], x[:, :8])
+    parts = [(x[:691], sequences(nk, n_new[:2], ctx[:2], table[:2])), (x[691:], sequences(nk, n_new[2:], ctx[2:], table[2:]))]
+    torch.cuda.synchronize()
+    got = []
+    for y, seqs in parts:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got.append(b.append(seqs, rope, y[:, 8:10], y[:, 10:], y[:, :8]))
+    torch.cuda.synchronize()
+    assert torch.equal(torch.cat(got), want)
+    for t, u in ((a.k, b.k), (a.v, b.v), (a.k_scale, b.k_scale), (a.v_scale, b.v_scale)):
+        assert torch.equal(t, u)
+    sel.sync_errors()

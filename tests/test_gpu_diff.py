@@ -76,6 +76,10 @@ SHAPES = [
     ([900, 140], [130, 67], 16, 2, 128, 512),
     ([150, 333], [90, 33], 4, 2, 128, 64),
     ([3000, 10], [230, 1], 2, 2, 64, 128),
+    ([90, 5], [3, 1], 128, 2, 64, 16),                 # 64 rows of one token
+    ([90, 40], [7, 40], 128, 2, 128, 32),
+    ([17, 3], [1, 2], 512, 512, 64, 16),               # more pairs than workgroup slots a range
+    ([70], [60], 256, 256, 128, 64),
 ]
 
 
@@ -593,3 +597,36 @@ def test_longest_sequence(nk, sel, n_new):
     for j in range(2):
         want = (1 - lam[j]) * v
         assert (np.abs(o[:, j] - want) <= (1 + abs(lam[j])) * lim + np.abs(want) * 2.0 ** -8 + 1e-30).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_sequences_of_prompts(nk, sel, dim):
+    """More sequences than a wavefront finds by itself, some long enough to be split."""
+    rng = np.random.default_rng(6)
+    n_new = [int(x) for x in rng.integers(0, 3, 400)]
+    ctx = [int(x) for x in rng.integers(0, 40, 400)]
+    n_new[7], ctx[7], n_new[300], ctx[300], ctx[399], n_new[399] = 200, 333, 70, 3001, 1500, 1
+    c, table, q = case(nk, sel, 643, ctx, n_new, 4, 2, dim, 64, "bf16")
+    lam, norm = weights(43, 4, dim)
+    o = run(upload(nk, sel, c), sequences(nk, n_new, ctx, table), q.cuda(), lam, norm)
+    sel.sync_errors()
+    _say(check(c, table, ctx, n_new, q, o, lam, norm))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_two_calls_at_once(nk, sel, dim):
+    """Calls on two streams, each with its workspace, over one cache."""
+    ctx, n_new = [9000, 300, 2000], [1, 1, 1]
+    c, table, q = case(nk, sel, 644, ctx, n_new, 8, 2, dim, 64, "bf16")
+    lam, norm = (dev(x, np.float32) for x in weights(44, 8, dim))
+    cache, seqs, qs = upload(nk, sel, c), sequences(nk, n_new, ctx, table), [q.cuda(), -q.cuda()]
+    want = [cache.attend_diff(seqs, x, lam, norm=norm) for x in qs]
+    torch.cuda.synchronize()
+    got = []
+    for x in qs:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got.append([cache.attend_diff(seqs, x, lam, norm=norm) for _ in range(5)])
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(w, x) for x in g)
+    sel.sync_errors()

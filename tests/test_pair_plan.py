@@ -16,6 +16,11 @@ using namespace blockplan;
 using namespace pairplan;
 extern "C" uint32_t len(uint32_t steps, uint32_t C) { return even_steps(steps, C); }
 extern "C" uint32_t parts(uint32_t steps, uint32_t C) { return even_parts(steps, C); }
+extern "C" uint32_t narrow(void) { return kNarrow; }
+extern "C" int same_steps(uint32_t target, uint32_t fine, uint64_t work) {
+    const Split y{1, 16, target, fine, 4, 2};
+    return narrow_steps(y, (uint32_t)work) == range_steps(y, work);
+}
 extern "C" void plan(uint32_t n_seq, uint32_t max_pages, uint32_t btl, uint64_t n_tok, uint64_t max_tok, const uint64_t *off,
                      const uint32_t *ctx, uint32_t G, uint32_t tile_rows, uint32_t target, uint32_t fine, uint64_t *out) {
     Kv a{};
@@ -62,6 +67,17 @@ def test_even_ranges_cover_a_tile_once(lib):
             else:
                 assert n % 2 == 0 and n <= C and p >= 2 and (p - 1) * n < steps <= p * n
                 assert p <= -(-steps // C)
+
+
+def test_ranges_by_32_bits(lib):
+    """As by 64, up to the most that the kernels sum so: a sum that wrapped
+    would name more ranges than the host makes room for."""
+    rng = np.random.default_rng(0)
+    most = 64 * ((1 << lib.narrow()) - 1)
+    works = [0, 1, 3, 39, 40, 41, most, most - 1, most - 383] + [int(x) for x in np.exp2(rng.uniform(0, np.log2(most), 3000))]
+    for work in works:
+        for target, fine in ((1, 1), (1, 2), (7, 7), (320, 320), (384, 1024)):
+            assert lib.same_steps(target, fine, ctypes.c_uint64(work)), (work, target, fine)
 
 
 @pytest.mark.parametrize("seed", range(20))
