@@ -22,11 +22,11 @@ extern "C" int same_steps(uint32_t target, uint32_t fine, uint64_t work) {
     return narrow_steps(y, (uint32_t)work) == range_steps(y, work);
 }
 extern "C" void plan(uint32_t n_seq, uint32_t max_pages, uint32_t btl, uint64_t n_tok, uint64_t max_tok, const uint64_t *off,
-                     const uint32_t *ctx, uint32_t G, uint32_t tile_rows, uint32_t target, uint32_t fine, uint64_t *out) {
+                     const uint32_t *ctx, uint32_t G, uint32_t tile_rows, uint32_t target, uint32_t fine, uint32_t least, uint64_t *out) {
     Kv a{};
     a.n_seq = n_seq; a.max_pages = max_pages; a.btl = btl; a.n_tok = n_tok;
     a.max_tok = (uint32_t)(max_tok < n_tok ? max_tok : n_tok); a.off = off; a.ctx = ctx;
-    Split y{G, tile_rows, target, fine, 4, 2};
+    Split y{G, tile_rows, target, fine, least, 2};
     unsigned long long work = 0;
     for (int pass = 0; pass < 2; ++pass) {
         const uint32_t C = pass ? range_steps(y, work) : 0;
@@ -93,12 +93,13 @@ def test_capacities_hold_for_any_offsets(lib, seed):
         ctx = np.minimum(np.exp(rng.uniform(0, 13, n_seq)), (max_pages << btl) + 1).astype(np.uint32)
         pairs = int(rng.choice([1, 2, 3, 4, 8, 16, 512]))
         slots = -(-512 // pairs)
-        target = max(1, int(rng.choice([slots // 2, 5 * slots // 8, 3 * slots // 4])))
-        fine = int(rng.choice([target, 2 * slots]))
+        tile_rows = int(rng.choice([16, 32, 128]))
+        target = slots if tile_rows == 128 else max(1, int(rng.choice([slots // 2, 5 * slots // 8, 3 * slots // 4])))
+        fine = target if tile_rows == 128 else int(rng.choice([target, 2 * slots]))
         out = np.zeros(6, np.uint64)
         lib.plan(*(ctypes.c_uint32(v) for v in (n_seq, max_pages, btl)), ctypes.c_uint64(n_tok),
                  ctypes.c_uint64(int(rng.choice([n_tok, 1 + n_tok // 7]))), ctypes.c_void_p(off.ctypes.data),
                  ctypes.c_void_p(ctx.ctypes.data), ctypes.c_uint32(int(rng.choice([1, 3, 8, 64]))),
-                 ctypes.c_uint32(int(rng.choice([16, 32]))), ctypes.c_uint32(target), ctypes.c_uint32(fine),
+                 ctypes.c_uint32(tile_rows), ctypes.c_uint32(target), ctypes.c_uint32(fine), ctypes.c_uint32(8 if tile_rows == 128 else 4),
                  ctypes.c_void_p(out.ctypes.data))
         assert out[0] <= out[3] and out[1] <= out[4] and out[2] <= out[5], (seed, out)
