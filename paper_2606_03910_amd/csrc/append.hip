@@ -229,7 +229,7 @@ __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, 
     const Kv &kv = g.move.kv;
     const Turn &turn = g.rows.turn;
     Place pl;
-    if (!find_place(kv, task, pl)) return;
+    if (!find_place<THREADS>(kv, task, pl)) return;
     const uint64_t at = (uint64_t)pl.page * kv.hk + h;
     uint8_t *dst = kv.k + at * head_bytes(kv, D);
     const uint16_t *src = (const uint16_t *)g.move.k + (uint64_t)h * D;
@@ -381,10 +381,11 @@ __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, 
 }
 
 // The queries of up to `chunk` rows of one sequence.
+template <int THREADS>
 __device__ inline void append_queries(const AppendArgs &a, uint32_t task) {
     const Kv &kv = a.move.kv;
     uint32_t rest;
-    const uint32_t s = locate(kv, task, [&](const Head &h) { return row_chunks(h, a.chunk); }, &rest);
+    const uint32_t s = locate<THREADS>(kv, task, [&](const Head &h) { return row_chunks(h, a.chunk); }, &rest);
     if (s >= kv.n_seq) return;
     const Head h = seq_head(kv, s);
     const uint32_t t = rest * a.chunk;
@@ -392,19 +393,19 @@ __device__ inline void append_queries(const AppendArgs &a, uint32_t task) {
 }
 
 // All of a small call: latency.
-template <int D>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
+template <int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a) {
     if (blockIdx.x < a.row_tasks) {
-        append_queries(a, blockIdx.x);
+        append_queries<THREADS>(a, blockIdx.x);
         return;
     }
     const uint32_t i = blockIdx.x - a.row_tasks, task = i % a.store_tasks, r = i / a.store_tasks, h = r % a.move.kv.hk;
     const bool vals = r >= a.move.kv.hk;
     if (r == 0) report_bad(a.move.kv, task, a.store_tasks);
     if (vals)
-        store_block<D, kThreads>(a.move, a.rows.half, task, h, true);
+        store_block<D, THREADS>(a.move, a.rows.half, task, h, true);
     else
-        append_keys<D, kThreads, 4>(a, task, h);
+        append_keys<D, THREADS, 4>(a, task, h);
 }
 
 // A large call's queries and keys: the keys' arithmetic beside the queries'
@@ -415,7 +416,7 @@ __global__ __launch_bounds__(512, 4) void append_large_kernel(AppendArgs a) {
     const uint32_t keys = a.store_tasks * a.move.kv.hk, all = a.row_tasks + keys;
     const uint32_t k = (uint32_t)((uint64_t)blockIdx.x * keys / all);
     if ((uint32_t)((uint64_t)(blockIdx.x + 1) * keys / all) == k) {
-        append_queries(a, blockIdx.x - k);
+        append_queries<512>(a, blockIdx.x - k);
         return;
     }
     const uint32_t task = k % a.store_tasks, h = k / a.store_tasks;
@@ -445,15 +446,31 @@ netkv_status make_turn(netkv_handle h, const netkv_rope_t *rope, uint32_t head_d
     return NETKV_OK;
 }
 
+// Threads of a workgroup that takes a block's rows in one pass (append_keys' and
+// store_block's kEach), `groups` of 256 or more; 512 stands for a large call's
+// kernels.  256 where the card holds all of them at once, five on each CU: one
+// head's tokens are then as soon done by more threads.  Else 64, of which a CU
+// holds 20.  us with what is read back, 256, 64: 64 single tokens of 8 heads of 128
+// dimensions (1,088 groups) 20.7, 23.4, 256 (4,352) 37, 26, 200 times four 43, 32,
+// 5 prompts of up to 5,003 of 5 heads of 64 in blocks of 32 38, 30, 16 of 4,096 of 8
+// heads of 128 in blocks of 16 260, 204.
+uint32_t append_threads(const Kv &kv, uint32_t D, uint64_t groups) {
+    const uint32_t bt = 1u << kv.btl, elems = (kv.max_tok < bt ? kv.max_tok : bt) * D;
+    if (elems > 256 * 64) return 512;
+    return elems <= 64 * 64 && kv.n_seq <= kThreads && groups > 5 * 256 ? 64u : 256u;
+}
+
 template <int D>
-void launch_append(const AppendArgs &a, uint32_t block_rows, hipStream_t s) {
-    // blocks that a workgroup of 256 takes in one pass (append_keys' and store_block's kEach)
-    if (block_rows * D <= 256 * 64) {
-        append_kernel<D><<<a.row_tasks + a.store_tasks * a.move.kv.hk * 2, kThreads, 0, s>>>(a);
-        return;
+void launch_append(const AppendArgs &a, uint32_t threads, hipStream_t s) {
+    const uint32_t keys = a.store_tasks * a.move.kv.hk;
+    if (threads == 64) {
+        append_kernel<D, 64><<<a.row_tasks + 2 * keys, 64, 0, s>>>(a);
+    } else if (threads == 256) {
+        append_kernel<D, 256><<<a.row_tasks + 2 * keys, 256, 0, s>>>(a);
+    } else {
+        append_large_kernel<D><<<a.row_tasks + keys, 512, 0, s>>>(a);
+        append_values_kernel<D><<<dim3(a.store_tasks, a.move.kv.hk), 1024, 0, s>>>(a);
     }
-    append_large_kernel<D><<<a.row_tasks + a.store_tasks * a.move.kv.hk, 512, 0, s>>>(a);
-    append_values_kernel<D><<<dim3(a.store_tasks, a.move.kv.hk), 1024, 0, s>>>(a);
 }
 
 }  // namespace
@@ -526,6 +543,8 @@ extern "C" netkv_status netkv_kv_append(netkv_handle h, const netkv_kv_t *kv, co
     a.move.v_stride = v_stride;
     RowArgs &r = a.rows;
     r.half = dtype == NETKV_FP16;
+    const uint64_t tasks = store_groups(kv_);
+    const uint32_t threads = append_threads(kv_, kv->head_dim, tasks * kv_.hk * 2 + (n_heads ? kv_.n_tok / 16 : 0));
     uint64_t row_tasks = 0;
     if (n_heads) {
         r.x = (const uint16_t *)q;
@@ -535,21 +554,20 @@ extern "C" netkv_status netkv_kv_append(netkv_handle h, const netkv_kv_t *kv, co
         r.heads = n_heads;
         r.dim = kv->head_dim;
         r.units = units_of(r.turn.pairs, kv->head_dim, in_place);
-        a.chunk = kv_.max_tok < 16 ? 1 : 16;
+        a.chunk = kv_.max_tok < 16 ? 1 : threads == 64 ? 4 : 16;
         row_tasks = row_groups(kv_, a.chunk);
     }
-    const uint64_t tasks = store_groups(kv_), groups = row_tasks + tasks * kv_.hk * 2;
+    const uint64_t groups = row_tasks + tasks * kv_.hk * 2;
     // workgroups of up to 512, or of 1,024 along a head
     if (!grid_fits(groups, 512) || !grid_fits(tasks, 1024)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many rows for one call");
     a.row_tasks = (uint32_t)row_tasks;
     a.store_tasks = (uint32_t)tasks;
-    const uint32_t block_rows = kv_.max_tok < kv->block_tokens ? kv_.max_tok : kv->block_tokens;
     DeviceScope scope(netkv_internal_device(h));
     hipStream_t s = (hipStream_t)stream;
     switch (kv->head_dim) {
-        case 64: launch_append<64>(a, block_rows, s); break;
-        case 128: launch_append<128>(a, block_rows, s); break;
-        default: launch_append<256>(a, block_rows, s); break;
+        case 64: launch_append<64>(a, threads, s); break;
+        case 128: launch_append<128>(a, threads, s); break;
+        default: launch_append<256>(a, threads, s); break;
     }
     return launched(h, "append launch failed");
 }

@@ -1280,7 +1280,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(MoveArgs a, bool half) {
     const uint32_t task = blockIdx.x, h = blockIdx.y;
     if (h == 0) report_bad(kv, task, gridDim.x);
     uint32_t rest;
-    const uint32_t s = locate(kv, task, [&](const Head &h) { return read_steps(h); }, &rest);
+    const uint32_t s = locate<kThreads>(kv, task, [&](const Head &h) { return read_steps(h); }, &rest);
     if (s >= kv.n_seq) return;
     const Head hd = seq_head(kv, s);
     const uint32_t start = hd.ctx - hd.n, bt = 1u << kv.btl, tile = min(bt, kStep);

@@ -7,19 +7,21 @@
 namespace blockdev {
 
 // The `task`-th of the sequences' consecutive shares, where count(h) is how
-// many sequence h has: found by the whole workgroup, 256 sequences at a time.
+// many sequence h has: found by the whole workgroup of THREADS, 256 sequences at
+// a time or as many as it has threads.
 // Returns the sequence (n_seq if there is none) and the share in `rest`.  Those
 // that count have less than 2^32 (store_groups, read_groups).  Every workgroup
 // goes through the sequences before its own, so a call's time grows with their
 // square from some thousands on: single tokens of 1,024, 4,096, 16,384 and 65,535
 // sequences (8 heads of 128 dimensions) are stored in 66 us, 399 us, 4.3 ms and
 // 58 ms and read in 23 us, 164 us, 2.0 ms and 26 ms.
-template <typename F>
+template <int THREADS, typename F>
 __device__ inline uint32_t locate(const Kv &a, uint32_t task, F count, uint32_t *rest) {
     constexpr uint32_t kFalls = ~0u;      // a sequence whose rows are not good: every sum after it stays this
-    __shared__ uint32_t sums[kWaves], found, left, ends[16];
-    const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) & (kWaves - 1);
-    const bool in = threadIdx.x < kThreads;
+    constexpr int kEach = THREADS < kThreads ? THREADS : kThreads, kGroups = kEach / 64;
+    __shared__ uint32_t sums[kGroups], found, left, ends[16];
+    const int lane = threadIdx.x & 63, w = (threadIdx.x >> 6) & (kGroups - 1);
+    const bool in = threadIdx.x < kEach;
     if (threadIdx.x == 0) found = a.n_seq;
     uint32_t before = 0;
     auto look = [&](uint32_t s, uint32_t x) {              // whether that was the last chunk to look at
@@ -31,7 +33,7 @@ __device__ inline uint32_t locate(const Kv &a, uint32_t task, F count, uint32_t 
         if (in && lane == 63) sums[w] = y;
         __syncthreads();
         uint32_t base = before;
-        for (int v = 0; v < kWaves; ++v) {
+        for (int v = 0; v < kGroups; ++v) {
             if (v < w) base = __builtin_elementwise_add_sat(base, sums[v]);
             before = __builtin_elementwise_add_sat(before, sums[v]);
         }
@@ -45,7 +47,7 @@ __device__ inline uint32_t locate(const Kv &a, uint32_t task, F count, uint32_t 
     };
     uint32_t named = 0;
     for (bool again = false;; again = true) {
-        for (uint32_t s0 = 0; s0 < a.n_seq; s0 += kThreads) {
+        for (uint32_t s0 = 0; s0 < a.n_seq; s0 += kEach) {
             const uint32_t s = s0 + threadIdx.x;
             const bool is = in && s < a.n_seq;
             uint32_t x = 0;
@@ -150,10 +152,11 @@ struct Place {
 
 // The task-th block that the rows touch; false if there is none, or its page
 // is not one.
+template <int THREADS>
 __device__ inline bool find_place(const Kv &kv, uint32_t task, Place &p) {
     uint32_t rest;
     const uint32_t bt = 1u << kv.btl;
-    const uint32_t s = locate(kv, task, [&](const Head &h) { return stored_blocks(kv, h); }, &rest);
+    const uint32_t s = locate<THREADS>(kv, task, [&](const Head &h) { return stored_blocks(kv, h); }, &rest);
     if (s >= kv.n_seq) return false;
     const Head hd = seq_head(kv, s);
     const uint32_t start = hd.ctx - hd.n;                     // the first new token
@@ -191,7 +194,7 @@ __device__ __forceinline__ void store_block(const MoveArgs &a, bool half, uint32
     const Kv &kv = a.kv;
     const uint32_t bt = 1u << kv.btl;
     Place pl;
-    if (!find_place(kv, task, pl)) return;
+    if (!find_place<THREADS>(kv, task, pl)) return;
     const uint32_t page = pl.page, p0 = pl.p0, p1 = pl.p1;
     const uint64_t row0 = pl.row0;
     const uint16_t *src = (const uint16_t *)(vals ? a.v : a.k);

@@ -229,6 +229,9 @@ APPENDS = [
     ([600, 90], [590, 90], 0, 3, 256, 64, 240, 1, False, True),
     ([300] * 3, [290, 0, 17], 70, 1, 128, 256, 128, 3, False, False),
     ([9, 1], [2, 1], 512, 256, 64, 16, 64, 1, False, False),
+    ([90, 33, 5, 70] * 4, [60, 1, 5, 37] * 4, 7, 64, 128, 32, 64, 1, False, True),      # a wavefront a block and head
+    ([17, 40, 64] * 40, [2, 40, 33] * 40, 3, 5, 256, 16, 96, 3, True, False),
+    ([100] * 250, [1] * 250, 9, 4, 64, 64, 64, 1, False, False),
 ]
 
 
@@ -623,27 +626,27 @@ def test_positions_wider_than_the_call(nk, sel):
     sel.sync_errors()
 
 
-@pytest.mark.parametrize("n_seq", [7, 701])
-def test_append_rows_of_two_sequences(nk, sel, n_seq):
+@pytest.mark.parametrize("n_seq,hk", [(7, 2), (701, 2), (200, 64)])
+def test_append_rows_of_two_sequences(nk, sel, n_seq, hk):
     """Rows that an earlier sequence names are that one's: of all sequences that
     begin among them nothing is stored."""
     off = ([0, 20] * n_seq)[:n_seq - 1] + [20, 21]
-    rng, c, table, x = filled(([20] * n_seq, [0] * n_seq, 4, 2, 64, 32, 64, 1, False, False))
-    x = torch.from_numpy(rng.standard_normal((21, 8, 64))).to(torch.bfloat16)
+    rng, c, table, x = filled(([20] * n_seq, [0] * n_seq, 4, hk, 64, 32, 64, 1, False, False))
+    x = torch.from_numpy(rng.standard_normal((21, 4 + 2 * hk, 64))).to(torch.bfloat16)
     tab = T.table(20, 64, rng)
     cache, xd = upload(nk, sel, c), x.cuda()
     before = [t.clone() for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
     out = torch.full((21, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda")
-    cache.append(sequences(nk, None, [20] * n_seq, table, n_tok=21, max_tok=20, off=off), nk.Rope(sel, dev(tab, np.float32)), xd[:, 4:6],
-                 xd[:, 6:], xd[:, :4], out=out)
+    cache.append(sequences(nk, None, [20] * n_seq, table, n_tok=21, max_tok=20, off=off), nk.Rope(sel, dev(tab, np.float32)), xd[:, 4:4 + hk],
+                 xd[:, 4 + hk:], xd[:, :4], out=out)
     with pytest.raises(nk.NetKVError, match="block cache"):
         sel.sync_errors()
     pos = np.concatenate([np.arange(20), [19]])[None]
     check_rotated(out, x[:, :4], tab, pos, [0] * 32, False)
     f = x.double().numpy()
-    keys = T.rotate(f[:, 4:6], tab, pos, [0] * 32, False)
+    keys = T.rotate(f[:, 4:4 + hk], tab, pos, [0] * 32, False)
     two = table[[0, n_seq - 1]]
-    ref_store(c, two, [20, 20], [20, 1], keys, f[:, 6:])
+    ref_store(c, two, [20, 20], [20, 1], keys, f[:, 4 + hk:])
     same_cache(cache, c, two, [20, 20])
     rest = np.setdiff1d(np.arange(c.shape[0]), two[:, 0])
     for t, b in zip((cache.k, cache.v, cache.k_scale, cache.v_scale), before):
