@@ -572,8 +572,8 @@ typedef struct {
  * n_rows with several axes); a position >= n_pos makes its pairs NaN and is
  * reported by netkv_sync_errors.  transpose: by the negative angles, which is the
  * gradient of the rotation for x from that for out.  Each output is
- * a c +- b s to 2^-23 of it, rounded once to dtype, also where the products
- * cancel (down to 2^-149).  head_dim: a multiple of 8 from 16 to 1024.  Any order
+ * a c +- b s to 2^-23 of it and 2^-48 of its products, rounded once to dtype, also
+ * where the products cancel (down to 2^-149).  head_dim: a multiple of 8 from 16 to 1024.  Any order
  * of pos; needs no loads.  Asynchronous; allocates nothing.  ECAPACITY: more than
  * 2^32 - 1 threads, in workgroups of 256. */
 netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *rope, uint64_t n_rows, const uint32_t *pos,
@@ -591,8 +591,8 @@ netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *rope, uint64_
  * NaN in q_out and in the cache.  q_out may be q itself; else it must not
  * overlap q, k or v (EINVAL).  Sequences that netkv_kv_store leaves out are left
  * out, their rows of q_out and those past the last sequence left as they were.
- * Time, capacity and all else as for netkv_kv_store, and a workgroup of 256 or
- * more threads for each of up to 16 query rows. */
+ * Time, capacity and all else as for netkv_kv_store, and a workgroup of up to 512
+ * threads for each of up to 16 query rows. */
 netkv_status netkv_kv_append(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
                              const netkv_rope_t *rope, const uint32_t *pos, uint64_t pos_stride, const void *q,
                              uint32_t n_heads, uint64_t q_stride, void *q_out, uint64_t q_out_stride, const void *k,
@@ -667,7 +667,8 @@ netkv_status netkv_kv_attend_diff(netkv_handle h, const netkv_kv_t *kv, const ne
                                   void *work, uint64_t work_bytes, void *stream);
 
 /* Bytes of work for a netkv_kv_attend_diff of these shapes, from the host values
- * only: at most 300 MB. */
+ * only: at most 300 MB, and 48 bytes for each tile of 16 of a sequence's max_tok *
+ * n_heads / n_kv_heads rows. */
 netkv_status netkv_kv_attend_diff_workspace(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
                                             uint32_t n_heads, uint64_t *bytes);
 

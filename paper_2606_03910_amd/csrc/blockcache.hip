@@ -1,7 +1,7 @@
 // The decode instance's block cache for MI355X (gfx950): keys and values of
 // resident blocks in 8 bits, and the operators on them.
 //
-//   store_kernel    -- new keys and values quantised into their blocks.
+//   store_kernel    -- new keys and values quantised into their blocks (store_block).
 //   read_kernel     -- tokens given back in 16 bits.
 //   plan_kernel     -- a call's work list: (sequence, row tile, token range).
 //   attend_kernel   -- attention of up to 32 rows over a token range.

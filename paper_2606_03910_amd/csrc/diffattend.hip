@@ -289,7 +289,13 @@ __device__ __forceinline__ float weights_of(const f32x4 (&st)[2], float sc, floa
 // As attend_kernel, each wavefront for one map: the first and third take the
 // first map, the others the second, two steps of the range at a time.  The two
 // that work on one step read its values once from memory and once from the
-// caches.  Joined through LDS.
+// caches.  Joined through LDS.  Both maps in one wavefront would read them once,
+// but with twice the sums in registers, one wavefront a SIMD: 64 sequences of up to
+// 16,384 tokens 174 us, 8 of 131,071 378, 200 of up to 1,000 80 and not 51.  Bound by
+// memory: 8 sequences of 131,071 tokens, 8 KV heads of 128 dimensions (2.1 GB) 360
+// us, 5.9 TB/s; 64 of up to 16,384 (0.68 GB) 162, 4.2 TB/s, by the ends of unequal
+// ranges.  One row after 700 tokens takes 13 us, its chain of loads: lengths,
+// pages, keys, and through LDS.
 template <int D, int NT, bool HALF, bool SMALL>
 __global__ __launch_bounds__(kThreads, 2) void pair_kernel(PairArgs a) {
     typedef typename Elem<HALF>::T T;
@@ -622,6 +628,16 @@ __global__ __launch_bounds__(kThreads, 2) void pair_kernel(PairArgs a) {
 // values k + 1 with its own (slot 2 k + 2: values k - 1 were last read in slot
 // 2 k + 1, values k + 1 are first read in slot 2 k + 4).  At the end the second
 // map's rows go to the first group through LDS.
+// Bound by what stands beside the products: a slot's softmax of 64 rows, its
+// rounding and the widening of the step after take some 2,000 cycles of its
+// vector instructions, the other group's products 1,600.  Two chunks of 1,024 rows
+// after 31,744 tokens, 64 and 8 heads of 128 dimensions (3.2 TFLOP) 3.2 ms, 1,000
+// TFLOP/s, 83 % of a large matrix product's rate; six prompts of up to 2,777, 64 and 16
+// heads of 64 (233 GFLOP) 440 us, 530 TFLOP/s: a tile has 17 steps, of which the first
+// and the masked one take nearly twice the others' 2 us, and 9 us beside them.
+// Measured and not kept: loads straight into LDS (chunks 3.8 ms: what they wait
+// for is not the memory), more priority for the products (no change), and the
+// widening in loops of its own behind them (registers do not suffice).
 template <int D, int NT, int STEP, bool HALF, bool SMALL>
 __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs a) {
     typedef typename Elem<HALF>::T T;
@@ -1127,7 +1143,8 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     }
 }
 
-// Joins the ranges of one row, each map as join_row does, by WAVES wavefronts.
+// Joins the ranges of one row, each map as join_row does, by WAVES wavefronts:
+// 7 to 9 us for what up to 512 workgroups left, latency.
 template <int VD, bool HALF, int WAVES>
 __device__ inline void join_pair(const PairArgs &a, const Join &j, uint32_t p, uint32_t tr, f32x4 *lo, float *factor, float (*red)[kWaves]) {
     typedef typename Elem<HALF>::T T;

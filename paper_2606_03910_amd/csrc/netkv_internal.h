@@ -1,6 +1,7 @@
 // Declarations shared by the library's translation units (netkv.hip, the
 // selection path and the handle; flowsim.hip, the flow-level transfer
-// simulation; blockcache.hip and evict.hip, the block cache's operators).  Not part of the public interface (include/netkv.h).
+// simulation; blockcache.hip, append.hip, diffattend.hip and evict.hip, the block
+// cache's operators).  Not part of the public interface (include/netkv.h).
 #pragma once
 
 #include <hip/hip_runtime.h>
