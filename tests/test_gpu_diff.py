@@ -80,6 +80,10 @@ SHAPES = [
     ([90, 40], [7, 40], 128, 2, 128, 32),
     ([17, 3], [1, 2], 512, 512, 64, 16),               # more pairs than workgroup slots a range
     ([70], [60], 256, 256, 128, 64),
+    ([448, 100], [1, 1], 16, 2, 128, 64),              # the longest that are not split, and one step more
+    ([449, 100], [1, 1], 16, 2, 128, 64),
+    ([768, 500], [2, 1], 8, 2, 64, 16),
+    ([769, 500], [2, 1], 8, 2, 64, 16),
 ]
 
 

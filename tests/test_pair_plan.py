@@ -100,6 +100,6 @@ def test_capacities_hold_for_any_offsets(lib, seed):
         lib.plan(*(ctypes.c_uint32(v) for v in (n_seq, max_pages, btl)), ctypes.c_uint64(n_tok),
                  ctypes.c_uint64(int(rng.choice([n_tok, 1 + n_tok // 7]))), ctypes.c_void_p(off.ctypes.data),
                  ctypes.c_void_p(ctx.ctypes.data), ctypes.c_uint32(int(rng.choice([1, 3, 8, 64]))),
-                 ctypes.c_uint32(tile_rows), ctypes.c_uint32(target), ctypes.c_uint32(fine), ctypes.c_uint32(8 if tile_rows == 128 else 4),
+                 ctypes.c_uint32(tile_rows), ctypes.c_uint32(target), ctypes.c_uint32(fine), ctypes.c_uint32(8 if tile_rows == 128 else int(rng.choice([4, 7, 12]))),
                  ctypes.c_void_p(out.ctypes.data))
         assert out[0] <= out[3] and out[1] <= out[4] and out[2] <= out[5], (seed, out)
