@@ -460,7 +460,8 @@ netkv_status make_turn(netkv_handle h, const netkv_rope_t *rope, uint32_t head_d
 // store_block's kEach), `groups` of 256 or more; 512 stands for a large call's
 // kernels.  256 where the card holds all of them at once, five on each CU: one
 // head's tokens are then as soon done by more threads.  Else 64, of which a CU
-// holds 20.  us with what is read back, 256, 64: 64 single tokens of 8 heads of 128
+// holds 20, where they keep a block's rows and find their sequence in four looks
+// at most.  us with what is read back, 256, 64: 64 single tokens of 8 heads of 128
 // dimensions (1,088 groups) 20.7, 23.4, 256 (4,352) 37, 26, 200 times four 43, 32,
 // 5 prompts of up to 5,003 of 5 heads of 64 in blocks of 32 38, 30, 16 of 4,096 of 8
 // heads of 128 in blocks of 16 260, 204.

@@ -47,6 +47,7 @@ struct PairArgs : PlanArgs {
     float root_eps, gain;
     float *part;                     // [slot][pair][map][tile_rows][2 D]
     f32x4 *part_ml;                  // [slot][pair][map][tile_rows] m, l, y
+    uint32_t by_size;                // pair_kernel's longest ranges first
 };
 
 // 1 / sqrt(mean of o^2 + eps) of a row as a product of two factors: with its
@@ -130,15 +131,29 @@ __device__ inline uint32_t wave_sums(uint32_t x) {
     return x;
 }
 
+// The largest of the wavefront.
+__device__ inline uint32_t wave_most(uint32_t x) {
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
 // The work list as a wavefront has it in its registers, as Shares: each lane
 // takes up to four sequences in a row (n_seq <= kListed), and a row tile's
 // ranges are of one length; a sequence's last tiles, which see most, come
 // first.  By sums across lanes in place of LDS shuffles and by 32-bit divisions,
 // against Shares: six prompts of up to 2,777 tokens of which every workgroup takes
 // 17 steps (D = 64, 16 KV heads) 439 us and 448, the first tiles first 447.
+// BY_SIZE: a call's longest ranges first, by quarters of the longest's length.
+template <bool BY_SIZE>
 struct PairShares {
-    uint32_t rt[4], len[4], parts[4], per;
-    uint32_t items, slots, joins, own_items, own_slots, own_joins;   // sums up to this lane, and its own
+    static constexpr int kSizes = BY_SIZE ? 4 : 1;
+    uint32_t rt[4], len[4], parts[4], per, most;
+    uint32_t items[kSizes], slots, joins, own_items[kSizes], own_slots, own_joins;   // sums up to this lane, and its own
     bool bad;
 
     __device__ explicit PairShares(const PairArgs &a) {
@@ -178,31 +193,62 @@ struct PairShares {
             for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d, 64);
             C = range_steps(a, work);
         }
-        own_items = own_slots = own_joins = 0;
+        own_slots = own_joins = most = 0;
+#pragma unroll
+        for (int z = 0; z < kSizes; ++z) own_items[z] = 0;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
             len[j] = parts[j] = 1;
             if (j >= per) continue;
             len[j] = even_steps(kt[j], C);
             parts[j] = even_parts(kt[j], C);
-            own_items += rt[j] * parts[j];
+            if (!BY_SIZE) own_items[0] += rt[j] * parts[j];
             own_slots += parts[j] > 1 ? rt[j] * parts[j] : 0u;
             own_joins += parts[j] > 1 ? rt[j] : 0u;
+            most = max(most, len[j]);
         }
-        items = wave_sums(own_items);
+        if (BY_SIZE) {
+            most = wave_most(most);
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+                for (int z = 0; z < kSizes; ++z) own_items[z] += j < per && size(j) == z ? rt[j] * parts[j] : 0u;
+        }
+#pragma unroll
+        for (int z = 0; z < kSizes; ++z) items[z] = wave_sums(own_items[z]);
         slots = wave_sums(own_slots);
         joins = wave_sums(own_joins);
     }
 
+    // By how much of the longest range's length: more than 3/4, 1/2, 1/4, less.
+    __device__ int size(uint32_t j) const {
+        int z = 0;
+#pragma unroll
+        for (int k = 1; k < kSizes; ++k) z += len[j] <= most * k / kSizes ? 1 : 0;
+        return z;
+    }
+
     // Item or join i; false if there are not so many.
     __device__ bool item(const PairArgs &a, uint32_t i, Item &it) const {
-        const uint64_t past = __ballot(items > i);
+        uint32_t sum = items[0], own = own_items[0];
+        int which = 0;
+#pragma unroll
+        for (int z = 1; z < kSizes; ++z) {
+            const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)items[z - 1], 63);
+            const bool past = which == z - 1 && i >= all;
+            const uint32_t x = items[z], y = own_items[z];
+            i -= past ? all : 0u;
+            which = past ? z : which;
+            sum = past ? x : sum;
+            own = past ? y : own;
+        }
+        const uint64_t past = __ballot(sum > i);
         if (!past) return false;
         const int l = __ffsll((unsigned long long)past) - 1;
-        uint32_t at = items - own_items, slot = slots - own_slots, seq = 0, p = 1, n = 1, rest = 0, tiles = 0;
+        uint32_t at = sum - own, slot = slots - own_slots, seq = 0, p = 1, n = 1, rest = 0, tiles = 0;
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t x = rt[j] * parts[j];
+            const uint32_t y = rt[j] * parts[j], x = size(j) == which ? y : 0u;
             if (i >= at && i < at + x) {
                 seq = (threadIdx.x & 63) * per + j;
                 p = parts[j];
@@ -212,7 +258,7 @@ struct PairShares {
                 break;
             }
             at += x;
-            slot += parts[j] > 1 ? x : 0u;
+            slot += parts[j] > 1 ? y : 0u;
         }
         auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); };
         p = of(p);
@@ -251,9 +297,10 @@ struct PairShares {
 };
 
 // find_item by it.
+template <bool BY_SIZE>
 __device__ inline bool find_range(const PairArgs &a, uint32_t i, Item &it, Head &hd) {
     if (a.items) return find_item(a, i, it, hd);
-    const PairShares sh(a);
+    const PairShares<BY_SIZE> sh(a);
     if (blockIdx.x == 0 && __builtin_expect(__any(sh.bad), 0)) fill_bad(a);
     if (!sh.item(a, i, it)) return false;
     auto one = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
@@ -293,7 +340,7 @@ __device__ __forceinline__ float weights_of(const f32x4 (&st)[2], float sc, floa
 // but with twice the sums in registers, one wavefront a SIMD: 64 sequences of up to
 // 16,384 tokens 174 us, 8 of 131,071 378, 200 of up to 1,000 80 and not 51.  Bound by
 // memory: 8 sequences of 131,071 tokens, 8 KV heads of 128 dimensions (2.1 GB) 360
-// us, 5.9 TB/s; 64 of up to 16,384 (0.68 GB) 162, 4.2 TB/s, by the ends of unequal
+// us, 5.9 TB/s; 64 of up to 16,384 (0.68 GB) 157, 4.3 TB/s, by the ends of unequal
 // ranges.  One row after 700 tokens takes 13 us, its chain of loads: lengths,
 // pages, keys, and through LDS.
 template <int D, int NT, bool HALF, bool SMALL>
@@ -309,7 +356,7 @@ __global__ __launch_bounds__(kThreads, 2) void pair_kernel(PairArgs a) {
     const uint32_t p = blockIdx.x % a.pairs, item = blockIdx.x / a.pairs;
     Item it;
     Head hd;
-    if (!find_range(a, item, it, hd)) return;
+    if (!(a.by_size ? find_range<true>(a, item, it, hd) : find_range<false>(a, item, it, hd))) return;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
     const uint32_t map = w & 1, first = it.k0 + (w >> 1);
     const uint32_t c = lane & 15, g = lane >> 4;
@@ -659,7 +706,7 @@ __global__ __launch_bounds__(kPromptThreads, 2) void pair_prompt_kernel(PairArgs
     const uint32_t p = blockIdx.x % a.pairs, item = blockIdx.x / a.pairs;
     Item it;
     Head hd;
-    if (!find_range(a, item, it, hd)) return;
+    if (!find_range<false>(a, item, it, hd)) return;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // known to be uniform
     const bool second = w >= 4;
     const uint32_t map = second;
@@ -1264,7 +1311,7 @@ __global__ __launch_bounds__(kThreads) void pair_join_kernel(PairArgs a, uint32_
     if (a.joins) {
         all(a.head->n_joins, [&](uint32_t i) { return a.joins[i]; });
     } else {
-        const PairShares sh(a);
+        const PairShares<false> sh(a);
         all(sh.n_joins(), [&](uint32_t i) { return sh.join(i); });
     }
 }
@@ -1274,6 +1321,7 @@ __global__ __launch_bounds__(kThreads) void pair_join_kernel(PairArgs a, uint32_
 struct PairLayout : Split {
     uint32_t pairs;
     bool rows;             // pair_prompt_kernel
+    bool by_size;          // longest ranges first
     int NT;                // row tiles of pair_kernel
     uint32_t item_cap, slot_cap, join_cap, tile_most;
     uint64_t head, items, joins, ml, part, total;
@@ -1317,6 +1365,12 @@ netkv_status make_pair_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t 
     const uint64_t steps_most = (((uint64_t)a.max_pages << a.btl) + kStep - 1) / kStep;
     const uint32_t whole = D == 64 ? 12 : 7;
     y.least = y.rows ? 8 : steps_most <= whole ? whole : 4;
+    // Longest ranges first where a range can have more than 32 steps: us, in the
+    // sequences' order and so, 8 KV heads of 128 dimensions, 200 of up to 16,384 tokens
+    // 497, 406, 120 of up to 8,000 208, 162, 16 of up to 30,000 62, 54, 64 of up to 16,384
+    // 170, 164; 8 of 131,071 367, 370.  Shorter ones gain less than finding the order
+    // takes: 37 of up to 5,003 and 6 KV heads of 64 25.4, 27.
+    y.by_size = !y.rows && tiles > 1 && tiles * steps_most > 32 * ranges;
     y.round = 2;
     const Caps caps = caps_of(a, y);
     if (!grid_fits(caps.items * y.pairs, y.rows ? kPromptThreads : kThreads)) return netkv_internal_fail(h, NETKV_ECAPACITY, "too many query rows for one call");
@@ -1416,6 +1470,7 @@ extern "C" netkv_status netkv_kv_attend_diff(netkv_handle h, const netkv_kv_t *k
         launch_plan(t, s);
     }
     t.pairs = y.pairs;
+    t.by_size = y.by_size;
     t.tile_log = y.rows ? 7 : y.NT == 2 ? 5 : 4;
     t.q_stride = q_stride;
     t.q = q;

@@ -617,6 +617,23 @@ def test_many_sequences_of_prompts(nk, sel, dim):
     _say(check(c, table, ctx, n_new, q, o, lam, norm))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim,n_seq,n_new", [(64, 70, 1), (128, 70, 3), (128, 250, 1), (64, 33, 9)])
+def test_ragged_sequences_of_long_tables(nk, sel, dim, n_seq, n_new, dtype):
+    """Ranges of all lengths, the longest first; tables wider than any sequence."""
+    rng = np.random.default_rng(7)
+    ctx = [int(x) for x in np.exp(rng.uniform(np.log(1), np.log(3000), n_seq))]
+    ctx[0], ctx[5], ctx[n_seq - 1] = 3, 3000, 2999
+    new = [n_new] * n_seq
+    new[3], ctx[3], ctx[4] = 0, 50, 0
+    c, table, q = case(nk, sel, 645, ctx, new, 4, 2, dim, 64, dtype)
+    lam, norm = weights(45, 4, dim)
+    wide = np.concatenate([table, np.full((n_seq, 2048 - table.shape[1]), 1 << 30)], 1)      # never read
+    o = run(upload(nk, sel, c), sequences(nk, new, ctx, wide), q.cuda(), lam, norm)
+    sel.sync_errors()
+    _say(check(c, table, ctx, new, q, o, lam, norm))
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 def test_two_calls_at_once(nk, sel, dim):
     """Calls on two streams, each with its workspace, over one cache."""
