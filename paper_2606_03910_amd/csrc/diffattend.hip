@@ -339,8 +339,8 @@ __device__ __forceinline__ float weights_of(const f32x4 (&st)[2], float sc, floa
 // caches.  Joined through LDS.  Both maps in one wavefront would read them once,
 // but with twice the sums in registers, one wavefront a SIMD: 64 sequences of up to
 // 16,384 tokens 174 us, 8 of 131,071 378, 200 of up to 1,000 80 and not 51.  Bound by
-// memory: 8 sequences of 131,071 tokens, 8 KV heads of 128 dimensions (2.1 GB) 360
-// us, 5.9 TB/s; 64 of up to 16,384 (0.68 GB) 157, 4.3 TB/s, by the ends of unequal
+// memory: 8 sequences of 131,071 tokens, 8 KV heads of 128 dimensions (2.1 GB) 355
+// us, 6.0 TB/s; 64 of up to 16,384 (0.68 GB) 154, 4.4 TB/s, by the ends of unequal
 // ranges.  One row after 700 tokens takes 13 us, its chain of loads: lengths,
 // pages, keys, and through LDS.
 template <int D, int NT, bool HALF, bool SMALL>
