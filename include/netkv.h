@@ -585,7 +585,8 @@ netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *rope, uint64_
  * q_out as by netkv_rope_rotate ([n_tok][n_heads][head_dim]; n_heads 0: none, q and q_out are
  * not looked at), k rotated and v as it is stored as by netkv_kv_store.  A rotated
  * key is rounded once, from a c +- b s in 64 bits to its 8 bits, and the scale is
- * that of the unrounded keys.  pos as for netkv_rope_rotate, for the rows of the
+ * that of the unrounded keys; one past 448 * 2^127, which no scale holds, is as one
+ * that is not finite.  pos as for netkv_rope_rotate, for the rows of the
  * token arrays; NULL: a row's position on every axis is its token's place in its
  * sequence (0 for the first).  A position >= n_pos is reported, and its pairs are
  * NaN in q_out and in the cache.  q_out may be q itself; else it must not

@@ -138,6 +138,22 @@ __device__ inline uint32_t to_odd(double x) {
     return u | min(rest, 1u) | (hi >> 16 & 0x8000u);
 }
 
+// The largest key that a scale holds, 448 * 2^127; past it a key is as one that
+// is not finite.
+constexpr double kMostKey = 448.0 * 0x1p127;
+
+// The upper half of a key's bits without its sign, to odd; 0 for one that no scale holds.
+__device__ inline uint32_t upper_odd(double x) {
+    const uint64_t bits = __builtin_bit_cast(uint64_t, fabs(x));
+    return fabs(x) <= kMostKey ? (uint32_t)(bits >> 32) | (uint32_t)((uint32_t)bits != 0) : 0u;
+}
+
+// scale_for (blockstore.h) of such a one.
+__device__ inline float scale_for_upper(uint32_t most) {
+    const int e = (int)(most >> 20) - 1023 + ((most & 0xFFFFFu) <= 0xC0000u ? -8 : -7);
+    return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
+}
+
 // ------------------------------------------------------------------ rows
 
 struct RowArgs {
@@ -224,8 +240,10 @@ struct AppendArgs {
 // 64 bits, where the products of 16-bit elements and 32-bit cosines are exact,
 // and rounded once, to 8 bits: in fp32 one in some hundred thousand would
 // come out a step off, and a block's scale by a factor of two.  Between the
-// largest value and the rounding it is held in 16 bits, to odd (to_odd).  The
-// products in 64 bits and the roundings to odd bound it where calls are large:
+// largest value and the rounding it is held in 16 bits, to odd (to_odd), where
+// these have two bits more than the block's 8: not past fp32's largest, nor where
+// the block's steps (from 2^-9 of its scale) near bfloat16's smallest, 2^-133.
+// Such blocks are computed once more from 64 bits.  The products in 64 bits and the roundings to odd bound it where calls are large:
 // 131,214 rows of 8 heads of 128 dimensions 220 us, of which the memory needs 80.
 template <int D, int THREADS, int kEach>
 __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, uint32_t h) {
@@ -321,42 +339,62 @@ __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, 
     }
 
     float *scale = kv.ks + at;
-    float sc = scale_for(__uint_as_float(top << 16));
-    if (pl.p0) {
-        const float was = *scale;
-        sc = was > sc ? was : sc;
-        if (was != sc) {
+    const float was = pl.p0 ? *scale : 0.0f;
+    auto or_present = [&](float x) { return was > x ? was : x; };
+    float sc = or_present(scale_for(__uint_as_float(top << 16)));
+    // the new scale, and what the block holds under it
+    auto rescale = [&]() {
+        if (pl.p0 && was != sc) {
             const float ratio = was / sc;
             for (uint32_t i = threadIdx.x; i < pl.p0 * (D / 4); i += THREADS) ((uint32_t *)dst)[i] = rescale4(((uint32_t *)dst)[i], ratio);
         }
-    }
-    __syncthreads();   // every thread has read the old scale
-    if (threadIdx.x == 0) *scale = sc;
-    if (__builtin_expect((__float_as_uint(sc) & 0x7FFFFFu) != 0, 0)) {
-        // a scale that is no power of two, from another program: over it what was
-        // rounded to 16 bits would be rounded twice, so all once more from 64
-#pragma unroll 1
-        for (uint32_t e = threadIdx.x; e < units; e += THREADS) {
+        __syncthreads();   // every thread has read the old scale
+        if (threadIdx.x == 0) *scale = sc;
+    };
+    // Once more from 64 bits: keys past fp32's largest, which are held as
+    // bfloat16's largest; a scale that is no power of two, from another program,
+    // over which what is held would be rounded twice; scales under which half of
+    // the smallest step is bfloat16's smallest (2^-133 under 2^-123) or less.
+    const bool far = top == kNotFinite - 1;
+    if (__builtin_expect(far || (top && sc < 0x1p-122f) || (__float_as_uint(sc) & 0x7FFFFFu) != 0, 0)) {
+        auto in_64_bits = [&](uint32_t e, const Unit &w, auto take) {
             const uint16_t *from = src + (pl.row0 + e / kUnits) * g.move.k_stride;
-            const Unit w = unit(e);
             const u32x4 v[2] = {*(const u32x4 *)(from + w.lo), *(const u32x4 *)(from + w.hi)};
-            float y[16];
-            auto over = [&](double x) { return odd_f32(x / (double)sc); };
             if (w.turns) {
                 turned(e, v, [&](int j, double p, double q) {
-                    y[turn.interleaved ? 2 * j : j] = over(p);
-                    y[turn.interleaved ? 2 * j + 1 : 8 + j] = over(q);
+                    take(turn.interleaved ? 2 * j : j, p);
+                    take(turn.interleaved ? 2 * j + 1 : 8 + j, q);
                 });
             } else {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) y[j] = over(to_f32(half_of(v[j / 8], j % 8), half));
+                for (int j = 0; j < 16; ++j) take(j, (double)to_f32(half_of(v[j / 8], j % 8), half));
             }
+        };
+        if (far) {
+            uint32_t most = 0;
+#pragma unroll 1
+            for (uint32_t e = threadIdx.x; e < units; e += THREADS)
+                in_64_bits(e, unit(e), [&](int, double x) { most = max(most, upper_odd(x)); });
+            for (int d = 32; d; d >>= 1) most = max(most, (uint32_t)__shfl_xor(most, d, 64));
+            __syncthreads();   // every thread has read red
+            if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = most;
+            __syncthreads();
+            for (int i = 0; i < THREADS / 64; ++i) most = max(most, red[0][i]);
+            sc = or_present(scale_for_upper(most));
+        }
+        rescale();
+#pragma unroll 1
+        for (uint32_t e = threadIdx.x; e < units; e += THREADS) {
+            const Unit w = unit(e);
+            float y[16];
+            in_64_bits(e, w, [&](int j, double x) { y[j] = fabs(x) <= kMostKey ? odd_f32(x / (double)sc) : NAN; });
             uint8_t *p = dst + (uint64_t)(pl.p0 + e / kUnits) * D;
             *(u32x2 *)(p + w.lo) = u32x2{narrow4(y, 1.0f), narrow4(y + 4, 1.0f)};
             *(u32x2 *)(p + w.hi) = u32x2{narrow4(y + 8, 1.0f), narrow4(y + 12, 1.0f)};
         }
         return;
     }
+    rescale();
     const float inv = 1.0f / sc;
     const bool plain = any < kNotFinite;
     for (uint32_t base = 0; base < units; base += THREADS * kEach) {
