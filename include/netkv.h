@@ -573,8 +573,8 @@ typedef struct {
  * reported by netkv_sync_errors.  transpose: by the negative angles, which is the
  * gradient of the rotation for x from that for out.  Each output is
  * a c +- b s to 2^-23 of it and 2^-48 of its products, rounded once to dtype, also
- * where the products cancel (down to 2^-149).  head_dim: a multiple of 8 from 16 to 1024.  Any order
- * of pos; needs no loads.  Asynchronous; allocates nothing.  ECAPACITY: more than
+ * where the products cancel (down to 2^-149) or are past fp32's largest.
+ * head_dim: a multiple of 8 from 16 to 1024.  Any order of pos; needs no loads.  Asynchronous; allocates nothing.  ECAPACITY: more than
  * 2^32 - 1 threads, in workgroups of 256. */
 netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *rope, uint64_t n_rows, const uint32_t *pos,
                                uint64_t pos_stride, const void *x, uint64_t x_stride, void *out,

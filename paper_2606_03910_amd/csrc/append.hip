@@ -107,10 +107,17 @@ __device__ inline uint32_t pack16(float x, float y, bool half) {
 }
 
 // a c - b s of 16-bit a, b to 1.5 units of fp32's last place, also where the
-// products cancel: what the first product loses comes back.
+// products cancel: what the first product loses comes back.  b s is not past
+// fp32's largest.
 __device__ inline float cross(float a, float c, float b, float s) {
     const float w = b * s, e = fmaf(b, s, -w), t = fmaf(a, c, -w);
     return e == e ? t - e : t;        // w not finite
+}
+
+// The same for any b s: where it is, from 64 bits, in which the products are exact.
+__device__ inline float cross_any(float a, float c, float b, float s) {
+    const float y = cross(a, c, b, s);
+    return y == y ? y : (float)fma((double)a, (double)c, -((double)b * (double)s));
 }
 
 // A double to fp32, to odd where it is not exact.
@@ -188,6 +195,45 @@ __device__ inline void turn_unit(const Turn &t, bool half, const Angles &g, u32x
     }
 }
 
+// The largest of a unit's sines.  Up to 1 no product of it is past fp32's largest.
+__device__ inline float most_sine(const Angles &g) {
+    float x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x = fmaxf(x, fabsf(g.s[i]));
+    return x;
+}
+
+// Whether one may be, of the heads that a thread has.
+__device__ inline bool past_fp32(const u32x4 (&lo)[kHeadsEach], const u32x4 (&hi)[kHeadsEach], bool half, float sine) {
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (uint32_t i = 0; i < 4 * kHeadsEach; ++i) {
+        top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, lo[i / 4][i % 4] & 0x7FFF7FFFu));
+        top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, hi[i / 4][i % 4] & 0x7FFF7FFFu));
+    }
+    return !(to_f32(max(top[0], top[1]), half) * sine < INFINITY);
+}
+
+// A unit of `heads` heads turned whatever its products, an element after another
+// (slower, but in no more registers than turn_unit).
+__device__ inline void turn_any(const RowArgs &r, const Angles &g, const Unit &p, const uint16_t *x, uint16_t *out, uint32_t heads) {
+#pragma unroll 1
+    for (uint32_t j = 0; j < 8 * heads; ++j) {
+        const uint32_t k = j & 7, at = j / 8 * r.dim;
+        const uint32_t ia = at + p.lo + (r.turn.interleaved ? 2 * k : k), ib = r.turn.interleaved ? ia + 1 : at + p.hi + k;
+        float c = g.c[0], s = g.s[0];
+#pragma unroll
+        for (uint32_t i = 1; i < 8; ++i) {
+            c = k == i ? g.c[i] : c;
+            s = k == i ? g.s[i] : s;
+        }
+        const float ea = to_f32(x[ia], r.half), eb = to_f32(x[ib], r.half);
+        const uint32_t y = pack16(cross_any(ea, c, eb, s), cross_any(eb, c, ea, -s), r.half);
+        out[ia] = (uint16_t)y;
+        out[ib] = (uint16_t)(y >> 16);
+    }
+}
+
 // Rows [row, row + n) of the arrays; a row's position is `place` and on if the
 // turn has none of its own.
 __device__ inline void rotate_rows(const RowArgs &a, uint64_t row, uint32_t n, uint32_t place) {
@@ -206,7 +252,14 @@ __device__ inline void rotate_rows(const RowArgs &a, uint64_t row, uint32_t n, u
             xh[j] = *(const u32x4 *)(from + (p.both ? p.hi : p.lo));
         }
         Angles g;
-        if (p.turns) load_angles(a.turn, row + t, place + t, u, g);
+        if (p.turns) {
+            load_angles(a.turn, row + t, place + t, u, g);
+            const float sine = most_sine(g);
+            if (__builtin_expect(sine > 1.0f && past_fp32(xl, xh, a.half, sine), 0)) {
+                turn_any(a, g, p, x, out, last + 1);
+                continue;
+            }
+        }
 #pragma unroll
         for (uint32_t j = 0; j < kHeadsEach; ++j) {
             if (j > last) continue;

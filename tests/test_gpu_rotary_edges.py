@@ -1,11 +1,11 @@
-"""Appended keys at both ends of fp32's range, against the plain form in 64
-bits.  Needs an MI355X and the built library."""
+"""Appended keys and rotations at both ends of fp32's range, against plain forms in
+64 bits.  Needs an MI355X and the built library."""
 import numpy as np
 import pytest
 
 from tests import blockcache_ref as R
 from tests import rope_ref as T
-from tests.test_gpu_append import own_places
+from tests.test_gpu_append import check_rotated, own_places
 from tests.test_gpu_block_cache import HALF, dev, ref_store, same_cache, sequences, upload
 
 pytestmark = pytest.mark.gpu
@@ -114,6 +114,39 @@ def test_append_keys_into_pages_of_small_scales(nk, sel, e):
     tab = np.concatenate([cos, rng.choice([-1.0, 0.0, 1.0], m.shape) * 2.0 ** (e + 80 - 9 - 30)], 1).astype(np.float32)
     x = np.full((n, 4, 64), 2.0 ** -80) * rng.choice([-1.0, 1.0], (n, 4, 64))
     append_and_compare(nk, sel, shape, torch.from_numpy(x).to(torch.bfloat16), tab, scales=2.0 ** e)
+
+
+# ------------------------------------------------------------------ products past fp32
+
+@pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("dtype,scale", [("bf16", 1.25), ("bf16", 4.0), ("fp16", 2.0 ** 116), ("fp16", 2.0 ** 126)])
+def test_rotate_products_past_fp32(nk, sel, dtype, scale, inter, transpose):
+    """Finite elements whose products with a scaled table are past fp32's largest:
+    the sum is infinite, or finite where they cancel, and never NaN."""
+    rng = np.random.default_rng(740)
+    n, big = 600, 3.3e38 if dtype == "bf16" else 65000.0
+    # factors of 8 bits, so that elements equal to them cancel to 0
+    tab = (torch.from_numpy(T.table(n, 64, rng)).to(torch.bfloat16).double().numpy() * scale).astype(np.float32)
+    x = rng.standard_normal((n, 5, 64))
+    x[:, 0] = big * rng.choice([-1.0, 1.0], (n, 64))
+    x[:, 1] *= np.where(rng.random((n, 64)) < 0.2, big / 5, 1.0)
+    first, second = (slice(0, 64, 2), slice(1, 64, 2)) if inter else (slice(0, 32), slice(32, 64))
+    c, s = tab[:, :32].astype(np.float64) / scale, tab[:, 32:].astype(np.float64) / scale
+    x[:, 2, first], x[:, 2, second] = 0.9 * big * s, 0.9 * big * c          # a cos - b sin nearly cancels
+    power = 2.0 ** 127 if dtype == "bf16" else 2.0 ** 15
+    x[:, 3, first], x[:, 3, second] = power * c, -power * s                 # b cos + a sin cancels
+    x[:, 4, first] = 1.0                                                    # b alone is large
+    x[:, 4, second] = big
+    x = torch.from_numpy(np.clip(x, -big, big)).to(HALF[dtype])
+    rope = nk.Rope(sel, dev(tab, np.float32), interleaved=inter)
+    pos = np.arange(n)[None]
+    got = rope.rotate(x.cuda(), dev(pos, np.int32).view(torch.uint32), transpose=transpose)
+    assert not torch.isnan(got).any()
+    _say(check_rotated(got, x, tab, pos, [0] * 32, inter, transpose))
+    wide = torch.isinf(got)
+    assert wide.any() and not wide.all()
+    sel.sync_errors()
 
 
 @pytest.mark.parametrize("e", [-133, -130, -126, -124, -121, -116, 110, 126])
