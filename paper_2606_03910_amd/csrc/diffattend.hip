@@ -1344,7 +1344,11 @@ netkv_status make_pair_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t 
     y.NT = D == 128 || most <= 16 ? 1 : 2;
     y.tile_rows = !y.rows ? 16u * y.NT : 128u;
     y.tile_most = (uint32_t)(most < y.tile_rows ? most : y.tile_rows);
-    // Ranges a pair, of the card's 512 workgroup slots.  Prompts: as make_layout's.
+    // Ranges a pair, of the card's 512 workgroup slots.  Prompts: no more than those in
+    // all, which bounds the workspace (1,024 slots of 128 rows) and leaves none for
+    // a second turn; us, rounded up to more and so: 128 dimensions, 300 rows after
+    // 16,084 tokens of 20 pairs 302, 252, 128 after 3,968 of 200 pairs 288, 266, 256 after
+    // 32,512 of 3 pairs 477, 479, 64 dimensions, the first 185, 155.
     // Few rows, 128 dimensions: one workgroup a CU streams as fast as two, whose
     // second reads of the values miss the caches more often, so few tiles (long
     // sequences) get 256 ranges in all; where unequal tiles leave some short 320,
@@ -1355,7 +1359,7 @@ netkv_status make_pair_layout(netkv_handle h, const Kv &a, uint32_t D, uint32_t 
     // us, 256, 384, 512 and 1,024: 64 of up to 16,384 and 8 pairs 197, 170, 159, 37 of
     // up to 5,003 and 3 pairs 30, 27, 31.
     const uint64_t slots = (512u + y.pairs - 1) / y.pairs, tiles = (uint64_t)a.n_seq * ((most + y.tile_rows - 1) / y.tile_rows);
-    uint64_t ranges = slots;
+    uint64_t ranges = y.pairs < 512 ? 512u / y.pairs : 1u;
     if (!y.rows) ranges = D == 64 ? 3 * slots / 4 : tiles <= slots / 8 || tiles > slots ? slots / 2 : 5 * slots / 8;
     y.target = (uint32_t)(ranges ? ranges : 1);
     y.fine = y.rows || D == 128 ? y.target : (uint32_t)(2 * slots);
