@@ -525,11 +525,13 @@ class Rope:
     table f32[n_pos][rot_dim], rot_dim / 2 cosines and as many sines of every
     position; axis: each pair's (a sequence of rot_dim / 2 numbers below 4), all
     of one axis if None; interleaved: pairs of neighbours, else of halves.  A
-    program keeps it for all layers and steps."""
+    program keeps it for all layers and steps.  No gradient for the table."""
 
     def __init__(self, sel: "Selector", table: torch.Tensor, axis: Optional[Iterable[int]] = None,
                  interleaved: bool = False):
         c = netkv_rope_t()
+        if isinstance(table, torch.Tensor):
+            _no_gradient(table, "table")
         c.table = _dptr(table, torch.float32, None, "table")
         _on_all(sel.device, table=table)
         if table.dim() != 2:
