@@ -1,8 +1,10 @@
-"""Differential attention's workspace.  Needs an MI355X and the built library."""
+"""Differential attention's rounding of small weights, and its workspace's bound.
+Needs an MI355X and the built library."""
 import numpy as np
 import pytest
 
-from tests.test_gpu_block_cache import sequences
+from tests import blockcache_ref as R
+from tests.test_gpu_block_cache import dev, sequences, upload
 
 pytestmark = pytest.mark.gpu
 
@@ -26,6 +28,56 @@ def sel(nk):
     s = nk.Selector(0)
     yield s
     s.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("dim,n_new,ctx,block", [
+    (64, 1, 32768, 512), (64, 7, 5000, 16), (64, 2, 600, 64), (128, 2, 9000, 64), (128, 1, 400, 32), (128, 9, 3000, 16),
+    (64, 70, 5000, 16), (64, 60, 32768, 512), (64, 200, 500, 64), (128, 40, 32768, 512), (128, 40, 5000, 16), (128, 90, 300, 64)])
+def test_a_dominant_token_leaves_the_others(nk, sel, dim, n_new, ctx, block, where, dtype):
+    """One token far above many equal ones whose values alone are not zero: the
+    output is what those keep of the weight, of the first map alone and of the
+    second one nearly alone (lambda -8); few rows and prompts, split and whole.
+
+    Relative limit: a weight e^-S of the largest is rounded by half of the
+    larger of 2^-10 of itself and 2^-30 of the largest, so relatively by
+    max(2^-11, 2^-31 e^S); the others' values are 1, so all of them may be off
+    to the same side.  Scores are exact (ones and zeros, one product with the
+    scale) up to S 2^-23 by that product and S log2(e) 2^-23 by the exponential's
+    argument, twice; the exponential and sums in fp32, at most 2^9 one after
+    the other, 2^-15 in all; the maps' sum, both of one sign here, 2^-23 twice; and
+    the output's own half step."""
+    heads, hk = 16, 4
+    rng = np.random.default_rng(95)
+    table, pages = R.tables(rng, [ctx], block)
+    c = R.Cache(pages, hk, dim, block, rng)
+    c.ks[:], c.vs[:] = 1.0, 1.0
+    c.k[:], c.v[:] = 0, 0x38                               # 0 and 1.0
+    tok = dict(first=0, middle=ctx // 2 + 5, last=ctx - n_new)[where]
+    c.k[table[0, tok // block], :, tok % block] = 0x38
+    c.v[table[0, tok // block], :, tok % block] = 0
+    cache, seqs = upload(nk, sel, c), sequences(nk, [n_new], [ctx], table)
+    q = torch.ones((n_new, heads, dim), dtype=torch.bfloat16 if dtype == "bf16" else torch.float16, device="cuda")
+    lam = np.tile([0.0, -8.0], heads // 4)
+    q[:, 2::4] *= 0.5                                      # the first map of the pairs of -8: half of S
+    lam_d = dev(lam, np.float32)
+    _say(dim, n_new, ctx, block, where, dtype)
+    for S in (0.0, 9.0, 14.0, 17.5, 19.0):
+        o = cache.attend_diff(seqs, q, lam_d, scale=S / dim).double().cpu().numpy()
+        s = dim * float(np.float32(S / dim))
+        for t in range(n_new):
+            seen = ctx - n_new + t + 1
+            others = seen - (tok < seen)
+            assert others < seen
+            keep = lambda s: others / (others + np.exp(s))
+            rel = lambda s: max(2.0 ** -11, 2.0 ** -31 * np.exp(s)) + s * 2.0 ** -21 + 2.0 ** -15
+            for j, l in enumerate(lam):
+                first = s / 2 if l else s
+                want = keep(first) - l * keep(s)
+                lim = rel(first) * keep(first) + abs(l) * rel(s) * keep(s) + (2.0 ** -22 + torch.finfo(q.dtype).eps / 2) * want
+                assert (np.abs(o[t, j] - want) <= lim).all(), (S, t, j, o[t, j].min() / want, o[t, j].max() / want)
+    sel.sync_errors()
 
 
 @pytest.mark.parametrize("dim", [64, 128])
