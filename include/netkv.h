@@ -574,8 +574,9 @@ typedef struct {
  * gradient of the rotation for x from that for out.  Each output is
  * a c +- b s to 2^-23 of it and 2^-48 of its products, rounded once to dtype, also
  * where the products cancel (down to 2^-149) or are past fp32's largest.
- * head_dim: a multiple of 8 from 16 to 1024.  Any order of pos; needs no loads.  Asynchronous; allocates nothing.  ECAPACITY: more than
- * 2^32 - 1 threads, in workgroups of 256. */
+ * head_dim: a multiple of 8 from 16 to 1024.  Any order of pos; needs no loads.
+ * Asynchronous; allocates nothing.  ECAPACITY: more than 2^32 - 1 threads, in
+ * workgroups of 256. */
 netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *rope, uint64_t n_rows, const uint32_t *pos,
                                uint64_t pos_stride, const void *x, uint64_t x_stride, void *out,
                                uint64_t out_stride, uint32_t n_heads, uint32_t head_dim, int dtype, int transpose,
@@ -593,7 +594,7 @@ netkv_status netkv_rope_rotate(netkv_handle h, const netkv_rope_t *rope, uint64_
  * overlap q, k or v (EINVAL).  Sequences that netkv_kv_store leaves out are left
  * out, their rows of q_out and those past the last sequence left as they were.
  * Time, capacity and all else as for netkv_kv_store, and a workgroup of up to 512
- * threads for each of up to 16 query rows. */
+ * threads for each of up to 16 query rows, which looks for its sequence as well. */
 netkv_status netkv_kv_append(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs,
                              const netkv_rope_t *rope, const uint32_t *pos, uint64_t pos_stride, const void *q,
                              uint32_t n_heads, uint64_t q_stride, void *q_out, uint64_t q_out_stride, const void *k,
@@ -661,7 +662,7 @@ netkv_status netkv_kv_attend_workspace(netkv_handle h, const netkv_kv_t *kv, con
  * maps' difference and the norm are fp32, and out is rounded once.  No block
  * weights, no gradient.  One form for the call, by max_tok * n_heads /
  * n_kv_heads rows (more than 192 or 48 at head_dim 64 or 128: the form for
- * prompts). */
+ * prompts, in which single tokens take up to 2.2 times as long: a call each). */
 netkv_status netkv_kv_attend_diff(netkv_handle h, const netkv_kv_t *kv, const netkv_kv_seqs_t *seqs, const void *q,
                                   int dtype, uint32_t n_heads, uint64_t q_stride, float scale, const float *lambda,
                                   const float *norm, float eps, float gain, void *out, uint64_t out_stride,

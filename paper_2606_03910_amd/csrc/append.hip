@@ -272,8 +272,9 @@ __device__ inline void rotate_rows(const RowArgs &a, uint64_t row, uint32_t n, u
 }
 
 // Bound by memory: 16,384 rows of 32 heads of 128 elements of which 64 turn (269 MB)
-// 56 us, 4.8 TB/s; 10,007 of 16 heads of 80 on two axes (51 MB) 15 us: 834
-// workgroups at once, each with one chain of positions, table rows and rows.
+// 59 us, 4.6 TB/s; 10,007 of 16 heads of 80 on two axes (51 MB) 15.6 us: 834
+// workgroups at once, each with one chain of positions, table rows and rows, and
+// nearly every wavefront with a unit whose pairs are on both axes.
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RowArgs a, uint32_t rows, uint32_t chunk) {
     const uint32_t row = blockIdx.x * chunk;
     rotate_rows(a, row, min(chunk, rows - row), 0);
@@ -490,7 +491,7 @@ __device__ inline void append_queries(const AppendArgs &a, uint32_t task) {
 
 // All of a small call: bound by the chain of lengths, pages, rows and the
 // largest of them.  64 single tokens of 64 and 8 heads of 128 dimensions 13 us, 10,231 rows
-// of 15 and 5 heads of 64 dimensions in blocks of 32 (64 MB) 23 us, 2.8 TB/s.
+// of 15 and 5 heads of 64 dimensions in blocks of 32 (64 MB) 24 us, 2.7 TB/s.
 template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a) {
     if (blockIdx.x < a.row_tasks) {

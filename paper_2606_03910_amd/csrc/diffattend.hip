@@ -336,13 +336,15 @@ __device__ __forceinline__ float weights_of(const f32x4 (&st)[2], float sc, floa
 // As attend_kernel, each wavefront for one map: the first and third take the
 // first map, the others the second, two steps of the range at a time.  The two
 // that work on one step read its values once from memory and once from the
-// caches.  Joined through LDS.  Both maps in one wavefront would read them once,
+// caches.  Joined through LDS.  (At 128 dimensions 39 to 43 registers are kept in
+// private memory: four from before the steps to behind them, the others while a NaN
+// value that only some rows see is looked for; none within an ordinary step.)  Both maps in one wavefront would read them once,
 // but with twice the sums in registers, one wavefront a SIMD: 64 sequences of up to
 // 16,384 tokens 174 us, 8 of 131,071 378, 200 of up to 1,000 80 and not 51.  Bound by
-// memory: 8 sequences of 131,071 tokens, 8 KV heads of 128 dimensions (2.1 GB) 355
-// us, 6.0 TB/s; 64 of up to 16,384 (0.68 GB) 154, 4.4 TB/s, by the ends of unequal
-// ranges.  One row after 700 tokens takes 13 us, its chain of loads: lengths,
-// pages, keys, and through LDS.
+// memory: 8 sequences of 131,071 tokens, 8 KV heads of 128 dimensions (2.1 GB) 367
+// us with the join, 5.8 TB/s; 64 of up to 16,384 (0.68 GB) 165, 4.1 TB/s, by the ends
+// of unequal ranges.  One row after 700 tokens takes 14 us, its chain of loads:
+// lengths, pages, keys, and through LDS.
 template <int D, int NT, bool HALF, bool SMALL>
 __global__ __launch_bounds__(kThreads, 2) void pair_kernel(PairArgs a) {
     typedef typename Elem<HALF>::T T;
@@ -675,13 +677,18 @@ __global__ __launch_bounds__(kThreads, 2) void pair_kernel(PairArgs a) {
 // values k + 1 with its own (slot 2 k + 2: values k - 1 were last read in slot
 // 2 k + 1, values k + 1 are first read in slot 2 k + 4).  At the end the second
 // map's rows go to the first group through LDS.
-// Bound by what stands beside the products: a slot's softmax of 64 rows, its
-// rounding and the widening of the step after take some 2,000 cycles of its
-// vector instructions, the other group's products 1,600.  Two chunks of 1,024 rows
-// after 31,744 tokens, 64 and 8 heads of 128 dimensions (3.2 TFLOP) 3.2 ms, 1,000
-// TFLOP/s, 83 % of a large matrix product's rate; six prompts of up to 2,777, 64 and 16
-// heads of 64 (233 GFLOP) 440 us, 530 TFLOP/s: a tile has 17 steps, of which the first
-// and the masked one take nearly twice the others' 2 us, and 9 us beside them.
+// Two chunks of 1,024 rows after 31,744 tokens, 64 and 8 heads of 128 dimensions (3.2
+// TFLOP) 3,240 us with all launches, 990 TFLOP/s, 81 % of a large matrix product's
+// rate; six prompts of up to 2,777, 64 and 16 heads of 64 (233 GFLOP) 443 us, 525 TFLOP/s:
+// a tile has 17 steps, of which the first and the masked one take nearly twice the
+// others' 2 us, and 9 us beside them.  The chunks are bound by the chains in a slot,
+// which two wavefronts a SIMD do not cover: of its 1,880 cycles the matrix unit
+// works for 770 and vector instructions for 630.  The prompts, in blocks of 16 tokens,
+// by both units in turn, as there the groups are in step: of a step's 4,800 cycles
+// two wavefronts' products take 1,540 and their vector instructions 2,900.  Counted
+// over the chunks (prompts) the matrix unit is busy 41 (25) % of the time, vector
+// instructions 44 (53), LDS 31 (17), and a wavefront waits for the other group or for
+// data for 40 (37) % of its own.
 // Measured and not kept: loads straight into LDS (chunks 3.8 ms: what they wait
 // for is not the memory), more priority for the products (no change), and the
 // widening in loops of its own behind them (registers do not suffice).
