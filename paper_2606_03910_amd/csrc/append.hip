@@ -297,8 +297,9 @@ struct AppendArgs {
 // largest value and the rounding it is held in 16 bits, to odd (to_odd), where
 // these have two bits more than the block's 8: not past fp32's largest, nor where
 // the block's steps (from 2^-9 of its scale) near bfloat16's smallest, 2^-133.
-// Such blocks are computed once more from 64 bits.  The products in 64 bits and the roundings to odd bound it where calls are large:
-// 131,214 rows of 8 heads of 128 dimensions 220 us, of which the memory needs 80.
+// Such blocks are computed once more from 64 bits.  The products in 64 bits and
+// the roundings to odd bound it where calls are large: 131,214 rows of 8 heads of
+// 128 dimensions 220 us, of which the memory needs 80.
 template <int D, int THREADS, int kEach>
 __device__ __forceinline__ void append_keys(const AppendArgs &g, uint32_t task, uint32_t h) {
     constexpr uint32_t kUnits = D / 16;                       // of a token; a thread keeps kEach

@@ -65,7 +65,7 @@ def append_and_compare(nk, sel, shape, x, tab, scales=None):
 
 
 @pytest.mark.parametrize("shape", range(len(SHAPES)))
-@pytest.mark.parametrize("scale", [1.0, 1.25, 64.0, 160.0])
+@pytest.mark.parametrize("scale", [1.0, 1.25, 64.0, 160.0, 400.0, 2.0 ** 100])
 def test_append_keys_past_the_largest_fp32(nk, sel, shape, scale):
     """Finite keys of 3.4e38 and more, beside ordinary ones and such that are not
     finite; with a scaled table up to and past 448 * 2^127."""
@@ -79,7 +79,10 @@ def test_append_keys_past_the_largest_fp32(nk, sel, shape, scale):
     if n > 4:
         x[4, 0, 3], x[3, hk - 1, 1] = np.inf, np.nan
     k = append_and_compare(nk, sel, SHAPES[shape], torch.from_numpy(x).to(torch.bfloat16), tab)
-    _say(shape, scale, "keys past fp32:", int((np.abs(k[np.isfinite(k)]) > 3.4e38).sum()))
+    wide = np.abs(k[np.isfinite(k)]) > 3.4e38
+    _say(shape, scale, "keys past fp32:", int(wide.sum()), "past the largest scale:", int(np.isinf(k).sum()))
+    # what the case is for is there (2^100 takes every such key past the largest scale)
+    assert n < 100 or ((wide.any() or scale == 2.0 ** 100) and (np.isinf(k).sum() > 100 or scale < 200))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
